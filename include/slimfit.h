@@ -269,6 +269,38 @@ int32_t slimfit_gelu_backward_dequant(const uint8_t *codes, const float *scales,
                                       const void *dy, void *dx, int32_t dt, void *stream);
 
 /* ------------------------------------------------------------------------
+ * (b'') Gated activations around the low-bit cache of their input (decoder
+ *     models' feed-forward layers; the placement is the paper's for GELU): rows
+ *     x = [gate | up] of 2 F elements,
+ *         y = act(gate) * up,
+ *     and (codes, scales) = slimfit_quant_pack of all rows * 2 F elements of x,
+ *     bit for bit, x read once.  Backward, with gate^ and up^ from the cache,
+ *         dx = [dy * up^ * act'(gate^) | dy * act(gate^)].
+ *     act: SLIMFIT_ACT_SILU  act(g) = g / (1 + e^-g),  SLIMFIT_ACT_GELU the exact
+ *     form of (b').  fp32 arithmetic: y within (6e-7 + 2e-7 * |gate|) * |up * gate|
+ *     + 1e-6 * |y| of the fp64 value, either half of dx within (6e-7 + 2e-7 *
+ *     |gate^|) * (1 + |gate^|) * |dy * up^| resp. (6e-7 + 2e-7 * |gate^|) * |dy *
+ *     gate^| of its own plus 1e-6 relative, bf16 results within one further bf16
+ *     rounding; results below 1e-37 may come out as 0.
+ *
+ *  x, dx : DEVICE, rows * 2 F elements of dt;  y, dy : DEVICE, rows * F.  16-byte
+ *          aligned; x and y, dx and dy must not share memory (INVALID_ARG).
+ *  bits  : 4 | 8; forward also 0: nothing is kept, codes and scales are not
+ *          looked at (nor mode, block, frac_bits).
+ *  mode, block, frac_bits, codes, scales, errors: as in (b).
+ *  F has to be a multiple of 4 (fp32) or 8 (bf16), with mode BLOCK of block as
+ *  well, so that a block lies in one half of one row, and at most 2^24
+ *  (ERR_UNSUPPORTED).
+ * ---------------------------------------------------------------------- */
+typedef enum { SLIMFIT_ACT_SILU = 0, SLIMFIT_ACT_GELU = 1 } slimfit_act;
+
+int32_t slimfit_gated_quant_pack(const void *x, int32_t dt, int64_t rows, int64_t F, int32_t act, int32_t mode, int32_t bits, int32_t block,
+                                 int32_t frac_bits, void *y, uint8_t *codes, float *scales, void *stream);
+
+int32_t slimfit_gated_backward_dequant(const uint8_t *codes, const float *scales, int64_t rows, int64_t F, int32_t act, int32_t mode, int32_t bits,
+                                       int32_t block, int32_t frac_bits, const void *dy, void *dx, int32_t dt, void *stream);
+
+/* ------------------------------------------------------------------------
  * (c) Pruning to values + indices -- Alg. 5 and the appendix on pruning:
  *     sort from largest to smallest with indices, keep the first k, store
  *     them with their indices (the dense size is rows x cols, which the
@@ -525,6 +557,78 @@ int32_t slimfit_merge_heads(const void *q, const void *kt, const void *v, int32_
                             int32_t heads, int32_t head_dim, float q_scale, void *qkv, void *stream);
 
 /* ------------------------------------------------------------------------
+ * (c-rot) The rows of a QKV projection apart as in (c-qkv), with the norm of
+ *     each query and key head and the rotation by the token's position in the
+ *     same pass, keys and values shared by groups of query heads, and the
+ *     low-bit cache of what the backward pass reads.  Each row x of head_dim
+ *     elements of a query or key head:
+ *         rstd = 1 / sqrt(mean(x^2) + eps),      y = x * rstd * gamma,
+ *     then the first rotary_dim elements in pairs (a, b), by the angle that row
+ *     p of the table has for the pair, p being the token's position:
+ *         (a, b) -> (a cos - b sin, b cos + a sin);
+ *     q = q_scale * that, k^T as it is, v copied.  fp32 arithmetic (fixed-order
+ *     sums), rounded to dt once: rstd within 8e-7 relative, an element within 1.2e-6 of
+ *     |a cos| + |b sin| before that rounding.  (A row of zeros with eps 0 is NaN.)
+ *
+ *  qkv : DEVICE [batch, tokens, q_heads + 2 * kv_heads, head_dim]: queries, keys, values.
+ *  q   : DEVICE [batch, q_heads, tokens, head_dim].
+ *  kt  : DEVICE [batch, kv_heads, head_dim, tokens].
+ *  v   : DEVICE [batch, kv_heads, tokens, head_dim].
+ *        Contiguous, 16-byte aligned, of type dt, none sharing memory with another
+ *        (INVALID_ARG).  q_heads has to be a multiple of kv_heads (INVALID_ARG).
+ *  gamma_q, gamma_k : DEVICE float[head_dim], 16-byte aligned.  Both NULL: there is
+ *        no norm (eps, rstd, codes and scales are not looked at, bits has to be 0).
+ *  table : DEVICE float[positions, rotary_dim], 16-byte aligned: the cosines of the
+ *        rotary_dim / 2 pairs' angles, then their sines.  rotary_dim 0: no rotation,
+ *        table may be NULL.
+ *  pairing : SLIMFIT_ROTARY_HALVES pairs element i with i + rotary_dim / 2,
+ *        SLIMFIT_ROTARY_ADJACENT element 2 i with 2 i + 1.
+ *  position_ids : DEVICE int32[batch, tokens], 4-byte aligned, or NULL: token t
+ *        stands at t (positions >= tokens, else INVALID_ARG).  A token whose id is
+ *        outside [0, positions) is not rotated (padding).
+ *  rstd : DEVICE float[batch * tokens, q_heads + kv_heads], 4-byte aligned.
+ *  bits : 0 keeps nothing (the backward pass reads qkv again).  4 | 8: codes and
+ *        scales are those of slimfit_quant_pack(BLOCK) on the query and key columns
+ *        of qkv, laid out as [batch * tokens, q_heads + kv_heads, head_dim]; head_dim has
+ *        to be a multiple of block (ERR_UNSUPPORTED).
+ *  head_dim : a multiple of 4 (fp32) or 8 (bf16), at most 256; rotary_dim: a
+ *        multiple of 8 (fp32) or 16 (bf16), at most head_dim; batch * tokens below
+ *        2^31 (ERR_UNSUPPORTED).
+ *
+ *  slimfit_heads_norm_rotate_backward : the gradients together again.  With g the
+ *        gradient of a query (times q_scale) or key row, rotated back, x~ = x^ * rstd,
+ *             dgamma = sum over rows of g * x~,
+ *             dx = rstd * (g gamma - x~ * mean(g gamma x~));
+ *        without a norm dx = g.  x^ is what the cache gives back, or (bits 0) qkv's
+ *        own columns; rstd is the forward pass's.  dqkv's value columns are dv.
+ *        dgamma_q, dgamma_k : DEVICE float[head_dim], both, or both NULL (frozen: no
+ *        sums are formed and no workspace is needed).  fp32 sums over a
+ *        workgroup's rows (at most 2048), fp64 across; no atomics: the same call gives the same bits.
+ *        workspace : DEVICE, 16-byte aligned, of the bytes that
+ *        slimfit_heads_norm_rotate_workspace reports; contents overwritten.
+ *        qkv : as in the forward pass; looked at with a norm and bits 0 only.
+ *        dx within 2e-6 of rstd * (|g gamma| + |x~| * mean|g gamma x~|), dgamma within 6.5e-6 of sum |g x~|, |g| being
+ *        the sum of the sizes of g's two terms; bf16 dx within one further rounding.
+ * ---------------------------------------------------------------------- */
+typedef enum { SLIMFIT_ROTARY_HALVES = 0, SLIMFIT_ROTARY_ADJACENT = 1 } slimfit_rotary;
+
+int32_t slimfit_heads_norm_rotate_forward(const void *qkv, int32_t dt, int64_t batch, int32_t tokens, int32_t q_heads, int32_t kv_heads,
+                                          int32_t head_dim, const float *gamma_q, const float *gamma_k, float eps, const float *table,
+                                          int32_t positions, int32_t rotary_dim, int32_t pairing, const int32_t *position_ids, float q_scale,
+                                          int32_t bits, int32_t block, void *q, void *kt, void *v, float *rstd, uint8_t *codes, float *scales,
+                                          void *stream);
+
+int32_t slimfit_heads_norm_rotate_workspace(int32_t dt, int64_t batch, int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                            size_t *bytes);
+
+int32_t slimfit_heads_norm_rotate_backward(const void *dq, const void *dkt, const void *dv, const void *qkv, const uint8_t *codes,
+                                           const float *scales, int32_t bits, int32_t block, const float *rstd, int32_t dt, int64_t batch,
+                                           int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim, const float *gamma_q,
+                                           const float *gamma_k, const float *table, int32_t positions, int32_t rotary_dim, int32_t pairing,
+                                           const int32_t *position_ids, float q_scale, void *dqkv, float *dgamma_q, float *dgamma_k,
+                                           void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * Product of fp32 matrices (the dense products of the linear layers):
  *        out[i][j] = sum over k of a[i][k] * b[j][k]     (b_deep != 0: b is N x K)
  *        out[i][j] = sum over k of a[i][k] * b[k][j]     (b_deep == 0: b is K x N)
@@ -540,6 +644,30 @@ int32_t slimfit_product_workspace(int64_t M, int64_t N, int64_t K, size_t *bytes
 
 int32_t slimfit_product(const float *a, const float *b, int32_t b_deep, int64_t M, int64_t N, int64_t K, float *out,
                         void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * (b-dw) Weight gradient of a linear layer straight from the low-bit cache of its
+ *     input -- Alg. 4's active layer, which keeps its input in 8 (or 4) bits:
+ *         dw[n][k] = sum over m of dy[m][n] * x^[m][k],   x^ = code * scale,
+ *     x^ formed on the way into the matrix cores and never written to memory.
+ *  dy     : DEVICE, M x N of dt.       dw : DEVICE, N x K of dt, every element written (zeros for M = 0).
+ *  codes, scales : DEVICE, as slimfit_quant_pack(BLOCK, bits, block) left them for the M x K input; K has to be a
+ *           multiple of block (ERR_UNSUPPORTED), so that a block lies in one row.
+ *  fp32   : dy * scale is rounded once, taken apart exactly into three bf16 numbers and multiplied by the codes, whole
+ *           numbers that bf16 holds; fp32 sums:
+ *           |dw - exact| <= (2 M + 8) * 2^-23 * sum |dy||x^| + M * 2^-120
+ *           (products dy * scale of 2^127 and more are outside of this).
+ *  bf16   : x^ rounded to bf16 (the value slimfit_dequant_unpack stores), fp32 sums, rounded to bf16 once:
+ *           |dw - exact| <= (2^-8 + (2 M + 8) * 2^-23) * sum |dy||x^| + 2^-8 * |dw|.
+ *  Deterministic: the order of the sums goes by the sizes and types alone.
+ *  workspace : DEVICE, 16-byte aligned, of the bytes that slimfit_weight_grad_dequant_workspace reports (0 for most sizes);
+ *           contents overwritten.
+ *  dy, codes, scales 16-byte aligned, dw too; none shares memory with dw (INVALID_ARG).  N and K up to 2^20 (ERR_UNSUPPORTED).
+ * ---------------------------------------------------------------------- */
+int32_t slimfit_weight_grad_dequant_workspace(int32_t dt, int32_t block, int64_t M, int64_t N, int64_t K, size_t *bytes);
+
+int32_t slimfit_weight_grad_dequant(const void *dy, int32_t dt, const uint8_t *codes, const float *scales, int32_t bits, int32_t block, int64_t M,
+                                    int64_t N, int64_t K, void *dw, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
  * (d) Inter-layer scheduling on the host -- Alg. 1 and Sec. 3.2 / Fig. 4:

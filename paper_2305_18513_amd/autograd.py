@@ -26,6 +26,14 @@ fp32 operands of sizes at which it is the quicker one, and torch's otherwise.
                      pairs and V are cached.  Backward: dP = dO @ V^T (dense
                      product, torch's), dV = P^^T @ dO with P^ restored from the
                      pairs, dlogits from the pairs as in SoftmaxFunction.
+  GatedFunction      y = act(gate) * up of rows [gate | up]; caches them in `bits`
+                     bits, or nothing where no gradient is asked for; backward from
+                     the cache.
+  HeadsNormRotateFunction  (q, k^T, v) as SplitHeadsFunction, keys and values shared by
+                     groups of query heads, each query and key head normed and
+                     turned by its token's position in the same pass; caches the
+                     query and key columns in `bits` bits (0: keeps the rows
+                     themselves) and rstd; norms that are frozen get no gradients.
   SplitHeadsFunction (q, k^T, v) of the attention products from the rows of a QKV
                      projection in one pass, their gradients back in another.
   MatmulFunction     out = a @ b with both operands cached in 8 bits (the paper's
@@ -34,7 +42,8 @@ fp32 operands of sizes at which it is the quicker one, and torch's otherwise.
                      require a gradient (frozen by the scheduler) keeps nothing of
                      its input and returns no weight gradient; an active one keeps
                      its input in `bits` bits and forms the weight gradient from
-                     the dequantised input.
+                     the dequantised input (`straight`: from the codes themselves,
+                     by the library's own product, where a block lies in one row).
 
 All tensors are CUDA tensors (fp32 or bf16 activations; gamma / beta and the
 kept standardised values fp32); the kernels run on torch's current stream.
@@ -276,6 +285,76 @@ class SplitHeadsFunction(torch.autograd.Function):
         return dqkv, None, None
 
 
+class GatedFunction(torch.autograd.Function):
+    """y = act(gate) * up for x = [gate | up] (..., 2 F); ``act`` is binding.ACT_SILU or ACT_GELU, F a multiple of ``block``."""
+
+    @staticmethod
+    def forward(ctx, x: torch.Tensor, act: int, bits: int = 8, block: int = 64):
+        F = x.shape[-1] // 2
+        x2 = x.contiguous().view(-1, x.shape[-1])
+        y = torch.empty(x2.shape[0], F, dtype=x.dtype, device=x.device)
+        if not ctx.needs_input_grad[0]:
+            sf.gated_quant_pack(x2, act, sf.Q_BLOCK, 0, block, 0, y, None, None)
+            return y.view(*x.shape[:-1], F)
+        codes = torch.empty(sf.packed_bytes(x2.numel(), bits), dtype=torch.uint8, device=x.device)
+        scales = torch.empty(sf.num_blocks(x2.numel(), block), dtype=torch.float32, device=x.device)
+        sf.gated_quant_pack(x2, act, sf.Q_BLOCK, bits, block, 0, y, codes, scales)
+        ctx.save_for_backward(codes, scales)
+        ctx.meta = (act, bits, block, x.shape)
+        return y.view(*x.shape[:-1], F)
+
+    @staticmethod
+    def backward(ctx, grad_output: torch.Tensor):
+        codes, scales = ctx.saved_tensors
+        act, bits, block, shape = ctx.meta
+        dy = grad_output.contiguous().view(-1, shape[-1] // 2)
+        dx = torch.empty(dy.shape[0], shape[-1], dtype=dy.dtype, device=dy.device)
+        sf.gated_backward_dequant(codes, scales, act, sf.Q_BLOCK, bits, block, 0, dy, dx)
+        return dx.view(shape), None, None, None
+
+
+class HeadsNormRotateFunction(torch.autograd.Function):
+    """(q, k^T, v) of the attention products from the rows (B, T, (heads + 2 * kv_heads) * D) of a QKV projection.  gamma_q, gamma_k
+    (both None: no norm), table (None: no rotation; binding.rotary_table), pairing, position_ids: binding.heads_norm_rotate_forward.
+    A head's D has to be a multiple of ``block`` where ``bits`` is not 0; without a norm nothing is kept."""
+
+    @staticmethod
+    def forward(ctx, qkv: torch.Tensor, gamma_q, gamma_k, heads: int, kv_heads: int, table, pairing: int = sf.ROTARY_HALVES, position_ids=None,
+                q_scale: float = 1.0, eps: float = 1e-6, bits: int = 8, block: int = 64):
+        B, T, width = qkv.shape
+        D = width // (heads + 2 * kv_heads)
+        norm = gamma_q is not None
+        qkv = qkv.contiguous()
+        q = torch.empty(B, heads, T, D, dtype=qkv.dtype, device=qkv.device)
+        kt = torch.empty(B, kv_heads, D, T, dtype=qkv.dtype, device=qkv.device)
+        v = torch.empty(B, kv_heads, T, D, dtype=qkv.dtype, device=qkv.device)
+        keeps = norm and any(ctx.needs_input_grad[:3])
+        bits = bits if keeps else 0
+        rstd = codes = scales = None
+        if norm:
+            rstd = torch.empty(B * T, heads + kv_heads, dtype=torch.float32, device=qkv.device)
+        if bits:
+            n = B * T * (heads + kv_heads) * D
+            codes = torch.empty(sf.packed_bytes(n, bits), dtype=torch.uint8, device=qkv.device)
+            scales = torch.empty(sf.num_blocks(n, block), dtype=torch.float32, device=qkv.device)
+        sf.heads_norm_rotate_forward(qkv, gamma_q, gamma_k, eps, table, pairing, position_ids, q_scale, bits, block, q, kt, v, rstd, codes, scales)
+        ctx.save_for_backward(qkv if keeps and not bits else None, codes, scales, rstd if keeps else None, gamma_q, gamma_k, table, position_ids)
+        ctx.meta = (qkv.shape, pairing, q_scale, bits, block)
+        return q, kt, v
+
+    @staticmethod
+    def backward(ctx, dq: torch.Tensor, dkt: torch.Tensor, dv: torch.Tensor):
+        qkv, codes, scales, rstd, gamma_q, gamma_k, table, position_ids = ctx.saved_tensors
+        shape, pairing, q_scale, bits, block = ctx.meta
+        dqkv = torch.empty(shape, dtype=dq.dtype, device=dq.device)
+        dgamma_q = dgamma_k = None
+        if gamma_q is not None and any(ctx.needs_input_grad[1:3]):
+            dgamma_q, dgamma_k = (torch.empty_like(g) for g in (gamma_q, gamma_k))
+        sf.heads_norm_rotate_backward(dq.contiguous(), dkt.contiguous(), dv.contiguous(), qkv, codes, scales, bits, block, rstd, gamma_q, gamma_k,
+                                      table, pairing, position_ids, q_scale, dqkv, dgamma_q, dgamma_k)
+        return (dqkv, dgamma_q, dgamma_k) + (None,) * 9
+
+
 def _plain(t: torch.Tensor) -> bool:
     """Whether a kernel may be handed the tensor's memory as it is."""
     return (type(t) in (torch.Tensor, torch.nn.Parameter) and torch._C._has_storage(t) and t.is_cuda
@@ -337,10 +416,11 @@ class LinearFunction(torch.autograd.Function):
     keeps nothing of x and produces no weight gradient; an active one keeps x as ``bits``-bit block-scaled codes
     and forms its weight gradient from the dequantised x^.  The library's fp32 product (sizes: ``_quicker``) holds all bits of
     its operands and is no further from the exact one than fp32 additions in any order; where the program allows torch fewer
-    bits (``torch.set_float32_matmul_precision``) the products are torch's."""
+    bits (``torch.set_float32_matmul_precision``) the products are torch's.  ``straight``: the weight gradient is formed from
+    the codes themselves where the layer's inputs are a multiple of ``block``; x^ is not written to memory."""
 
     @staticmethod
-    def forward(ctx, x: torch.Tensor, weight: torch.Tensor, bias, bits: int = 8, block: int = 64):
+    def forward(ctx, x: torch.Tensor, weight: torch.Tensor, bias, bits: int = 8, block: int = 64, straight: bool = False):
         y = _dense(x, weight, True) if bias is None else None
         if y is None:
             y = torch.nn.functional.linear(x, weight, bias)
@@ -349,6 +429,7 @@ class LinearFunction(torch.autograd.Function):
         if weight.requires_grad:
             codes, scales = _quantise(x, bits, block)
             ctx.cache = (bits, block, x.shape, x.dtype)
+            ctx.straight = straight
             ctx.save_for_backward(weight, codes, scales)
         else:
             ctx.save_for_backward(weight)
@@ -366,10 +447,26 @@ class LinearFunction(torch.autograd.Function):
         dw = None
         if ctx.cache is not None:
             bits, block, shape, dtype = ctx.cache
-            x_hat = _dequantise(ctx.saved_tensors[1], ctx.saved_tensors[2], bits, block, shape, dtype)
-            dw = dy2.t().mm(x_hat.view(-1, shape[-1]))
+            codes, scales = ctx.saved_tensors[1:]
+            if ctx.straight:
+                dw = _straight(dy2, codes, scales, bits, block, shape[-1], dtype)
+            if dw is None:
+                dw = dy2.t().mm(_dequantise(codes, scales, bits, block, shape, dtype).view(-1, shape[-1]))
         db = dy2.sum(0) if ctx.bias_active else None
-        return dx, dw, db, None, None
+        return dx, dw, db, None, None, None
+
+
+def _straight(dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bits: int, block: int, K: int, dtype):
+    """dy.T @ x^ from x's codes, or None where that is torch's: blocks that straddle rows, types that differ, products that are
+    watched, tensors that are not the kernel's to read."""
+    if K % block != 0 or dy.dtype != dtype or _watched() or dy.get_device() != torch.cuda.current_device():
+        return None
+    dy = dy.contiguous()
+    if not all(_plain(t) for t in (dy, codes, scales)):
+        return None
+    dw = torch.empty(dy.shape[1], K, dtype=dtype, device=dy.device)
+    sf.weight_grad_dequant(dy, codes, scales, bits, block, dw)
+    return dw
 
 
 def _rows_of_vectors(dim: int, t: torch.Tensor) -> bool:

@@ -44,6 +44,8 @@ _native, _native_missing = _load_native()
 F32, BF16 = 0, 1
 Q_FIXED, Q_BLOCK = 0, 1
 PRUNE_TOPK, PRUNE_THRESHOLD = 0, 1
+ACT_SILU, ACT_GELU = 0, 1
+ROTARY_HALVES, ROTARY_ADJACENT = 0, 1
 GLOBAL_TILE = 4096                 # SLIMFIT_GLOBAL_TILE: granularity of prune_global's tile pointers
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_HIP, ERR_POINTER = range(7)
@@ -57,6 +59,9 @@ EXPORTS = (
     "slimfit_restore_scores", "slimfit_softmax_prune", "slimfit_softmax_backward_pruned", "slimfit_prune_global_workspace", "slimfit_global_tile_ptr_len", "slimfit_prune_global",
     "slimfit_restore_global", "slimfit_layernorm_forward", "slimfit_prune_global_standardized",
     "slimfit_layernorm_backward_pruned", "slimfit_layernorm_forward_quant_pack", "slimfit_layernorm_backward_dequant", "slimfit_layernorm_backward", "slimfit_layernorm_param_grads_workspace", "slimfit_layernorm_param_grads",
+    "slimfit_gated_quant_pack", "slimfit_gated_backward_dequant",
+    "slimfit_heads_norm_rotate_forward", "slimfit_heads_norm_rotate_workspace", "slimfit_heads_norm_rotate_backward",
+    "slimfit_weight_grad_dequant_workspace", "slimfit_weight_grad_dequant",
     "slimfit_split_heads", "slimfit_merge_heads", "slimfit_product_workspace", "slimfit_product",
     "slimfit_freeze_count", "slimfit_ils_select", "slimfit_ils_select_blocks",
     "slimfit_ils_update", "slimfit_schedule_random", "slimfit_schedule_progressive",
@@ -76,6 +81,15 @@ def _require(ok: bool) -> None:
     is a segment shared by many tensors: an output tensor that is too small has to be caught here."""
     if not ok:
         raise ValueError("tensor arguments do not agree in shape or dtype with what the call expects")
+
+
+def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
+    """The library launches on the current device's stream: a tensor of another device (or of the host) is refused."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
+            raise ValueError("every tensor has to be on the current GPU, this one is on %s" % t.device)
+        if t is not None and (t.is_neg() or t._is_zerotensor()):
+            raise ValueError("a tensor's values have to be what its memory holds")
 
 
 _lib = None
@@ -395,6 +409,79 @@ def gelu_backward_dequant(codes: torch.Tensor, scales: Optional[torch.Tensor], m
         _dev(codes), _dev(scales), C.c_int64(dx.numel()), C.c_int32(mode), C.c_int32(bits), C.c_int32(block),
         C.c_int32(frac_bits), _dev(dy), _dev(dx), C.c_int32(_dt(dx)), _stream(stream))
     _check(rc, "gelu_backward_dequant")
+
+
+# ---------------------------------------------------------------- (b'') gated activations around the cache of their input
+
+_native_gated_quant_pack = _fast("gated_quant_pack")
+
+
+def gated_quant_pack(x: torch.Tensor, act: int, mode: int, bits: int, block: int, frac_bits: int, y: torch.Tensor,
+                     codes: Optional[torch.Tensor], scales: Optional[torch.Tensor], stream=None) -> None:
+    """y = act(gate) * up for the rows x = [gate | up] (rows, 2 F), and (codes, scales) = quant_pack(x) in the same pass; with
+    ``bits`` 0 nothing is kept."""
+    rc = _native_gated_quant_pack(x, act, mode, bits, block, frac_bits, y, codes, scales, stream)
+    if rc is not NotImplemented:
+        return None if rc is None else _check(rc, "gated_quant_pack")
+    _require(x.dim() == 2 and y.dim() == 2 and y.dtype == x.dtype and y.shape[0] == x.shape[0] and x.shape[1] == 2 * y.shape[1])
+    _require(x.is_contiguous() and y.is_contiguous())
+    _require(bits == 0 or (codes is not None and _cache_fits(x.numel(), mode, bits, block, codes, scales)))
+    _on_current_device(x, y, codes, scales)
+    rc = lib().slimfit_gated_quant_pack(
+        _dev(x), C.c_int32(_dt(x)), C.c_int64(x.shape[0]), C.c_int64(y.shape[1]), C.c_int32(act), C.c_int32(mode), C.c_int32(bits),
+        C.c_int32(block), C.c_int32(frac_bits), _dev(y), _dev(codes), _dev(scales), _stream(stream))
+    _check(rc, "gated_quant_pack")
+
+
+_native_gated_backward_dequant = _fast("gated_backward_dequant")
+
+
+def gated_backward_dequant(codes: torch.Tensor, scales: Optional[torch.Tensor], act: int, mode: int, bits: int, block: int, frac_bits: int,
+                           dy: torch.Tensor, dx: torch.Tensor, stream=None) -> None:
+    """dx = [dy * up^ * act'(gate^) | dy * act(gate^)], gate^ and up^ what the cache gives back; they stay in registers."""
+    rc = _native_gated_backward_dequant(codes, scales, act, mode, bits, block, frac_bits, dy, dx, stream)
+    if rc is not NotImplemented:
+        return None if rc is None else _check(rc, "gated_backward_dequant")
+    _require(dx.dim() == 2 and dy.dim() == 2 and dy.dtype == dx.dtype and dy.shape[0] == dx.shape[0] and dx.shape[1] == 2 * dy.shape[1])
+    _require(dx.is_contiguous() and dy.is_contiguous() and _cache_fits(dx.numel(), mode, bits, block, codes, scales))
+    _on_current_device(codes, scales, dy, dx)
+    rc = lib().slimfit_gated_backward_dequant(
+        _dev(codes), _dev(scales), C.c_int64(dy.shape[0]), C.c_int64(dy.shape[1]), C.c_int32(act), C.c_int32(mode), C.c_int32(bits),
+        C.c_int32(block), C.c_int32(frac_bits), _dev(dy), _dev(dx), C.c_int32(_dt(dx)), _stream(stream))
+    _check(rc, "gated_backward_dequant")
+
+
+# ---------------------------------------------------------------- (b-dw) weight gradients from the cache
+
+def weight_grad_dequant_workspace(dtype: torch.dtype, block: int, M: int, N: int, K: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().slimfit_weight_grad_dequant_workspace(C.c_int32(_dt(torch.empty(0, dtype=dtype))), C.c_int32(block), C.c_int64(M), C.c_int64(N),
+                                                       C.c_int64(K), C.byref(out)), "weight_grad_dequant_workspace")
+    return int(out.value)
+
+
+_native_weight_grad_dequant = _fast("weight_grad_dequant")
+
+
+def weight_grad_dequant(dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bits: int, block: int, dw: torch.Tensor,
+                        workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dw (N x K) = dy (M x N) transposed times the M x K input as its cache gives it back; K a multiple of ``block``."""
+    rc = _native_weight_grad_dequant(dy, codes, scales, bits, block, dw, workspace, stream)
+    if rc is not NotImplemented:
+        return None if rc is None else _check(rc, "weight_grad_dequant")
+    _require(dy.dim() == 2 and dw.dim() == 2 and dw.dtype == dy.dtype and dw.shape[0] == dy.shape[1])
+    _require(dy.is_contiguous() and dw.is_contiguous())
+    M, N = dy.shape
+    K = dw.shape[1]
+    _require(_cache_fits(M * K, Q_BLOCK, bits, block, codes, scales))
+    _on_current_device(dy, codes, scales, dw, workspace)
+    need = weight_grad_dequant_workspace(dy.dtype, block, M, N, K)
+    if need or workspace is not None:
+        workspace = _own_workspace(workspace, need, dy.device, stream)
+    rc = lib().slimfit_weight_grad_dequant(
+        _dev(dy), C.c_int32(_dt(dy)), _dev(codes), _dev(scales), C.c_int32(bits), C.c_int32(block), C.c_int64(M), C.c_int64(N), C.c_int64(K),
+        _dev(dw), _dev(workspace), C.c_size_t(0 if workspace is None else workspace.numel()), _stream(stream))
+    _check(rc, "weight_grad_dequant")
 
 
 # ---------------------------------------------------------------- (c) Alg. 5
@@ -727,6 +814,105 @@ def merge_heads(q: torch.Tensor, kt: torch.Tensor, v: torch.Tensor, q_scale: flo
     rc = lib().slimfit_merge_heads(_dev(q), _dev(kt), _dev(v), C.c_int32(_dt(qkv)), C.c_int64(batch), C.c_int32(tokens), C.c_int32(heads),
                                    C.c_int32(dim), C.c_float(q_scale), _dev(qkv), _stream(stream))
     _check(rc, "merge_heads")
+
+
+# ---------------------------------------------------------------- (c-rot) norm and rotation of the heads
+
+def rotary_table(positions: int, rotary_dim: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """The (positions, rotary_dim) table of cosines and sines that heads_norm_rotate_* read: pair i of place p turns by
+    p * base ** (-2 i / rotary_dim), formed in 64 bits."""
+    angle = torch.arange(positions, device=device, dtype=torch.float64)[:, None] * base ** (
+        -torch.arange(0, rotary_dim, 2, device=device, dtype=torch.float64) / max(1, rotary_dim))
+    return torch.cat((angle.cos(), angle.sin()), 1).float().contiguous()
+
+
+def _rotate_ok(qkv: torch.Tensor, q: torch.Tensor, kt: torch.Tensor, v: torch.Tensor, gammas, table, ids, rstd, codes, scales, bits: int,
+               block: int) -> None:
+    """Shapes, types and sizes of what the two calls have in common (the values of numbers are the library's to judge)."""
+    _require(q.dim() == 4 and kt.dim() == 4 and v.dim() == 4 and qkv.dim() == 3)
+    B, Hq, T, D = q.shape
+    Hk = v.shape[1]
+    _require(v.shape == (B, Hk, T, D) and kt.shape == (B, Hk, D, T) and qkv.shape == (B, T, (Hq + 2 * Hk) * D))
+    _require(all(t.is_contiguous() and t.dtype == qkv.dtype for t in (qkv, q, kt, v)))
+    present = [g is not None for g in gammas]
+    _require(len(set(present)) == 1)
+    _require(all(g is None or (g.dtype == torch.float32 and g.numel() == D and g.is_contiguous()) for g in gammas))
+    _require(table is None or (table.dim() == 2 and table.dtype == torch.float32 and table.is_contiguous()))
+    _require(ids is None or (ids.dtype == torch.int32 and ids.numel() == B * T and ids.is_contiguous()))
+    if present[0]:
+        _require(rstd is not None and rstd.dtype == torch.float32 and rstd.is_contiguous() and rstd.numel() >= B * T * (Hq + Hk))
+    _require(bits == 0 or (codes is not None and _cache_fits(B * T * (Hq + Hk) * D, Q_BLOCK, bits, block, codes, scales)))
+
+
+def _table_sizes(table: Optional[torch.Tensor]):
+    return (0, 0) if table is None else (table.shape[0], table.shape[1])
+
+
+_native_heads_norm_rotate_forward = _fast("heads_norm_rotate_forward")
+
+
+def heads_norm_rotate_forward(qkv: torch.Tensor, gamma_q: Optional[torch.Tensor], gamma_k: Optional[torch.Tensor], eps: float,
+                              table: Optional[torch.Tensor], pairing: int, position_ids: Optional[torch.Tensor], q_scale: float, bits: int,
+                              block: int, q: torch.Tensor, kt: torch.Tensor, v: torch.Tensor, rstd: Optional[torch.Tensor],
+                              codes: Optional[torch.Tensor], scales: Optional[torch.Tensor], stream=None) -> None:
+    """The rows (batch, tokens, (q_heads + 2 kv_heads) * dim) of a QKV projection apart into q (batch, q_heads, tokens, dim), the
+    transposed k (batch, kv_heads, dim, tokens) and v, each query and key head normed and turned by its token's row of
+    ``table`` on the way, with the cache of the query and key columns (``bits`` 0: none)."""
+    rc = _native_heads_norm_rotate_forward(qkv, gamma_q, gamma_k, eps, table, pairing, position_ids, q_scale, bits, block, q, kt, v, rstd, codes,
+                                           scales, stream)
+    if rc is not NotImplemented:
+        return None if rc is None else _check(rc, "heads_norm_rotate_forward")
+    _rotate_ok(qkv, q, kt, v, (gamma_q, gamma_k), table, position_ids, rstd, codes, scales, bits, block)
+    _on_current_device(qkv, gamma_q, gamma_k, table, position_ids, q, kt, v, rstd, codes, scales)
+    B, Hq, T, D = q.shape
+    positions, rotary = _table_sizes(table)
+    rc = lib().slimfit_heads_norm_rotate_forward(
+        _dev(qkv), C.c_int32(_dt(qkv)), C.c_int64(B), C.c_int32(T), C.c_int32(Hq), C.c_int32(v.shape[1]), C.c_int32(D), _dev(gamma_q), _dev(gamma_k),
+        C.c_float(eps), _dev(table), C.c_int32(positions), C.c_int32(rotary), C.c_int32(pairing), _dev(position_ids), C.c_float(q_scale),
+        C.c_int32(bits), C.c_int32(block), _dev(q), _dev(kt), _dev(v), _dev(rstd), _dev(codes), _dev(scales), _stream(stream))
+    _check(rc, "heads_norm_rotate_forward")
+
+
+def heads_norm_rotate_workspace(dtype: torch.dtype, batch: int, tokens: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().slimfit_heads_norm_rotate_workspace(C.c_int32(_dt(torch.empty(0, dtype=dtype))), C.c_int64(batch), C.c_int32(tokens),
+                                                     C.c_int32(q_heads), C.c_int32(kv_heads), C.c_int32(head_dim), C.byref(out)),
+           "heads_norm_rotate_workspace")
+    return int(out.value)
+
+
+_native_heads_norm_rotate_backward = _fast("heads_norm_rotate_backward")
+
+
+def heads_norm_rotate_backward(dq: torch.Tensor, dkt: torch.Tensor, dv: torch.Tensor, qkv: Optional[torch.Tensor], codes: Optional[torch.Tensor],
+                               scales: Optional[torch.Tensor], bits: int, block: int, rstd: Optional[torch.Tensor],
+                               gamma_q: Optional[torch.Tensor], gamma_k: Optional[torch.Tensor], table: Optional[torch.Tensor], pairing: int,
+                               position_ids: Optional[torch.Tensor], q_scale: float, dqkv: torch.Tensor, dgamma_q: Optional[torch.Tensor] = None,
+                               dgamma_k: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The gradients of q, the transposed k and v together into the rows of dqkv, through rotation and norm, and the norms' own
+    gradients where they are given.  x comes from the cache, or (``bits`` 0) from ``qkv``."""
+    rc = _native_heads_norm_rotate_backward(dq, dkt, dv, qkv, codes, scales, bits, block, rstd, gamma_q, gamma_k, table, pairing, position_ids,
+                                            q_scale, dqkv, dgamma_q, dgamma_k, workspace, stream)
+    if rc is not NotImplemented:
+        return None if rc is None else _check(rc, "heads_norm_rotate_backward")
+    _rotate_ok(dqkv, dq, dkt, dv, (gamma_q, gamma_k), table, position_ids, rstd, codes, scales, bits, block)
+    B, Hq, T, D = dq.shape
+    Hk = dv.shape[1]
+    reads = gamma_q is not None and bits == 0
+    _require(not reads or (qkv is not None and qkv.shape == dqkv.shape and qkv.dtype == dqkv.dtype and qkv.is_contiguous()))
+    _require((dgamma_q is None) == (dgamma_k is None) and (dgamma_q is None or gamma_q is not None))
+    _require(all(g is None or (g.dtype == torch.float32 and g.numel() == D and g.is_contiguous()) for g in (dgamma_q, dgamma_k)))
+    _on_current_device(dq, dkt, dv, qkv if reads else None, codes, scales, rstd, gamma_q, gamma_k, table, position_ids, dqkv, dgamma_q, dgamma_k,
+                       workspace)
+    if dgamma_q is not None:
+        workspace = _own_workspace(workspace, heads_norm_rotate_workspace(dqkv.dtype, B, T, Hq, Hk, D), dqkv.device, stream)
+    positions, rotary = _table_sizes(table)
+    rc = lib().slimfit_heads_norm_rotate_backward(
+        _dev(dq), _dev(dkt), _dev(dv), _dev(qkv) if reads else None, _dev(codes), _dev(scales), C.c_int32(bits), C.c_int32(block), _dev(rstd),
+        C.c_int32(_dt(dqkv)), C.c_int64(B), C.c_int32(T), C.c_int32(Hq), C.c_int32(Hk), C.c_int32(D), _dev(gamma_q), _dev(gamma_k), _dev(table),
+        C.c_int32(positions), C.c_int32(rotary), C.c_int32(pairing), _dev(position_ids), C.c_float(q_scale), _dev(dqkv), _dev(dgamma_q),
+        _dev(dgamma_k), _dev(workspace), C.c_size_t(0 if workspace is None else workspace.numel()), _stream(stream))
+    _check(rc, "heads_norm_rotate_backward")
 
 
 def product_workspace(M: int, N: int, K: int) -> int:

@@ -51,6 +51,13 @@ inline void launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t lds, hipS
 }
 #endif
 
+// whether two ranges of bytes share any
+inline bool meet(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + b_bytes && y < x + a_bytes;
+}
+
 inline bool aligned_to(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline bool dtype_ok(int32_t dt) { return dt == SLIMFIT_F32 || dt == SLIMFIT_BF16; }
 inline size_t dtype_size(int32_t dt) { return dt == SLIMFIT_F32 ? 4 : 2; }
@@ -72,6 +79,17 @@ __device__ __forceinline__ void store_global(V *p, V v)
     if (NT) __builtin_nontemporal_store(v, p);
     else *p = v;
 }
+
+// The quotient of n < 2^31 by d >= 1: floor(((high word of m n) + n) / 2^s), s = ceil(log2 d), m = floor(2^32 (2^s - d) / d) + 1.
+struct Divide {
+    uint32_t m, s;
+    explicit Divide(uint32_t d) : s(0)
+    {
+        while (((uint64_t)1 << s) < d) ++s;
+        m = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << s) - d)) / d + 1);
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (__umulhi(m, n) + n) >> s; }
+};
 
 // ---- DPP lane exchange --------------------------------------------------------
 // A DPP "row" is 16 consecutive lanes.  The controls used here only permute
@@ -108,6 +126,28 @@ __device__ __forceinline__ uint32_t group_max_u32(uint32_t v, int G)
     if (G >= 64) {
         const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
         v = max(r[0], r[1]);
+    }
+    return v;
+}
+
+// sum over such a group, in an order of its own that every lane shares
+__device__ __forceinline__ float group_sum_f32(float v, int G)
+{
+    v += dpp_f32<kDppXor1>(v);
+    v += dpp_f32<kDppXor2>(v);
+    if (G >= 8) v += dpp_f32<kDppHalfMirror>(v);
+    if (G >= 16) v += dpp_f32<kDppMirror>(v);
+    if (G >= 32) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, v);
+        const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        const uint32_t a = r[0], b = r[1];                 // (a bit_cast of an element itself takes the vector's first)
+        v = __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+    }
+    if (G >= 64) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, v);
+        const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        const uint32_t a = r[0], b = r[1];
+        v = __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
     }
     return v;
 }

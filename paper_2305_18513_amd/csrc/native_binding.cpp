@@ -11,6 +11,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -29,7 +30,9 @@ namespace {
     X(softmax_prune) X(softmax_backward_pruned) X(prune_global_standardized) X(prune_global_workspace)                 \
     X(layernorm_forward) X(layernorm_backward) X(layernorm_backward_pruned) X(layernorm_forward_quant_pack)            \
     X(layernorm_backward_dequant) X(layernorm_param_grads) X(layernorm_param_grads_workspace) X(layer_delta_run)         \
-    X(split_heads) X(merge_heads) X(product)
+    X(split_heads) X(merge_heads) X(product) X(gated_quant_pack) X(gated_backward_dequant)                             \
+    X(heads_norm_rotate_forward) X(heads_norm_rotate_backward) X(heads_norm_rotate_workspace)                          \
+    X(weight_grad_dequant) X(weight_grad_dequant_workspace)
 #define X(name) decltype(&slimfit_##name) name##_fn = nullptr;
 SLIMFIT_CALLS(X)
 #undef X
@@ -577,6 +580,174 @@ PyObject *product(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     SLIMFIT_RUN(product_fn(xp, yp, y_deep, M, N, K, op, nullptr, 0, st));
 }
 
+// every tensor on the current device, whose stream the library launches on
+template <typename... Ts>
+bool here(Ts... t)
+{
+    const auto now = c10::hip::current_device();
+    bool all = true;
+    ((all = all && (!t || t->get_device() == now)), ...);
+    return all;
+}
+
+PyObject *gated_quant_pack(PyObject *, PyObject *const *args, Py_ssize_t n_args)
+{
+    Args a(args, n_args, 10);
+    const at::Tensor *x = a.tensor();
+    const int32_t act = a.i32(), mode = a.i32(), bits = a.i32(), block = a.i32(), frac = a.i32();
+    const at::Tensor *y = a.tensor(), *codes = a.tensor_or_none(), *scales = a.tensor_or_none();
+    void *st = a.stream();
+    if (a.ok)
+        a.need(x->dim() == 2 && y->dim() == 2 && activation(x) && same_type(x, y) && x->size(0) == y->size(0) && x->size(1) == 2 * y->size(1) &&
+               (bits == 0 || (codes && cache_fits(x->numel(), mode, bits, block, codes, scales))) && here(x, y, codes, scales));
+    if (!a.ok) return general();
+    const void *xp = ptr(x);
+    void *yp = ptr(y);
+    auto *cp = ptr<uint8_t>(codes);
+    auto *sp = ptr<float>(scales);
+    const int32_t dt = dtype_of(x);
+    const int64_t rows = y->size(0), F = y->size(1);
+    SLIMFIT_RUN(gated_quant_pack_fn(xp, dt, rows, F, act, mode, bits, block, frac, yp, cp, sp, st));
+}
+
+PyObject *gated_backward_dequant(PyObject *, PyObject *const *args, Py_ssize_t n_args)
+{
+    Args a(args, n_args, 10);
+    const at::Tensor *codes = a.tensor(), *scales = a.tensor_or_none();
+    const int32_t act = a.i32(), mode = a.i32(), bits = a.i32(), block = a.i32(), frac = a.i32();
+    const at::Tensor *dy = a.tensor(), *dx = a.tensor();
+    void *st = a.stream();
+    if (a.ok)
+        a.need(dx->dim() == 2 && dy->dim() == 2 && activation(dx) && same_type(dx, dy) && dx->size(0) == dy->size(0) &&
+               dx->size(1) == 2 * dy->size(1) && cache_fits(dx->numel(), mode, bits, block, codes, scales) && here(codes, scales, dy, dx));
+    if (!a.ok) return general();
+    auto *cp = ptr<uint8_t>(codes);
+    auto *sp = ptr<float>(scales);
+    const void *gp = ptr(dy);
+    void *dp = ptr(dx);
+    const int32_t dt = dtype_of(dx);
+    const int64_t rows = dy->size(0), F = dy->size(1);
+    SLIMFIT_RUN(gated_backward_dequant_fn(cp, sp, rows, F, act, mode, bits, block, frac, gp, dp, dt, st));
+}
+
+PyObject *weight_grad_dequant(PyObject *, PyObject *const *args, Py_ssize_t n_args)
+{
+    Args a(args, n_args, 8);
+    const at::Tensor *dy = a.tensor(), *codes = a.tensor(), *scales = a.tensor();
+    const int32_t bits = a.i32(), block = a.i32();
+    const at::Tensor *dw = a.tensor(), *workspace = a.tensor_or_none();
+    void *st = a.stream();
+    int64_t M = 0, N = 0, K = 0;
+    size_t need = 0;
+    if (a.ok) {
+        a.need(dy->dim() == 2 && dw->dim() == 2 && activation(dy) && same_type(dy, dw) && dw->size(0) == dy->size(1));
+        if (a.ok) {
+            M = dy->size(0), N = dy->size(1), K = dw->size(1);
+            a.need(cache_fits(M * K, SLIMFIT_Q_BLOCK, bits, block, codes, scales) && here(dy, codes, scales, dw, workspace) &&
+                   weight_grad_dequant_workspace_fn(dtype_of(dy), block, M, N, K, &need) == SLIMFIT_OK);
+        }
+    }
+    Scratch w;
+    if (!a.ok || ((need > 0 || workspace) && !w.take(workspace, a.own_stream, need, dy))) return general();
+    const void *yp = ptr(dy);
+    auto *cp = ptr<uint8_t>(codes);
+    auto *sp = ptr<float>(scales);
+    void *wp = ptr(dw);
+    const int32_t dt = dtype_of(dy);
+    SLIMFIT_RUN(weight_grad_dequant_fn(yp, dt, cp, sp, bits, block, M, N, K, wp, w.at, w.bytes, st));
+}
+
+// What the two calls of heads_norm_rotate share: sizes, and that tensors agree with them.
+struct Heads {
+    int64_t B, T, Hq, Hk, D;
+    int32_t positions = 0, rotary = 0;
+    bool read(const at::Tensor *qkv, const at::Tensor *q, const at::Tensor *kt, const at::Tensor *v, const at::Tensor *gq, const at::Tensor *gk,
+              const at::Tensor *table, const at::Tensor *ids, const at::Tensor *rstd, const at::Tensor *codes, const at::Tensor *scales, int32_t bits,
+              int32_t block)
+    {
+        if (q->dim() != 4 || kt->dim() != 4 || v->dim() != 4 || qkv->dim() != 3) return false;
+        B = q->size(0), Hq = q->size(1), T = q->size(2), D = q->size(3), Hk = v->size(1);
+        if (Hq > INT32_MAX || T > INT32_MAX || D > INT32_MAX || Hk > INT32_MAX) return false;
+        if (v->size(0) != B || v->size(2) != T || v->size(3) != D || kt->size(0) != B || kt->size(1) != Hk || kt->size(2) != D || kt->size(3) != T ||
+            qkv->size(0) != B || qkv->size(1) != T || qkv->size(2) != (Hq + 2 * Hk) * D)
+            return false;
+        if (!activation(qkv) || !same_type(qkv, q) || !same_type(qkv, kt) || !same_type(qkv, v)) return false;
+        if ((gq == nullptr) != (gk == nullptr)) return false;
+        if (gq && (!f32(gq) || !f32(gk) || gq->numel() != D || gk->numel() != D || !rstd || !f32(rstd) || rstd->numel() < B * T * (Hq + Hk))) return false;
+        if (table) {
+            if (table->dim() != 2 || !f32(table) || table->size(0) > INT32_MAX || table->size(1) > INT32_MAX) return false;
+            positions = (int32_t)table->size(0), rotary = (int32_t)table->size(1);
+        }
+        if (ids && (!is(ids, at::kInt) || ids->numel() != B * T)) return false;
+        return bits == 0 || (codes && cache_fits(B * T * (Hq + Hk) * D, SLIMFIT_Q_BLOCK, bits, block, codes, scales));
+    }
+};
+
+PyObject *heads_norm_rotate_forward(PyObject *, PyObject *const *args, Py_ssize_t n_args)
+{
+    Args a(args, n_args, 17);
+    const at::Tensor *qkv = a.tensor(), *gq = a.tensor_or_none(), *gk = a.tensor_or_none();
+    const float eps = a.f32();
+    const at::Tensor *table = a.tensor_or_none();
+    const int32_t pairing = a.i32();
+    const at::Tensor *ids = a.tensor_or_none();
+    const float q_scale = a.f32();
+    const int32_t bits = a.i32(), block = a.i32();
+    const at::Tensor *q = a.tensor(), *kt = a.tensor(), *v = a.tensor(), *rstd = a.tensor_or_none(), *codes = a.tensor_or_none(),
+                     *scales = a.tensor_or_none();
+    void *st = a.stream();
+    Heads h;
+    if (a.ok)
+        a.need(h.read(qkv, q, kt, v, gq, gk, table, ids, rstd, codes, scales, bits, block) &&
+               here(qkv, gq, gk, table, ids, q, kt, v, rstd, codes, scales));
+    if (!a.ok) return general();
+    const void *xp = ptr(qkv);
+    const float *gqp = ptr<float>(gq), *gkp = ptr<float>(gk), *tp = ptr<float>(table);
+    const int32_t *ip = ptr<int32_t>(ids);
+    void *qp = ptr(q), *kp = ptr(kt), *vp = ptr(v);
+    float *rp = ptr<float>(rstd), *sp = ptr<float>(scales);
+    uint8_t *cp = ptr<uint8_t>(codes);
+    const int32_t dt = dtype_of(qkv);
+    SLIMFIT_RUN(heads_norm_rotate_forward_fn(xp, dt, h.B, (int32_t)h.T, (int32_t)h.Hq, (int32_t)h.Hk, (int32_t)h.D, gqp, gkp, eps, tp, h.positions,
+                                             h.rotary, pairing, ip, q_scale, bits, block, qp, kp, vp, rp, cp, sp, st));
+}
+
+PyObject *heads_norm_rotate_backward(PyObject *, PyObject *const *args, Py_ssize_t n_args)
+{
+    Args a(args, n_args, 20);
+    const at::Tensor *dq = a.tensor(), *dkt = a.tensor(), *dv = a.tensor(), *qkv = a.tensor_or_none(), *codes = a.tensor_or_none(),
+                     *scales = a.tensor_or_none();
+    const int32_t bits = a.i32(), block = a.i32();
+    const at::Tensor *rstd = a.tensor_or_none(), *gq = a.tensor_or_none(), *gk = a.tensor_or_none(), *table = a.tensor_or_none();
+    const int32_t pairing = a.i32();
+    const at::Tensor *ids = a.tensor_or_none();
+    const float q_scale = a.f32();
+    const at::Tensor *dqkv = a.tensor(), *dgq = a.tensor_or_none(), *dgk = a.tensor_or_none(), *workspace = a.tensor_or_none();
+    void *st = a.stream();
+    Heads h;
+    size_t need = 0;
+    const bool reads = gq && bits == 0;
+    if (a.ok) {
+        a.need(h.read(dqkv, dq, dkt, dv, gq, gk, table, ids, rstd, codes, scales, bits, block) &&
+               (!reads || (qkv && qkv->sizes() == dqkv->sizes() && same_type(qkv, dqkv))) && (dgq == nullptr) == (dgk == nullptr) &&
+               (!dgq || (gq && f32(dgq) && f32(dgk) && dgq->numel() == h.D && dgk->numel() == h.D)) &&
+               here(dq, dkt, dv, reads ? qkv : nullptr, codes, scales, rstd, gq, gk, table, ids, dqkv, dgq, dgk, workspace));
+        if (a.ok && dgq)
+            a.need(heads_norm_rotate_workspace_fn(dtype_of(dqkv), h.B, (int32_t)h.T, (int32_t)h.Hq, (int32_t)h.Hk, (int32_t)h.D, &need) == SLIMFIT_OK);
+    }
+    Scratch w;
+    if (!a.ok || (dgq && !w.take(workspace, a.own_stream, need, dqkv))) return general();
+    const void *qp = ptr(dq), *kp = ptr(dkt), *vp = ptr(dv), *xp = reads ? ptr(qkv) : nullptr;
+    const uint8_t *cp = ptr<uint8_t>(codes);
+    const float *sp = ptr<float>(scales), *rp = ptr<float>(rstd), *gqp = ptr<float>(gq), *gkp = ptr<float>(gk), *tp = ptr<float>(table);
+    const int32_t *ip = ptr<int32_t>(ids);
+    void *op = ptr(dqkv);
+    float *dgqp = ptr<float>(dgq), *dgkp = ptr<float>(dgk);
+    const int32_t dt = dtype_of(dqkv);
+    SLIMFIT_RUN(heads_norm_rotate_backward_fn(qp, kp, vp, xp, cp, sp, bits, block, rp, dt, h.B, (int32_t)h.T, (int32_t)h.Hq, (int32_t)h.Hk, (int32_t)h.D,
+                                              gqp, gkp, tp, h.positions, h.rotary, pairing, ip, q_scale, op, dgqp, dgkp, w.at, w.bytes, st));
+}
+
 // a C++ exception must not cross into the interpreter (torch's allocator raises one when memory runs out: the general
 // path, which asks again, raises torch's own)
 template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)>
@@ -620,7 +791,8 @@ PyMethodDef methods[] = {
     METHOD(restore_scores), METHOD(softmax_prune), METHOD(softmax_backward_pruned), METHOD(prune_global_standardized),
     METHOD(layernorm_forward), METHOD(layernorm_backward), METHOD(layernorm_backward_pruned), METHOD(layernorm_forward_quant_pack),
     METHOD(layernorm_backward_dequant), METHOD(layernorm_param_grads), METHOD(layer_delta_run), METHOD(split_heads), METHOD(merge_heads),
-    METHOD(product),
+    METHOD(product), METHOD(gated_quant_pack), METHOD(gated_backward_dequant), METHOD(heads_norm_rotate_forward),
+    METHOD(heads_norm_rotate_backward), METHOD(weight_grad_dequant),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
