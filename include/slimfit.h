@@ -593,7 +593,7 @@ int32_t slimfit_merge_heads(const void *q, const void *kt, const void *v, int32_
  *        to be a multiple of block (ERR_UNSUPPORTED).
  *  head_dim : a multiple of 4 (fp32) or 8 (bf16), at most 256; rotary_dim: a
  *        multiple of 8 (fp32) or 16 (bf16), at most head_dim; batch * tokens below
- *        2^31 (ERR_UNSUPPORTED).
+ *        2^31, a row of qkv at most 2^20 elements (ERR_UNSUPPORTED).
  *
  *  slimfit_heads_norm_rotate_backward : the gradients together again.  With g the
  *        gradient of a query (times q_scale) or key row, rotated back, x~ = x^ * rstd,

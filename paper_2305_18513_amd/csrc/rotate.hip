@@ -13,401 +13,570 @@
 // words apart) into their transposed place: 16 bytes along the tokens where those are aligned, single elements otherwise.
 #include "elements.hpp"
 
+#include <type_traits>
+
 namespace slimfit {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kPasses = 4;
+constexpr int kHeld = 2;                   // passes whose angles are held at a time
 constexpr int kTileWords = 4096 + 256;     // 1024 / L rows of 4 L + 1 words, L >= 4
 
 struct Shape {
     uint32_t rows, tokens, q_heads, kv_heads, dim;         // rows = batch * tokens
     uint32_t per, q_units, units;                          // heads a query (or value) unit, units of queries, of all
     uint32_t positions, half;                              // half = rotary_dim / 2; 0: no rotation
-    uint32_t adjacent, norm;
+    uint32_t adjacent;
     int group, block_shift;                                // lanes of a quantisation block; log2 of its elements
     float eps, inv_dim, q_scale;
     Divide by_tokens, by_dim, by_units;
 };
 
-// cos and signed sin of the E elements at e0 of a row: turned(y)[i] = y[i] c[i] + partner(y)[i] s[i]
-template <int E>
+// Workgroups go to the eight XCDs in turn; an XCD's take consecutive units, so that what the heads of a row write side by side
+// (codes, scales, rstd) becomes whole lines in its L2.
+__device__ __forceinline__ uint32_t in_turn(uint32_t b, uint32_t n)
+{
+    const uint32_t each = n / 8;
+    return b < each * 8 ? b % 8 * each + b / 8 : b;
+}
+
+// N floats, N * 4 bytes aligned
+template <int N>
+__device__ __forceinline__ void load_floats(const float *p, float (&f)[N])
+{
+    typedef float Run __attribute__((ext_vector_type(N < 4 ? N : 4)));
+#pragma unroll
+    for (int i = 0; i < N; i += N < 4 ? N : 4) {
+        const Run r = *reinterpret_cast<const Run *>(p + i);
+#pragma unroll
+        for (int k = 0; k < (N < 4 ? N : 4); ++k) f[i + k] = r[k];
+    }
+}
+// What the E elements at e0 of a row become: c x + s partner(x), without the row's rstd.  BACK: by the angle back.
+template <int E, bool BACK>
 __device__ __forceinline__ void load_angles(const float *__restrict__ table, const int32_t *__restrict__ ids, const Shape &z, uint32_t row, uint32_t t,
                                             uint32_t e0, float (&c)[E], float (&s)[E])
 {
 #pragma unroll
     for (int i = 0; i < E; ++i) { c[i] = 1.0f; s[i] = 0.0f; }
-    if (row >= z.rows || e0 >= 2 * z.half) return;
     const uint32_t place = ids ? (uint32_t)ids[row] : t;
-    if (place >= z.positions) return;                      // padding
+    if (e0 >= 2 * z.half || place >= z.positions) return;              // what is not turned, and padding
     const float *at = table + (int64_t)place * (2 * z.half);
     if (z.adjacent) {
-        at += e0 / 2;
+        float a[E / 2], b[E / 2];
+        load_floats<E / 2>(at + e0 / 2, a);
+        load_floats<E / 2>(at + z.half + e0 / 2, b);
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            c[i] = at[i / 2];
-            s[i] = i % 2 ? at[z.half + i / 2] : -at[z.half + i / 2];
+            c[i] = a[i / 2];
+            s[i] = (i % 2 == 0) != BACK ? -b[i / 2] : b[i / 2];
         }
     } else {
         const bool low = e0 < z.half;
         at += low ? e0 : e0 - z.half;
+        load_floats<E>(at, c);
+        load_floats<E>(at + z.half, s);
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            c[i] = at[i];
-            s[i] = low ? -at[z.half + i] : at[z.half + i];
-        }
+        for (int i = 0; i < E; ++i) s[i] = low != BACK ? -s[i] : s[i];
     }
 }
-// from: the lane that holds the partners (its own where the pairs are neighbours or nothing is turned).  BACK: by the angle back.
-template <int E, bool BACK>
-__device__ __forceinline__ void turn(float (&y)[E], const float (&c)[E], const float (&s)[E], int from, const Shape &z)
+// c and s times a factor and the gains of the elements and of their partners; from: the lane of those
+template <int E>
+__device__ __forceinline__ void weigh_angles(const float *__restrict__ gains, float factor, int from, const Shape &z, uint32_t e0, float (&c)[E], float (&s)[E])
 {
-    if (z.half == 0) return;
+    float own[E], other[E];
+    load_floats<E>(gains + e0, own);
+#pragma unroll
+    for (int i = 0; i < E; ++i) own[i] *= factor;
+    if (z.adjacent) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) other[i] = own[i ^ 1];
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i) other[i] = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(from * 4, __builtin_bit_cast(int, own[i])));
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        c[i] *= own[i];
+        s[i] *= other[i];
+    }
+}
+// c x + s partner(x) of a vector; from: the lane that holds the partners, where they are not its own neighbours
+template <typename T>
+__device__ __forceinline__ void turn(const typename Vec<T>::raw &x, const float (&f)[Vec<T>::V], const float (&c)[Vec<T>::V], const float (&s)[Vec<T>::V],
+                                     int from, const Shape &z, float (&y)[Vec<T>::V])
+{
+    constexpr int E = Vec<T>::V;
     float other[E];
     if (z.adjacent) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) other[i] = y[i ^ 1];
-    } else {
+        for (int i = 0; i < E; ++i) other[i] = f[i ^ 1];
+    } else {                                               // as they lie in memory: four words
+        const u32x4 mine = __builtin_bit_cast(u32x4, x);
+        u32x4 theirs;
 #pragma unroll
-        for (int i = 0; i < E; ++i)
-            other[i] = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(from * 4, __builtin_bit_cast(int, y[i])));
+        for (int i = 0; i < 4; ++i) {
+            const int word = (int)mine[i];
+            theirs[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(from * 4, word);
+        }
+        Vec<T>::unpack(__builtin_bit_cast(typename Vec<T>::raw, theirs), other);
     }
 #pragma unroll
-    for (int i = 0; i < E; ++i) y[i] = fmaf(other[i], BACK ? -s[i] : s[i], y[i] * c[i]);
+    for (int i = 0; i < E; ++i) y[i] = fmaf(other[i], s[i], f[i] * c[i]);
 }
 
-// A workgroup's rows of one key head between their two layouts.  One thread moves E tokens (of two elements in bf16) where
-// every token row begins on 16 bytes, one element otherwise.
-template <typename T, int ROWS, bool IN>
-__device__ __forceinline__ void through_tile(uint32_t *tile, uint32_t pitch, T *kt, const Shape &z, uint32_t row0, uint32_t head)
+// A workgroup's rows of one key head between their two layouts: a thread moves E tokens of WIDE elements, 16 bytes of each (a row of
+// tokens may begin anywhere: the card takes vectors at their elements' alignment), or one element at a time where a run of E
+// ends past its batch, or where no row is that long.
+template <typename T, int ROWS, bool IN, bool WHOLE>
+__device__ __forceinline__ void through(uint32_t *tile, uint32_t pitch, T *kt, const Shape &z, uint32_t row0, uint32_t head)
 {
-    constexpr int E = Vec<T>::V, WIDE = sizeof(T) == 2 ? 2 : 1;
-    auto place = [&](uint32_t row, uint32_t d) {           // of element d of this head of a token
-        const uint32_t b = z.by_tokens(row), t = row - b * z.tokens;
-        return kt + (((int64_t)b * z.kv_heads + head) * z.dim + d) * z.tokens + t;
+    constexpr uint32_t E = Vec<T>::V, WIDE = 4 / sizeof(T), RUNS = ROWS / E;
+    typedef uint32_t Run __attribute__((ext_vector_type(4), aligned(2)));
+    T *const elements = reinterpret_cast<T *>(tile);
+    const uint32_t step = pitch * WIDE;
+    // Rows that all begin on 16 bytes stream past the caches; of others, two workgroups share lines, which the L2 puts together
+    // (37 x 12 heads x 197 x 64 fp32 forward 36.3 -> 33.0 us and backward 45 -> 39; 8 x 8 x 2048 x 128 bf16, the other way, 104 -> 108).
+    auto fetch = [&](const T *at) { return load_global<WHOLE>(reinterpret_cast<const Run *>(at)); };
+    auto put = [&](T *at, Run v) { store_global<WHOLE>(reinterpret_cast<Run *>(at), v); };
+    auto one = [&](T *at, uint32_t r, uint32_t d) {
+        if constexpr (IN) elements[r * step + d] = *at;
+        else *at = elements[r * step + d];
     };
-    if (z.tokens % E == 0) {
-        constexpr uint32_t CHUNKS = ROWS / E;
-        for (uint32_t i = threadIdx.x; i < CHUNKS * (z.dim / WIDE); i += kThreads) {
-            const uint32_t r = i % CHUNKS * E, d = i / CHUNKS * WIDE;
-            if (row0 + r >= z.rows) continue;              // (rows is a multiple of E)
-            T *at = place(row0 + r, d);
-            uint32_t *words = tile + r * pitch + d / WIDE;
-            if constexpr (WIDE == 1) {
-                if constexpr (IN) {
-                    const u32x4 v = load_global<true>(reinterpret_cast<const u32x4 *>(at));
-#pragma unroll
-                    for (int e = 0; e < E; ++e) words[e * pitch] = v[e];
-                } else {
-                    u32x4 v;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) v[e] = words[e * pitch];
-                    store_global<true>(reinterpret_cast<u32x4 *>(at), v);
-                }
-            } else {
-                if constexpr (IN) {
-                    const u32x4 a = load_global<true>(reinterpret_cast<const u32x4 *>(at));
-                    const u32x4 b = load_global<true>(reinterpret_cast<const u32x4 *>(at + z.tokens));
-#pragma unroll
-                    for (int e = 0; e < E; e += 2) {
-                        words[e * pitch] = __builtin_amdgcn_perm(b[e / 2], a[e / 2], 0x05040100u);
-                        words[(e + 1) * pitch] = __builtin_amdgcn_perm(b[e / 2], a[e / 2], 0x07060302u);
-                    }
-                } else {
-                    u32x4 a, b;
-#pragma unroll
-                    for (int e = 0; e < E; e += 2) {
-                        const uint32_t x = words[e * pitch], y = words[(e + 1) * pitch];
-                        a[e / 2] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-                        b[e / 2] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-                    }
-                    store_global<true>(reinterpret_cast<u32x4 *>(at), a);
-                    store_global<true>(reinterpret_cast<u32x4 *>(at + z.tokens), b);
-                }
-            }
+    if (!WHOLE && z.tokens < E) {                          // along the elements, then the tokens
+        for (uint32_t i = threadIdx.x; i < ROWS * z.dim; i += kThreads) {
+            const uint32_t r = z.by_dim(i), d = i - r * z.dim, row = row0 + r, b = z.by_tokens(row), t = row - b * z.tokens;
+            if (row < z.rows) one(kt + (((int64_t)b * z.kv_heads + head) * z.dim + d) * z.tokens + t, r, d);
         }
         return;
     }
-    T *elements = reinterpret_cast<T *>(tile);
-    const uint32_t step = pitch * (4 / sizeof(T));
-    const bool along = z.tokens >= 8;                      // along the tokens, or (few of them) along the elements
-    for (uint32_t i = threadIdx.x; i < ROWS * z.dim; i += kThreads) {
-        const uint32_t q = along ? i / ROWS : z.by_dim(i);
-        const uint32_t r = along ? i % ROWS : q, d = along ? q : i - q * z.dim;
-        if (row0 + r >= z.rows) continue;
-        if constexpr (IN) elements[r * step + d] = *place(row0 + r, d);
-        else *place(row0 + r, d) = elements[r * step + d];
+    for (uint32_t i = threadIdx.x; i < RUNS * (z.dim / WIDE); i += kThreads) {
+        const uint32_t r = i % RUNS * E, d = i / RUNS * WIDE, row = row0 + r;
+        if (row >= z.rows) continue;
+        const uint32_t b = z.by_tokens(row), t = row - b * z.tokens;
+        T *at = kt + (((int64_t)b * z.kv_heads + head) * z.dim + d) * z.tokens + t;
+        if (!WHOLE && t + E > z.tokens) {
+            for (uint32_t e = 0; e < E && row + e < z.rows; ++e) {
+                const uint32_t bb = z.by_tokens(row + e), tt = row + e - bb * z.tokens;
+                T *to = kt + (((int64_t)bb * z.kv_heads + head) * z.dim + d) * z.tokens + tt;
+                for (uint32_t k = 0; k < WIDE; ++k) one(to + (int64_t)k * z.tokens, r + e, d + k);
+            }
+            continue;
+        }
+        uint32_t *words = tile + r * pitch + d / WIDE;
+        if constexpr (WIDE == 1) {
+            if constexpr (IN) {
+                const Run v = fetch(at);
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e) words[e * pitch] = v[e];
+            } else {
+                Run v;
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e) v[e] = words[e * pitch];
+                put(at, v);
+            }
+        } else {
+            T *const next = at + z.tokens;
+            if constexpr (IN) {
+                const Run v = fetch(at);
+                const Run u = fetch(next);
+#pragma unroll
+                for (uint32_t e = 0; e < E; e += 2) {
+                    words[e * pitch] = __builtin_amdgcn_perm(u[e / 2], v[e / 2], 0x05040100u);
+                    words[(e + 1) * pitch] = __builtin_amdgcn_perm(u[e / 2], v[e / 2], 0x07060302u);
+                }
+            } else {
+                Run v, u;
+#pragma unroll
+                for (uint32_t e = 0; e < E; e += 2) {
+                    const uint32_t x = words[e * pitch], y = words[(e + 1) * pitch];
+                    v[e / 2] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                    u[e / 2] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+                }
+                put(at, v);
+                put(next, u);
+            }
+        }
     }
 }
 
-template <typename T, int L, int BITS>
+template <typename T, int ROWS, bool IN>
+__device__ __forceinline__ void through_tile(uint32_t *tile, uint32_t pitch, T *kt, const Shape &z, uint32_t row0, uint32_t head)
+{
+    if (z.tokens % Vec<T>::V == 0) through<T, ROWS, IN, true>(tile, pitch, kt, z, row0, head);
+    else through<T, ROWS, IN, false>(tile, pitch, kt, z, row0, head);
+}
+
+// the T at byte `at` (below 2^31) from a place that is the same for the workgroup
+template <typename P, typename T>
+__device__ __forceinline__ P *beyond(T *base, uint32_t at)
+{
+    using C = std::conditional_t<std::is_const_v<T>, const char, char>;
+    return reinterpret_cast<P *>(reinterpret_cast<C *>(base) + at);
+}
+
+// A thread's place: rows row0 + pass * SLOTS + slot, elements e0 .. e0 + E - 1 of each head.  Lanes past a head's end do what the
+// lanes L / 2 before them do (whole quantisation blocks, where there are any), rows past the last what the last does, to the same
+// places: no load or store stands behind a branch, and each is waited for by itself.  counts: 0 for such a lane, 1 otherwise.
+template <typename T, int L>
+struct Place {
+    static constexpr int E = Vec<T>::V, SLOTS = kThreads / L, ROWS = SLOTS * kPasses;
+    uint32_t unit, tiled, row0, lane, slot, e0;
+    float counts;
+    __device__ __forceinline__ Place(const Shape &z, uint32_t first)
+    {
+        const uint32_t at = first + in_turn(blockIdx.x, gridDim.x);
+        tiled = __builtin_amdgcn_readfirstlane(z.by_units(at));
+        unit = at - tiled * z.units;
+        row0 = tiled * ROWS;
+        lane = threadIdx.x % L;
+        slot = threadIdx.x / L;
+        const uint32_t vectors = z.dim / E;                // more than L / 2, or L is 4 and nothing is cached
+        counts = lane < vectors ? 1.0f : 0.0f;
+        if (lane >= vectors) lane = lane >= L / 2 && lane - L / 2 < vectors ? lane - L / 2 : 0;
+        e0 = lane * E;
+    }
+    __device__ __forceinline__ uint32_t line(const Shape &z, int pass) const    // of the tile's rows
+    {
+        return min(pass * SLOTS + slot, z.rows - 1 - row0);
+    }
+    __device__ __forceinline__ bool twice(const Shape &z, int pass) const { return row0 + pass * SLOTS + slot >= z.rows; }
+    // element e0 of a head of a token in a tensor (batch, heads, tokens, dim)
+    __device__ __forceinline__ int64_t apart(const Shape &z, uint32_t row, uint32_t heads) const
+    {
+        const uint32_t batch = z.by_tokens(row), token = row - batch * z.tokens;
+        return ((int64_t)batch * heads * z.tokens + token) * z.dim + e0;
+    }
+    __device__ __forceinline__ int partner(const Shape &z) const               // the lane of the wave that holds this one's partners
+    {
+        const int own = (threadIdx.x & (kWave - 1) & ~(L - 1)) + lane;
+        return z.adjacent || e0 >= 2 * z.half ? own : e0 < z.half ? own + (int)(z.half / E) : own - (int)(z.half / E);
+    }
+};
+
+// The values' way between the rows and (batch, head, token, element)
+template <typename T, int L, bool SPLIT>
+__device__ __forceinline__ void copy_values(const Place<T, L> &w, const Shape &z, T *rows, T *v)
+{
+    using raw = typename Vec<T>::raw;
+    const uint32_t every = z.q_heads + 2 * z.kv_heads, h0 = (w.unit - z.q_units - z.kv_heads) * z.per, h1 = min(h0 + z.per, z.kv_heads);
+    rows += ((int64_t)w.row0 * every + z.q_heads + z.kv_heads) * z.dim;
+    uint32_t at[kPasses];
+    T *to[kPasses];
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+        const uint32_t line = w.line(z, p);
+        at[p] = (line * every * z.dim + w.e0) * (uint32_t)sizeof(T);
+        to[p] = v + w.apart(z, w.row0 + line, z.kv_heads);
+    }
+    const int64_t head = (int64_t)z.tokens * z.dim;
+    for (uint32_t h = h0; h < h1; ++h) {
+        T *const base = rows + h * z.dim;
+        raw x[kPasses];
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) x[p] = load_global<true>(SPLIT ? beyond<const raw>(base, at[p]) : reinterpret_cast<const raw *>(to[p] + h * head));
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) store_global<true>(SPLIT ? reinterpret_cast<raw *>(to[p] + h * head) : beyond<raw>(base, at[p]), x[p]);
+    }
+}
+
+// MODE: no norm, a norm and no cache, or the bits of its cache
+constexpr int kNoNorm = 0, kNoCache = 1;
+
+template <typename T, int L, int MODE, bool KEY>
+__device__ __forceinline__ void forward_heads(const Place<T, L> &w, const Shape &z, uint32_t *tile, const T *qkv, const float *gains, const float *table,
+                                              const int32_t *ids, T *q, float *rstd, uint8_t *codes, float *scales)
+{
+    using raw = typename Vec<T>::raw;
+    constexpr int E = Vec<T>::V, BITS = MODE > kNoCache ? MODE : 8;
+    const uint32_t every = z.q_heads + 2 * z.kv_heads, normed = z.q_heads + z.kv_heads;
+    const uint32_t h0 = KEY ? z.q_heads + w.unit - z.q_units : w.unit * z.per, h1 = KEY ? h0 + 1 : min(h0 + z.per, z.q_heads);
+    const int from = w.partner(z);
+    const uint32_t pitch = z.dim * sizeof(T) / 4 + 1;
+    const int64_t head = (int64_t)z.tokens * z.dim;
+    for (int half = 0; half < kPasses; half += kHeld) {
+        float c[kHeld][E], s[kHeld][E];
+        uint32_t line[kHeld], at[kHeld];                   // the row in the tile, the vector of its first head
+        T *to[kHeld];
+#pragma unroll
+        for (int p = 0; p < kHeld; ++p) {
+            line[p] = w.line(z, half + p);
+            const uint32_t row = w.row0 + line[p];
+            at[p] = (line[p] * every * z.dim + w.e0) * (uint32_t)sizeof(T);
+            if constexpr (!KEY) to[p] = q + w.apart(z, row, z.q_heads);
+            load_angles<E, false>(table, ids, z, row, row - z.by_tokens(row) * z.tokens, w.e0, c[p], s[p]);
+            if constexpr (MODE != kNoNorm) {
+                weigh_angles<E>(gains, KEY ? 1.0f : z.q_scale, from, z, w.e0, c[p], s[p]);
+            } else if constexpr (!KEY) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) { c[p][i] *= z.q_scale; s[p][i] *= z.q_scale; }
+            }
+        }
+        const T *rows = qkv + (int64_t)w.row0 * every * z.dim;
+        raw x[kHeld];
+        auto load = [&](uint32_t h) {
+#pragma unroll
+            for (int p = 0; p < kHeld; ++p) x[p] = load_global<true>(beyond<const raw>(rows + h * z.dim, at[p]));
+        };
+        auto take = [&](uint32_t h, auto more) {
+            raw now[kHeld];
+            float f[kHeld][E];
+#pragma unroll
+            for (int p = 0; p < kHeld; ++p) {
+                now[p] = x[p];
+                Vec<T>::unpack(now[p], f[p]);
+            }
+            if constexpr (decltype(more)::value) load(h + 1);
+            if constexpr (MODE > kNoCache) {
+                uint32_t a[kHeld];
+#pragma unroll
+                for (int p = 0; p < kHeld; ++p) {
+                    float m = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < E; ++i) m = fmaxf(m, fabsf(f[p][i]));
+                    a[p] = group_max_u32(__builtin_bit_cast(uint32_t, m), z.group);
+                }
+                float mult[kHeld], scale;
+                quad_scales<BITS, kHeld>(a, (int)threadIdx.x, mult, scale);
+                static_assert(kHeld == 2, "a lane's scale is that of the pass of its lowest bit");
+                const uint32_t own = threadIdx.x & 1 ? line[1] : line[0];
+                *beyond<float>(scales + ((((int64_t)w.row0 * normed + h) * z.dim) >> z.block_shift), (own * normed * z.dim + w.e0) >> z.block_shift << 2) = scale;
+                uint8_t *base = codes + ((int64_t)w.row0 * normed + h) * z.dim * BITS / 8;
+#pragma unroll
+                for (int p = 0; p < kHeld; ++p) {
+                    uint32_t word[2];
+                    pack_codes<BITS, E>(f[p], mult[p], word);
+                    const uint32_t place = (line[p] * normed * z.dim + w.e0) * BITS / 8;
+                    if (E * BITS == 16) *beyond<uint16_t>(base, place) = (uint16_t)word[0];
+                    else if (E * BITS == 32) *beyond<uint32_t>(base, place) = word[0];
+                    else *beyond<u32x2>(base, place) = u32x2{word[0], word[1]};
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < kHeld; ++p) {
+                float y[E];
+                turn<T>(now[p], f[p], c[p], s[p], from, z, y);
+                if constexpr (MODE != kNoNorm) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < E; ++i) sum = fmaf(f[p][i], f[p][i], sum);
+                    const float r = __builtin_amdgcn_rsqf(fmaf(group_sum_f32(sum * w.counts, L), z.inv_dim, z.eps));
+                    *beyond<float>(rstd + ((int64_t)w.row0 * normed + h), line[p] * normed * 4) = r;
+#pragma unroll
+                    for (int i = 0; i < E; ++i) y[i] *= r;
+                }
+                const raw out = Vec<T>::pack(y);
+                if constexpr (!KEY) {
+                    store_global<true>(reinterpret_cast<raw *>(to[p] + h * head), out);
+                } else {
+                    uint32_t *words = tile + line[p] * pitch + w.lane * 4;
+                    const u32x4 held = __builtin_bit_cast(u32x4, out);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) words[i] = held[i];
+                }
+            }
+        };
+        load(h0);
+        for (uint32_t h = h0; h + 1 < h1; ++h) take(h, std::true_type{});
+        take(h1 - 1, std::false_type{});
+    }
+}
+
+template <typename T, int L, int MODE>
 __global__ void __launch_bounds__(kThreads)
 forward_kernel(const T *__restrict__ qkv, const float *__restrict__ gamma_q, const float *__restrict__ gamma_k, const float *__restrict__ table,
                const int32_t *__restrict__ ids, T *__restrict__ q, T *__restrict__ kt, T *__restrict__ v, float *__restrict__ rstd,
                uint8_t *__restrict__ codes, float *__restrict__ scales, Shape z, uint32_t first)
 {
-    using raw = typename Vec<T>::raw;
-    constexpr int E = Vec<T>::V, SLOTS = kThreads / L, ROWS = SLOTS * kPasses;
     __shared__ uint32_t tile[kTileWords];
-    const uint32_t at = first + blockIdx.x, tiled = z.by_units(at), unit = at - tiled * z.units, row0 = tiled * ROWS;
-    const uint32_t lane = threadIdx.x % L, slot = threadIdx.x / L, e0 = lane * E;
-    const bool in_head = e0 < z.dim;
-    const uint32_t every = z.q_heads + 2 * z.kv_heads, normed = z.q_heads + z.kv_heads;
-    uint32_t row[kPasses], batch[kPasses], token[kPasses];
-#pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        row[p] = row0 + p * SLOTS + slot;
-        batch[p] = z.by_tokens(row[p]);
-        token[p] = row[p] - batch[p] * z.tokens;
-    }
-    auto load = [&](uint32_t head, raw(&to)[kPasses]) {    // head of the projection's row
-#pragma unroll
-        for (int p = 0; p < kPasses; ++p) {
-            to[p] = raw{};
-            if (row[p] < z.rows && in_head) to[p] = load_global<true>(reinterpret_cast<const raw *>(qkv + ((int64_t)row[p] * every + head) * z.dim + e0));
-        }
-    };
-    if (unit >= z.q_units + z.kv_heads) {                  // values
-        const uint32_t h0 = (unit - z.q_units - z.kv_heads) * z.per, h1 = min(h0 + z.per, z.kv_heads);
-        for (uint32_t h = h0; h < h1; ++h) {
-            raw x[kPasses];
-            load(normed + h, x);
-#pragma unroll
-            for (int p = 0; p < kPasses; ++p)
-                if (row[p] < z.rows && in_head)
-                    store_global<true>(reinterpret_cast<raw *>(v + (((int64_t)batch[p] * z.kv_heads + h) * z.tokens + token[p]) * z.dim + e0), x[p]);
-        }
-        return;
-    }
-    const bool key = unit >= z.q_units;
-    const uint32_t h0 = key ? z.q_heads + unit - z.q_units : unit * z.per, h1 = key ? h0 + 1 : min(h0 + z.per, z.q_heads);
-    float c[kPasses][E], s[kPasses][E], gamma[E];
-    const int mine = threadIdx.x & (kWave - 1);
-    int from = mine;
-    if (!z.adjacent && e0 < 2 * z.half) from += (e0 < z.half ? 1 : -1) * (int)(z.half / E);
-#pragma unroll
-    for (int p = 0; p < kPasses; ++p) load_angles<E>(table, ids, z, row[p], token[p], e0, c[p], s[p]);
-    const float factor = key ? 1.0f : z.q_scale;
-    {
-        const float *g = key ? gamma_k : gamma_q;
-#pragma unroll
-        for (int i = 0; i < E; ++i) gamma[i] = z.norm && in_head ? g[e0 + i] : 1.0f;
-    }
-    const uint32_t pitch = z.dim * sizeof(T) / 4 + 1;
-    for (uint32_t h = h0; h < h1; ++h) {
-        raw x[kPasses];
-        load(h, x);
-        float f[kPasses][E];
-#pragma unroll
-        for (int p = 0; p < kPasses; ++p) Vec<T>::unpack(x[p], f[p]);
-        if constexpr (BITS != 0) {
-            uint32_t a[kPasses];
-#pragma unroll
-            for (int p = 0; p < kPasses; ++p) {
-                float m = 0.0f;
-#pragma unroll
-                for (int i = 0; i < E; ++i) m = fmaxf(m, fabsf(f[p][i]));
-                a[p] = group_max_u32(__builtin_bit_cast(uint32_t, m), z.group);
-            }
-            float mult[kPasses], scale;
-            quad_scales<BITS, kPasses>(a, (int)threadIdx.x, mult, scale);
-            const uint32_t own = threadIdx.x & (z.group - 1), own_row = row0 + own * SLOTS + slot;
-            if (own < kPasses && own_row < z.rows && in_head)            // lanes 0 .. 3 of a block store a pass's scale each
-                scales[(((int64_t)own_row * normed + h) * z.dim + e0) >> z.block_shift] = scale;
-#pragma unroll
-            for (int p = 0; p < kPasses; ++p) {
-                if (row[p] >= z.rows || !in_head) continue;
-                uint32_t w[2];
-                pack_codes<BITS, E>(f[p], mult[p], w);
-                uint8_t *dst = codes + (((int64_t)row[p] * normed + h) * z.dim + e0) * BITS / 8;
-                if (E * BITS == 16) store_global<true>(reinterpret_cast<uint16_t *>(dst), (uint16_t)w[0]);
-                else if (E * BITS == 32) store_global<true>(reinterpret_cast<uint32_t *>(dst), w[0]);
-                else store_global<true>(reinterpret_cast<u32x2 *>(dst), u32x2{w[0], w[1]});
-            }
-        }
-#pragma unroll
-        for (int p = 0; p < kPasses; ++p) {
-            if (z.norm) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int i = 0; i < E; ++i) sum = fmaf(f[p][i], f[p][i], sum);
-                const float r = __builtin_amdgcn_rsqf(fmaf(group_sum_f32(sum, L), z.inv_dim, z.eps));
-                if (lane == 0 && row[p] < z.rows) rstd[(int64_t)row[p] * normed + h] = r;
-#pragma unroll
-                for (int i = 0; i < E; ++i) f[p][i] = f[p][i] * r * gamma[i];
-            }
-            turn<E, false>(f[p], c[p], s[p], from, z);
-#pragma unroll
-            for (int i = 0; i < E; ++i) f[p][i] *= factor;
-            const raw out = Vec<T>::pack(f[p]);
-            if (!key) {
-                if (row[p] < z.rows && in_head)
-                    store_global<true>(reinterpret_cast<raw *>(q + (((int64_t)batch[p] * z.q_heads + h) * z.tokens + token[p]) * z.dim + e0), out);
-            } else if (in_head) {
-                uint32_t *words = tile + (p * SLOTS + slot) * pitch + lane * 4;
-                const u32x4 held = __builtin_bit_cast(u32x4, out);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) words[i] = held[i];
-            }
-        }
-    }
-    if (key) {                                             // (uniform for the workgroup)
+    const Place<T, L> w(z, first);
+    if (w.unit >= z.q_units + z.kv_heads) {
+        copy_values<T, L, true>(w, z, const_cast<T *>(qkv), v);
+    } else if (w.unit < z.q_units) {
+        forward_heads<T, L, MODE, false>(w, z, tile, qkv, gamma_q, table, ids, q, rstd, codes, scales);
+    } else {
+        forward_heads<T, L, MODE, true>(w, z, tile, qkv, gamma_k, table, ids, q, rstd, codes, scales);
         __syncthreads();
-        through_tile<T, ROWS, false>(tile, pitch, kt, z, row0, h0 - z.q_heads);
+        through_tile<T, Place<T, L>::ROWS, false>(tile, z.dim * sizeof(T) / 4 + 1, kt, z, w.row0, w.unit - z.q_units);
+    }
+}
+
+// sums: of g x~, over the thread's rows
+template <typename T, int L, int MODE, bool KEY>
+__device__ __forceinline__ void backward_heads(const Place<T, L> &w, const Shape &z, const uint32_t *tile, const T *dq, const T *qkv, const uint8_t *codes,
+                                               const float *scales, const float *rstd, const float *gains, const float *table, const int32_t *ids, T *dqkv,
+                                               float (&sums)[Vec<T>::V])
+{
+    using raw = typename Vec<T>::raw;
+    constexpr int E = Vec<T>::V, BITS = MODE > kNoCache ? MODE : 8;
+    const uint32_t every = z.q_heads + 2 * z.kv_heads, normed = z.q_heads + z.kv_heads;
+    const uint32_t h0 = KEY ? z.q_heads + w.unit - z.q_units : w.unit * z.per, h1 = KEY ? h0 + 1 : min(h0 + z.per, z.q_heads);
+    const int from = w.partner(z);
+    const uint32_t pitch = z.dim * sizeof(T) / 4 + 1;
+    const int64_t head = (int64_t)z.tokens * z.dim;
+    float gamma[MODE == kNoNorm ? 1 : E];
+    if constexpr (MODE != kNoNorm) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) gamma[i] = gains[w.e0 + i];
+    }
+    for (int half = 0; half < kPasses; half += kHeld) {
+        float c[kHeld][E], s[kHeld][E], counts[kHeld];
+        uint32_t line[kHeld];
+        const T *at[kHeld];
+#pragma unroll
+        for (int p = 0; p < kHeld; ++p) {
+            line[p] = w.line(z, half + p);
+            counts[p] = w.twice(z, half + p) ? 0.0f : 1.0f;
+            const uint32_t row = w.row0 + line[p];
+            if constexpr (!KEY) at[p] = dq + w.apart(z, row, z.q_heads);
+            load_angles<E, true>(table, ids, z, row, row - z.by_tokens(row) * z.tokens, w.e0, c[p], s[p]);
+            if constexpr (!KEY) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) { c[p][i] *= z.q_scale; s[p][i] *= z.q_scale; }
+            }
+        }
+        raw grad[kHeld], x[kHeld];
+        uint32_t word[kHeld][2];
+        float step[kHeld], r[kHeld];
+        auto load = [&](uint32_t h) {
+#pragma unroll
+            for (int p = 0; p < kHeld; ++p) {
+                if constexpr (KEY) {
+                    const uint32_t *words = tile + line[p] * pitch + w.lane * 4;
+                    grad[p] = __builtin_bit_cast(raw, u32x4{words[0], words[1], words[2], words[3]});
+                } else {
+                    grad[p] = load_global<true>(reinterpret_cast<const raw *>(at[p] + h * head));
+                }
+                if constexpr (MODE == kNoCache) {
+                    x[p] = load_global<true>(beyond<const raw>(qkv + ((int64_t)w.row0 * every + h) * z.dim, (line[p] * every * z.dim + w.e0) * (uint32_t)sizeof(T)));
+                } else if constexpr (MODE > kNoCache) {
+                    const uint8_t *base = codes + ((int64_t)w.row0 * normed + h) * z.dim * BITS / 8;
+                    const uint32_t place = line[p] * normed * z.dim + w.e0;
+                    word[p][1] = 0u;
+                    if (E * BITS == 16) word[p][0] = *beyond<const uint16_t>(base, place * BITS / 8);
+                    else if (E * BITS == 32) word[p][0] = *beyond<const uint32_t>(base, place * BITS / 8);
+                    else {
+                        const u32x2 t = *beyond<const u32x2>(base, place * BITS / 8);
+                        word[p][0] = t.x;
+                        word[p][1] = t.y;
+                    }
+                    step[p] = *beyond<const float>(scales + ((((int64_t)w.row0 * normed + h) * z.dim) >> z.block_shift), place >> z.block_shift << 2);
+                }
+                if constexpr (MODE != kNoNorm) r[p] = *beyond<const float>(rstd + ((int64_t)w.row0 * normed + h), line[p] * normed * 4);
+            }
+        };
+        auto take = [&](uint32_t h, auto more) {
+            T *const rows = dqkv + ((int64_t)w.row0 * every + h) * z.dim;
+            float g[kHeld][E], xn[kHeld][E], root[kHeld];
+#pragma unroll
+            for (int p = 0; p < kHeld; ++p) {
+                float f[E];
+                Vec<T>::unpack(grad[p], f);
+                turn<T>(grad[p], f, c[p], s[p], from, z, g[p]);
+                if constexpr (MODE == kNoCache) {
+                    root[p] = r[p];
+                    Vec<T>::unpack(x[p], xn[p]);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) xn[p][i] *= root[p];
+                } else if constexpr (MODE > kNoCache) {
+                    root[p] = r[p];
+                    const float by = step[p] * root[p];
+#pragma unroll
+                    for (int i = 0; i < E; ++i) xn[p][i] = (float)code_field<BITS>(word[p][i * BITS / 32], i % (32 / BITS)) * by;
+                }
+            }
+            if constexpr (decltype(more)::value) load(h + 1);
+#pragma unroll
+            for (int p = 0; p < kHeld; ++p) {
+                if constexpr (MODE != kNoNorm) {
+                    float dot = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < E; ++i) {
+                        sums[i] = fmaf(g[p][i] * counts[p], xn[p][i], sums[i]);
+                        g[p][i] *= gamma[i];
+                        dot = fmaf(g[p][i], xn[p][i], dot);
+                    }
+                    dot = group_sum_f32(dot * w.counts, L) * z.inv_dim;
+#pragma unroll
+                    for (int i = 0; i < E; ++i) g[p][i] = root[p] * fmaf(-xn[p][i], dot, g[p][i]);
+                }
+                store_global<true>(beyond<raw>(rows, (line[p] * every * z.dim + w.e0) * (uint32_t)sizeof(T)), Vec<T>::pack(g[p]));
+            }
+        };
+        load(h0);
+        for (uint32_t h = h0; h + 1 < h1; ++h) take(h, std::true_type{});
+        take(h1 - 1, std::false_type{});
     }
 }
 
 // partial: [units of queries, units of keys] x row tiles x dim sums of a workgroup each, or null where they are not asked for
-template <typename T, int L, int BITS>
+template <typename T, int L, int MODE>
 __global__ void __launch_bounds__(kThreads)
 backward_kernel(const T *__restrict__ dq, const T *__restrict__ dkt, const T *__restrict__ dv, const T *__restrict__ qkv, const uint8_t *__restrict__ codes,
                 const float *__restrict__ scales, const float *__restrict__ rstd, const float *__restrict__ gamma_q, const float *__restrict__ gamma_k,
                 const float *__restrict__ table, const int32_t *__restrict__ ids, T *__restrict__ dqkv, float *__restrict__ partial, Shape z, uint32_t first)
 {
-    using raw = typename Vec<T>::raw;
     constexpr int E = Vec<T>::V, SLOTS = kThreads / L, ROWS = SLOTS * kPasses;
     __shared__ uint32_t tile[kTileWords];
-    const uint32_t at = first + blockIdx.x, tiled = z.by_units(at), unit = at - tiled * z.units, row0 = tiled * ROWS;
-    const uint32_t lane = threadIdx.x % L, slot = threadIdx.x / L, e0 = lane * E;
-    const bool in_head = e0 < z.dim;
-    const uint32_t every = z.q_heads + 2 * z.kv_heads, normed = z.q_heads + z.kv_heads;
-    uint32_t row[kPasses], batch[kPasses], token[kPasses];
-    bool has[kPasses];
+    const Place<T, L> w(z, first);
+    float sums[E];
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        row[p] = row0 + p * SLOTS + slot;
-        batch[p] = z.by_tokens(row[p]);
-        token[p] = row[p] - batch[p] * z.tokens;
-        has[p] = row[p] < z.rows && in_head;
-    }
-    if (unit >= z.q_units + z.kv_heads) {                  // values
-        const uint32_t h0 = (unit - z.q_units - z.kv_heads) * z.per, h1 = min(h0 + z.per, z.kv_heads);
-        for (uint32_t h = h0; h < h1; ++h) {
-            raw x[kPasses];
-#pragma unroll
-            for (int p = 0; p < kPasses; ++p)
-                if (has[p]) x[p] = load_global<true>(reinterpret_cast<const raw *>(dv + (((int64_t)batch[p] * z.kv_heads + h) * z.tokens + token[p]) * z.dim + e0));
-#pragma unroll
-            for (int p = 0; p < kPasses; ++p)
-                if (has[p]) store_global<true>(reinterpret_cast<raw *>(dqkv + ((int64_t)row[p] * every + normed + h) * z.dim + e0), x[p]);
-        }
+    for (int i = 0; i < E; ++i) sums[i] = 0.0f;
+    if (w.unit >= z.q_units + z.kv_heads) {
+        copy_values<T, L, false>(w, z, dqkv, const_cast<T *>(dv));
         return;
     }
-    const bool key = unit >= z.q_units;
-    const uint32_t h0 = key ? z.q_heads + unit - z.q_units : unit * z.per, h1 = key ? h0 + 1 : min(h0 + z.per, z.q_heads);
-    const uint32_t pitch = z.dim * sizeof(T) / 4 + 1;
-    if (key) through_tile<T, ROWS, true>(tile, pitch, const_cast<T *>(dkt), z, row0, h0 - z.q_heads);
-    float c[kPasses][E], s[kPasses][E], gamma[E], sum_gamma[E];
-    const int mine = threadIdx.x & (kWave - 1);
-    int from = mine;
-    if (!z.adjacent && e0 < 2 * z.half) from += (e0 < z.half ? 1 : -1) * (int)(z.half / E);
-#pragma unroll
-    for (int p = 0; p < kPasses; ++p) load_angles<E>(table, ids, z, row[p], token[p], e0, c[p], s[p]);
-    const float factor = key ? 1.0f : z.q_scale;
-    {
-        const float *g = key ? gamma_k : gamma_q;
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            gamma[i] = z.norm && in_head ? g[e0 + i] : 1.0f;
-            sum_gamma[i] = 0.0f;
-        }
+    if (w.unit < z.q_units) {
+        backward_heads<T, L, MODE, false>(w, z, tile, dq, qkv, codes, scales, rstd, gamma_q, table, ids, dqkv, sums);
+    } else {
+        through_tile<T, ROWS, true>(tile, z.dim * sizeof(T) / 4 + 1, const_cast<T *>(dkt), z, w.row0, w.unit - z.q_units);
+        __syncthreads();
+        backward_heads<T, L, MODE, true>(w, z, tile, dq, qkv, codes, scales, rstd, gamma_k, table, ids, dqkv, sums);
     }
-    if (key) __syncthreads();
-    for (uint32_t h = h0; h < h1; ++h) {
-        raw grad[kPasses], x[kPasses];
-        uint32_t w[kPasses][2];
-        float step[kPasses], r[kPasses];
-#pragma unroll
-        for (int p = 0; p < kPasses; ++p) {
-            grad[p] = x[p] = raw{};
-            w[p][0] = w[p][1] = 0u;
-            step[p] = r[p] = 0.0f;
-            if (!has[p]) continue;
-            if (key) {
-                const uint32_t *words = tile + (p * SLOTS + slot) * pitch + lane * 4;
-                grad[p] = __builtin_bit_cast(raw, u32x4{words[0], words[1], words[2], words[3]});
-            } else {
-                grad[p] = load_global<true>(reinterpret_cast<const raw *>(dq + (((int64_t)batch[p] * z.q_heads + h) * z.tokens + token[p]) * z.dim + e0));
-            }
-            if (!z.norm) continue;
-            const int64_t element = ((int64_t)row[p] * normed + h) * z.dim + e0;
-            if constexpr (BITS == 0) {
-                x[p] = load_global<true>(reinterpret_cast<const raw *>(qkv + ((int64_t)row[p] * every + h) * z.dim + e0));
-            } else {
-                const uint8_t *src = codes + element * BITS / 8;
-                if (E * BITS == 16) w[p][0] = load_global<true>(reinterpret_cast<const uint16_t *>(src));
-                else if (E * BITS == 32) w[p][0] = load_global<true>(reinterpret_cast<const uint32_t *>(src));
-                else { const u32x2 t = load_global<true>(reinterpret_cast<const u32x2 *>(src)); w[p][0] = t.x; w[p][1] = t.y; }
-                step[p] = scales[element >> z.block_shift];
-            }
-            r[p] = rstd[(int64_t)row[p] * normed + h];
-        }
-#pragma unroll
-        for (int p = 0; p < kPasses; ++p) {
-            float g[E];
-            Vec<T>::unpack(grad[p], g);
-#pragma unroll
-            for (int i = 0; i < E; ++i) g[i] *= factor;
-            turn<E, true>(g, c[p], s[p], from, z);
-            if (z.norm) {
-                float xn[E], dot = 0.0f;
-                if constexpr (BITS == 0) {
-                    Vec<T>::unpack(x[p], xn);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < E; ++i) xn[i] = (float)code_field<BITS>(w[p][i * BITS / 32], i % (32 / BITS)) * step[p];
-                }
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    xn[i] *= r[p];
-                    sum_gamma[i] = fmaf(g[i], xn[i], sum_gamma[i]);
-                    g[i] *= gamma[i];
-                    dot = fmaf(g[i], xn[i], dot);
-                }
-                dot = group_sum_f32(dot, L) * z.inv_dim;
-#pragma unroll
-                for (int i = 0; i < E; ++i) g[i] = r[p] * fmaf(-xn[i], dot, g[i]);
-            }
-            if (has[p]) store_global<true>(reinterpret_cast<raw *>(dqkv + ((int64_t)row[p] * every + h) * z.dim + e0), Vec<T>::pack(g));
-        }
-    }
-    if (partial) {                                         // (uniform for the launch)
+    if constexpr (MODE != kNoNorm) {
+        if (!partial) return;                              // (uniform for the launch)
         __syncthreads();                                   // the tile is read
-        float *sums = reinterpret_cast<float *>(tile);     // SLOTS x dim
-        if (in_head) {
+        float *rows = reinterpret_cast<float *>(tile);     // SLOTS x dim
+        if (w.counts != 0.0f) {
 #pragma unroll
-            for (int i = 0; i < E; ++i) sums[slot * z.dim + e0 + i] = sum_gamma[i];
+            for (int i = 0; i < E; ++i) rows[w.slot * z.dim + w.e0 + i] = sums[i];
         }
         __syncthreads();
         const uint32_t tiles = (z.rows + ROWS - 1) / ROWS;
-        float *to = partial + ((int64_t)unit * tiles + tiled) * z.dim;
+        float *to = partial + ((int64_t)w.unit * tiles + w.tiled) * z.dim;
         for (uint32_t d = threadIdx.x; d < z.dim; d += kThreads) {
             float total = 0.0f;
-            for (int k = 0; k < SLOTS; ++k) total += sums[k * z.dim + d];
+            for (int k = 0; k < SLOTS; ++k) total += rows[k * z.dim + d];
             to[d] = total;
         }
     }
 }
 
-// dgamma[d] = sum over the partial sums of its side.  A workgroup: 16 columns, 16 slices of the rows.
-__global__ void __launch_bounds__(kThreads)
+// dgamma[d] = sum over the partial sums of its side.  A workgroup: 16 columns, 64 slices of the rows.
+constexpr int kGammaThreads = 1024;
+__global__ void __launch_bounds__(kGammaThreads)
 gamma_kernel(const float *__restrict__ partial, uint32_t dim, int64_t q_rows, int64_t k_rows, float *__restrict__ dgamma_q, float *__restrict__ dgamma_k)
 {
-    __shared__ double sums[kThreads];
+    constexpr int SLICES = kGammaThreads / 16;
+    __shared__ double sums[kGammaThreads];
     const uint32_t blocks = gridDim.x / 2, side = blockIdx.x / blocks, d = blockIdx.x % blocks * 16 + threadIdx.x % 16, slice = threadIdx.x / 16;
     const float *from = partial + (side ? q_rows * dim : 0);
     const int64_t n = side ? k_rows : q_rows;
     double total = 0.0;
     if (d < dim) {
 #pragma unroll 8
-        for (int64_t i = slice; i < n; i += 16) total += (double)from[i * dim + d];
+        for (int64_t i = slice; i < n; i += SLICES) total += (double)from[i * dim + d];
     }
     sums[threadIdx.x] = total;
     __syncthreads();
-    if (slice == 0 && d < dim) {
-        for (int k = 1; k < 16; ++k) total += sums[k * 16 + threadIdx.x];
-        (side ? dgamma_k : dgamma_q)[d] = (float)total;
+    if (slice < 4) {
+#pragma unroll
+        for (int k = 4; k < SLICES; k += 4) total += sums[k * 16 + threadIdx.x];
+        sums[threadIdx.x] = total;
     }
+    __syncthreads();
+    if (slice == 0 && d < dim) (side ? dgamma_k : dgamma_q)[d] = (float)((sums[threadIdx.x] + sums[threadIdx.x + 16]) + (sums[threadIdx.x + 32] + sums[threadIdx.x + 48]));
 }
 
 int lanes_of(int32_t dt, int32_t dim)
@@ -418,10 +587,10 @@ int lanes_of(int32_t dt, int32_t dim)
     return L;
 }
 
-// Heads a query (or value) workgroup takes one after the other: as many as leave four workgroups to a compute unit, at most 8.
+// Heads a query (or value) workgroup takes one after the other: as many as leave four workgroups to a compute unit, at most 4.
 int heads_each(int64_t tiles, int32_t heads)
 {
-    int per = 8;
+    int per = 4;
     while (per > 1 && tiles * ((heads + per - 1) / per) < 1024) per /= 2;
     return per;
 }
@@ -431,7 +600,7 @@ int32_t validate(int32_t dt, int64_t batch, int32_t tokens, int32_t q_heads, int
     if (!dtype_ok(dt) || batch < 0 || tokens < 0 || q_heads < 1 || kv_heads < 1 || dim < 1 || q_heads % kv_heads != 0) return SLIMFIT_ERR_INVALID_ARG;
     if (dim % (dt == SLIMFIT_F32 ? 4 : 8) != 0 || dim > 256) return SLIMFIT_ERR_UNSUPPORTED;
     if (batch == 0 || tokens == 0) return SLIMFIT_OK;
-    if (batch >= ((int64_t)1 << 31) / tokens || q_heads > (1 << 20)) return SLIMFIT_ERR_UNSUPPORTED;
+    if (batch >= ((int64_t)1 << 31) / tokens || ((int64_t)q_heads + 2 * (int64_t)kv_heads) * dim > (1 << 20)) return SLIMFIT_ERR_UNSUPPORTED;
     return SLIMFIT_OK;
 }
 
@@ -483,12 +652,12 @@ int32_t check_rotation(const Rotation &r, int64_t rows)
     return rc;
 }
 
-Shape shape_of(const Plan &p, const Rotation &r, int32_t dt, int64_t batch, int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t dim, bool norm,
-               float eps, float q_scale, int32_t bits, int32_t block)
+Shape shape_of(const Plan &p, const Rotation &r, int32_t dt, int64_t batch, int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t dim, float eps, float q_scale, int32_t bits,
+               int32_t block)
 {
     const uint32_t units = (uint32_t)(p.q_units + kv_heads + p.v_units);
     Shape z = {(uint32_t)(batch * tokens), (uint32_t)tokens, (uint32_t)q_heads, (uint32_t)kv_heads, (uint32_t)dim, (uint32_t)p.per, (uint32_t)p.q_units,
-               units, (uint32_t)r.positions, (uint32_t)r.rotary_dim / 2, r.pairing == SLIMFIT_ROTARY_ADJACENT, norm, 4, 0, eps, 1.0f / (float)dim, q_scale,
+               units, (uint32_t)r.positions, (uint32_t)r.rotary_dim / 2, r.rotary_dim > 0 && r.pairing == SLIMFIT_ROTARY_ADJACENT, 4, 0, eps, 1.0f / (float)dim, q_scale,
                Divide((uint32_t)tokens), Divide((uint32_t)dim), Divide(units)};
     if (bits != 0) {
         z.group = block / (dt == SLIMFIT_F32 ? 4 : 8);
@@ -497,12 +666,13 @@ Shape shape_of(const Plan &p, const Rotation &r, int32_t dt, int64_t batch, int3
     return z;
 }
 
-// f(T{}, L, BITS) for the call's type, lanes a head and bits
+// f(T{}, L, MODE) for the call's type, lanes a head and mode
 template <typename F>
-void choose(int32_t dt, int L, int32_t bits, F f)
+void choose(int32_t dt, int L, bool norm, int32_t bits, F f)
 {
     auto with_bits = [&](auto t, auto l) {
-        if (bits == 0) f(t, l, std::integral_constant<int, 0>{});
+        if (!norm) f(t, l, std::integral_constant<int, kNoNorm>{});
+        else if (bits == 0) f(t, l, std::integral_constant<int, kNoCache>{});
         else if (bits == 4) f(t, l, std::integral_constant<int, 4>{});
         else f(t, l, std::integral_constant<int, 8>{});
     };
@@ -569,12 +739,12 @@ extern "C" int32_t slimfit_heads_norm_rotate_forward(const void *qkv, int32_t dt
         if ((rc = check_device_range(codes, n * (size_t)bits / 8)) != SLIMFIT_OK) return rc;
         if ((rc = check_device_range(scales, n / (size_t)block * 4)) != SLIMFIT_OK) return rc;
     }
-    const Shape z = shape_of(plan, turn, dt, batch, tokens, q_heads, kv_heads, head_dim, norm, eps, q_scale, bits, block);
+    const Shape z = shape_of(plan, turn, dt, batch, tokens, q_heads, kv_heads, head_dim, eps, q_scale, bits, block);
     hipStream_t st = static_cast<hipStream_t>(stream);
     constexpr int64_t kMost = kMaxGridThreads / kThreads;
     for (int64_t first = 0; first < plan.blocks; first += kMost) {
         const unsigned here = (unsigned)(plan.blocks - first < kMost ? plan.blocks - first : kMost);
-        choose(dt, plan.L, bits, [&](auto t, auto l, auto b) {
+        choose(dt, plan.L, norm, bits, [&](auto t, auto l, auto b) {
             using T = decltype(t);
             launch(forward_kernel<T, decltype(l)::value, decltype(b)::value>, here, kThreads, 0, st, static_cast<const T *>(qkv), gamma_q, gamma_k, table,
                    position_ids, static_cast<T *>(q), static_cast<T *>(kt), static_cast<T *>(v), rstd, codes, scales, z, (uint32_t)first);
@@ -619,7 +789,7 @@ extern "C" int32_t slimfit_heads_norm_rotate_backward(const void *dq, const void
     if (empty) {
         if (!want) return SLIMFIT_OK;
         if ((rc = check_gammas()) != SLIMFIT_OK) return rc;
-        launch(gamma_kernel, gamma_blocks, kThreads, 0, st, nullptr, (uint32_t)head_dim, 0, 0, dgamma_q, dgamma_k);      // sums of nothing
+        launch(gamma_kernel, gamma_blocks, kGammaThreads, 0, st, nullptr, (uint32_t)head_dim, 0, 0, dgamma_q, dgamma_k);      // sums of nothing
         return launch_status();
     }
     if (!dq || !dkt || !dv || !dqkv || (reads && !qkv) || (norm && !rstd) || (bits != 0 && (!codes || !scales))) return SLIMFIT_ERR_INVALID_ARG;
@@ -655,12 +825,12 @@ extern "C" int32_t slimfit_heads_norm_rotate_backward(const void *dq, const void
         if ((rc = check_device_range(codes, n * (size_t)bits / 8)) != SLIMFIT_OK) return rc;
         if ((rc = check_device_range(scales, n / (size_t)block * 4)) != SLIMFIT_OK) return rc;
     }
-    const Shape z = shape_of(plan, turn, dt, batch, tokens, q_heads, kv_heads, head_dim, norm, 0.0f, q_scale, bits, block);
+    const Shape z = shape_of(plan, turn, dt, batch, tokens, q_heads, kv_heads, head_dim, 0.0f, q_scale, bits, block);
     float *partial = want ? static_cast<float *>(workspace) : nullptr;
     constexpr int64_t kMost = kMaxGridThreads / kThreads;
     for (int64_t first = 0; first < plan.blocks; first += kMost) {
         const unsigned here = (unsigned)(plan.blocks - first < kMost ? plan.blocks - first : kMost);
-        choose(dt, plan.L, bits, [&](auto t, auto l, auto b) {
+        choose(dt, plan.L, norm, bits, [&](auto t, auto l, auto b) {
             using T = decltype(t);
             launch(backward_kernel<T, decltype(l)::value, decltype(b)::value>, here, kThreads, 0, st, static_cast<const T *>(dq),
                    static_cast<const T *>(dkt), static_cast<const T *>(dv), static_cast<const T *>(qkv), codes, scales, rstd, gamma_q, gamma_k, table,
@@ -668,7 +838,7 @@ extern "C" int32_t slimfit_heads_norm_rotate_backward(const void *dq, const void
         });
     }
     if (want)
-        launch(gamma_kernel, gamma_blocks, kThreads, 0, st, partial, (uint32_t)head_dim, plan.tiles * plan.q_units, plan.tiles * (int64_t)kv_heads, dgamma_q,
+        launch(gamma_kernel, gamma_blocks, kGammaThreads, 0, st, partial, (uint32_t)head_dim, plan.tiles * plan.q_units, plan.tiles * (int64_t)kv_heads, dgamma_q,
                dgamma_k);
     return launch_status();
 }
