@@ -11,13 +11,14 @@
 // fewer tiles than the compute units can hold, the rows are shared out and the parts added up in order by a second kernel.
 #include "common.hpp"
 
+#include <type_traits>
+
 namespace slimfit {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;
-constexpr int kTileN = 128;
 
 typedef __amdgpu_buffer_rsrc_t Buffer;
 __device__ __forceinline__ Buffer buffer_of(const void *at, int64_t bytes)      // bytes from `at` to the matrix's end; reads past it give 0
@@ -26,164 +27,187 @@ __device__ __forceinline__ Buffer buffer_of(const void *at, int64_t bytes)      
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(at), 0, (int)(uint32_t)n, 0x00020000);
 }
 
-// code c of BITS bits in byte (or nibble) i of a word whose fields have 2^(BITS-1) added: (field - 2^(BITS-1)) * step, exact but
-// for the product's one rounding
+// field i of a word whose fields have 2^(BITS-1) added: 0 .. 2^BITS - 1
 template <int BITS>
 __device__ __forceinline__ float field(uint32_t word, int i)
 {
     return (float)((word >> (i * BITS)) & ((1u << BITS) - 1));
 }
 
-template <typename T, int TK> struct Config;
-template <> struct Config<uint16_t, 128> { static constexpr int STEP = 64, PARTS = 1, KW = 4, MW = 8; };
-template <> struct Config<float, 64> { static constexpr int STEP = 32, PARTS = 3, KW = 2, MW = 4; };
-template <> struct Config<float, 32> { static constexpr int STEP = 32, PARTS = 3, KW = 2, MW = 2; };
+// A tile of dw is TN x TK, a step 32 rows of the sum.  WAVES_N x WAVES_K waves.
+template <typename T, int TN, int TK> struct Config;
+template <> struct Config<uint16_t, 256, 128> { static constexpr int PARTS = 1, WAVES_N = 2, STAGES = 2; };
+template <> struct Config<uint16_t, 128, 128> { static constexpr int PARTS = 1, WAVES_N = 2, STAGES = 2; };
+template <> struct Config<float, 128, 64> { static constexpr int PARTS = 3, WAVES_N = 4, STAGES = 2; };
+template <> struct Config<float, 128, 32> { static constexpr int PARTS = 3, WAVES_N = 4, STAGES = 2; };
 
-template <int ROW_BYTES>
-__device__ __forceinline__ int chunk_at(int row, int chunk)
-{
-    return row * ROW_BYTES + ((chunk ^ ((row >> 1) & (ROW_BYTES / 16 - 1))) << 4);
-}
+constexpr int kStep = 32;
+// a row of a tile in LDS: 32 bytes more than it holds, so that sixteen rows' 32 bytes, which a transposing read takes, are in
+// different banks two by two
+constexpr int pitch_of(int columns) { return columns * 2 + 32; }
 
 struct Sizes {
     int64_t M, N, K, split_rows;           // split_rows: rows of a part, a multiple of the step
-    int tiles_n, tiles_k, block_shift;
+    int tiles_n, tiles_k, splits, block_shift;
 };
 
-template <typename T, int BITS, int TK, bool ODD>
-__global__ void __launch_bounds__(kThreads)
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 *LdsVector;
+// eight rows of one column, from a tile whose rows lie along the columns: rows 4 g .. 4 g + 3 and 16 + 4 g .. of the step for the lanes
+// of group g = lane / 16 (the order of the sum is the same for both operands, so any is), column lane % 16 of sixteen
+template <int PITCH>
+__device__ __forceinline__ bf16x8 fragment(const char *at)
+{
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsVector)(at));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsVector)(at + 16 * PITCH));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// How dy is read, 16 bytes a thread: its rows begin on 16 bytes; they begin anywhere, and the last vector of a row is the one that ends
+// with it; or (rows shorter than a vector) element by element.
+enum Rows { kAligned, kAnywhere, kShort };
+
+template <typename T, int BITS, int TN, int TK, Rows ROWS>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 2)
 weight_kernel(const T *__restrict__ dy, const uint8_t *__restrict__ codes, const float *__restrict__ scales, T *__restrict__ dw,
               float *__restrict__ parts, Sizes z)
 {
-    using C = Config<T, TK>;
-    constexpr int STEP = C::STEP, PARTS = C::PARTS, KW = C::KW, MW = C::MW, ROW = STEP * 2, CHUNKS = STEP / 8;
-    constexpr bool WIDE = sizeof(T) == 4;
-    constexpr int CA = CHUNKS / 4;                         // runs of eight rows of dy a thread
-    constexpr int FN = kTileN / 2 / 16, FK = TK / 2 / 16;
-    constexpr int PART = kTileN * ROW;
-    __shared__ __align__(16) char lds[PARTS * PART + TK * ROW];
+    using C = Config<T, TN, TK>;
+    constexpr int PARTS = C::PARTS, WAVES_N = C::WAVES_N, WAVES_K = 4 / WAVES_N, FN = TN / WAVES_N / 16, FK = TK / WAVES_K / 16;
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int E = 16 / sizeof(T);                      // elements of dy a thread takes at a time
+    constexpr int LINE = TN / E, LINES = kThreads / LINE, PASSES = kStep / LINES;
+    constexpr int CODES = kStep * TK / kThreads;           // codes a thread takes, of one row
+    constexpr int PY = pitch_of(TN), PX = pitch_of(TK), PART = kStep * PY, STAGE = PARTS * PART + kStep * PX;
+    __shared__ __align__(16) char stage[STAGE];
     const int t = threadIdx.x, lane = t & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int tiles = z.tiles_n * z.tiles_k;
-    const int per = tiles / 8, b0 = (int)blockIdx.x, id = b0 < per * 8 ? (b0 % 8) * per + b0 / 8 : b0;
+    // Workgroups go to the eight XCDs in turn; an XCD's take bands of four tile rows, column by column, of one part of the sum
+    const int tiles = z.tiles_n * z.tiles_k, all = tiles * z.splits;
+    const int each = all / 8, b0 = (int)blockIdx.x, turn = b0 < each * 8 ? (b0 % 8) * each + b0 / 8 : b0;
+    const int split = turn / tiles, id = turn % tiles;
     const int band = id / (4 * z.tiles_k), in_band = id % (4 * z.tiles_k), height = min(4, z.tiles_n - 4 * band);
-    const int64_t n0 = (int64_t)(band * 4 + in_band % height) * kTileN, k0 = (int64_t)(in_band / height) * TK;
-    const int64_t m0 = (int64_t)blockIdx.y * z.split_rows, m1 = min(m0 + z.split_rows, z.M);
-    const int steps = (int)((m1 - m0 + STEP - 1) / STEP);
+    const int64_t n0 = (int64_t)(band * 4 + in_band % height) * TN, k0 = (int64_t)(in_band / height) * TK;
+    const int64_t m0 = (int64_t)split * z.split_rows, m1 = min(m0 + z.split_rows, z.M);
+    const int steps = m1 > m0 ? (int)((m1 - m0 + kStep - 1) / kStep) : 0;
 
     const int64_t dy_row = z.N * (int64_t)sizeof(T), code_row = z.K * BITS / 8, scale_row = (z.K >> z.block_shift) * 4;
-    int at_dy[CA][8], at_code[MW], at_scale[WIDE ? 8 * CA : MW];
+    const int ny = t % LINE * E, my = t / LINE, kx = t % (TK / CODES) * CODES, mx = t / (TK / CODES);
+    int at_dy[PASSES], at_scale[F32 ? PASSES : 1];
 #pragma unroll
-    for (int q = 0; q < CA; ++q) {
+    for (int p = 0; p < PASSES; ++p) at_dy[p] = (int)((p * LINES + my) * dy_row + (ROWS == kAnywhere ? min(n0 + ny, z.N - E) : n0 + ny) * (int64_t)sizeof(T));
+    // columns by which the thread's vector begins before its place (past the row's end it does not matter where)
+    const int before = ROWS == kAnywhere && n0 + ny < z.N ? (int)(n0 + ny - min(n0 + ny, z.N - E)) : 0;
+    const int at_code = (int)(mx * code_row + (k0 + kx) * BITS / 8);
+    if constexpr (F32) {                                   // (the tile lies in one block)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) at_dy[q][i] = (int)(((wave * CA + q) * 8 + i) * dy_row + (n0 + 2 * lane) * (int64_t)sizeof(T));
-    }
-    constexpr int ACROSS = TK / KW;
-    const int kx = t % ACROSS * KW, mx = t / ACROSS * MW;  // the thread's codes of the tile
-    static_assert(kThreads / ACROSS * MW == STEP, "the codes of a step");
-#pragma unroll
-    for (int i = 0; i < MW; ++i) at_code[i] = (int)((mx + i) * code_row + (k0 + kx) * BITS / 8);
-    if constexpr (WIDE) {
-#pragma unroll
-        for (int i = 0; i < 8 * CA; ++i) at_scale[i] = (int)((wave * CA * 8 + i) * scale_row + (k0 >> z.block_shift) * 4);
+        for (int p = 0; p < PASSES; ++p) at_scale[p] = (int)((p * LINES + my) * scale_row + (k0 >> z.block_shift) * 4);
     } else {
-#pragma unroll
-        for (int i = 0; i < MW; ++i) at_scale[i] = (int)((mx + i) * scale_row + ((k0 + kx) >> z.block_shift) * 4);
+        at_scale[0] = (int)(mx * scale_row + ((k0 + kx) >> z.block_shift) * 4);
     }
 
-    uint32_t hy[CA][8][WIDE ? 2 : 1], hc[MW];
-    float hs[WIDE ? 8 * CA : MW];
+    struct Held {
+        u32x4 y[PASSES];
+        uint32_t c[CODES * BITS >= 32 ? CODES * BITS / 32 : 1];
+        float s[F32 ? PASSES : 1];
+    } held;
     auto load = [&](int64_t m) {
         const Buffer by = buffer_of(reinterpret_cast<const char *>(dy) + m * dy_row, (z.M - m) * dy_row);
         const Buffer bc = buffer_of(codes + m * code_row, (z.M - m) * code_row);
         const Buffer bs = buffer_of(reinterpret_cast<const char *>(scales) + m * scale_row, (z.M - m) * scale_row);
 #pragma unroll
-        for (int q = 0; q < CA; ++q) {
+        for (int p = 0; p < PASSES; ++p) {
+            if constexpr (ROWS != kShort) {
+                const auto v = __builtin_amdgcn_raw_buffer_load_b128(by, at_dy[p], 0, 0);
+                held.y[p] = u32x4{v[0], v[1], v[2], v[3]};
+            } else if constexpr (F32) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if constexpr (WIDE) {
-                    if constexpr (ODD) {
-                        hy[q][i][0] = __builtin_amdgcn_raw_buffer_load_b32(by, at_dy[q][i], 0, 0);
-                        hy[q][i][1] = __builtin_amdgcn_raw_buffer_load_b32(by, at_dy[q][i] + 4, 0, 0);
-                    } else {
-                        const auto v = __builtin_amdgcn_raw_buffer_load_b64(by, at_dy[q][i], 0, 0);
-                        hy[q][i][0] = v[0];
-                        hy[q][i][1] = v[1];
-                    }
-                } else if constexpr (ODD) {
-                    hy[q][i][0] = (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(by, at_dy[q][i], 0, 0) |
-                                  (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(by, at_dy[q][i] + 2, 0, 0) << 16;
-                } else {
-                    hy[q][i][0] = __builtin_amdgcn_raw_buffer_load_b32(by, at_dy[q][i], 0, 0);
-                }
+                for (int i = 0; i < 4; ++i) held.y[p][i] = __builtin_amdgcn_raw_buffer_load_b32(by, at_dy[p] + 4 * i, 0, 0);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    held.y[p][i] = (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(by, at_dy[p] + 4 * i, 0, 0) |
+                                   (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(by, at_dy[p] + 4 * i + 2, 0, 0) << 16;
             }
         }
+        constexpr int BYTES = CODES * BITS / 8;
+        if constexpr (BYTES == 16) {
+            const auto v = __builtin_amdgcn_raw_buffer_load_b128(bc, at_code, 0, 0);
 #pragma unroll
-        for (int i = 0; i < MW; ++i) {
-            constexpr int BYTES = KW * BITS;               // in bits
-            if constexpr (BYTES == 32) hc[i] = __builtin_amdgcn_raw_buffer_load_b32(bc, at_code[i], 0, 0);
-            else if constexpr (BYTES == 16) hc[i] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(bc, at_code[i], 0, 0);
-            else hc[i] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(bc, at_code[i], 0, 0);
+            for (int i = 0; i < 4; ++i) held.c[i] = v[i];
+        } else if constexpr (BYTES == 8) {
+            const auto v = __builtin_amdgcn_raw_buffer_load_b64(bc, at_code, 0, 0);
+            held.c[0] = v[0];
+            held.c[1] = v[1];
+        } else if constexpr (BYTES == 4) {
+            held.c[0] = __builtin_amdgcn_raw_buffer_load_b32(bc, at_code, 0, 0);
+        } else {
+            held.c[0] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(bc, at_code, 0, 0);
         }
 #pragma unroll
-        for (int i = 0; i < (WIDE ? 8 * CA : MW); ++i) hs[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(bs, at_scale[i], 0, 0));
+        for (int i = 0; i < (F32 ? PASSES : 1); ++i) {
+            const uint32_t v = __builtin_amdgcn_raw_buffer_load_b32(bs, at_scale[i], 0, 0);
+            held.s[i] = __builtin_bit_cast(float, v);
+        }
     };
     auto store = [&]() {
 #pragma unroll
-        for (int q = 0; q < CA; ++q) {
-            const int chunk = wave * CA + q;
-            if constexpr (WIDE) {
+        for (int p = 0; p < PASSES; ++p) {
+            char *to = stage + (p * LINES + my) * PY + ny * 2;
+            auto put = [&](char *at, const auto &words, auto n) {          // n words of two columns each
+                constexpr int W = decltype(n)::value;
+                if (ROWS == kAnywhere && before != 0) {    // those of its columns that are in its place; the thread before it has the others
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {              // columns 2 lane and 2 lane + 1
-                    uint32_t h[4], m[4], l[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float a = __builtin_bit_cast(float, hy[q][2 * i][c]) * hs[q * 8 + 2 * i];
-                        float b = __builtin_bit_cast(float, hy[q][2 * i + 1][c]) * hs[q * 8 + 2 * i + 1];
-                        h[i] = bf16_narrow2(a, b);
-                        a -= __builtin_bit_cast(float, h[i] << 16);
-                        b -= __builtin_bit_cast(float, h[i] & 0xFFFF0000u);
-                        m[i] = bf16_narrow2(a, b);
-                        a -= __builtin_bit_cast(float, m[i] << 16);
-                        b -= __builtin_bit_cast(float, m[i] & 0xFFFF0000u);
-                        l[i] = bf16_narrow2(a, b);
-                    }
-                    char *to = lds + chunk_at<ROW>(2 * lane + c, chunk);
-                    *reinterpret_cast<u32x4 *>(to) = u32x4{h[0], h[1], h[2], h[3]};
-                    *reinterpret_cast<u32x4 *>(to + PART) = u32x4{m[0], m[1], m[2], m[3]};
-                    *reinterpret_cast<u32x4 *>(to + 2 * PART) = u32x4{l[0], l[1], l[2], l[3]};
+                    for (int i = 0; i < 2 * W; ++i)
+                        if (i >= before) reinterpret_cast<uint16_t *>(at)[i - before] = (uint16_t)(words[i / 2] >> (i % 2 * 16));
+                } else if constexpr (W == 4) {
+                    *reinterpret_cast<u32x4 *>(at) = u32x4{words[0], words[1], words[2], words[3]};
+                } else {
+                    *reinterpret_cast<u32x2 *>(at) = u32x2{words[0], words[1]};
                 }
+            };
+            if constexpr (!F32) {
+                put(to, held.y[p], std::integral_constant<int, 4>{});
             } else {
-                uint32_t even[4], odd[4];
+                uint32_t h[2], m[2], l[2];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    even[i] = __builtin_amdgcn_perm(hy[q][2 * i + 1][0], hy[q][2 * i][0], 0x05040100u);
-                    odd[i] = __builtin_amdgcn_perm(hy[q][2 * i + 1][0], hy[q][2 * i][0], 0x07060302u);
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t u = held.y[p][2 * i], v = held.y[p][2 * i + 1];
+                    float a = __builtin_bit_cast(float, u) * held.s[p], b = __builtin_bit_cast(float, v) * held.s[p];
+                    h[i] = bf16_narrow2(a, b);
+                    a -= __builtin_bit_cast(float, h[i] << 16);
+                    b -= __builtin_bit_cast(float, h[i] & 0xFFFF0000u);
+                    m[i] = bf16_narrow2(a, b);
+                    a -= __builtin_bit_cast(float, m[i] << 16);
+                    b -= __builtin_bit_cast(float, m[i] & 0xFFFF0000u);
+                    l[i] = bf16_narrow2(a, b);
                 }
-                *reinterpret_cast<u32x4 *>(lds + chunk_at<ROW>(2 * lane, chunk)) = u32x4{even[0], even[1], even[2], even[3]};
-                *reinterpret_cast<u32x4 *>(lds + chunk_at<ROW>(2 * lane + 1, chunk)) = u32x4{odd[0], odd[1], odd[2], odd[3]};
+                put(to, h, std::integral_constant<int, 2>{});
+                put(to + PART, m, std::integral_constant<int, 2>{});
+                put(to + 2 * PART, l, std::integral_constant<int, 2>{});
             }
         }
         constexpr uint32_t kFlip = BITS == 8 ? 0x80808080u : 0x88888888u;
         constexpr float kBias = BITS == 8 ? 128.0f : 8.0f;
+        uint32_t x[CODES / 2];
 #pragma unroll
-        for (int c = 0; c < KW; ++c) {
-            uint32_t x[MW / 2];
-#pragma unroll
-            for (int i = 0; i < MW; i += 2) {
-                float a = field<BITS>(hc[i] ^ kFlip, c), b = field<BITS>(hc[i + 1] ^ kFlip, c);
-                if constexpr (WIDE) {
-                    a -= kBias;
-                    b -= kBias;
-                } else {                                   // (field - bias) * scale, rounded once: bias * scale is exact
-                    a = fmaf(a, hs[i], -kBias * hs[i]);
-                    b = fmaf(b, hs[i + 1], -kBias * hs[i + 1]);
-                }
-                x[i / 2] = bf16_narrow2(a, b);
+        for (int i = 0; i < CODES; i += 2) {
+            const uint32_t word = held.c[i * BITS / 32] ^ kFlip;
+            float a = field<BITS>(word, i % (32 / BITS)), b = field<BITS>(word, i % (32 / BITS) + 1);
+            if constexpr (F32) {
+                a -= kBias;
+                b -= kBias;
+            } else {                                       // (field - bias) * scale, rounded once: bias * scale is exact
+                a = fmaf(a, held.s[0], -kBias * held.s[0]);
+                b = fmaf(b, held.s[0], -kBias * held.s[0]);
             }
-            char *to = lds + PARTS * PART + chunk_at<ROW>(kx + c, mx / 8) + mx % 8 * 2;
-            if constexpr (MW == 8) *reinterpret_cast<u32x4 *>(to) = u32x4{x[0], x[1], x[2], x[3]};
-            else if constexpr (MW == 4) *reinterpret_cast<u32x2 *>(to) = u32x2{x[0], x[1]};
-            else *reinterpret_cast<uint32_t *>(to) = x[0];
+            x[i / 2] = bf16_narrow2(a, b);
+        }
+        char *to = stage + PARTS * PART + mx * PX + kx * 2;
+        if constexpr (CODES >= 8) {
+#pragma unroll
+            for (int i = 0; i < CODES / 8; ++i) reinterpret_cast<u32x4 *>(to)[i] = u32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+        } else {
+            *reinterpret_cast<u32x2 *>(to) = u32x2{x[0], x[1]};
         }
     };
 
@@ -193,26 +217,24 @@ weight_kernel(const T *__restrict__ dy, const uint8_t *__restrict__ codes, const
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    const int wn = (wave >> 1) * (kTileN / 2), wk = (wave & 1) * (TK / 2);
+    const int wn = wave / WAVES_K * (TN / WAVES_N), wk = wave % WAVES_K * (TK / WAVES_K);
+    const int place = 4 * (lane >> 4) + (lane & 15) / 4, column = (lane & 3) * 4;      // of the lane's first four elements
+    const int read_y = place * PY + (wn + column) * 2, read_x = PARTS * PART + place * PX + (wk + column) * 2;
     load(m0);
     for (int s = 0; s < steps; ++s) {
         store();
-        load(m0 + (int64_t)(s + 1) * STEP);                // past the last step: the next part's rows, or none
+        load(m0 + (int64_t)(s + 1) * kStep);           // past the last step: the next part's rows, or zeros
         __syncthreads();
+        bf16x8 fx[FK];
 #pragma unroll
-        for (int h = 0; h < STEP / 32; ++h) {
-            bf16x8 fx[FK];
+        for (int i = 0; i < FK; ++i) fx[i] = fragment<PX>(stage + read_x + i * 32);
 #pragma unroll
-            for (int i = 0; i < FK; ++i)
-                fx[i] = *reinterpret_cast<const bf16x8 *>(lds + PARTS * PART + chunk_at<ROW>(wk + i * 16 + (lane & 15), h * 4 + (lane >> 4)));
+        for (int j = 0; j < FN; ++j) {
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
+            for (int p = PARTS - 1; p >= 0; --p) {         // small parts first
+                const bf16x8 fy = fragment<PY>(stage + read_y + p * PART + j * 32);
 #pragma unroll
-                for (int p = PARTS - 1; p >= 0; --p) {     // small parts first
-                    const bf16x8 fy = *reinterpret_cast<const bf16x8 *>(lds + p * PART + chunk_at<ROW>(wn + j * 16 + (lane & 15), h * 4 + (lane >> 4)));
-#pragma unroll
-                    for (int i = 0; i < FK; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[i], fy, acc[i][j], 0, 0, 0);
-                }
+                for (int i = 0; i < FK; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[i], fy, acc[i][j], 0, 0, 0);
             }
         }
         __syncthreads();
@@ -226,8 +248,8 @@ weight_kernel(const T *__restrict__ dy, const uint8_t *__restrict__ codes, const
             const int64_t k = k0 + wk + i * 16 + (lane >> 4) * 4;
             if (k >= z.K) continue;
             const f32x4 v = acc[i][j];
-            if (parts) *reinterpret_cast<f32x4 *>(parts + (int64_t)blockIdx.y * z.N * z.K + n * z.K + k) = v;
-            else if constexpr (WIDE) *reinterpret_cast<f32x4 *>(dw + n * z.K + k) = v;
+            if (parts) *reinterpret_cast<f32x4 *>(parts + (int64_t)split * z.N * z.K + n * z.K + k) = v;
+            else if constexpr (F32) *reinterpret_cast<f32x4 *>(dw + n * z.K + k) = v;
             else *reinterpret_cast<u32x2 *>(dw + n * z.K + k) = u32x2{bf16_narrow2(v[0], v[1]), bf16_narrow2(v[2], v[3])};
         }
     }
@@ -248,19 +270,48 @@ join_kernel(const float *__restrict__ parts, int count, int64_t vectors, T *__re
 
 int64_t tiles_of(int64_t n, int tile) { return (n + tile - 1) / tile; }
 
+// How wide the tiles are and among how many workgroups a tile's sum is shared: what takes the least time by this count of
+// microseconds, measured over 20 sizes from 300 x 300 x 256 to 16384 x 4096 x 1024.  A step of 32 rows takes a + b * (workgroups on
+// the fullest compute unit), of which `most` go on one at a time; rows of dy that begin anywhere cost `ragged` as much.  Parts are
+// written and read again at 4.2 TB/s by a launch of 3 us.  (Chosen: 16384 x 4096 x 1024 bf16 256 wide in 4 parts 165 us, 128 wide in 3
+// 187, in one 322; 4096 x 768 x 768 128 wide in 6 24.3, in one 72; 12608 x 1024 x 4096 fp32 in 4 391, in one 461.)
+struct Pace {
+    int tile_n, most;
+    float a, b, ragged;
+};
+constexpr Pace kNarrow = {128, 4, 0.40f, 0.23f, 1.25f}, kWide = {256, 2, 0.39f, 0.39f, 1.6f}, kSplit = {128, 4, 0.45f, 0.39f, 1.25f};
+
 struct Plan {
-    int tile_k, step;
+    int tile_n, tile_k;
     int64_t tiles, splits, split_rows;
     Plan(int32_t dt, int32_t block, int64_t M, int64_t N, int64_t K)
     {
         tile_k = dt == SLIMFIT_BF16 ? 128 : block >= 64 ? 64 : 32;
-        step = dt == SLIMFIT_BF16 ? 64 : 32;
-        tiles = tiles_of(N, kTileN) * tiles_of(K, tile_k);
-        const int64_t steps = M / step + 1;
-        splits = 1;
-        while (splits < 32 && tiles * splits * 2 <= 768 && steps >= splits * 2 * 4) splits *= 2;
-        split_rows = tiles_of(tiles_of(M, (int)splits), step) * step;
-        if (split_rows == 0) split_rows = step;
+        const int64_t steps = tiles_of(M, kStep);
+        const bool ragged = N % (dt == SLIMFIT_BF16 ? 8 : 4) != 0;
+        float best = 0.0f;
+        auto look = [&](const Pace &p) {
+            const int64_t t = tiles_of(N, p.tile_n) * tiles_of(K, tile_k), full = 256 * p.most;
+            for (const int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+                if (s > 1 && steps < 2 * s) break;
+                const int64_t groups = t * s, rest = groups % full;
+                const float step = (float)(groups / full) * (p.a + p.b * (float)p.most) + (rest ? p.a + p.b * (float)tiles_of(rest, 256) : 0.0f);
+                const float join = s > 1 ? 3.0f + (float)s * (float)N * (float)K * (8.0f / 4.2e6f) : 0.0f;
+                const float time = (float)tiles_of(steps, s) * step * (ragged ? p.ragged : 1.0f) + join;
+                if (best == 0.0f || time < best) {
+                    best = time;
+                    tile_n = p.tile_n;
+                    tiles = t;
+                    splits = s;
+                }
+            }
+        };
+        tile_n = 128;
+        tiles = splits = 1;
+        look(dt == SLIMFIT_BF16 ? kNarrow : kSplit);
+        if (dt == SLIMFIT_BF16) look(kWide);
+        split_rows = tiles_of(steps, splits) * kStep;
+        if (split_rows == 0) split_rows = kStep;
     }
     size_t workspace(int64_t N, int64_t K) const { return splits > 1 ? (size_t)splits * (size_t)N * (size_t)K * 4 : 0; }
 };
@@ -272,20 +323,21 @@ int32_t validate(int32_t dt, int64_t M, int64_t N, int64_t K)
     return SLIMFIT_OK;
 }
 
-template <typename T, int TK>
+template <typename T, int TN, int TK>
 void launch_weight(const void *dy, const uint8_t *codes, const float *scales, int bits, const Sizes &z, const Plan &plan, void *dw, float *parts, hipStream_t st)
 {
-    const dim3 grid((unsigned)plan.tiles, (unsigned)plan.splits);
+    const unsigned grid = (unsigned)(plan.tiles * plan.splits);
     const T *y = static_cast<const T *>(dy);
     T *out = static_cast<T *>(dw);
-    const bool odd = z.N % 2 != 0;
-    if (bits == 8) {
-        if (odd) launch(weight_kernel<T, 8, TK, true>, grid, kThreads, 0, st, y, codes, scales, out, parts, z);
-        else launch(weight_kernel<T, 8, TK, false>, grid, kThreads, 0, st, y, codes, scales, out, parts, z);
-    } else {
-        if (odd) launch(weight_kernel<T, 4, TK, true>, grid, kThreads, 0, st, y, codes, scales, out, parts, z);
-        else launch(weight_kernel<T, 4, TK, false>, grid, kThreads, 0, st, y, codes, scales, out, parts, z);
-    }
+    constexpr int E = 16 / sizeof(T);
+    auto go = [&](auto b) {
+        constexpr int BITS = decltype(b)::value;
+        if (z.N % E == 0) launch(weight_kernel<T, BITS, TN, TK, kAligned>, grid, kThreads, 0, st, y, codes, scales, out, parts, z);
+        else if (z.N > E) launch(weight_kernel<T, BITS, TN, TK, kAnywhere>, grid, kThreads, 0, st, y, codes, scales, out, parts, z);
+        else launch(weight_kernel<T, BITS, TN, TK, kShort>, grid, kThreads, 0, st, y, codes, scales, out, parts, z);
+    };
+    if (bits == 8) go(std::integral_constant<int, 8>{});
+    else go(std::integral_constant<int, 4>{});
 }
 
 }  // namespace
@@ -329,11 +381,12 @@ extern "C" int32_t slimfit_weight_grad_dequant(const void *dy, int32_t dt, const
     if ((rc = check_device_range(codes, code_bytes)) != SLIMFIT_OK) return rc;
     if ((rc = check_device_range(scales, scale_bytes)) != SLIMFIT_OK) return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const Sizes z = {M, N, K, plan.split_rows, (int)tiles_of(N, kTileN), (int)tiles_of(K, plan.tile_k), __builtin_ctz((unsigned)block)};
+    const Sizes z = {M, N, K, plan.split_rows, (int)tiles_of(N, plan.tile_n), (int)tiles_of(K, plan.tile_k), (int)plan.splits, __builtin_ctz((unsigned)block)};
     float *parts = need > 0 ? static_cast<float *>(workspace) : nullptr;
-    if (dt == SLIMFIT_BF16) launch_weight<uint16_t, 128>(dy, codes, scales, bits, z, plan, dw, parts, st);
-    else if (plan.tile_k == 64) launch_weight<float, 64>(dy, codes, scales, bits, z, plan, dw, parts, st);
-    else launch_weight<float, 32>(dy, codes, scales, bits, z, plan, dw, parts, st);
+    if (dt == SLIMFIT_BF16 && plan.tile_n == 256) launch_weight<uint16_t, 256, 128>(dy, codes, scales, bits, z, plan, dw, parts, st);
+    else if (dt == SLIMFIT_BF16) launch_weight<uint16_t, 128, 128>(dy, codes, scales, bits, z, plan, dw, parts, st);
+    else if (plan.tile_k == 64) launch_weight<float, 128, 64>(dy, codes, scales, bits, z, plan, dw, parts, st);
+    else launch_weight<float, 128, 32>(dy, codes, scales, bits, z, plan, dw, parts, st);
     if (parts) {
         const int64_t vectors = N * K / 4;
         const unsigned blocks = (unsigned)((vectors + kThreads - 1) / kThreads);
