@@ -538,6 +538,46 @@ def frozen_encoder_block(x: torch.Tensor, p: dict, heads: int, wrapped: bool, ke
     return y + h
 
 
+def decoder_block_params(hidden: int, heads: int, kv_heads: int, ffn: int, device="cuda", seed: int = 0, dtype=torch.float32):
+    """Random weights of one decoder block: QKV for ``heads`` query and ``kv_heads`` key and value heads, their norms' gains,
+    projection, gated feed-forward of width ``ffn``, two LayerNorms."""
+    g = torch.Generator(device=device).manual_seed(seed)
+    dim = hidden // heads
+
+    def mat(rows, cols):
+        return torch.nn.Parameter((torch.randn(rows, cols, generator=g, device=device) * 0.03).to(dtype))
+
+    def vec(size, value):
+        return torch.nn.Parameter(torch.full((size,), value, device=device))
+
+    return {"wqkv": mat((heads + 2 * kv_heads) * dim, hidden), "wo": mat(hidden, hidden), "w1": mat(2 * ffn, hidden), "w2": mat(hidden, ffn),
+            "gq": vec(dim, 1.0), "gk": vec(dim, 1.0), "g1": vec(hidden, 1.0), "b1": vec(hidden, 0.0), "g2": vec(hidden, 1.0), "b2": vec(hidden, 0.0)}
+
+
+def decoder_block(x: torch.Tensor, p: dict, heads: int, kv_heads: int, table, position_ids=None, keep_ppm: int = 100000, bits: int = 8,
+                  block: int = 64, act: int = sf.ACT_SILU) -> torch.Tensor:
+    """One pre-LN decoder block (causal attention, queries and keys normed and turned, gated feed-forward) with the compressed
+    caches of this module.  Whether a layer is frozen is read off its weight: a frozen one keeps nothing of its input (a
+    LayerNorm the ``keep_ppm`` largest entries), an active one forms its weight gradient from its ``bits``-bit cache."""
+    B, T, H = x.shape
+    D, group = H // heads, heads // kv_heads
+
+    def norm(t, gamma, beta):
+        frozen = not gamma.requires_grad
+        return LayerNormFunction.apply(t, gamma, beta, 1e-5, frozen, keep_ppm, 0 if frozen else bits, block)
+
+    qkv = LinearFunction.apply(norm(x, p["g1"], p["b1"]), p["wqkv"], None, bits, block, True)
+    q, kt, v = HeadsNormRotateFunction.apply(qkv, p["gq"], p["gk"], heads, kv_heads, table, sf.ROTARY_HALVES, position_ids, 1.0 / D ** 0.5, 1e-6, bits,
+                                             block if D % block == 0 else 32)
+    s = MatmulFunction.apply(q.view(B, kv_heads, group * T, D), kt, bits, block)           # heads that share keys are rows of one product
+    later = torch.ones(T, T, dtype=torch.bool, device=x.device).triu(1)
+    s = s.view(B, kv_heads, group, T, T).masked_fill(later, -1e30).view(B, kv_heads, group * T, T)
+    a = SoftmaxMatmulFunction.apply(s, v, keep_ppm, bits, block).view(B, heads, T, D).transpose(1, 2).reshape(B, T, H)
+    y = x + LinearFunction.apply(a, p["wo"], None, bits, block, True)
+    h = LinearFunction.apply(norm(y, p["g2"], p["b2"]), p["w1"], None, bits, block, True)
+    return y + LinearFunction.apply(GatedFunction.apply(h, act, bits, block), p["w2"], None, bits, block, True)
+
+
 def held_activation_bytes(fn) -> tuple:
     """(bytes that stay allocated between the forward pass of ``fn`` and its backward pass, apart from the output;
     milliseconds of forward + backward)."""

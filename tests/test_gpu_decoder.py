@@ -1,0 +1,223 @@
+"""GPU: the calls around a decoder layer's cached activations together, as a block uses them; captured, on other streams and
+devices, through the native binding and without it."""
+import math
+
+import pytest
+import torch
+
+from paper_2305_18513_amd import autograd as ag
+from paper_2305_18513_amd import binding as sf
+from tests.gpu_util import require_gpu
+from tests.test_gpu_native_binding import _general, _outcome, _variants
+
+pytestmark = pytest.mark.gpu
+
+
+def _plain_block(x, p, heads, kv_heads, table, act):
+    """The same block in plain torch."""
+    F = torch.nn.functional
+    B, T, H = x.shape
+    D = H // heads
+    h = F.layer_norm(x, (H,), p["g1"], p["b1"], 1e-5)
+    q, k, v = (h @ p["wqkv"].t()).view(B, T, -1, D).split((heads, kv_heads, kv_heads), 2)
+    cos, sin = table[:T, None, : D // 2], table[:T, None, D // 2 :]
+
+    def turn(t, gain):
+        t = t * torch.rsqrt(t.square().mean(-1, keepdim=True) + 1e-6) * gain
+        a, b = t.chunk(2, -1)
+        return torch.cat((a * cos - b * sin, b * cos + a * sin), -1).transpose(1, 2)
+
+    q, k = turn(q, p["gq"]), turn(k, p["gk"])
+    k, v = (t.repeat_interleave(heads // kv_heads, 1) for t in (k, v.transpose(1, 2)))
+    s = (q @ k.transpose(-1, -2) / math.sqrt(D)).masked_fill(torch.ones(T, T, dtype=torch.bool, device=x.device).triu(1), -torch.inf)
+    y = x + (torch.softmax(s, -1) @ v).transpose(1, 2).reshape(B, T, H) @ p["wo"].t()
+    gate, up = (F.layer_norm(y, (H,), p["g2"], p["b2"], 1e-5) @ p["w1"].t()).chunk(2, -1)
+    return y + ((F.silu(gate) if act == sf.ACT_SILU else F.gelu(gate)) * up) @ p["w2"].t()
+
+
+@pytest.mark.parametrize("act", [sf.ACT_SILU, sf.ACT_GELU])
+@pytest.mark.parametrize("hidden,heads,kv_heads,T", [(256, 4, 2, 48), (128, 4, 1, 33)])
+def test_block_and_its_gradients(hidden, heads, kv_heads, T, act):
+    require_gpu()
+    g = torch.Generator(device="cuda").manual_seed(T)
+    p = ag.decoder_block_params(hidden, heads, kv_heads, 2 * hidden, "cuda", 1)
+    table = sf.rotary_table(64, hidden // heads)
+    x = torch.randn(2, T, hidden, generator=g, device="cuda", requires_grad=True)
+    dout = torch.randn(2, T, hidden, generator=g, device="cuda")
+    out = ag.decoder_block(x, p, heads, kv_heads, table, None, 1000000, 8, 32, act)
+    wide = {n: t.detach().double().requires_grad_(True) for n, t in p.items()}
+    xw = x.detach().double().requires_grad_(True)
+    want = _plain_block(xw, wide, heads, kv_heads, table.double(), act)
+    # fp32 sums of up to 2 * hidden terms, six of them one after the other: 6 * 512 * 2^-24 of the largest value at the most
+    assert float((out.double() - want).abs().max()) <= 6 * 512 * 2.0 ** -24 * float(want.abs().max())
+    got = torch.autograd.grad(out, [x, *p.values()], dout)
+    ref = torch.autograd.grad(want, [xw, *wide.values()], dout.double())
+    for name, a, b in zip(["x", *p], got, ref):
+        # a cache of 8 bits is off by a step / sqrt 12, in blocks of 32 normal entries 2.3 / 127 / sqrt 12 = 0.5 % of its values: a
+        # dozen of them (two norms, the heads, three products with two operands each, four linear layers, the gate) added up
+        assert float((a.double() - b).norm() / b.norm()) <= 12 * 0.005, name
+
+
+def test_block_frozen_and_active():
+    require_gpu()
+    p = ag.decoder_block_params(128, 4, 2, 256, "cuda", 1, torch.bfloat16)
+    table = sf.rotary_table(80, 32)
+    x = torch.randn(2, 70, 128, device="cuda").bfloat16().requires_grad_(True)
+    active = torch.autograd.grad(ag.decoder_block(x, p, 4, 2, table).float().sum(), [x, *p.values()])
+    assert all(bool(torch.isfinite(t.float()).all()) for t in active) and all(bool(t.any()) for t in active[1:])
+    for t in p.values():
+        t.requires_grad_(False)
+    (dx,) = torch.autograd.grad(ag.decoder_block(x, p, 4, 2, table).float().sum(), x)
+    assert bool(torch.isfinite(dx.float()).all())
+    with torch.no_grad():
+        first = ag.decoder_block(x, p, 4, 2, table)
+        # a later start is another place in the table, for one token as for all
+        ids = torch.arange(70, device="cuda", dtype=torch.int32).expand(2, 70).contiguous()
+        assert torch.equal(first, ag.decoder_block(x, p, 4, 2, table, ids))
+        assert not torch.equal(first, ag.decoder_block(x, p, 4, 2, table, ids.flip(1).contiguous()))
+
+
+def _calls(dt):
+    """name -> (function, arguments, positions of the outputs)"""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    f32, u8 = torch.float32, torch.uint8
+
+    def randn(*shape, dtype=dt):
+        return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+    def empty(*shape, dtype=dt):
+        return torch.empty(*shape, dtype=dtype, device="cuda")
+
+    B, T, Hq, Hk, D = 2, 9, 4, 2, 64
+    n = B * T * (Hq + Hk) * D
+    x = randn(7, 256)
+    codes, scales = empty(7 * 128, dtype=u8), empty(7 * 256 // 64, dtype=f32)
+    sf.quant_pack(x.view(-1), sf.Q_BLOCK, 4, 64, 0, codes, scales)
+    qkv, table = randn(B, T, (Hq + 2 * Hk) * D), sf.rotary_table(32, D)
+    hc, hs, rstd = empty(n, dtype=u8), empty(n // 32, dtype=f32), empty(B * T * (Hq + Hk), dtype=f32)
+    gains = randn(D, dtype=f32), randn(D, dtype=f32)
+    ids = torch.arange(B * T, dtype=torch.int32, device="cuda").view(B, T)
+    q, kt, v = empty(B, Hq, T, D), empty(B, Hk, D, T), empty(B, Hk, T, D)
+    sf.heads_norm_rotate_forward(qkv, *gains, 1e-6, table, 0, ids, 0.125, 8, 32, q, kt, v, rstd, hc, hs)
+    grads = randn(B, Hq, T, D), randn(B, Hk, D, T), randn(B, Hk, T, D)
+    ws = empty(sf.heads_norm_rotate_workspace(dt, B, T, Hq, Hk, D), dtype=u8)
+    M, N, K = 4100, 24, 64
+    wc, wsc = empty(M * K, dtype=u8), empty(M * K // 32, dtype=f32)
+    sf.quant_pack(randn(M * K), sf.Q_BLOCK, 8, 32, 0, wc, wsc)
+    need = sf.weight_grad_dequant_workspace(dt, 32, M, N, K)
+    assert need > 0
+    back = [*grads, None, hc, hs, 8, 32, rstd, *gains, table, 0, ids, 0.125]
+    return {
+        "gated_quant_pack": (sf.gated_quant_pack, [x, 0, sf.Q_BLOCK, 4, 64, 0, empty(7, 128), empty(7 * 128, dtype=u8), empty(7 * 4, dtype=f32)], (6, 7, 8)),
+        "gated_quant_pack_none": (sf.gated_quant_pack, [x, 1, sf.Q_FIXED, 0, 0, 0, empty(7, 128), None, None], (6,)),
+        "gated_backward_dequant": (sf.gated_backward_dequant, [codes, scales, 1, sf.Q_BLOCK, 4, 64, 0, randn(7, 128), empty(7, 256)], (8,)),
+        "heads_norm_rotate_forward": (sf.heads_norm_rotate_forward, [qkv, *gains, 1e-6, table, 0, ids, 0.125, 8, 32, q, kt, v, rstd.clone(), hc.clone(),
+                                                                     hs.clone()], (10, 11, 12, 13, 14, 15)),
+        "heads_norm_rotate_forward_plain": (sf.heads_norm_rotate_forward, [qkv, None, None, 0.0, None, 1, None, 0.125, 0, 0, q, kt, v, None, None, None],
+                                            (10, 11, 12)),
+        "heads_norm_rotate_backward": (sf.heads_norm_rotate_backward, [*back, empty(B, T, 8 * D), empty(D, dtype=f32), empty(D, dtype=f32), ws], (15, 16, 17)),
+        "heads_norm_rotate_backward_own": (sf.heads_norm_rotate_backward, [*back, empty(B, T, 8 * D), empty(D, dtype=f32), empty(D, dtype=f32)],
+                                           (15, 16, 17)),
+        "heads_norm_rotate_backward_frozen": (sf.heads_norm_rotate_backward, [*grads, qkv, None, None, 0, 0, rstd, *gains, table, 0, ids, 0.125,
+                                                                              empty(B, T, 8 * D)], (15,)),
+        "weight_grad_dequant": (sf.weight_grad_dequant, [randn(M, N), wc, wsc, 8, 32, empty(N, K), empty(need, dtype=u8)], (5,)),
+        "weight_grad_dequant_own": (sf.weight_grad_dequant, [randn(M, N), wc, wsc, 8, 32, empty(N, K)], (5,)),
+    }
+
+
+NAMES = ["gated_quant_pack", "gated_quant_pack_none", "gated_backward_dequant", "heads_norm_rotate_forward", "heads_norm_rotate_forward_plain",
+         "heads_norm_rotate_backward", "heads_norm_rotate_backward_own", "heads_norm_rotate_backward_frozen", "weight_grad_dequant",
+         "weight_grad_dequant_own"]
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("name", NAMES)
+def test_native_and_general_path_give_the_same(name, dt):
+    require_gpu()
+    fn, args, outs = _calls(dt)[name]
+    outputs = [args[i] for i in outs]
+    assert getattr(sf, "_native_" + fn.__name__)(*args, *([None] * (fn.__code__.co_argcount - len(args)))) is None     # taken
+    assert _outcome(lambda: fn(*args), outputs) == _outcome(lambda: _general(fn, *args), outputs)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert _outcome(lambda: fn(*args, stream=stream), outputs) == _outcome(lambda: _general(fn, *args, stream=stream), outputs)
+    for i, a in enumerate(args):
+        for other in _variants(a):
+            changed = list(args)
+            changed[i] = other
+            got, want = _outcome(lambda: fn(*changed), outputs), _outcome(lambda: _general(fn, *changed), outputs)
+            assert got == want, "argument %d as %r" % (i, type(other))
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_captured_calls_replay_to_the_eager_results(dt):
+    """With workspaces of their own, two graphs of them, replayed in turn with inputs that change in between."""
+    require_gpu()
+    calls = [_calls(dt)[n] for n in NAMES]
+    outputs = [args[i] for _, args, outs in calls for i in outs]
+    inputs = [a for _, args, outs in calls for i, a in enumerate(args) if isinstance(a, torch.Tensor) and i not in outs and a.dtype == dt]
+
+    def run():
+        for fn, args, _ in calls:
+            fn(*args)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for graph in graphs:
+        with torch.cuda.graph(graph, stream=side):
+            run()
+    noise = torch.empty(1 << 20, device="cuda")
+    for replay in range(4):
+        for t in inputs:
+            t.copy_(torch.randn(t.shape, device="cuda").to(dt))
+        run()
+        torch.cuda.synchronize()
+        eager = [t.clone() for t in outputs]
+        for t in outputs:
+            t.view(torch.uint8).fill_(0xCD)
+        noise.normal_()
+        graphs[replay % 2].replay()
+        torch.cuda.synchronize()
+        for t, want in zip(outputs, eager):
+            assert torch.equal(t.view(torch.uint8), want.view(torch.uint8)), replay
+
+
+def test_work_goes_on_the_current_stream():
+    require_gpu()
+    fn, args, _ = _calls(torch.bfloat16)["weight_grad_dequant_own"]
+    fn(*args)
+    want, dy = args[5].clone(), args[0].clone()
+    s, big = torch.cuda.Stream(), torch.randn(1 << 22, device="cuda")
+    args[0].zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(20):
+            big = big.clone()
+        args[0].copy_(dy)
+        fn(*args)                                                      # after what the stream holds, workspace and all
+        big = big.clone()
+    s.synchronize()
+    assert torch.equal(args[5], want)
+    with pytest.raises(ValueError):
+        fn(*args, stream=s.cuda_stream)                                # a stream of one's own wants a workspace of one's own
+
+
+def test_calls_on_two_streams_at_once():
+    require_gpu()
+    for name in ("heads_norm_rotate_backward_own", "weight_grad_dequant_own"):
+        sets = [_calls(torch.float32)[name] for _ in range(2)]
+        for fn, args, _ in sets:
+            fn(*args)
+        want = [[args[i].clone() for i in outs] for _, args, outs in sets]
+        streams = [torch.cuda.Stream() for _ in sets]
+        torch.cuda.synchronize()
+        for _ in range(10):
+            for stream, (fn, args, _) in zip(streams, sets):
+                with torch.cuda.stream(stream):
+                    fn(*args)
+        torch.cuda.synchronize()
+        for (fn, args, outs), kept in zip(sets, want):
+            assert all(torch.equal(args[i], k) for i, k in zip(outs, kept))
