@@ -662,7 +662,8 @@ int32_t slimfit_product(const float *a, const float *b, int32_t b_deep, int64_t 
  *  Deterministic: the order of the sums goes by the sizes and types alone.
  *  workspace : DEVICE, 16-byte aligned, of the bytes that slimfit_weight_grad_dequant_workspace reports (0 for most sizes);
  *           contents overwritten.
- *  dy, codes, scales 16-byte aligned, dw too; none shares memory with dw (INVALID_ARG).  N and K up to 2^20 (ERR_UNSUPPORTED).
+ *  dy, codes, scales 16-byte aligned, dw too; none shares memory with dw (INVALID_ARG).  N and K up to 2^20, and no
+ *           more tiles of 128 x 32 than a launch can have workgroups, 2^23 (ERR_UNSUPPORTED).
  * ---------------------------------------------------------------------- */
 int32_t slimfit_weight_grad_dequant_workspace(int32_t dt, int32_t block, int64_t M, int64_t N, int64_t K, size_t *bytes);
 

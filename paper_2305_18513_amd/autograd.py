@@ -45,6 +45,10 @@ fp32 operands of sizes at which it is the quicker one, and torch's otherwise.
                      the dequantised input (`straight`: from the codes themselves,
                      by the library's own product, where a block lies in one row).
 
+A backward pass may be captured into a HIP graph once no eager graph of the same leaves is alive (torch's engine would
+tie the capture to the stream of the eager one, which ends the process): capture the first pass on a side stream after
+a warm-up there, as torch's own notes have it, and let go of every loss computed before.
+
 All tensors are CUDA tensors (fp32 or bf16 activations; gamma / beta and the
 kept standardised values fp32); the kernels run on torch's current stream.
 """
@@ -52,6 +56,7 @@ from __future__ import annotations
 
 import torch
 from torch.autograd import forward_ad
+from torch.autograd.function import once_differentiable
 
 from . import binding as sf
 
@@ -304,6 +309,7 @@ class GatedFunction(torch.autograd.Function):
         return y.view(*x.shape[:-1], F)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_output: torch.Tensor):
         codes, scales = ctx.saved_tensors
         act, bits, block, shape = ctx.meta
@@ -343,6 +349,7 @@ class HeadsNormRotateFunction(torch.autograd.Function):
         return q, kt, v
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq: torch.Tensor, dkt: torch.Tensor, dv: torch.Tensor):
         qkv, codes, scales, rstd, gamma_q, gamma_k, table, position_ids = ctx.saved_tensors
         shape, pairing, q_scale, bits, block = ctx.meta
@@ -567,8 +574,9 @@ def decoder_block(x: torch.Tensor, p: dict, heads: int, kv_heads: int, table, po
         return LayerNormFunction.apply(t, gamma, beta, 1e-5, frozen, keep_ppm, 0 if frozen else bits, block)
 
     qkv = LinearFunction.apply(norm(x, p["g1"], p["b1"]), p["wqkv"], None, bits, block, True)
-    q, kt, v = HeadsNormRotateFunction.apply(qkv, p["gq"], p["gk"], heads, kv_heads, table, sf.ROTARY_HALVES, position_ids, 1.0 / D ** 0.5, 1e-6, bits,
-                                             block if D % block == 0 else 32)
+    # a cache's blocks lie in one head; heads that have no whole block keep the rows themselves
+    q, kt, v = HeadsNormRotateFunction.apply(qkv, p["gq"], p["gk"], heads, kv_heads, table, sf.ROTARY_HALVES, position_ids, 1.0 / D ** 0.5, 1e-6,
+                                             bits if D % 32 == 0 else 0, block if D % block == 0 else 32)
     s = MatmulFunction.apply(q.view(B, kv_heads, group * T, D), kt, bits, block)           # heads that share keys are rows of one product
     later = torch.ones(T, T, dtype=torch.bool, device=x.device).triu(1)
     s = s.view(B, kv_heads, group, T, T).masked_fill(later, -1e30).view(B, kv_heads, group * T, T)

@@ -425,6 +425,8 @@ def gated_quant_pack(x: torch.Tensor, act: int, mode: int, bits: int, block: int
         return None if rc is None else _check(rc, "gated_quant_pack")
     _require(x.dim() == 2 and y.dim() == 2 and y.dtype == x.dtype and y.shape[0] == x.shape[0] and x.shape[1] == 2 * y.shape[1])
     _require(x.is_contiguous() and y.is_contiguous())
+    if bits == 0:
+        codes = scales = None                              # not looked at
     _require(bits == 0 or (codes is not None and _cache_fits(x.numel(), mode, bits, block, codes, scales)))
     _on_current_device(x, y, codes, scales)
     rc = lib().slimfit_gated_quant_pack(
@@ -862,6 +864,8 @@ def heads_norm_rotate_forward(qkv: torch.Tensor, gamma_q: Optional[torch.Tensor]
                                            scales, stream)
     if rc is not NotImplemented:
         return None if rc is None else _check(rc, "heads_norm_rotate_forward")
+    if bits == 0:
+        codes = scales = None                              # not looked at
     _rotate_ok(qkv, q, kt, v, (gamma_q, gamma_k), table, position_ids, rstd, codes, scales, bits, block)
     _on_current_device(qkv, gamma_q, gamma_k, table, position_ids, q, kt, v, rstd, codes, scales)
     B, Hq, T, D = q.shape
@@ -895,6 +899,8 @@ def heads_norm_rotate_backward(dq: torch.Tensor, dkt: torch.Tensor, dv: torch.Te
                                             q_scale, dqkv, dgamma_q, dgamma_k, workspace, stream)
     if rc is not NotImplemented:
         return None if rc is None else _check(rc, "heads_norm_rotate_backward")
+    if bits == 0:
+        codes = scales = None                              # not looked at
     _rotate_ok(dqkv, dq, dkt, dv, (gamma_q, gamma_k), table, position_ids, rstd, codes, scales, bits, block)
     B, Hq, T, D = dq.shape
     Hk = dv.shape[1]

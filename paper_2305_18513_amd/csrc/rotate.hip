@@ -5,12 +5,18 @@
 //   forward   y = rot(x * rstd * gamma), rstd = (mean x^2 + eps)^-1/2; q = q_scale y, k^T = y^T, v = x
 //   backward  g = rot^-1(dy), dgamma = sum g x~, dx = rstd (g gamma - x~ mean(g gamma x~)), x~ = x^ rstd
 //
-// A head's row is L lanes' 16-byte vectors (L a power of two; those past the head's end hold zeros), so that the row's sum
-// is a butterfly over L lanes, the element that one is turned with is in the lane's own vector or in that of one lane, and a
-// quantisation block is block / E lanes.  A workgroup owns 1024 / L rows (token by token, batch by batch) in four passes,
-// whose blocks' divisions a quad of lanes shares, and one head of the keys, or several of the queries or values one after
-// the other, with the angles of its rows held in registers for all of them.  Keys go through LDS (rows an odd number of
-// words apart) into their transposed place: 16 bytes along the tokens where those are aligned, single elements otherwise.
+// A head's row is L lanes' 16-byte vectors (L a power of two), so that the row's sum is a butterfly over L lanes, the element that one
+// is turned with is in the lane's own vector or in that of one other lane, and a quantisation block is block / E lanes.  A workgroup
+// owns 1024 / L rows (token by token, batch by batch) in four passes, or half as many in two, and one head of the keys, or up to
+// four of the queries or values one after the other, the angles of two passes' rows, times gains and factor, in registers for all of
+// them.  Keys go through LDS (rows an odd number of words apart) into their transposed place.  No load or store of the head loop stands
+// behind a branch: behind one, each load was waited for together with the stores before it (16384 x 48 heads of 128, bf16, 8 bits,
+// forward 159 us, with them free 149, with the angles and gains in vectors 119, four heads a workgroup instead of eight 103).
+//
+// Bound by HBM, with a third on top for the ramp of each workgroup's angles and for the vector instructions (145 a 16-byte vector, half of
+// the time) that do not overlap with it: that size 103 us forward (486 MB, 4.7 TB/s) and 100 backward; 64 wide heads 55 and 57
+// (239 MB each); 7289 x 36 of 64 fp32 34 and 36; copies without norm and rotation 5.2 to 5.4 TB/s; a 1 : 1 stream of the card 6.2.
+// Fewer registers (five and six waves a SIMD by spilling) and angles for one pass or four at a time were slower.
 #include "elements.hpp"
 
 #include <type_traits>
@@ -229,12 +235,12 @@ __device__ __forceinline__ P *beyond(T *base, uint32_t at)
 
 // A thread's place: rows row0 + pass * SLOTS + slot, elements e0 .. e0 + E - 1 of each head.  Lanes past a head's end do what the
 // lanes L / 2 before them do (whole quantisation blocks, where there are any), rows past the last what the last does, to the same
-// places: no load or store stands behind a branch, and each is waited for by itself.  counts: 0 for such a lane, 1 otherwise.
+// places: no load or store stands behind a branch, and each is waited for by itself.  counts: not such a lane.
 template <typename T, int L>
 struct Place {
     static constexpr int E = Vec<T>::V, SLOTS = kThreads / L;
     uint32_t unit, tiled, row0, n_rows, lane, slot, e0;
-    float counts;
+    bool counts;
     __device__ __forceinline__ Place(const Shape &z, uint32_t first)
     {
         const uint32_t at = first + in_turn(blockIdx.x, gridDim.x);
@@ -245,8 +251,8 @@ struct Place {
         lane = threadIdx.x % L;
         slot = threadIdx.x / L;
         const uint32_t vectors = z.dim / E;                // more than L / 2, or L is 4 and nothing is cached
-        counts = lane < vectors ? 1.0f : 0.0f;
-        if (lane >= vectors) lane = lane >= L / 2 && lane - L / 2 < vectors ? lane - L / 2 : 0;
+        counts = lane < vectors;
+        if (!counts) lane = lane >= L / 2 && lane - L / 2 < vectors ? lane - L / 2 : 0;
         e0 = lane * E;
     }
     __device__ __forceinline__ uint32_t line(const Shape &z, int pass) const    // of the tile's rows
@@ -389,7 +395,7 @@ __device__ __forceinline__ void forward_heads(const Place<T, L> &w, const Part &
                     float sum = 0.0f;
 #pragma unroll
                     for (int i = 0; i < E; ++i) sum = fmaf(f[p][i], f[p][i], sum);
-                    const float r = __builtin_amdgcn_rsqf(fmaf(group_sum_f32(sum * w.counts, L), z.inv_dim, z.eps));
+                    const float r = __builtin_amdgcn_rsqf(fmaf(group_sum_f32(w.counts ? sum : 0.0f, L), z.inv_dim, z.eps));
                     *beyond<float>(rstd + ((int64_t)w.row0 * normed + h), line[p] * normed * 4) = r;
 #pragma unroll
                     for (int i = 0; i < E; ++i) y[i] *= r;
@@ -527,7 +533,7 @@ __device__ __forceinline__ void backward_heads(const Place<T, L> &w, const Part 
                         g[p][i] *= gamma[i];
                         dot = fmaf(g[p][i], xn[p][i], dot);
                     }
-                    dot = group_sum_f32(dot * w.counts, L) * z.inv_dim;
+                    dot = group_sum_f32(w.counts ? dot : 0.0f, L) * z.inv_dim;
 #pragma unroll
                     for (int i = 0; i < E; ++i) g[p][i] = root[p] * fmaf(-xn[p][i], dot, g[p][i]);
                 }
@@ -570,7 +576,7 @@ backward_kernel(const T *__restrict__ dq, const T *__restrict__ dkt, const T *__
         if (!partial) return;                              // (uniform for the launch)
         __syncthreads();                                   // the tile is read
         float *rows = reinterpret_cast<float *>(tile);     // SLOTS x dim
-        if (w.counts != 0.0f) {
+        if (w.counts) {
 #pragma unroll
             for (int i = 0; i < E; ++i) rows[w.slot * z.dim + w.e0 + i] = sums[i];
         }

@@ -1,14 +1,22 @@
 // Weight gradient of an active linear layer straight from the low-bit cache of its input (Alg. 4's dW = dY^T X with X as the
 // cache gives it back): dw[n][k] = sum over m of dy[m][n] code[m][k] scale[m][k / block].
 //
-// Both operands lie across the sum: eight rows m of two columns are read as words, turned in registers and written to LDS as
-// runs along m, which is what a lane hands to v_mfma_f32_16x16x32_bf16.  The codes become bf16 on that way.
+// Both operands lie across the sum.  Their rows go to LDS as they lie, 32 rows of the sum a step, the codes as bf16, and the reads turn
+// them (ds_read_b64_tr_b16): a lane gets eight rows of one column, which is what it hands to v_mfma_f32_16x16x32_bf16.
 //   bf16  x^ = code * scale rounded to bf16, as the cache gives it to a bf16 tensor.
 //   fp32  the scale goes onto dy (a tile lies in one block), whose product is rounded to fp32 once and taken apart exactly
 //         into three bf16 numbers; the codes are whole numbers that bf16 holds.  Three products in place of the six that two
 //         fp32 operands take.
 // Rows past M are read as zeros by the bounds of the buffer descriptors, which move along with the steps.  Where there are
 // fewer tiles than the compute units can hold, the rows are shared out and the parts added up in order by a second kernel.
+//
+// 4096 x 1024 over 16384 bf16 rows 160 to 190 us with the parts' sum (the card's clock follows its load: short bursts are the faster
+// ones), 720 to 860 TFLOP/s; torch's product of the same sizes, x^ in memory as bf16, takes 200, and a product of 8192^3 runs at 1240.
+// 1024 x 4096 over 12608 fp32 rows 394 to 447 us, 240 to 270 TFLOP/s; torch's fp32 product 750.  What bounds it is how far loading,
+// forming operands and multiplying overlap: without the loads 149 of 194 us, without forming operands 134, with operands of
+// zeros 158 (fp32 342, 255 and 421 of 470).  Tried and no faster at that size: two LDS stages with loads one and two steps ahead
+// (184 and 187), two groups of four waves that form and multiply in turn (190 to 197), operands turned in registers on the
+// way in (247); fp32 alike (465 to 490), its single stage with four workgroups a compute unit 431.
 #include "common.hpp"
 
 #include <type_traits>
@@ -36,10 +44,10 @@ __device__ __forceinline__ float field(uint32_t word, int i)
 
 // A tile of dw is TN x TK, a step 32 rows of the sum.  WAVES_N x WAVES_K waves.
 template <typename T, int TN, int TK> struct Config;
-template <> struct Config<uint16_t, 256, 128> { static constexpr int PARTS = 1, WAVES_N = 2, STAGES = 2; };
-template <> struct Config<uint16_t, 128, 128> { static constexpr int PARTS = 1, WAVES_N = 2, STAGES = 2; };
-template <> struct Config<float, 128, 64> { static constexpr int PARTS = 3, WAVES_N = 4, STAGES = 2; };
-template <> struct Config<float, 128, 32> { static constexpr int PARTS = 3, WAVES_N = 4, STAGES = 2; };
+template <> struct Config<uint16_t, 256, 128> { static constexpr int PARTS = 1, WAVES_N = 2; };
+template <> struct Config<uint16_t, 128, 128> { static constexpr int PARTS = 1, WAVES_N = 2; };
+template <> struct Config<float, 128, 64> { static constexpr int PARTS = 3, WAVES_N = 4; };
+template <> struct Config<float, 128, 32> { static constexpr int PARTS = 3, WAVES_N = 4; };
 
 constexpr int kStep = 32;
 // a row of a tile in LDS: 32 bytes more than it holds, so that sixteen rows' 32 bytes, which a transposing read takes, are in

@@ -49,7 +49,7 @@ def test_block_and_its_gradients(hidden, heads, kv_heads, T, act):
     xw = x.detach().double().requires_grad_(True)
     want = _plain_block(xw, wide, heads, kv_heads, table.double(), act)
     # fp32 sums of up to 2 * hidden terms, six of them one after the other: 6 * 512 * 2^-24 of the largest value at the most
-    assert float((out.double() - want).abs().max()) <= 6 * 512 * 2.0 ** -24 * float(want.abs().max())
+    assert float((out.double() - want).abs().max().detach()) <= 6 * 512 * 2.0 ** -24 * float(want.abs().max().detach())
     got = torch.autograd.grad(out, [x, *p.values()], dout)
     ref = torch.autograd.grad(want, [xw, *wide.values()], dout.double())
     for name, a, b in zip(["x", *p], got, ref):
@@ -221,3 +221,40 @@ def test_calls_on_two_streams_at_once():
         torch.cuda.synchronize()
         for (fn, args, outs), kept in zip(sets, want):
             assert all(torch.equal(args[i], k) for i, k in zip(outs, kept))
+
+
+def test_gradients_of_gradients_are_refused():
+    require_gpu()
+    x = torch.randn(2, 3, 128, device="cuda", requires_grad=True)
+    outs = (ag.GatedFunction.apply(x, sf.ACT_SILU, 8, 64), ag.HeadsNormRotateFunction.apply(x, None, None, 2, 1, None)[0])
+    for out in outs:
+        (dx,) = torch.autograd.grad(out.square().sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError):
+            torch.autograd.grad(dx.sum(), x)
+
+
+def test_a_captured_step_replays_to_the_eager_gradients():
+    """Every eager graph of the leaves is gone when the capture begins: torch's engine ends the process otherwise."""
+    require_gpu()
+    p = ag.decoder_block_params(128, 4, 2, 256, "cuda", 1)
+    table = sf.rotary_table(64, 32)
+    x = torch.randn(2, 40, 128, device="cuda", requires_grad=True)
+    leaves, dout = [x, *p.values()], torch.randn(2, 40, 128, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            want = torch.autograd.grad(ag.decoder_block(x, p, 4, 2, table), leaves, dout)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = torch.autograd.grad(ag.decoder_block(x, p, 4, 2, table), leaves, dout)
+    noise = torch.empty(1 << 20, device="cuda")
+    for _ in range(3):
+        for t in got:
+            t.zero_()
+        noise.normal_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -179,6 +179,19 @@ def test_many_heads_and_rows(dtype):
     _check(Case(16, 512, 32, 8, 128, 128, DT[dtype], bits=8, block=64))
 
 
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("D", [64, 80])
+def test_rows_whose_squares_overflow(D, dtype):
+    """The mean of the squares is infinite, rstd 0 and the row too, whether its lanes are all in the head or not."""
+    require_gpu()
+    c = Case(1, 9, 2, 1, D, 0, DT[dtype])
+    c.qkv[0, 3] = 3e19
+    out = c.buffers()
+    c.forward(out)
+    q = out["q"].t.view(1, 2, 9, D).float()
+    assert bool(torch.isfinite(q).all()) and not q[:, :, 3].any() and bool(q[:, :, 2].any()) and not out["rstd"].t.view(9, 3)[3].any()
+
+
 def test_plain_splits_are_split_heads():
     """Neither norm nor rotation, keys not shared: what split_heads and merge_heads do, to the bit."""
     require_gpu()
