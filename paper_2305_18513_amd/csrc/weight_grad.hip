@@ -35,13 +35,6 @@ __device__ __forceinline__ Buffer buffer_of(const void *at, int64_t bytes)      
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(at), 0, (int)(uint32_t)n, 0x00020000);
 }
 
-// field i of a word whose fields have 2^(BITS-1) added: 0 .. 2^BITS - 1
-template <int BITS>
-__device__ __forceinline__ float field(uint32_t word, int i)
-{
-    return (float)((word >> (i * BITS)) & ((1u << BITS) - 1));
-}
-
 // A tile of dw is TN x TK, a step 32 rows of the sum.  WAVES_N x WAVES_K waves.
 template <typename T, int TN, int TK> struct Config;
 template <> struct Config<uint16_t, 256, 128> { static constexpr int PARTS = 1, WAVES_N = 2; };
@@ -194,19 +187,13 @@ weight_kernel(const T *__restrict__ dy, const uint8_t *__restrict__ codes, const
                 put(to + 2 * PART, l, std::integral_constant<int, 2>{});
             }
         }
-        constexpr uint32_t kFlip = BITS == 8 ? 0x80808080u : 0x88888888u;
-        constexpr float kBias = BITS == 8 ? 128.0f : 8.0f;
         uint32_t x[CODES / 2];
 #pragma unroll
         for (int i = 0; i < CODES; i += 2) {
-            const uint32_t word = held.c[i * BITS / 32] ^ kFlip;
-            float a = field<BITS>(word, i % (32 / BITS)), b = field<BITS>(word, i % (32 / BITS) + 1);
-            if constexpr (F32) {
-                a -= kBias;
-                b -= kBias;
-            } else {                                       // (field - bias) * scale, rounded once: bias * scale is exact
-                a = fmaf(a, held.s[0], -kBias * held.s[0]);
-                b = fmaf(b, held.s[0], -kBias * held.s[0]);
+            float a = (float)code_field<BITS>(held.c[i * BITS / 32], i % (32 / BITS)), b = (float)code_field<BITS>(held.c[i * BITS / 32], i % (32 / BITS) + 1);
+            if constexpr (!F32) {
+                a *= held.s[0];
+                b *= held.s[0];
             }
             x[i / 2] = bf16_narrow2(a, b);
         }

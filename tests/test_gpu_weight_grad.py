@@ -105,6 +105,28 @@ def test_fp32_entries_of_any_size(size):
     _check(dw, dy, x)
 
 
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("bits", [8, 4])
+def test_inputs_of_the_largest_size(bits, dtype):
+    """Inputs of the type's lowest and largest value: times zero gradients, of masked rows, they are nothing, times small ones finite."""
+    require_gpu()
+    g = torch.Generator(device="cuda").manual_seed(17)
+    x = torch.randn(70, 64, generator=g, device="cuda").to(DT[dtype])
+    x[3], x[40, ::2] = torch.finfo(x.dtype).min, torch.finfo(x.dtype).max
+    dy = torch.randn(70, 24, generator=g, device="cuda").to(DT[dtype])
+    dy[3], dy[40] = 0.0, 0.0
+    codes, scales = torch.empty(70 * 64 * bits // 8, dtype=torch.uint8, device="cuda"), torch.empty(70 * 2, device="cuda")
+    sf.quant_pack(x.view(-1), sf.Q_BLOCK, bits, 32, 0, codes, scales)
+    code = torch.empty(70 * 64, device="cuda")
+    sf.dequant_unpack(codes, torch.ones_like(scales), sf.Q_BLOCK, bits, 32, 0, code)
+    x_hat = (code.double().view(-1, 32) * scales.double()[:, None]).view(70, 64)
+    dw = torch.empty(24, 64, dtype=x.dtype, device="cuda")
+    for rows in (dy, torch.where(torch.arange(70, device="cuda")[:, None] == 3, 2.0 ** -40, 0.0).expand(70, 24).to(x.dtype).contiguous()):
+        sf.weight_grad_dequant(rows, codes, scales, bits, 32, dw)
+        assert bool(dw.isfinite().all())
+        _check(dw, rows, x_hat)
+
+
 def test_offsets_past_32_bits():
     """Rows whose codes, and whose gradients, lie past 4 GB."""
     require_gpu()
