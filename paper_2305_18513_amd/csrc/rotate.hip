@@ -60,15 +60,16 @@ __device__ __forceinline__ void load_floats(const float *p, float (&f)[N])
         for (int k = 0; k < (N < 4 ? N : 4); ++k) f[i + k] = r[k];
     }
 }
-// What the E elements at e0 of a row become: c x + s partner(x), without the row's rstd.  BACK: by the angle back.
+// What the E elements at e0 of a row become: c x + s partner(x), without the row's rstd.  BACK: by the angle back.  False: they are not
+// turned, s is 0.
 template <int E, bool BACK>
-__device__ __forceinline__ void load_angles(const float *__restrict__ table, const int32_t *__restrict__ ids, const Shape &z, uint32_t row, uint32_t t,
+__device__ __forceinline__ bool load_angles(const float *__restrict__ table, const int32_t *__restrict__ ids, const Shape &z, uint32_t row, uint32_t t,
                                             uint32_t e0, float (&c)[E], float (&s)[E])
 {
 #pragma unroll
     for (int i = 0; i < E; ++i) { c[i] = 1.0f; s[i] = 0.0f; }
     const uint32_t place = ids ? (uint32_t)ids[row] : t;
-    if (e0 >= 2 * z.half || place >= z.positions) return;              // what is not turned, and padding
+    if (e0 >= 2 * z.half || place >= z.positions) return false;        // and padding
     const float *at = table + (int64_t)place * (2 * z.half);
     if (z.adjacent) {
         float a[E / 2], b[E / 2];
@@ -87,6 +88,7 @@ __device__ __forceinline__ void load_angles(const float *__restrict__ table, con
 #pragma unroll
         for (int i = 0; i < E; ++i) s[i] = low != BACK ? -s[i] : s[i];
     }
+    return true;
 }
 // c and s times a factor and the gains of the elements and of their partners; from: the lane of those
 template <int E>
@@ -109,23 +111,25 @@ __device__ __forceinline__ void weigh_angles(const float *__restrict__ gains, fl
         s[i] *= other[i];
     }
 }
-// c x + s partner(x) of a vector; from: the lane that holds the partners, where they are not its own neighbours
+// c x + s partner(x) of a vector; from: the lane that holds the partners, where they are not its own neighbours.  Those of a vector that
+// is not turned count as 0, whatever they are (0 times infinity would not be nothing).
 template <typename T>
 __device__ __forceinline__ void turn(const typename Vec<T>::raw &x, const float (&f)[Vec<T>::V], const float (&c)[Vec<T>::V], const float (&s)[Vec<T>::V],
-                                     int from, const Shape &z, float (&y)[Vec<T>::V])
+                                     bool turned, int from, const Shape &z, float (&y)[Vec<T>::V])
 {
     constexpr int E = Vec<T>::V;
     float other[E];
     if (z.adjacent) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) other[i] = f[i ^ 1];
+        for (int i = 0; i < E; ++i) other[i] = turned ? f[i ^ 1] : 0.0f;
     } else {                                               // as they lie in memory: four words
         const u32x4 mine = __builtin_bit_cast(u32x4, x);
         u32x4 theirs;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int word = (int)mine[i];
-            theirs[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(from * 4, word);
+            const uint32_t got = (uint32_t)__builtin_amdgcn_ds_bpermute(from * 4, word);
+            theirs[i] = turned ? got : 0u;
         }
         Vec<T>::unpack(__builtin_bit_cast(typename Vec<T>::raw, theirs), other);
     }
@@ -331,6 +335,7 @@ __device__ __forceinline__ void forward_heads(const Place<T, L> &w, const Part &
     const int64_t head = (int64_t)z.tokens * z.dim;
     for (int half = 0; half < (int)z.passes; half += kHeld) {
         float c[kHeld][E], s[kHeld][E];
+        bool turned[kHeld];                                // (asked without a norm: a row of one that holds an infinity is lost)
         uint32_t line[kHeld], at[kHeld];                   // the row in the tile, the vector of its first head
         T *to[kHeld];
 #pragma unroll
@@ -339,7 +344,7 @@ __device__ __forceinline__ void forward_heads(const Place<T, L> &w, const Part &
             const uint32_t row = w.row0 + line[p];
             at[p] = (line[p] * every * z.dim + w.e0) * (uint32_t)sizeof(T);
             if constexpr (!KEY) to[p] = apart + w.apart(z, row, part.heads) - part.first * head;
-            load_angles<E, false>(table, ids, z, row, row - z.by_tokens(row) * z.tokens, w.e0, c[p], s[p]);
+            turned[p] = load_angles<E, false>(table, ids, z, row, row - z.by_tokens(row) * z.tokens, w.e0, c[p], s[p]);
             if constexpr (MODE != kNoNorm) {
                 weigh_angles<E>(gains, part.factor, from, z, w.e0, c[p], s[p]);
             } else {
@@ -390,7 +395,7 @@ __device__ __forceinline__ void forward_heads(const Place<T, L> &w, const Part &
 #pragma unroll
             for (int p = 0; p < kHeld; ++p) {
                 float y[E];
-                turn<T>(now[p], f[p], c[p], s[p], from, z, y);
+                turn<T>(now[p], f[p], c[p], s[p], MODE != kNoNorm || turned[p], from, z, y);
                 if constexpr (MODE != kNoNorm) {
                     float sum = 0.0f;
 #pragma unroll
@@ -460,6 +465,7 @@ __device__ __forceinline__ void backward_heads(const Place<T, L> &w, const Part 
     }
     for (int half = 0; half < (int)z.passes; half += kHeld) {
         float c[kHeld][E], s[kHeld][E], counts[kHeld];
+        bool turned[kHeld];
         uint32_t line[kHeld];
         const T *at[kHeld];
 #pragma unroll
@@ -468,7 +474,7 @@ __device__ __forceinline__ void backward_heads(const Place<T, L> &w, const Part 
             counts[p] = w.twice(z, half + p) ? 0.0f : 1.0f;
             const uint32_t row = w.row0 + line[p];
             if constexpr (!KEY) at[p] = apart + w.apart(z, row, part.heads) - part.first * head;
-            load_angles<E, true>(table, ids, z, row, row - z.by_tokens(row) * z.tokens, w.e0, c[p], s[p]);
+            turned[p] = load_angles<E, true>(table, ids, z, row, row - z.by_tokens(row) * z.tokens, w.e0, c[p], s[p]);
 #pragma unroll
             for (int i = 0; i < E; ++i) { c[p][i] *= part.factor; s[p][i] *= part.factor; }
         }
@@ -509,7 +515,7 @@ __device__ __forceinline__ void backward_heads(const Place<T, L> &w, const Part 
             for (int p = 0; p < kHeld; ++p) {
                 float f[E];
                 Vec<T>::unpack(grad[p], f);
-                turn<T>(grad[p], f, c[p], s[p], from, z, g[p]);
+                turn<T>(grad[p], f, c[p], s[p], MODE != kNoNorm || turned[p], from, z, g[p]);
                 if constexpr (MODE == kNoCache) {
                     root[p] = r[p];
                     Vec<T>::unpack(x[p], xn[p]);

@@ -192,6 +192,33 @@ def test_rows_whose_squares_overflow(D, dtype):
     assert bool(torch.isfinite(q).all()) and not q[:, :, 3].any() and bool(q[:, :, 2].any()) and not out["rstd"].t.view(9, 3)[3].any()
 
 
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("pairing", [sf.ROTARY_HALVES, sf.ROTARY_ADJACENT])
+@pytest.mark.parametrize("T", [1, 19])
+def test_infinities_that_are_not_turned(T, pairing, dtype):
+    """Without a norm, past the turned elements and in padding, every element is its own."""
+    require_gpu()
+    B, Hq, Hk, D, R = 3, 4, 2, 64, 32
+    g = torch.Generator(device="cuda").manual_seed(5)
+    heads = torch.randn(B, T, Hq + 2 * Hk, D, generator=g, device="cuda").to(DT[dtype])
+    heads[:, :, :, R + 5 :: 7] = float("inf")
+    ids = torch.zeros(B, T, dtype=torch.int32, device="cuda")
+    ids[1], ids[2, ::2] = -1, 4                                                                    # padding
+    heads[1, :, :, ::9] = float("-inf")
+    heads[2, ::2, 1, 3] = float("inf")
+    q, kt, v = (torch.empty(B, n, *rest, dtype=heads.dtype, device="cuda") for n, rest in ((Hq, (T, D)), (Hk, (D, T)), (Hk, (T, D))))
+    back = torch.empty_like(heads).view(B, T, -1)
+    for table, places in ((sf.rotary_table(4, R), ids), (None, None)):                             # place 0: the angles are 0
+        x = heads.clone()
+        if table is None:
+            x[..., :R:3] = float("inf")
+        sf.heads_norm_rotate_forward(x.view(B, T, -1), None, None, 0.0, table, pairing, places, 0.5, 0, 0, q, kt, v, None, None, None)
+        assert torch.equal(q, x[:, :, :Hq].transpose(1, 2) * 0.5)
+        assert torch.equal(kt, x[:, :, Hq : Hq + Hk].permute(0, 2, 3, 1)) and torch.equal(v, x[:, :, Hq + Hk :].transpose(1, 2))
+        sf.heads_norm_rotate_backward(q, kt, v, None, None, None, 0, 0, None, None, None, table, pairing, places, 2.0, back)
+        assert torch.equal(back.view_as(x), x)
+
+
 def test_plain_splits_are_split_heads():
     """Neither norm nor rotation, keys not shared: what split_heads and merge_heads do, to the bit."""
     require_gpu()
