@@ -386,9 +386,12 @@ extern "C" int32_t slimfit_weight_grad_dequant(const void *dy, int32_t dt, const
     else launch_weight<float, 128, 32>(dy, codes, scales, bits, z, plan, dw, parts, st);
     if (parts) {
         const int64_t vectors = N * K / 4;
-        const unsigned blocks = (unsigned)((vectors + kThreads - 1) / kThreads);
-        if (dt == SLIMFIT_BF16) launch(join_kernel<uint16_t>, blocks, kThreads, 0, st, parts, (int)plan.splits, vectors, static_cast<uint16_t *>(dw), 0);
-        else launch(join_kernel<float>, blocks, kThreads, 0, st, parts, (int)plan.splits, vectors, static_cast<float *>(dw), 0);
+        constexpr int64_t kMost = kMaxGridThreads / kThreads * kThreads;
+        for (int64_t first = 0; first < vectors; first += kMost) {
+            const unsigned blocks = (unsigned)tiles_of(vectors - first < kMost ? vectors - first : kMost, kThreads);
+            if (dt == SLIMFIT_BF16) launch(join_kernel<uint16_t>, blocks, kThreads, 0, st, parts, (int)plan.splits, vectors, static_cast<uint16_t *>(dw), first);
+            else launch(join_kernel<float>, blocks, kThreads, 0, st, parts, (int)plan.splits, vectors, static_cast<float *>(dw), first);
+        }
     }
     return launch_status();
 }
