@@ -655,8 +655,9 @@ int32_t slimfit_product(const float *a, const float *b, int32_t b_deep, int64_t 
  *           multiple of block (ERR_UNSUPPORTED), so that a block lies in one row.
  *  fp32   : dy * scale is rounded once, taken apart exactly into three bf16 numbers and multiplied by the codes, whole
  *           numbers that bf16 holds; fp32 sums:
- *           |dw - exact| <= (2 M + 8) * 2^-23 * sum |dy||x^| + M * 2^-120
- *           (products dy * scale of 2^127 and more are outside of this).
+ *           |dw - exact| <= (2 M + 8) * 2^-23 * sum |dy||x^| + M * 2^-120.
+ *           Where that does not come out finite (a dy that is not, dy * scale past fp32 or bf16, a sum that overflows) the
+ *           element is the fp32 products' and sums' of dy and x^: infinite or NaN where those are.
  *  bf16   : x^ rounded to bf16 (the value slimfit_dequant_unpack stores), fp32 sums, rounded to bf16 once:
  *           |dw - exact| <= (2^-8 + (2 M + 8) * 2^-23) * sum |dy||x^| + 2^-8 * |dw|.
  *  Deterministic: the order of the sums goes by the sizes and types alone.

@@ -69,7 +69,7 @@ __device__ __forceinline__ bf16x8 fragment(const char *at)
 enum Rows { kAligned, kAnywhere, kShort };
 
 template <typename T, int BITS, int TN, int TK, Rows ROWS>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 2)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 2)
 weight_kernel(const T *__restrict__ dy, const uint8_t *__restrict__ codes, const float *__restrict__ scales, T *__restrict__ dw,
               float *__restrict__ parts, Sizes z)
 {
@@ -236,6 +236,8 @@ weight_kernel(const T *__restrict__ dy, const uint8_t *__restrict__ codes, const
         __builtin_amdgcn_s_setprio(0);
         __syncthreads();
     }
+    float *const sums = parts ? parts + (int64_t)split * z.N * z.K : F32 ? reinterpret_cast<float *>(dw) : nullptr;
+    bool odd = false;
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         const int64_t n = n0 + wn + j * 16 + (lane & 15);
@@ -245,9 +247,50 @@ weight_kernel(const T *__restrict__ dy, const uint8_t *__restrict__ codes, const
             const int64_t k = k0 + wk + i * 16 + (lane >> 4) * 4;
             if (k >= z.K) continue;
             const f32x4 v = acc[i][j];
-            if (parts) *reinterpret_cast<f32x4 *>(parts + (int64_t)split * z.N * z.K + n * z.K + k) = v;
-            else if constexpr (F32) *reinterpret_cast<f32x4 *>(dw + n * z.K + k) = v;
+            if (F32 || parts) *reinterpret_cast<f32x4 *>(sums + n * z.K + k) = v;
             else *reinterpret_cast<u32x2 *>(dw + n * z.K + k) = u32x2{bf16_narrow2(v[0], v[1]), bf16_narrow2(v[2], v[3])};
+            if constexpr (F32) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) odd |= !(__builtin_fabsf(v[q]) < __builtin_inff());
+            }
+        }
+    }
+    if constexpr (F32) {
+        // dy * scale that is infinite, NaN or rounds to bf16's infinity, or a sum that overflows: what comes out there is what the fp32
+        // matrix instructions make of dy and x^, for which the wave goes over its share of the tile again (12608 x 1024 x 4096 with all
+        // entries of dy NaN 3.0 ms in all).  Five waves a SIMD are asked for, or the compiler spends the registers that this leaves unused.
+        if (__builtin_amdgcn_ballot_w64(odd) == 0u) return;
+        static_assert(WAVES_K == 1, "a wave's columns are the tile's, which ends with a block and so within K");
+        const uint8_t *const px = codes + (k0 + (lane & 15)) * BITS / 8;
+        const float *const ps = scales + (k0 >> z.block_shift);
+#pragma unroll 1
+        for (int j = 0; j < FN; ++j) {
+            const int64_t n = n0 + wn + j * 16 + (lane & 15);
+            const T *const py = dy + min(n, z.N - 1);
+            f32x4 plain[FK];
+#pragma unroll
+            for (int i = 0; i < FK; ++i) plain[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+            for (int64_t m = m0; m < m1; m += 4) {         // lane l holds row m + l / 16 of both; rows past the part's end count as zeros
+                const int64_t row = min(m + (lane >> 4), m1 - 1);
+                const bool in = m + (lane >> 4) < m1;
+                const float step = ps[row * (z.K >> z.block_shift)], fy = in ? py[row * z.N] : 0.0f;
+#pragma unroll
+                for (int i = 0; i < FK; ++i) {
+                    const uint32_t code = px[row * code_row + i * 16 * BITS / 8];
+                    const float fx = in ? (float)code_field<BITS>(code, BITS == 8 ? 0 : lane & 1) * step : 0.0f;
+                    plain[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(fx, fy, plain[i], 0, 0, 0);
+                }
+            }
+            if (n >= z.N) continue;
+#pragma unroll
+            for (int i = 0; i < FK; ++i) {
+                f32x4 *const at = reinterpret_cast<f32x4 *>(sums + n * z.K + k0 + i * 16 + (lane >> 4) * 4);     // its own store above
+                f32x4 v = *at;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[q] = __builtin_fabsf(v[q]) < __builtin_inff() ? v[q] : plain[i][q];
+                *at = v;
+            }
         }
     }
 }

@@ -127,6 +127,41 @@ def test_inputs_of_the_largest_size(bits, dtype):
         _check(dw, rows, x_hat)
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("M,N,K,block", [(100, 40, 128, 64), (131, 41, 96, 32), (70, 3, 64, 32), (4200, 24, 64, 32)])
+def test_fp32_gradients_that_are_not_finite_or_overflow_with_the_scale(M, N, K, block, bits):
+    """Infinities and NaN come out where the product has them, and gradients that are infinite once the scale is on them, or once
+    rounded to a bf16 part, are finite where their codes make them so."""
+    require_gpu()
+    g = torch.Generator(device="cuda").manual_seed(M)
+    codes, scales, x = _cached(M, K, bits, block, M)
+    dy = torch.randn(M, N, generator=g, device="cuda") * 0.1
+    code = torch.randint(-7, 8, (M, K), generator=g, device="cuda")
+    large = 3.4e38                                                       # a step of bf16 below 2^128 and a quarter: rounds to infinity
+    code[11] = code[11].sign()
+    code[13] = 0
+    scales.view(M, -1)[11] = 1.0
+    scales.view(M, -1)[13] = 4.0
+    dy[11, 0] = large
+    dy[13, 1] = 2e38                                                     # times the scale: past fp32
+    dy[M - 1, N - 1] = float("-inf")
+    dy[M - 1, N - 2] = float("nan") if N > 3 else 0.0
+    if N > 3:
+        dy[2, 2], dy[9, 3], dy[M // 2, 3] = float("inf"), float("inf"), float("-inf")
+    raw = code.to(torch.int8).view(torch.uint8).view(-1)
+    codes.copy_(raw if bits == 8 else (raw[0::2] & 15) | (raw[1::2] << 4))
+    x = (code.double().view(-1, block) * scales.double().view(-1)[:, None]).view(M, K)
+    dw = Guarded(N * K, torch.float32)
+    sf.weight_grad_dequant(dy, codes, scales, bits, block, dw.t.view(N, K))
+    dw.check()
+    got = dw.t.view(N, K).double()
+    want, total = (sum((a[i : i + 50, :, None] * b[i : i + 50, None]).sum(0) for i in range(0, M, 50)) for a, b in ((dy.double(), x), (dy.double().abs(), x.abs())))
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.isinf(), want.isinf())
+    assert bool((got == want)[want.isinf()].all()) and bool(want[:2].isfinite().all()) and bool(want.isinf().any())
+    fine = want.isfinite()
+    assert bool(((got - want).abs() <= (2 * M + 8) * 2.0 ** -23 * total + M * 2.0 ** -120)[fine].all())
+
+
 def test_offsets_past_32_bits():
     """Rows whose codes, and whose gradients, lie past 4 GB."""
     require_gpu()
