@@ -290,6 +290,12 @@ class SplitHeadsFunction(torch.autograd.Function):
         return dqkv, None, None
 
 
+def _recorded(ctx) -> bool:
+    """Whether the call becomes part of a graph.  Inside forward gradients are off whatever the caller has, and requires_grad and
+    needs_input_grad do not tell, but a call under no_grad is linked to nothing.  (A traced context has no links to look at.)"""
+    return torch.compiler.is_compiling() or len(ctx.next_functions) > 0
+
+
 class GatedFunction(torch.autograd.Function):
     """y = act(gate) * up for x = [gate | up] (..., 2 F); ``act`` is binding.ACT_SILU or ACT_GELU, F a multiple of ``block``."""
 
@@ -298,7 +304,7 @@ class GatedFunction(torch.autograd.Function):
         F = x.shape[-1] // 2
         x2 = x.contiguous().view(-1, x.shape[-1])
         y = torch.empty(x2.shape[0], F, dtype=x.dtype, device=x.device)
-        if not ctx.needs_input_grad[0]:
+        if not (ctx.needs_input_grad[0] and _recorded(ctx)):
             sf.gated_quant_pack(x2, act, sf.Q_BLOCK, 0, block, 0, y, None, None)
             return y.view(*x.shape[:-1], F)
         codes = torch.empty(sf.packed_bytes(x2.numel(), bits), dtype=torch.uint8, device=x.device)
@@ -334,7 +340,7 @@ class HeadsNormRotateFunction(torch.autograd.Function):
         q = torch.empty(B, heads, T, D, dtype=qkv.dtype, device=qkv.device)
         kt = torch.empty(B, kv_heads, D, T, dtype=qkv.dtype, device=qkv.device)
         v = torch.empty(B, kv_heads, T, D, dtype=qkv.dtype, device=qkv.device)
-        keeps = norm and any(ctx.needs_input_grad[:3])
+        keeps = norm and any(ctx.needs_input_grad[:3]) and _recorded(ctx)
         bits = bits if keeps else 0
         rstd = codes = scales = None
         if norm:
@@ -433,7 +439,7 @@ class LinearFunction(torch.autograd.Function):
             y = torch.nn.functional.linear(x, weight, bias)
         ctx.cache = None                                   # descriptor of what is kept of x: nothing, or (bits, block, shape, dtype)
         ctx.bias_active = bias is not None and bias.requires_grad
-        if weight.requires_grad:
+        if weight.requires_grad and _recorded(ctx):
             codes, scales = _quantise(x, bits, block)
             ctx.cache = (bits, block, x.shape, x.dtype)
             ctx.straight = straight

@@ -139,3 +139,24 @@ def test_rotary_table():
     assert t.shape == (5, 8) and t.dtype == torch.float32
     angle = torch.arange(5).double()[:, None] * torch.tensor([1.0, 0.1, 0.01, 0.001]).double()
     assert torch.allclose(t.double(), torch.cat((angle.cos(), angle.sin()), 1), rtol=0, atol=2.0 ** -24)
+
+
+@pytest.mark.parametrize("grad", [True, False])
+def test_wrappers_keep_nothing_where_gradients_are_off(grad, monkeypatch):
+    """Trainable gains, weights and inputs under no_grad: the calls are asked for no cache and nothing is quantised."""
+    from paper_2305_18513_amd import autograd as ag
+
+    asked = []
+    monkeypatch.setattr(ag.sf, "gated_quant_pack", lambda x, act, mode, bits, *rest: asked.append(bits))
+    monkeypatch.setattr(ag.sf, "heads_norm_rotate_forward", lambda *a: asked.append(a[8]))
+    monkeypatch.setattr(ag.sf, "quant_pack", lambda x, mode, bits, *rest: asked.append(bits))
+
+    def leaf(*shape):
+        return torch.zeros(*shape, requires_grad=True)
+
+    with torch.set_grad_enabled(grad):
+        outs = [ag.GatedFunction.apply(leaf(2, 128), sf.ACT_SILU, 8, 32),
+                ag.HeadsNormRotateFunction.apply(torch.zeros(1, 2, 256), leaf(64), leaf(64), 2, 1, None)[0],
+                ag.LinearFunction.apply(torch.zeros(4, 64), leaf(8, 64), leaf(8))]
+    assert asked == ([8, 8, 8] if grad else [0, 0])
+    assert all(o.requires_grad == grad for o in outs)
