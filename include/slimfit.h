@@ -661,7 +661,8 @@ int32_t slimfit_product(const float *a, const float *b, int32_t b_deep, int64_t 
  *  bf16   : x^ rounded to bf16 (the value slimfit_dequant_unpack stores), fp32 sums, rounded to bf16 once:
  *           |dw - exact| <= (2^-8 + (2 M + 8) * 2^-23) * sum |dy||x^| + 2^-8 * |dw|.
  *  Deterministic: the order of the sums goes by the sizes and types alone.
- *  workspace : DEVICE, 16-byte aligned, of the bytes that slimfit_weight_grad_dequant_workspace reports (0 where no sum is shared out);
+ *  workspace : DEVICE, 16-byte aligned, of the bytes that slimfit_weight_grad_dequant_workspace reports (0 where no sum is shared out, and never more
+ *           than x^ in dt would take or 256 MiB, whichever is larger);
  *           contents overwritten.
  *  dy, codes, scales 16-byte aligned, dw too; none shares memory with dw (INVALID_ARG).  N and K up to 2^20, and no
  *           more tiles of 128 x 32 than a launch can have workgroups, 2^23 (ERR_UNSUPPORTED).

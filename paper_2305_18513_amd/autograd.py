@@ -430,7 +430,8 @@ class LinearFunction(torch.autograd.Function):
     and forms its weight gradient from the dequantised x^.  The library's fp32 product (sizes: ``_quicker``) holds all bits of
     its operands and is no further from the exact one than fp32 additions in any order; where the program allows torch fewer
     bits (``torch.set_float32_matmul_precision``) the products are torch's.  ``straight``: the weight gradient is formed from
-    the codes themselves where the layer's inputs are a multiple of ``block``; x^ is not written to memory."""
+    the codes themselves where the layer's inputs are a multiple of ``block``; x^ is not written to memory (sums that are shared
+    out take a workspace in its place, of its size or of 256 MiB at most)."""
 
     @staticmethod
     def forward(ctx, x: torch.Tensor, weight: torch.Tensor, bias, bits: int = 8, block: int = 64, straight: bool = False):

@@ -18,6 +18,7 @@
 // (184 and 187), two groups of four waves that form and multiply in turn (190 to 197), operands turned in registers on the
 // way in (247); fp32 alike (465 to 490), its single stage with four workgroups a compute unit 431.
 #include "common.hpp"
+#include "weight_plan.hpp"
 
 #include <type_traits>
 
@@ -42,7 +43,6 @@ template <> struct Config<uint16_t, 128, 128> { static constexpr int PARTS = 1, 
 template <> struct Config<float, 128, 64> { static constexpr int PARTS = 3, WAVES_N = 4; };
 template <> struct Config<float, 128, 32> { static constexpr int PARTS = 3, WAVES_N = 4; };
 
-constexpr int kStep = 32;
 // a row of a tile in LDS: 32 bytes more than it holds, so that sixteen rows' 32 bytes, which a transposing read takes, are in
 // different banks two by two
 constexpr int pitch_of(int columns) { return columns * 2 + 32; }
@@ -308,54 +308,6 @@ join_kernel(const float *__restrict__ parts, int count, int64_t vectors, T *__re
     else reinterpret_cast<u32x2 *>(dw)[i] = u32x2{bf16_narrow2(sum[0], sum[1]), bf16_narrow2(sum[2], sum[3])};
 }
 
-int64_t tiles_of(int64_t n, int tile) { return (n + tile - 1) / tile; }
-
-// How wide the tiles are and among how many workgroups a tile's sum is shared: what takes the least time by this count of
-// microseconds, measured over 20 sizes from 300 x 300 x 256 to 16384 x 4096 x 1024.  A step of 32 rows takes a + b * (workgroups on
-// the fullest compute unit), of which `most` go on one at a time; rows of dy that begin anywhere cost `ragged` as much.  Parts are
-// written and read again at 4.2 TB/s by a launch of 3 us.  (Chosen: 16384 x 4096 x 1024 bf16 256 wide in 4 parts 165 us, 128 wide in 3
-// 187, in one 322; 4096 x 768 x 768 128 wide in 6 25, in one 72; 12608 x 1024 x 4096 fp32 in 2 403, though 391 in 4, in one 461.)
-struct Pace {
-    int tile_n, most;
-    float a, b, ragged;
-};
-constexpr Pace kNarrow = {128, 4, 0.40f, 0.23f, 1.25f}, kWide = {256, 2, 0.39f, 0.39f, 1.6f}, kSplit = {128, 4, 0.45f, 0.39f, 1.25f};
-
-struct Plan {
-    int tile_n, tile_k;
-    int64_t tiles, splits, split_rows;
-    Plan(int32_t dt, int32_t block, int64_t M, int64_t N, int64_t K)
-    {
-        tile_k = dt == SLIMFIT_BF16 ? 128 : block >= 64 ? 64 : 32;
-        const int64_t steps = tiles_of(M, kStep);
-        const bool ragged = N % (dt == SLIMFIT_BF16 ? 8 : 4) != 0;
-        float best = 0.0f;
-        auto look = [&](const Pace &p) {
-            const int64_t t = tiles_of(N, p.tile_n) * tiles_of(K, tile_k), full = 256 * p.most;
-            for (const int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-                if (s > 1 && steps < 2 * s) break;
-                const int64_t groups = t * s, rest = groups % full;
-                const float step = (float)(groups / full) * (p.a + p.b * (float)p.most) + (rest ? p.a + p.b * (float)tiles_of(rest, 256) : 0.0f);
-                const float join = s > 1 ? 3.0f + (float)s * (float)N * (float)K * (8.0f / 4.2e6f) : 0.0f;
-                const float time = (float)tiles_of(steps, s) * step * (ragged ? p.ragged : 1.0f) + join;
-                if (best == 0.0f || time < best) {
-                    best = time;
-                    tile_n = p.tile_n;
-                    tiles = t;
-                    splits = s;
-                }
-            }
-        };
-        tile_n = 128;
-        tiles = splits = 1;
-        look(dt == SLIMFIT_BF16 ? kNarrow : kSplit);
-        if (dt == SLIMFIT_BF16) look(kWide);
-        split_rows = tiles_of(steps, splits) * kStep;
-        if (split_rows == 0) split_rows = kStep;
-    }
-    size_t workspace(int64_t N, int64_t K) const { return splits > 1 ? (size_t)splits * (size_t)N * (size_t)K * 4 : 0; }
-};
-
 int32_t validate(int32_t dt, int64_t M, int64_t N, int64_t K)
 {
     if (!dtype_ok(dt) || M < 0 || N < 0 || K < 0) return SLIMFIT_ERR_INVALID_ARG;
@@ -364,7 +316,7 @@ int32_t validate(int32_t dt, int64_t M, int64_t N, int64_t K)
 }
 
 template <typename T, int TN, int TK>
-void launch_weight(const void *dy, const uint8_t *codes, const float *scales, int bits, const Sizes &z, const Plan &plan, void *dw, float *parts, hipStream_t st)
+void launch_weight(const void *dy, const uint8_t *codes, const float *scales, int bits, const Sizes &z, const WeightPlan &plan, void *dw, float *parts, hipStream_t st)
 {
     const unsigned grid = (unsigned)(plan.tiles * plan.splits);
     const T *y = static_cast<const T *>(dy);
@@ -391,7 +343,7 @@ extern "C" int32_t slimfit_weight_grad_dequant_workspace(int32_t dt, int32_t blo
     if (rc != SLIMFIT_OK) return rc;
     if (block != 32 && block != 64 && block != 128 && block != 256) return SLIMFIT_ERR_UNSUPPORTED;
     if (!bytes) return SLIMFIT_ERR_INVALID_ARG;
-    *bytes = N == 0 || K == 0 ? 0 : Plan(dt, block, M, N, K).workspace(N, K);
+    *bytes = N == 0 || K == 0 ? 0 : WeightPlan(dt, block, M, N, K).workspace(N, K);
     return SLIMFIT_OK;
 }
 
@@ -408,7 +360,7 @@ extern "C" int32_t slimfit_weight_grad_dequant(const void *dy, int32_t dt, const
     const size_t e = dtype_size(dt), out = (size_t)N * (size_t)K * e, in = (size_t)M * (size_t)N * e, kept = (size_t)M * (size_t)K;
     const size_t code_bytes = kept * (size_t)bits / 8, scale_bytes = kept / (size_t)block * 4;
     if (meet(dw, out, dy, in) || meet(dw, out, codes, code_bytes) || meet(dw, out, scales, scale_bytes)) return SLIMFIT_ERR_INVALID_ARG;
-    const Plan plan(dt, block, M, N, K);
+    const WeightPlan plan(dt, block, M, N, K);
     const size_t need = plan.workspace(N, K);
     if (plan.tiles > kMaxGridThreads / kThreads / plan.splits) return SLIMFIT_ERR_UNSUPPORTED;
     if (need > 0) {
