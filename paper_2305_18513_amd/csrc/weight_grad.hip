@@ -324,9 +324,12 @@ void launch_weight(const void *dy, const uint8_t *codes, const float *scales, in
     constexpr int E = 16 / sizeof(T);
     auto go = [&](auto b) {
         constexpr int BITS = decltype(b)::value;
-        if (z.N % E == 0) launch(weight_kernel<T, BITS, TN, TK, kAligned>, grid, kThreads, 0, st, y, codes, scales, out, parts, z);
-        else if (z.N > E) launch(weight_kernel<T, BITS, TN, TK, kAnywhere>, grid, kThreads, 0, st, y, codes, scales, out, parts, z);
-        else launch(weight_kernel<T, BITS, TN, TK, kShort>, grid, kThreads, 0, st, y, codes, scales, out, parts, z);
+        if (z.N % E == 0) {
+            launch(weight_kernel<T, BITS, TN, TK, kAligned>, grid, kThreads, 0, st, y, codes, scales, out, parts, z);
+        } else if constexpr (TN < 256) {                   // (tiles 256 wide are planned for aligned rows alone)
+            if (z.N > E) launch(weight_kernel<T, BITS, TN, TK, kAnywhere>, grid, kThreads, 0, st, y, codes, scales, out, parts, z);
+            else launch(weight_kernel<T, BITS, TN, TK, kShort>, grid, kThreads, 0, st, y, codes, scales, out, parts, z);
+        }
     };
     if (bits == 8) go(std::integral_constant<int, 8>{});
     else go(std::integral_constant<int, 4>{});

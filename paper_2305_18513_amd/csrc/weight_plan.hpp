@@ -23,7 +23,8 @@ struct Pace {
     int tile_n, most;
     float a, b, ragged;
 };
-constexpr Pace kNarrow = {128, 4, 0.40f, 0.23f, 1.25f}, kWide = {256, 2, 0.39f, 0.39f, 1.6f}, kSplit = {128, 4, 0.45f, 0.39f, 1.25f};
+constexpr Pace kNarrow = {128, 4, 0.40f, 0.23f, 1.25f}, kSplit = {128, 4, 0.45f, 0.39f, 1.25f};
+constexpr Pace kWide = {256, 2, 0.39f, 0.39f, 0.0f};       // for rows of dy that begin on 16 bytes alone: others cost 1.6 times as much and never gain
 
 // The parts' memory is at most 256 MiB, a thousandth of the card's, or the size of x^, which this way of forming the product saves.
 // (16384 x 6144 x 4096 bf16 in 2 parts of 201 MB 838 us, in one 943; 16384 x 5120 x 5120 945 in 3 of 315 MB, 950 in one;
@@ -56,7 +57,7 @@ struct WeightPlan {
         for (const int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
             if (s > 1 && (steps < 2 * s || s * N * K * 4 > most)) break;
             look(dt == SLIMFIT_BF16 ? kNarrow : kSplit, s);
-            if (dt == SLIMFIT_BF16) look(kWide, s);
+            if (dt == SLIMFIT_BF16 && !ragged) look(kWide, s);
         }
         split_rows = tiles_of(steps, splits) * kStep;
         if (split_rows == 0) split_rows = kStep;

@@ -77,6 +77,22 @@ def test_long_sums_are_shared_out(M, N, K, block, dtype):
     assert e.value.status == sf.ERR_WORKSPACE
 
 
+# bf16 sizes whose tiles are 256 x 128 (test_weight_plan_cpu.py checks that they are): rows of dw and columns that end inside a tile,
+# several bands and columns of tiles, sums in one part and in several
+WIDE = [(333, 1032, 5280), (130, 2312, 2208), (70, 4104, 1312), (4100, 2312, 416), (6000, 520, 5280)]
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("M,N,K", WIDE)
+def test_wide_tiles(M, N, K, bits):
+    require_gpu()
+    assert (sf.weight_grad_dequant_workspace(torch.bfloat16, 32, M, N, K) > 0) == (M > 4000)
+    dy, codes, scales, dw = _run(M, N, K, bits, 32, torch.bfloat16, M)
+    again = torch.empty_like(dw)
+    sf.weight_grad_dequant(dy, codes, scales, bits, 32, again)
+    assert torch.equal(again, dw)
+
+
 @pytest.mark.parametrize("dtype", DT)
 def test_no_rows_and_zeros(dtype):
     require_gpu()
