@@ -472,13 +472,16 @@ class LinearFunction(torch.autograd.Function):
 
 def _straight(dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bits: int, block: int, K: int, dtype):
     """dy.T @ x^ from x's codes, or None where that is torch's: blocks that straddle rows, types that differ, products that are
-    watched, tensors that are not the kernel's to read."""
+    watched, tensors that are not the kernel's to read, gradients past what a call takes."""
+    N = dy.shape[1]
+    if max(N, K) > 1 << 20 or -(-N // 128) * -(-K // 32) > 1 << 23:
+        return None
     if K % block != 0 or dy.dtype != dtype or _watched() or dy.get_device() != torch.cuda.current_device():
         return None
     dy = dy.contiguous()
     if not all(_plain(t) for t in (dy, codes, scales)):
         return None
-    dw = torch.empty(dy.shape[1], K, dtype=dtype, device=dy.device)
+    dw = torch.empty(N, K, dtype=dtype, device=dy.device)
     sf.weight_grad_dequant(dy, codes, scales, bits, block, dw)
     return dw
 

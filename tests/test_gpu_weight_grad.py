@@ -223,6 +223,16 @@ def test_linear_function(dtype):
         assert bool(((grads[0][1].double() - grads[1][1].double()).abs() <= tol).all())
 
 
+def test_linear_function_past_what_a_call_takes():
+    """A layer of more outputs than that: torch's product, as without ``straight``."""
+    require_gpu()
+    N, K = (1 << 20) + 8, 64
+    x, w = torch.randn(3, K, device="cuda"), torch.randn(N, K, device="cuda").requires_grad_(True)
+    dy = torch.randn(3, N, device="cuda")
+    grads = [torch.autograd.grad(ag.LinearFunction.apply(x, w, None, 8, 64, straight), w, dy)[0] for straight in (False, True)]
+    assert torch.equal(*grads)
+
+
 def test_arguments():
     require_gpu()
     codes, scales, _ = _cached(64, 96, 8, 32, 0)
