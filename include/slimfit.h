@@ -277,11 +277,12 @@ int32_t slimfit_gelu_backward_dequant(const uint8_t *codes, const float *scales,
  *     bit for bit, x read once.  Backward, with gate^ and up^ from the cache,
  *         dx = [dy * up^ * act'(gate^) | dy * act(gate^)].
  *     act: SLIMFIT_ACT_SILU  act(g) = g / (1 + e^-g),  SLIMFIT_ACT_GELU the exact
- *     form of (b').  fp32 arithmetic: y within (6e-7 + 2e-7 * |gate|) * |up * gate|
- *     + 1e-6 * |y| of the fp64 value, either half of dx within (6e-7 + 2e-7 *
- *     |gate^|) * (1 + |gate^|) * |dy * up^| resp. (6e-7 + 2e-7 * |gate^|) * |dy *
- *     gate^| of its own plus 1e-6 relative, bf16 results within one further bf16
- *     rounding; results below 1e-37 may come out as 0.
+ *     form of (b').  fp32 arithmetic.  SiLU's y is within (6e-7 + 1e-7 |gate|) |y| +
+ *     1e-36 |up| of the fp64 value, GELU's within 4e-7 min(|gate|, 6) |up| + 1e-6 |y|
+ *     + 5e-15 |gate up|;
+ *     the second half of dx the same with dy for up and gate^ for gate, the first
+ *     within (6e-7 + 2e-7 min(|gate^|, 18)) |dy up^| + 1e-6 relative; bf16 results
+ *     within one further bf16 rounding; results below 1e-37 may come out as 0.
  *
  *  x, dx : DEVICE, rows * 2 F elements of dt;  y, dy : DEVICE, rows * F.  16-byte
  *          aligned; x and y, dx and dy must not share memory (INVALID_ARG).

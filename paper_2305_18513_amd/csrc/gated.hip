@@ -26,14 +26,17 @@ __device__ __forceinline__ float logistic(float x)
 {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.44269504088896340736f));
 }
+// erfc's argument is held at 6, the polynomial's least value (8e-15): held at 4.2 it would leave GELU 1.5e-9 of the gate, however far
+// below zero that is (setting it to 0 there instead: 7289 x 2 x 2048 fp32 forward and backward 65.6 -> 67.3 us).
+constexpr float kFar = 6.0f;
 template <bool GELU>
-__device__ __forceinline__ float act_value(float x) { return GELU ? gelu_f32(x) : x * logistic(x); }
+__device__ __forceinline__ float act_value(float x) { return GELU ? (0.5f * x) * twice_normal_cdf(x, kFar) : x * logistic(x); }
 // act(x) and act'(x)
 template <bool GELU>
 __device__ __forceinline__ void act_both(float x, float &value, float &slope)
 {
     if (GELU) {
-        const float cdf = 0.5f * twice_normal_cdf(x);
+        const float cdf = 0.5f * twice_normal_cdf(x, kFar);
         value = x * cdf;
         slope = cdf + x * (__builtin_amdgcn_exp2f(((-0.5f * x) * x) * 1.44269504088896340736f) * 0.39894228040143267794f);
     } else {

@@ -91,6 +91,51 @@ def test_fixed_point_caches_and_none(rows, F, dtype):
             _run(x, dy, act, sf.Q_FIXED, bits, 0, fb)
 
 
+def _off(got, want, tol, bf16):
+    """The largest |got - want| beyond ``tol``, half a step of bf16 and the smallest numbers."""
+    return float(((got.double() - want).abs() - tol - 1e-37 - (want.abs() * 2.0 ** -8 if bf16 else 0.0)).max())
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("act", [sf.ACT_SILU, sf.ACT_GELU])
+def test_gates_of_any_size(act, dtype):
+    """Gates far from zero, where an activation is its gate or nothing and its slope one or zero: tolerances as the header states
+    them, none of which grows with the size of a gate on the side where the result is nothing.  They count: for SiLU the
+    argument's rounding and constant (7.3e-8 of |gate|), a step each of exp2 and the reciprocal, the sum's and two products' half
+    steps; its slope's 1 - p keeps the absolute error of p, 1.8e-7, times the gate up to 17.4, beyond which 1 + e^-gate is 1; for
+    GELU 2.1e-7 of erfc, 1.2e-7 of 2 - erfc and three half steps, and 4.1e-15 of a gate below -8.5."""
+    require_gpu()
+    g = torch.Generator(device="cuda").manual_seed(9)
+    far = torch.logspace(0, 8, 2048, device="cuda")
+    gate = torch.cat((torch.linspace(-40, 40, 8192, device="cuda"), torch.linspace(-6.0, -5.9, 512, device="cuda"),
+                      torch.linspace(-105, -85, 512, device="cuda"), far, -far)).view(-1, 512)
+    up = torch.randn(gate.shape, generator=g, device="cuda")
+    x = torch.cat((gate, up), 1).to(DT[dtype])
+    bf16 = dtype == "bf16"
+    rows = gate.shape[0]
+    y, codes, scales = torch.empty(rows, 512, dtype=x.dtype, device="cuda"), torch.empty(rows * 1024, dtype=torch.uint8, device="cuda"), torch.empty(rows * 32, device="cuda")
+    sf.gated_quant_pack(x, act, sf.Q_BLOCK, 8, 32, 0, y, codes, scales)
+
+    def tol(g, u, value):
+        if act == sf.ACT_SILU:
+            return (6e-7 + 1e-7 * g.abs()) * (value * u).abs() + 1e-36 * u.abs()
+        return 4e-7 * g.abs().clamp(max=6.0) * u.abs() + 1e-6 * (value * u).abs() + 5e-15 * (g * u).abs()
+
+    g64, u64 = x.double().chunk(2, 1)
+    value, _ = _parts(g64, act)
+    assert _off(y, value * u64, tol(g64, u64, value), bf16) <= 0
+    dy = torch.randn(rows, 512, generator=g, device="cuda").to(x.dtype)
+    dx = torch.empty_like(x)
+    sf.gated_backward_dequant(codes, scales, act, sf.Q_BLOCK, 8, 32, 0, dy, dx)
+    xhat = torch.empty(x.numel(), device="cuda")
+    sf.dequant_unpack(codes, scales, sf.Q_BLOCK, 8, 32, 0, xhat)
+    g64, u64 = xhat.double().view(rows, 1024).chunk(2, 1)
+    value, slope = _parts(g64, act)
+    d = dy.double()
+    assert _off(dx[:, 512:], d * value, tol(g64, d, value), bf16) <= 0
+    assert _off(dx[:, :512], d * u64 * slope, (6e-7 + 2e-7 * g64.abs().clamp(max=18.0)) * (d * u64).abs() + 1e-6 * (d * u64 * slope).abs(), bf16) <= 0
+
+
 @pytest.mark.parametrize("dtype", DT)
 def test_blocks_of_zeros_and_of_tiny_numbers_are_kept_as_zeros(dtype):
     require_gpu()
