@@ -335,7 +335,7 @@ __device__ __forceinline__ void forward_heads(const Place<T, L> &w, const Part &
     const int64_t head = (int64_t)z.tokens * z.dim;
     for (int half = 0; half < (int)z.passes; half += kHeld) {
         float c[kHeld][E], s[kHeld][E];
-        bool turned[kHeld];                                // (asked without a norm: a row of one that holds an infinity is lost)
+        bool turned[kHeld];
         uint32_t line[kHeld], at[kHeld];                   // the row in the tile, the vector of its first head
         T *to[kHeld];
 #pragma unroll
@@ -395,7 +395,7 @@ __device__ __forceinline__ void forward_heads(const Place<T, L> &w, const Part &
 #pragma unroll
             for (int p = 0; p < kHeld; ++p) {
                 float y[E];
-                turn<T>(now[p], f[p], c[p], s[p], MODE != kNoNorm || turned[p], from, z, y);
+                turn<T>(now[p], f[p], c[p], s[p], turned[p], from, z, y);
                 if constexpr (MODE != kNoNorm) {
                     float sum = 0.0f;
 #pragma unroll
@@ -515,7 +515,7 @@ __device__ __forceinline__ void backward_heads(const Place<T, L> &w, const Part 
             for (int p = 0; p < kHeld; ++p) {
                 float f[E];
                 Vec<T>::unpack(grad[p], f);
-                turn<T>(grad[p], f, c[p], s[p], MODE != kNoNorm || turned[p], from, z, g[p]);
+                turn<T>(grad[p], f, c[p], s[p], turned[p], from, z, g[p]);
                 if constexpr (MODE == kNoCache) {
                     root[p] = r[p];
                     Vec<T>::unpack(x[p], xn[p]);

@@ -219,6 +219,40 @@ def test_infinities_that_are_not_turned(T, pairing, dtype):
         assert torch.equal(back.view_as(x), x)
 
 
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("pairing", [sf.ROTARY_HALVES, sf.ROTARY_ADJACENT])
+def test_infinities_that_are_not_turned_with_a_norm(pairing, dtype):
+    """A row that holds an infinity has an rstd of 0: the element is NaN and the others are 0, past the turned ones and in padding, and
+    an infinite gradient there is its own element's in the gains' sums."""
+    require_gpu()
+    c = Case(1, 21, 2, 1, 64, 32, DT[dtype], pairing)
+    c.ids = torch.arange(21, dtype=torch.int32, device="cuda").view(1, 21)
+    c.ids[0, 4] = -1
+    heads = c.qkv.view(1, 21, 4, 64)
+    heads[0, 0, 0, 0] = 1.0                                                     # (a head of zeros otherwise)
+    heads[0, 4, :3, 3] = float("inf")                                           # in padding
+    heads[0, 7, :3, 41] = float("-inf")                                         # past the turned elements
+    out = c.buffers()
+    c.forward(out)
+    q, kt = out["q"].t.view(1, 2, 21, 64).float(), out["kt"].t.view(1, 1, 64, 21).float()
+    for y in (q[0, 0], q[0, 1], kt[0, 0].t()):
+        for row, at in ((4, 3), (7, 41)):
+            assert bool(y[row, at].isnan()) and not y[row, :at].any() and not y[row, at + 1 :].any()
+        assert bool(y[[0, 1, 2, 3, 5, 6, *range(8, 21)]].isfinite().all())
+    c = Case(1, 21, 2, 1, 64, 32, DT[dtype], pairing)
+    c.ids = torch.arange(21, dtype=torch.int32, device="cuda").view(1, 21)
+    c.ids[0, 4] = -1
+    out = c.buffers()
+    c.forward(out)
+    dq, dkt, _ = c.grads
+    dq[0, 0, 4, 3], dq[0, 1, 7, 41] = float("inf"), float("inf")
+    dkt[0, 0, 3, 4], dkt[0, 0, 41, 7] = float("inf"), float("inf")
+    dqkv, dgq, dgk = torch.empty_like(c.qkv), torch.empty(64, device="cuda"), torch.empty(64, device="cuda")
+    c.backward(out, dqkv, dgq, dgk)
+    for dg in (dgq, dgk):
+        assert [i for i, fine in enumerate(dg.isfinite().tolist()) if not fine] == [3, 41]
+
+
 def test_plain_splits_are_split_heads():
     """Neither norm nor rotation, keys not shared: what split_heads and merge_heads do, to the bit."""
     require_gpu()
