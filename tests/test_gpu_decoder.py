@@ -58,6 +58,29 @@ def test_block_and_its_gradients(hidden, heads, kv_heads, T, act):
         assert float((a.double() - b).norm() / b.norm()) <= 12 * 0.005, name
 
 
+@pytest.mark.parametrize("act", [sf.ACT_SILU, sf.ACT_GELU])
+def test_block_and_its_gradients_in_bf16(act):
+    """Against the same block in 64 bits, on the same bf16 weights and inputs."""
+    require_gpu()
+    g = torch.Generator(device="cuda").manual_seed(6)
+    p = ag.decoder_block_params(256, 4, 2, 512, "cuda", 1, torch.bfloat16)
+    table = sf.rotary_table(64, 64)
+    x = torch.randn(2, 60, 256, generator=g, device="cuda").bfloat16().requires_grad_(True)
+    dout = torch.randn(2, 60, 256, generator=g, device="cuda").bfloat16()
+    out = ag.decoder_block(x, p, 4, 2, table, None, 1000000, 8, 32, act)
+    wide = {n: t.detach().double().requires_grad_(True) for n, t in p.items()}
+    xw = x.detach().double().requires_grad_(True)
+    want = _plain_block(xw, wide, 4, 2, table.double(), act)
+    # a tensor that is rounded to bf16 is off by 2^-8 / sqrt 3 * 0.72, below 2^-9, of its norm; 14 are on the way (two norms, four linear
+    # layers, q, k and their product, the probabilities and theirs, the gated one, two sums), added up
+    assert float((out.double() - want).detach().norm() / want.detach().norm()) <= 14 * 2.0 ** -9
+    got = torch.autograd.grad(out, [x, *p.values()], dout)
+    ref = torch.autograd.grad(want, [xw, *wide.values()], dout.double())
+    for name, a, b in zip(["x", *p], got, ref):
+        # and as many on the way back, besides a dozen caches of 8 bits (0.5 % each, as above)
+        assert float((a.double() - b).norm() / b.norm()) <= 28 * 2.0 ** -9 + 12 * 0.005, name
+
+
 def test_block_frozen_and_active():
     require_gpu()
     p = ag.decoder_block_params(128, 4, 2, 256, "cuda", 1, torch.bfloat16)

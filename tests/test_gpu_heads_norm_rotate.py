@@ -179,6 +179,35 @@ def test_many_heads_and_rows(dtype):
     _check(Case(16, 512, 32, 8, 128, 128, DT[dtype], bits=8, block=64))
 
 
+def test_offsets_past_32_bits():
+    """Rows past 2^31 elements and 4 GB of the projection: those at the end are what a call of them alone gives, to the bit."""
+    require_gpu()
+    T, few, Hq, Hk, D, bits, block = (1 << 21) + 37, 61, 6, 1, 128, 8, 64
+    g = torch.Generator(device="cuda").manual_seed(4)
+    gains = [torch.rand(D, generator=g, device="cuda") + 0.5 for _ in range(2)]
+    table = sf.rotary_table(100, D)
+
+    def empty(*shape, dtype=torch.bfloat16):
+        return torch.empty(*shape, dtype=dtype, device="cuda")
+
+    def both(qkv, dq, dkt, dv, ids):
+        n = qkv.shape[1]
+        q, kt, v, dqkv = empty(1, Hq, n, D), empty(1, Hk, D, n), empty(1, Hk, n, D), empty(*qkv.shape)
+        rstd, codes, scales = empty(n, Hq + Hk, dtype=torch.float32), empty(n, (Hq + Hk) * D, dtype=torch.uint8), empty(n, (Hq + Hk) * D // block, dtype=torch.float32)
+        sf.heads_norm_rotate_forward(qkv, *gains, 1e-6, table, sf.ROTARY_HALVES, ids, 0.125, bits, block, q, kt, v, rstd, codes.view(-1), scales)
+        sf.heads_norm_rotate_backward(dq, dkt, dv, None, codes.view(-1), scales, bits, block, rstd, *gains, table, sf.ROTARY_HALVES, ids, 0.125, dqkv)
+        return q[0].transpose(0, 1), kt[0].permute(2, 0, 1), v[0].transpose(0, 1), rstd, codes, scales, dqkv[0]
+
+    qkv, dq, dkt, dv = empty(1, T, (Hq + 2 * Hk) * D).zero_(), empty(1, Hq, T, D).zero_(), empty(1, Hk, D, T).zero_(), empty(1, Hk, T, D).zero_()
+    ids = torch.zeros(1, T, dtype=torch.int32, device="cuda")
+    small = [torch.randn(*shape, generator=g, device="cuda").bfloat16() for shape in ((1, few, (Hq + 2 * Hk) * D), (1, Hq, few, D), (1, Hk, D, few), (1, Hk, few, D))]
+    places = torch.randint(-2, 102, (1, few), generator=g, device="cuda").to(torch.int32)
+    qkv[:, -few:], dq[:, :, -few:], dkt[..., -few:], dv[:, :, -few:], ids[:, -few:] = *small, places
+    for far, near in zip(both(qkv, dq, dkt, dv, ids), both(*small, places)):
+        assert torch.equal(far[-few:], near)
+        assert not far[: T - few].any() if far.dtype != torch.float32 else bool((far[:100] == far[0]).all())
+
+
 @pytest.mark.parametrize("dtype", DT)
 @pytest.mark.parametrize("D", [64, 80])
 def test_rows_whose_squares_overflow(D, dtype):
