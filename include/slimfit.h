@@ -569,7 +569,9 @@ int32_t slimfit_merge_heads(const void *q, const void *kt, const void *v, int32_
  *         (a, b) -> (a cos - b sin, b cos + a sin);
  *     q = q_scale * that, k^T as it is, v copied.  fp32 arithmetic (fixed-order
  *     sums), rounded to dt once: rstd within 8e-7 relative, an element within 1.2e-6 of
- *     |a cos| + |b sin| before that rounding.  (A row of zeros with eps 0 is NaN.)
+ *     |a cos| + |b sin| before that rounding.  (A row of zeros with eps 0 is NaN, and so
+ *     may be one whose mean(x^2) + eps is below fp32's normal numbers; where it overflows, rstd
+ *     and the row are 0, an infinity in it NaN.)
  *
  *  qkv : DEVICE [batch, tokens, q_heads + 2 * kv_heads, head_dim]: queries, keys, values.
  *  q   : DEVICE [batch, q_heads, tokens, head_dim].
@@ -604,7 +606,7 @@ int32_t slimfit_merge_heads(const void *q, const void *kt, const void *v, int32_
  *        own columns; rstd is the forward pass's.  dqkv's value columns are dv.
  *        dgamma_q, dgamma_k : DEVICE float[head_dim], both, or both NULL (frozen: no
  *        sums are formed and no workspace is needed).  fp32 sums over a
- *        workgroup's rows (at most 2048), fp64 across; no atomics: the same call gives the same bits.
+ *        workgroup's rows (at most 1024), fp64 across; no atomics: the same call gives the same bits.
  *        workspace : DEVICE, 16-byte aligned, of the bytes that
  *        slimfit_heads_norm_rotate_workspace reports; contents overwritten.
  *        qkv : as in the forward pass; looked at with a norm and bits 0 only.

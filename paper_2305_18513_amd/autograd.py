@@ -45,9 +45,9 @@ fp32 operands of sizes at which it is the quicker one, and torch's otherwise.
                      the dequantised input (`straight`: from the codes themselves,
                      by the library's own product, where a block lies in one row).
 
-A backward pass may be captured into a HIP graph once no eager graph of the same leaves is alive (torch's engine would
-tie the capture to the stream of the eager one, which ends the process): capture the first pass on a side stream after
-a warm-up there, as torch's own notes have it, and let go of every loss computed before.
+A backward pass may be captured into a HIP graph once no eager graph of the same leaves is alive (with one, the process
+has ended in torch's end of the capture, probably because the engine ties the capture to the eager one's stream): capture
+the first pass on a side stream after a warm-up there, as torch's own notes have it, and let go of every loss computed before.
 
 All tensors are CUDA tensors (fp32 or bf16 activations; gamma / beta and the
 kept standardised values fp32); the kernels run on torch's current stream.
@@ -575,7 +575,8 @@ def decoder_block(x: torch.Tensor, p: dict, heads: int, kv_heads: int, table, po
                   block: int = 64, act: int = sf.ACT_SILU) -> torch.Tensor:
     """One pre-LN decoder block (causal attention, queries and keys normed and turned, gated feed-forward) with the compressed
     caches of this module.  Whether a layer is frozen is read off its weight: a frozen one keeps nothing of its input (a
-    LayerNorm the ``keep_ppm`` largest entries), an active one forms its weight gradient from its ``bits``-bit cache."""
+    LayerNorm the ``keep_ppm`` largest entries), an active one forms its weight gradient from its ``bits``-bit cache.  A place
+    outside of ``table`` leaves a token unturned, not unseen: padding has to come after the tokens that count."""
     B, T, H = x.shape
     D, group = H // heads, heads // kv_heads
 

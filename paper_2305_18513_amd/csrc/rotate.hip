@@ -13,10 +13,13 @@
 // behind a branch: behind one, each load was waited for together with the stores before it (16384 x 48 heads of 128, bf16, 8 bits,
 // forward 159 us, with them free 149, with the angles and gains in vectors 119, four heads a workgroup instead of eight 103).
 //
-// Bound by HBM, with a third on top for the ramp of each workgroup's angles and for the vector instructions (145 a 16-byte vector, half of
-// the time) that do not overlap with it: that size 103 us forward (486 MB, 4.7 TB/s) and 100 backward; 64 wide heads 55 and 57
-// (239 MB each); 7289 x 36 of 64 fp32 34 and 36; copies without norm and rotation 5.2 to 5.4 TB/s; a 1 : 1 stream of the card 6.2.
-// Fewer registers (five and six waves a SIMD by spilling) and angles for one pass or four at a time were slower.
+// Bound by HBM, with 30 to 65 % on top for the start of each workgroup (place, angles and gains are asked for one after the other, of
+// which only the angles have to wait for the place) and for the vector instructions (145 a 16-byte vector, half of the time) that
+// do not overlap with it: that size 103 us forward (486 MB, 4.7 TB/s) and 102 backward, four heads a workgroup; 64 wide heads, two a
+// workgroup, 55 and 58 (239 MB each, 38 at the stream's rate); 7289 x 36 of 64 fp32, one a workgroup, 36 and 36 (141 MB, 23);
+// copies without norm and rotation 5.2 to 5.4 TB/s; a 1 : 1 stream of the card 6.2.  bf16 runs with four waves a SIMD forward
+// (115 registers; five and six by spilling were slower) and three backward (162; four were not tried); angles for one pass or four
+// at a time were slower.
 #include "elements.hpp"
 
 #include <type_traits>
@@ -631,6 +634,8 @@ int lanes_of(int32_t dt, int32_t dim)
 }
 
 // Heads a query (or value) workgroup takes one after the other: as many as leave four workgroups to a compute unit, at most 4.
+// (Forward and backward in us with one, two and four: 16 384 x 48 heads of 128 bf16 251, 214, 213; 16 384 x 48 of 64, which take
+// two, 121, 112, 121, and at 16 000 tokens, where it is one, 119, 111, 119; 7296 x 36 of 64 fp32, one, 70, 70, 73.)
 int heads_each(int64_t tiles, int32_t heads)
 {
     int per = 4;
@@ -647,8 +652,11 @@ int32_t validate(int32_t dt, int64_t batch, int32_t tokens, int32_t q_heads, int
     return SLIMFIT_OK;
 }
 
-// A workgroup takes four passes, or two where that would be fewer workgroups than this (a prompt of 4097 x 40 heads of 96, 2600 of them,
-// 23.5 -> 19.0 us, 512 x 48 of 64 7.9 -> 7.3; 16384 x 48 of 64, 4096 of them, forward and backward 54 + 58 -> 56 + 65).
+// A workgroup takes four passes, or two where that would be fewer workgroups than this.  (Forward and backward in us with two and four,
+// and the workgroups of four: 48 heads of 64 bf16 with 8 bits, 8192 tokens 65 and 68, 3072, 16 384 tokens 120 and 112, 4096, though
+// 13 312 tokens 98 and 101, 4992; 48 of 128, 8192 tokens 109 and 115, 2304, 12 288 tokens 157 and 158, 3456; 40 of 96, nothing kept,
+// 4096 tokens 47 and 54, 2560, though 6144 tokens 66 and 64, 2304.  Forward alone a prompt of 4097 x 40 of 96 19.0 and 23.5, 2600,
+// 512 x 48 of 64 7.3 and 7.9, 192.)
 constexpr int64_t kBusy = 4000;
 
 struct Plan {

@@ -18,7 +18,8 @@ inline int64_t tiles_of(int64_t n, int tile) { return (n + tile - 1) / tile; }
 // microseconds, measured over 20 sizes from 300 x 300 x 256 to 16384 x 4096 x 1024.  A step of 32 rows takes a + b * (workgroups on
 // the fullest compute unit), of which `most` go on one at a time; rows of dy that begin anywhere cost `ragged` as much.  Parts are
 // written and read again at 4.2 TB/s by a launch of 3 us.  (Chosen: 16384 x 4096 x 1024 bf16 256 wide in 4 parts 165 us, 128 wide in 3
-// 187, in one 322; 4096 x 768 x 768 128 wide in 6 25, in one 72; 12608 x 1024 x 4096 fp32 in 2 403, though 391 in 4, in one 461.)
+// 187, in one 322; 4096 x 768 x 768 128 wide in 6 25, in one 72; 12608 x 1024 x 4096 fp32 in 2 403, in one 461; in 4, which the count
+// puts at 433 against 415, 391.)
 struct Pace {
     int tile_n, most;
     float a, b, ragged;
