@@ -16,7 +16,7 @@
 // Bound by HBM, with 30 to 65 % on top for the start of each workgroup (place, angles and gains are asked for one after the other, of
 // which only the angles have to wait for the place) and for the vector instructions (145 a 16-byte vector, half of the time) that
 // do not overlap with it: that size 103 us forward (486 MB, 4.7 TB/s) and 102 backward, four heads a workgroup; 64 wide heads, two a
-// workgroup, 55 and 58 (239 MB each, 38 at the stream's rate); 7289 x 36 of 64 fp32, one a workgroup, 36 and 36 (141 MB, 23);
+// workgroup, 56 and 57 (239 MB each, 38 at the stream's rate); 7289 x 36 of 64 fp32, one a workgroup, 36 and 36 (141 MB, 23);
 // copies without norm and rotation 5.2 to 5.4 TB/s; a 1 : 1 stream of the card 6.2.  bf16 runs with four waves a SIMD forward
 // (115 registers; five and six by spilling were slower) and three backward (162; four were not tried); angles for one pass or four
 // at a time were slower.
