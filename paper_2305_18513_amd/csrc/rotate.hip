@@ -653,10 +653,10 @@ int32_t validate(int32_t dt, int64_t batch, int32_t tokens, int32_t q_heads, int
 }
 
 // A workgroup takes four passes, or two where that would be fewer workgroups than this.  (Forward and backward in us with two and four,
-// and the workgroups of four: 48 heads of 64 bf16 with 8 bits, 8192 tokens 65 and 68, 3072, 16 384 tokens 120 and 112, 4096, though
-// 13 312 tokens 98 and 101, 4992; 48 of 128, 8192 tokens 109 and 115, 2304, 12 288 tokens 157 and 158, 3456; 40 of 96, nothing kept,
-// 4096 tokens 47 and 54, 2560, though 6144 tokens 66 and 64, 2304.  Forward alone a prompt of 4097 x 40 of 96 19.0 and 23.5, 2600,
-// 512 x 48 of 64 7.3 and 7.9, 192.)
+// and the workgroups of four: 48 heads of 64 bf16 with 8 bits, 16 384 tokens 120 and 112, 4096, though 13 312 tokens 98 and 101,
+// 4992; 48 of 128, 8192 tokens 109 and 115, 2304, 12 288 tokens 157 and 158, 3456; 40 of 96, nothing kept, 4096 tokens 47 and 54,
+// 2560, though 6144 tokens 66 and 64, 2304.  Forward alone a prompt of 4097 x 40 of 96 19.0 and 23.5, 2600, 512 x 48 of 64 7.3 and
+// 7.9, 192.)
 constexpr int64_t kBusy = 4000;
 
 struct Plan {
