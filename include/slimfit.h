@@ -16,8 +16,9 @@
  *    tensor); "host pointer" = ordinary process memory.  Each argument says
  *    which one it is.  The caller owns every buffer and keeps it alive until
  *    the stream has passed the call.  Inputs are never written; outputs are
- *    fully overwritten for the sizes given (the one argument that is both, the
- *    weights of slimfit_apply_update_layer_delta, is marked as such).
+ *    fully overwritten for the sizes given (the arguments that are both, the
+ *    weights of slimfit_apply_update_layer_delta and the weights and states of
+ *    slimfit_adamw_run, are marked as such).
  *  - Device pointers must be 16-byte aligned (SLIMFIT_ERR_ALIGNMENT), except
  *    where a narrower alignment is stated.
  *  - `stream` is a hipStream_t passed as void* (NULL = the default stream).
@@ -202,6 +203,60 @@ int32_t slimfit_apply_update_layer_delta(void *const *w, int32_t w_dt,
                                          const int64_t *numel, int32_t L, float eps,
                                          float *d_out, void *workspace, size_t workspace_bytes,
                                          void *stream);
+
+/* ------------------------------------------------------------------------
+ * (a'') AdamW over all tensors of a model, the distances of Eq. 1 in the same pass.  For
+ *     each weight w with gradient g (a layer at a time, t the number of the step, from 1):
+ *         g' = grad_factor g,   m' = beta1 m + (1 - beta1) g',   v' = beta2 v + ((1 - beta2) g') g',
+ *         d = -(lr weight_decay w + lr / (1 - beta1^t) m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)),
+ *         w' = w + d;      d_out = mean over the layer of |d| / max(|w|, floor)  (0 where d is 0).
+ *     fp32, each operation rounded; bf16 weights are rounded to nearest even once more.
+ *
+ *  w, grad, m, v : HOST arrays of L DEVICE pointers, 16-byte aligned; numel[i] elements each, of w_dt,
+ *                  grad_dt and the states' type.  w, m and v are read and written.  grad[i] NULL: the
+ *                  layer is frozen, nothing of it is touched and its distance is 0.
+ *  bits          : 32: m and v are float.  8: bytes, and a float for each `block` (32 | 64 | 128 | 256)
+ *                  elements in m_scales and v_scales (HOST arrays of L DEVICE pointers, 4-byte aligned,
+ *                  ceil(numel / block) floats; not looked at with 32).  The codes of
+ *                    m : e4m3 of m' * (448 / top), times scale = top / 448 (fp32 divisions), top the run's
+ *                        largest |m'|; 0 and scale 0 where top is 0 or 448 / top overflows;
+ *                    v : c > 0 is the fp32 number whose bits are the scale's + c * 2^20 (5 exponent and 3
+ *                        fraction bits), c = 0 is 0; the scale is 2^-30 of the power of two of the run's
+ *                        largest v', at least 2^-126; c = ((bits of v' + dither) >> 20) - (bits of the scale >> 20),
+ *                        held to 1 .. 255 for a v' that is not 0.  The dither, 20 bits, rounds up with the probability
+ *                        of what is cut off (to the nearest a v would never decay).  With
+ *                        mix(x): x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *= 0xBB67AE85, x ^= x >> 16
+ *                        of 32 bits, element j of layer i has the upper 20 bits of
+ *                        rotate_left(mix(mix(seed ^ mix(t ^ mix(i + 1))) + j / 4), 8 (j % 4)).
+ *                  States that are zeros (codes and scales too) are those before the first step.
+ *  copies        : HOST array of L DEVICE pointers or NULL: with fp32 weights, bf16 copies of them that are
+ *                  written too (an entry may be NULL), 16-byte aligned.
+ *  weight_decay  : HOST float[L], >= 0.
+ *  lr >= 0, beta1 and beta2 in [0, 1), eps > 0, 1 <= step < 2^32, floor >= 0.
+ *  live          : DEVICE float[3] or NULL: lr, step and grad_factor as they are when the kernel runs, in place
+ *                  of the arguments (a captured graph is replayed with other values; step up to 2^24).
+ *  frozen        : DEVICE uint8[L] or NULL: layers of 1 are frozen (the mask of slimfit_ils_select).
+ *  d_out         : DEVICE float[L] or NULL (no distances).
+ *  A gradient that is not finite makes its weight, and with 8 bits its block's states, NaN.
+ *  Nothing of a layer may share memory with another part of it (INVALID_ARG).  numel <= 2^33 (ERR_UNSUPPORTED).
+ *
+ *  slimfit_adamw_plan writes the table into the workspace (256-byte aligned, of the bytes that
+ *  slimfit_adamw_workspace reports), slimfit_adamw_run steps the planned layers; numel, L, types, bits and block
+ *  have to be the plan's, or nothing is touched and d_out is NaN.  Deterministic.
+ *  slimfit_adamw_states : the values that m's and v's codes stand for, n elements.
+ * ---------------------------------------------------------------------- */
+int32_t slimfit_adamw_workspace(int32_t L, const int64_t *numel, size_t *bytes);
+
+int32_t slimfit_adamw_plan(void *const *w, int32_t w_dt, const void *const *grad, int32_t grad_dt, void *const *m, void *const *v,
+                           float *const *m_scales, float *const *v_scales, void *const *copies, const float *weight_decay, int32_t bits,
+                           int32_t block, const int64_t *numel, int32_t L, void *workspace, size_t workspace_bytes, void *stream);
+
+int32_t slimfit_adamw_run(const int64_t *numel, int32_t L, int32_t w_dt, int32_t grad_dt, int32_t bits, int32_t block, double lr, double beta1,
+                          double beta2, double eps, int64_t step, float grad_factor, uint32_t seed, const float *live, const uint8_t *frozen,
+                          float floor, float *d_out, void *workspace, size_t workspace_bytes, void *stream);
+
+int32_t slimfit_adamw_states(const uint8_t *m, const float *m_scales, const uint8_t *v, const float *v_scales, int64_t n, int32_t block,
+                             float *m_out, float *v_out, void *stream);
 
 /* ------------------------------------------------------------------------
  * (b) Low-bit caching of saved activations -- Alg. 2 (appendix on the

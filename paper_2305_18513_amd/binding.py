@@ -54,6 +54,7 @@ EXPORTS = (
     "slimfit_status_string", "slimfit_version", "slimfit_set_pointer_checks", "slimfit_stream_probe",
     "slimfit_layer_delta_workspace", "slimfit_layer_delta_plan",
     "slimfit_layer_delta_run", "slimfit_layer_delta", "slimfit_layer_delta_static", "slimfit_layer_delta_apply_run", "slimfit_apply_update_layer_delta",
+    "slimfit_adamw_workspace", "slimfit_adamw_plan", "slimfit_adamw_run", "slimfit_adamw_states",
     "slimfit_packed_bytes", "slimfit_num_blocks", "slimfit_quant_pack",
     "slimfit_dequant_unpack", "slimfit_gelu_quant_pack", "slimfit_gelu_backward_dequant", "slimfit_keep_count", "slimfit_prune_scores",
     "slimfit_restore_scores", "slimfit_softmax_prune", "slimfit_softmax_backward_pruned", "slimfit_prune_global_workspace", "slimfit_global_tile_ptr_len", "slimfit_prune_global",
@@ -304,6 +305,81 @@ def apply_update_layer_delta(w: Sequence[torch.Tensor], delta: Sequence[torch.Te
         C.c_int32(L), C.c_float(eps), _dev(d_out), _dev(workspace),
         C.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream))
     _check(rc, "apply_update_layer_delta")
+
+
+# ---------------------------------------------------------------- (a'') AdamW
+
+def adamw_workspace(numel: Sequence[int]) -> int:
+    n = _numel_array(numel)
+    out = C.c_size_t(0)
+    _check(lib().slimfit_adamw_workspace(C.c_int32(n.size), C.c_void_p(n.ctypes.data), C.byref(out)), "adamw_workspace")
+    return int(out.value)
+
+
+def _maybe_ptr_array(tensors: Sequence[Optional[torch.Tensor]]):
+    return (C.c_void_p * max(1, len(tensors)))(*[None if t is None else _dev(t).value for t in tensors])
+
+
+def adamw_plan(w: Sequence[torch.Tensor], grad: Sequence[Optional[torch.Tensor]], m: Sequence[torch.Tensor], v: Sequence[torch.Tensor],
+               m_scales: Optional[Sequence[torch.Tensor]], v_scales: Optional[Sequence[torch.Tensor]], weight_decay: Sequence[float], bits: int,
+               block: int, workspace: torch.Tensor, copies: Optional[Sequence[Optional[torch.Tensor]]] = None, stream=None) -> None:
+    """Lays down where the weights, gradients (None: frozen) and states of all layers are.  ``bits`` 32: m and v are float32, scales
+    None; 8: uint8 codes and float32 scales of runs of ``block``.  ``copies``: bfloat16 tensors that follow float32 weights."""
+    L = len(w)
+    _require(all(len(s) == L for s in (grad, m, v, weight_decay)) and (copies is None or len(copies) == L))
+    present = [g for g in grad if g is not None]
+    _require(not L or (_same_dtype(w) and (not present or _same_dtype(present))))
+    held = torch.uint8 if bits == 8 else torch.float32
+    for i in range(L):
+        n = w[i].numel()
+        _require(grad[i] is None or grad[i].numel() == n)
+        _require(m[i].dtype == v[i].dtype == held and m[i].numel() == v[i].numel() == n)
+        if copies is not None and copies[i] is not None:
+            _require(w[i].dtype == torch.float32 and copies[i].dtype == torch.bfloat16 and copies[i].numel() == n)
+    if bits == 8:
+        _require(m_scales is not None and v_scales is not None and len(m_scales) == L and len(v_scales) == L)
+        _require(all(s.dtype == torch.float32 and s.numel() >= -(-w[i].numel() // max(block, 1)) for each in (m_scales, v_scales) for i, s in enumerate(each)))
+    _require(workspace.dtype == torch.uint8)
+    for each in (w, grad, m, v, copies or (), (m_scales if bits == 8 else None) or (), (v_scales if bits == 8 else None) or (), (workspace,)):
+        _on_current_device(*each)
+    numel = _numel_array([t.numel() for t in w])
+    decay = np.ascontiguousarray(weight_decay, dtype=np.float32)
+    rc = lib().slimfit_adamw_plan(
+        _ptr_array(w), C.c_int32(_dt(w[0]) if L else F32), _maybe_ptr_array(grad), C.c_int32(_dt(present[0]) if present else F32), _ptr_array(m),
+        _ptr_array(v), _ptr_array(m_scales) if bits == 8 else None, _ptr_array(v_scales) if bits == 8 else None,
+        None if copies is None else _maybe_ptr_array(copies), C.c_void_p(decay.ctypes.data), C.c_int32(bits), C.c_int32(block),
+        C.c_void_p(numel.ctypes.data), C.c_int32(L), _dev(workspace), C.c_size_t(workspace.numel()), _stream(stream))
+    _check(rc, "adamw_plan")
+
+
+def adamw_run(numel: Sequence[int], w_dt: int, grad_dt: int, bits: int, block: int, lr: float, beta1: float, beta2: float, eps: float, step: int,
+              workspace: torch.Tensor, grad_factor: float = 1.0, seed: int = 0, live: Optional[torch.Tensor] = None,
+              frozen: Optional[torch.Tensor] = None, floor: float = 0.0, d_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """One step of the planned layers.  ``live`` (float32: lr, step, grad_factor) takes the place of those arguments when the kernel
+    runs; ``frozen`` (uint8 or bool) leaves layers out; ``d_out`` receives the layers' distances."""
+    n = numel if isinstance(numel, np.ndarray) and numel.dtype == np.int64 and numel.flags.c_contiguous else _numel_array(numel)
+    _require(d_out is None or (d_out.dtype == torch.float32 and d_out.numel() >= n.size))
+    _require(live is None or (live.dtype == torch.float32 and live.numel() >= 3))
+    _require(frozen is None or (frozen.dtype in (torch.uint8, torch.bool) and frozen.numel() >= n.size))
+    _require(workspace.dtype == torch.uint8)
+    _on_current_device(workspace, live, frozen, d_out)
+    rc = lib().slimfit_adamw_run(
+        C.c_void_p(n.ctypes.data), C.c_int32(n.size), C.c_int32(w_dt), C.c_int32(grad_dt), C.c_int32(bits), C.c_int32(block), C.c_double(lr),
+        C.c_double(beta1), C.c_double(beta2), C.c_double(eps), C.c_int64(step), C.c_float(grad_factor), C.c_uint32(seed & 0xFFFFFFFF), _dev(live),
+        _dev(frozen), C.c_float(floor), _dev(d_out), _dev(workspace), C.c_size_t(workspace.numel()), _stream(stream))
+    _check(rc, "adamw_run")
+
+
+def adamw_states(m: torch.Tensor, m_scales: torch.Tensor, v: torch.Tensor, v_scales: torch.Tensor, block: int, m_out: torch.Tensor,
+                 v_out: torch.Tensor, stream=None) -> None:
+    """What 8-bit states stand for, as float32."""
+    n = m.numel()
+    _require(m.dtype == v.dtype == torch.uint8 and v.numel() == n and all(t.dtype == torch.float32 for t in (m_scales, v_scales, m_out, v_out)))
+    _require(m_out.numel() == n and v_out.numel() == n and min(m_scales.numel(), v_scales.numel()) >= -(-n // max(block, 1)))
+    _on_current_device(m, m_scales, v, v_scales, m_out, v_out)
+    rc = lib().slimfit_adamw_states(_dev(m), _dev(m_scales), _dev(v), _dev(v_scales), C.c_int64(n), C.c_int32(block), _dev(m_out), _dev(v_out),
+                                    _stream(stream))
+    _check(rc, "adamw_states")
 
 
 def stream_probe_bytes(in_vecs: int, ratio: int) -> int:

@@ -1,0 +1,540 @@
+// AdamW over all tensors of a model in one launch, with Eq. 1's distance of each layer from the same pass:
+//     g' = factor g,   m' = b1 m + (1 - b1) g',   v' = b2 v + ((1 - b2) g') g',
+//     d = -(lr decay w + lr / (1 - b1^t) * m' / (sqrt(v') / sqrt(1 - b2^t) + eps)),   w' = w + d,   distance = mean |d| / max(|w|, floor).
+//
+// As for the distances alone (layer_delta.hip) the tensors are cut into chunks of kChunk elements, a workgroup each, the table of
+// the tensors lies in the workspace, and each workgroup's sum of terms goes out in fp64 for a second launch that adds them in order.
+//
+// States in 8 bits, a scale for each run of `block` elements:
+//   m   e4m3 of m' * 448 / max|m'| (round to nearest even, the conversion instruction's), scale max|m'| / 448.
+//   v   5 exponent and 3 fraction bits over a power of two, 2^-31 to 1 of the run's largest exponent: code c > 0 stands for
+//       2^(c >> 3) (1 + (c & 7) / 8) times the scale, which is the fp32 number whose bits are the scale's + (c << 20); 0 is 0.
+//       Rounding to the nearest would never let a v decay (a step takes 0.001 of it, half a step of the code is 0.06), so v' is
+//       rounded up with the probability of what is cut off: 20 bits of dither are added to the fp32 bits before the cut.  The
+//       dither is a function of seed, step, tensor and place alone.  A v' that is not 0 never becomes 0 (m' / eps would explode).
+// m' and v' are rounded products and their rounded sum, without a fused multiply-add, so that the codes are defined.
+#include "common.hpp"
+
+namespace slimfit {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPer = 8;                      // elements of a thread's vectors
+constexpr int kPass = kThreads * kPer;
+constexpr int kChunk = 4 * kPass;            // a multiple of every block
+constexpr uint32_t kMagic = 0x534C4157u;     // "SLAW"
+constexpr int kPlanBatch = 32;
+
+struct Header {                              // 64 bytes at the start of the workspace
+    uint32_t magic;
+    int32_t n_layers;
+    int64_t total_chunks;
+    int32_t w_dt, grad_dt, bits, block;
+    int64_t pad[4];
+};
+static_assert(sizeof(Header) == 64, "header size");
+
+struct Entry {                               // 80 bytes
+    void *w;
+    const void *grad;                        // NULL: frozen
+    void *m, *v;
+    float *m_scales, *v_scales;
+    uint16_t *copy;                          // bf16 copy of fp32 weights, or NULL
+    int64_t numel, first_chunk;
+    float decay;
+    uint32_t pad;
+};
+static_assert(sizeof(Entry) == 80, "entry size");
+
+struct PlanBatch {
+    Entry e[kPlanBatch];
+};
+
+inline size_t table_bytes(int32_t L) { return (sizeof(Header) + sizeof(Entry) * (size_t)L + 255) & ~(size_t)255; }
+
+__global__ void plan_kernel(char *ws, Header h, int first, int count, PlanBatch batch)
+{
+    Entry *table = reinterpret_cast<Entry *>(ws + sizeof(Header));
+    const int t = threadIdx.x;
+    if (t < count) table[first + t] = batch.e[t];
+    if (first == 0 && t == 0) *reinterpret_cast<Header *>(ws) = h;
+}
+
+struct Step {
+    double beta1, beta2;
+    float b1, one_b1, b2, one_b2, eps, lr, rate, root, factor, floor;
+    uint32_t seed, step;
+};
+
+__host__ __device__ inline uint32_t mix(uint32_t x)
+{
+    x ^= x >> 16;
+    x *= 0x6A09E667u;                        // the fraction bits of sqrt 2 and sqrt 3
+    x ^= x >> 15;
+    x *= 0xBB67AE85u;
+    return x ^ (x >> 16);
+}
+
+__host__ __device__ inline double power(double b, uint32_t n)
+{
+    double p = 1.0;
+    for (; n; n >>= 1, b *= b)
+        if (n & 1u) p *= b;
+    return p;
+}
+
+template <typename T> __device__ __forceinline__ void load8(const T *p, float (&f)[kPer]);
+template <> __device__ __forceinline__ void load8<float>(const float *p, float (&f)[kPer])
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const f32x4 r = load_global<true>(reinterpret_cast<const f32x4 *>(p) + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[4 * i + j] = r[j];
+    }
+}
+template <> __device__ __forceinline__ void load8<uint16_t>(const uint16_t *p, float (&f)[kPer])
+{
+    const u32x4 r = load_global<true>(reinterpret_cast<const u32x4 *>(p));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t u = r[i];
+        f[2 * i] = __builtin_bit_cast(float, u << 16);
+        f[2 * i + 1] = __builtin_bit_cast(float, u & 0xFFFF0000u);
+    }
+}
+template <typename T> __device__ __forceinline__ void store8(T *p, const float (&f)[kPer]);
+template <> __device__ __forceinline__ void store8<float>(float *p, const float (&f)[kPer])
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) store_global<true>(reinterpret_cast<f32x4 *>(p) + i, f32x4{f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]});
+}
+template <> __device__ __forceinline__ void store8<uint16_t>(uint16_t *p, const float (&f)[kPer])
+{
+    store_global<true>(reinterpret_cast<u32x4 *>(p), u32x4{bf16_narrow2(f[0], f[1]), bf16_narrow2(f[2], f[3]), bf16_narrow2(f[4], f[5]), bf16_narrow2(f[6], f[7])});
+}
+__device__ __forceinline__ float load1(const float *p) { return *p; }
+__device__ __forceinline__ float load1(const uint16_t *p) { return bf16_widen(*p); }
+__device__ __forceinline__ void store1(float *p, float v) { *p = v; }
+__device__ __forceinline__ void store1(uint16_t *p, float v) { *p = (uint16_t)bf16_narrow(v); }
+
+// n of the eight elements (the last vector of a tensor may have fewer), 0 in place of the others
+template <typename T> __device__ __forceinline__ void load_some(const T *p, int n, float (&f)[kPer])
+{
+    if (n >= kPer) return load8<T>(p, f);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) f[j] = j < n ? load1(p + j) : 0.0f;
+}
+template <typename T> __device__ __forceinline__ void store_some(T *p, int n, const float (&f)[kPer])
+{
+    if (n >= kPer) return store8<T>(p, f);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (j < n) store1(p + j, f[j]);
+}
+__device__ __forceinline__ u32x2 load_codes(const uint8_t *p, int n)
+{
+    if (n >= kPer) return load_global<true>(reinterpret_cast<const u32x2 *>(p));
+    u32x2 c = {0u, 0u};
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (j < n) c[j / 4] |= (uint32_t)p[j] << (8 * (j % 4));
+    return c;
+}
+__device__ __forceinline__ void store_codes(uint8_t *p, int n, u32x2 c)
+{
+    if (n >= kPer) return store_global<true>(reinterpret_cast<u32x2 *>(p), c);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (j < n) p[j] = (uint8_t)(c[j / 4] >> (8 * (j % 4)));
+}
+
+__device__ __forceinline__ void decode_m(u32x2 c, float scale, float (&f)[kPer])
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[i], true);
+        f[4 * i] = a[0] * scale;
+        f[4 * i + 1] = a[1] * scale;
+        f[4 * i + 2] = b[0] * scale;
+        f[4 * i + 3] = b[1] * scale;
+    }
+}
+__device__ __forceinline__ void decode_v(u32x2 c, float scale, float (&f)[kPer])
+{
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const uint32_t code = (c[j / 4] >> (8 * (j % 4))) & 255u;
+        f[j] = code ? __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, scale) + (code << 20)) : 0.0f;
+    }
+}
+// m' of a run's lanes: codes, and the scale in every lane
+__device__ __forceinline__ u32x2 encode_m(const float (&m)[kPer], int lanes, float &scale)
+{
+    uint32_t top = 0u;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) top = max(top, __builtin_bit_cast(uint32_t, m[j]) & 0x7FFFFFFFu);
+    const float a = __builtin_bit_cast(float, group_max_u32(top, lanes));
+    const float up = 448.0f / a;
+    const bool fine = !__builtin_isinf(up);                 // not a run of zeros, nor one whose factor overflows
+    const float by = fine ? up : 0.0f;
+    scale = fine ? a / 448.0f : 0.0f;
+    u32x2 c;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(m[4 * i] * by, m[4 * i + 1] * by, 0, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(m[4 * i + 2] * by, m[4 * i + 3] * by, w, true);
+        c[i] = (uint32_t)w;
+    }
+    return c;
+}
+// v' likewise; `first`: the key of the tensor's dither plus the number of the fours before these elements
+__device__ __forceinline__ u32x2 encode_v(const float (&v)[kPer], int lanes, uint32_t first, float &scale)
+{
+    uint32_t top = 0u;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) top = max(top, __builtin_bit_cast(uint32_t, v[j]));
+    top = group_max_u32(top, lanes) >> 23;
+    top = top > 31u ? top - 30u : 1u;
+    scale = __builtin_bit_cast(float, top << 23);
+    u32x2 c = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t word = mix(first + (uint32_t)i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t bits = __builtin_bit_cast(uint32_t, v[4 * i + j]);
+            const uint32_t dither = (j == 0 ? word : __builtin_rotateleft32(word, 8 * j)) >> 12;
+            const int code = (int)((bits + dither) >> 20) - (int)(8u * top);
+            c[i] |= (bits ? (uint32_t)min(max(code, 1), 255) : 0u) << (8 * j);
+        }
+    }
+    return c;
+}
+
+template <typename TW, typename TG, int BITS, bool SCORE>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(const char *__restrict__ ws, int32_t L, int64_t total_chunks, int32_t block, Step s,
+                                                         const float *__restrict__ live, const uint8_t *__restrict__ frozen, double *__restrict__ partials)
+{
+    __shared__ double lds[kThreads / kWave];
+    const Header *h = reinterpret_cast<const Header *>(ws);
+    if (h->magic != kMagic || h->n_layers != L || h->total_chunks != total_chunks || h->bits != BITS || h->block != block ||
+        h->w_dt != (sizeof(TW) == 2 ? SLIMFIT_BF16 : SLIMFIT_F32) || h->grad_dt != (sizeof(TG) == 2 ? SLIMFIT_BF16 : SLIMFIT_F32))
+        return;                                             // no matching plan: touch nothing
+    const Entry *table = reinterpret_cast<const Entry *>(ws + sizeof(Header));
+    const int64_t chunk = blockIdx.x;
+    int lo = 0, hi = L - 1;                                 // the last tensor whose first_chunk <= chunk
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (table[mid].first_chunk <= chunk) lo = mid; else hi = mid - 1;
+    }
+    const Entry e = table[lo];
+    if (!e.grad || (frozen && frozen[lo])) {
+        if (SCORE && threadIdx.x == 0) partials[chunk] = 0.0;
+        return;
+    }
+    if (live) {
+        s.lr = live[0];
+        s.step = (uint32_t)live[1];
+        s.factor = live[2];
+        s.rate = (float)((double)s.lr / (1.0 - power(s.beta1, s.step)));
+        s.root = (float)(1.0 / __builtin_sqrt(1.0 - power(s.beta2, s.step)));
+    }
+    const int64_t off = (chunk - e.first_chunk) * kChunk;
+    const int len = (int)min((int64_t)kChunk, e.numel - off);
+    const int lanes = block / kPer;
+    const float decay = s.lr * e.decay;
+    const uint32_t key = BITS == 8 ? mix(s.seed ^ mix(s.step ^ mix((uint32_t)lo + 1u))) + (uint32_t)(off >> 2) : 0u;
+    double acc = 0.0;
+#pragma unroll
+    for (int p = 0; p < kChunk / kPass; ++p) {
+        if (p * kPass >= len) break;                        // (all threads together: lanes of a run stay together)
+        const int at = p * kPass + threadIdx.x * kPer;
+        const int n = min(len - at, kPer);
+        TW *const wp = static_cast<TW *>(e.w) + off + at;
+        float w[kPer], g[kPer], m[kPer], v[kPer];
+        load_some(wp, n, w);
+        load_some(static_cast<const TG *>(e.grad) + off + at, n, g);
+        const int64_t run = (off + at) / (BITS == 8 ? block : 1);
+        if constexpr (BITS == 32) {
+            load_some(static_cast<float *>(e.m) + off + at, n, m);
+            load_some(static_cast<float *>(e.v) + off + at, n, v);
+        } else {
+            const u32x2 cm = load_codes(static_cast<uint8_t *>(e.m) + off + at, n), cv = load_codes(static_cast<uint8_t *>(e.v) + off + at, n);
+            decode_m(cm, n > 0 ? e.m_scales[run] : 0.0f, m);
+            decode_v(cv, n > 0 ? e.v_scales[run] : 0.0f, v);
+        }
+        float to[kPer];
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const float gj = g[j] * s.factor;
+            m[j] = m[j] * s.b1 + gj * s.one_b1;
+            v[j] = v[j] * s.b2 + (gj * s.one_b2) * gj;
+            const float d = -(w[j] * decay + m[j] / (__builtin_sqrtf(v[j]) * s.root + s.eps) * s.rate);
+            to[j] = w[j] + d;
+            if constexpr (SCORE) {
+                const float q = __builtin_fabsf(d) / fmaxf(__builtin_fabsf(w[j]), s.floor);
+                acc += j < n && d != 0.0f ? (double)q : 0.0;
+            }
+        }
+        store_some(wp, n, to);
+        if (sizeof(TW) == 4 && e.copy) store_some(e.copy + off + at, n, to);
+        if constexpr (BITS == 32) {
+            store_some(static_cast<float *>(e.m) + off + at, n, m);
+            store_some(static_cast<float *>(e.v) + off + at, n, v);
+        } else {
+            if (n < kPer) {                                 // past the end: nothing that a run's largest could be
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    if (j >= n) m[j] = v[j] = 0.0f;
+            }
+            float ms, vs;
+            const u32x2 cm = encode_m(m, lanes, ms), cv = encode_v(v, lanes, key + (uint32_t)(at >> 2), vs);
+            store_codes(static_cast<uint8_t *>(e.m) + off + at, n, cm);
+            store_codes(static_cast<uint8_t *>(e.v) + off + at, n, cv);
+            if (n > 0 && (threadIdx.x & (lanes - 1)) == 0) {
+                e.m_scales[run] = ms;
+                e.v_scales[run] = vs;
+            }
+        }
+    }
+    if constexpr (SCORE) {
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) acc += __shfl_xor(acc, o, kWave);
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = acc;
+        __syncthreads();
+        if (threadIdx.x == 0) partials[chunk] = ((lds[0] + lds[1]) + lds[2]) + lds[3];
+    }
+}
+
+__global__ __launch_bounds__(kWave) void finish_kernel(const char *__restrict__ ws, int32_t L, int64_t total_chunks, Header want,
+                                                       const double *__restrict__ partials, float *__restrict__ d_out)
+{
+    const int layer = blockIdx.x;
+    const Header *h = reinterpret_cast<const Header *>(ws);
+    if (h->magic != kMagic || h->n_layers != L || h->total_chunks != total_chunks || h->bits != want.bits || h->block != want.block ||
+        h->w_dt != want.w_dt || h->grad_dt != want.grad_dt) {
+        if (threadIdx.x == 0) d_out[layer] = __builtin_nanf("");
+        return;
+    }
+    const Entry &e = reinterpret_cast<const Entry *>(ws + sizeof(Header))[layer];
+    const int64_t chunks = (e.numel + kChunk - 1) / kChunk;
+    double acc = 0.0;
+    for (int64_t c = threadIdx.x; c < chunks; c += kWave) acc += partials[e.first_chunk + c];
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) acc += __shfl_xor(acc, o, kWave);
+    if (threadIdx.x == 0) d_out[layer] = e.numel > 0 ? (float)(acc / (double)e.numel) : 0.0f;
+}
+
+__global__ __launch_bounds__(kThreads) void states_kernel(const uint8_t *__restrict__ m, const float *__restrict__ m_scales, const uint8_t *__restrict__ v,
+                                                          const float *__restrict__ v_scales, int64_t n, int shift, float *__restrict__ m_out,
+                                                          float *__restrict__ v_out, int64_t first)
+{
+    const int64_t at = first + ((int64_t)blockIdx.x * kThreads + threadIdx.x) * kPer;
+    if (at >= n) return;
+    const int some = (int)min((int64_t)kPer, n - at);
+    float a[kPer], b[kPer];
+    decode_m(load_codes(m + at, some), m_scales[at >> shift], a);
+    decode_v(load_codes(v + at, some), v_scales[at >> shift], b);
+    store_some(m_out + at, some, a);
+    store_some(v_out + at, some, b);
+}
+
+struct Layout {
+    int64_t chunks = 0;
+    size_t bytes = 0;
+};
+
+int32_t layout_of(int32_t L, const int64_t *numel, Layout *out)
+{
+    if (L < 0 || (L > 0 && !numel)) return SLIMFIT_ERR_INVALID_ARG;
+    int64_t chunks = 0;
+    for (int32_t i = 0; i < L; ++i) {
+        if (numel[i] < 0) return SLIMFIT_ERR_INVALID_ARG;
+        if (numel[i] > ((int64_t)1 << 33)) return SLIMFIT_ERR_UNSUPPORTED;       // the dither counts fours of elements in 32 bits
+        chunks += (numel[i] + kChunk - 1) / kChunk;
+    }
+    if (!grid_fits(chunks, kThreads)) return SLIMFIT_ERR_UNSUPPORTED;
+    out->chunks = chunks;
+    out->bytes = table_bytes(L) + sizeof(double) * (size_t)chunks;
+    return SLIMFIT_OK;
+}
+
+int32_t check_kind(int32_t w_dt, int32_t grad_dt, int32_t bits, int32_t block)
+{
+    if (!dtype_ok(w_dt) || !dtype_ok(grad_dt)) return SLIMFIT_ERR_INVALID_ARG;
+    if (bits != 8 && bits != 32) return SLIMFIT_ERR_UNSUPPORTED;
+    if (bits == 8 && block != 32 && block != 64 && block != 128 && block != 256) return SLIMFIT_ERR_UNSUPPORTED;
+    return SLIMFIT_OK;
+}
+
+int32_t check_workspace(const Layout &lay, const void *ws, size_t bytes)
+{
+    if (!ws || bytes < lay.bytes) return SLIMFIT_ERR_WORKSPACE;
+    if (!aligned_to(ws, 256)) return SLIMFIT_ERR_ALIGNMENT;
+    return check_device_range(ws, lay.bytes);
+}
+
+int32_t check_step(double lr, double beta1, double beta2, double eps, int64_t step, float floor)
+{
+    const bool fine = lr >= 0.0 && lr < __builtin_inf() && beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0 && eps > 0.0 && (float)eps > 0.0f &&
+                      eps < __builtin_inf() && step >= 1 && step <= 0xFFFFFFFFLL && floor >= 0.0f;
+    return fine ? SLIMFIT_OK : SLIMFIT_ERR_INVALID_ARG;
+}
+
+Header header_of(int32_t L, const Layout &lay, int32_t w_dt, int32_t grad_dt, int32_t bits, int32_t block)
+{
+    Header h = {};
+    h.magic = kMagic;
+    h.n_layers = L;
+    h.total_chunks = lay.chunks;
+    h.w_dt = w_dt;
+    h.grad_dt = grad_dt;
+    h.bits = bits;
+    h.block = bits == 8 ? block : 0;
+    return h;
+}
+
+template <typename TW, typename TG>
+void launch_adamw(int32_t bits, bool score, unsigned grid, hipStream_t st, const char *ws, int32_t L, int64_t chunks, int32_t block, const Step &s,
+                  const float *live, const uint8_t *frozen, double *partials)
+{
+    if (bits == 32 && score) launch(adamw_kernel<TW, TG, 32, true>, grid, kThreads, 0, st, ws, L, chunks, block, s, live, frozen, partials);
+    else if (bits == 32) launch(adamw_kernel<TW, TG, 32, false>, grid, kThreads, 0, st, ws, L, chunks, block, s, live, frozen, partials);
+    else if (score) launch(adamw_kernel<TW, TG, 8, true>, grid, kThreads, 0, st, ws, L, chunks, block, s, live, frozen, partials);
+    else launch(adamw_kernel<TW, TG, 8, false>, grid, kThreads, 0, st, ws, L, chunks, block, s, live, frozen, partials);
+}
+
+}  // namespace
+}  // namespace slimfit
+
+using namespace slimfit;
+
+extern "C" int32_t slimfit_adamw_workspace(int32_t L, const int64_t *numel, size_t *bytes)
+{
+    if (!bytes) return SLIMFIT_ERR_INVALID_ARG;
+    Layout lay;
+    const int32_t rc = layout_of(L, numel, &lay);
+    if (rc != SLIMFIT_OK) return rc;
+    *bytes = lay.bytes;
+    return SLIMFIT_OK;
+}
+
+extern "C" int32_t slimfit_adamw_plan(void *const *w, int32_t w_dt, const void *const *grad, int32_t grad_dt, void *const *m, void *const *v,
+                                      float *const *m_scales, float *const *v_scales, void *const *copies, const float *weight_decay, int32_t bits,
+                                      int32_t block, const int64_t *numel, int32_t L, void *workspace, size_t workspace_bytes, void *stream)
+{
+    StreamScope capture_aware(stream);
+    int32_t rc = check_kind(w_dt, grad_dt, bits, block);
+    if (rc != SLIMFIT_OK) return rc;
+    Layout lay;
+    if ((rc = layout_of(L, numel, &lay)) != SLIMFIT_OK) return rc;
+    if (L == 0) return SLIMFIT_OK;
+    if (!w || !grad || !m || !v || !weight_decay || (bits == 8 && (!m_scales || !v_scales))) return SLIMFIT_ERR_INVALID_ARG;
+    if (copies && w_dt != SLIMFIT_F32) return SLIMFIT_ERR_INVALID_ARG;
+    for (int pass = 0; pass < 2; ++pass) {                  // what can be told without the runtime comes first
+        if (pass == 1 && (rc = check_workspace(lay, workspace, workspace_bytes)) != SLIMFIT_OK) return rc;
+        for (int32_t i = 0; i < L; ++i) {
+            if (!(weight_decay[i] >= 0.0f) || __builtin_isinf(weight_decay[i])) return SLIMFIT_ERR_INVALID_ARG;
+            if (numel[i] == 0) continue;
+            const size_t n = (size_t)numel[i], held = bits == 8 ? n : 4 * n, runs = bits == 8 ? 4 * ((n + (size_t)block - 1) / (size_t)block) : 0;
+            const struct { const void *p; size_t bytes, align; bool needed; } part[] = {
+                {w[i], n * dtype_size(w_dt), 16, true}, {m[i], held, 16, true}, {v[i], held, 16, true},
+                {bits == 8 ? m_scales[i] : nullptr, runs, 4, bits == 8}, {bits == 8 ? v_scales[i] : nullptr, runs, 4, bits == 8},
+                {copies ? copies[i] : nullptr, 2 * n, 16, false}, {grad[i], n * dtype_size(grad_dt), 16, false}};
+            for (const auto &a : part) {
+                if (!a.p) {
+                    if (a.needed) return SLIMFIT_ERR_INVALID_ARG;
+                    continue;
+                }
+                if (pass == 0 && !aligned_to(a.p, a.align)) return SLIMFIT_ERR_ALIGNMENT;
+                if (pass == 0)
+                    for (const auto &b : part)
+                        if (&a != &b && b.p && meet(a.p, a.bytes, b.p, b.bytes)) return SLIMFIT_ERR_INVALID_ARG;
+                if (pass == 1 && (rc = check_device_range(a.p, a.bytes)) != SLIMFIT_OK) return rc;
+            }
+        }
+    }
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const Header h = header_of(L, lay, w_dt, grad_dt, bits, block);
+    int64_t next = 0;
+    for (int32_t first = 0; first < L; first += kPlanBatch) {
+        PlanBatch batch = {};
+        const int count = L - first < kPlanBatch ? L - first : kPlanBatch;
+        for (int t = 0; t < count; ++t) {
+            const int32_t i = first + t;
+            batch.e[t] = Entry{w[i], grad[i], m[i], v[i], bits == 8 ? m_scales[i] : nullptr, bits == 8 ? v_scales[i] : nullptr,
+                               copies ? static_cast<uint16_t *>(copies[i]) : nullptr, numel[i], next, weight_decay[i], 0u};
+            next += (numel[i] + kChunk - 1) / kChunk;
+        }
+        launch(plan_kernel, 1, kWave, 0, st, static_cast<char *>(workspace), h, first, count, batch);
+    }
+    return launch_status();
+}
+
+extern "C" int32_t slimfit_adamw_run(const int64_t *numel, int32_t L, int32_t w_dt, int32_t grad_dt, int32_t bits, int32_t block, double lr, double beta1,
+                                     double beta2, double eps, int64_t step, float grad_factor, uint32_t seed, const float *live, const uint8_t *frozen,
+                                     float floor, float *d_out, void *workspace, size_t workspace_bytes, void *stream)
+{
+    StreamScope capture_aware(stream);
+    int32_t rc = check_kind(w_dt, grad_dt, bits, block);
+    if (rc != SLIMFIT_OK) return rc;
+    if ((rc = check_step(lr, beta1, beta2, eps, step, floor)) != SLIMFIT_OK) return rc;
+    Layout lay;
+    if ((rc = layout_of(L, numel, &lay)) != SLIMFIT_OK) return rc;
+    if (L == 0) return SLIMFIT_OK;
+    if (!aligned_to(d_out, 4) || !aligned_to(live, 4)) return SLIMFIT_ERR_ALIGNMENT;
+    if ((rc = check_workspace(lay, workspace, workspace_bytes)) != SLIMFIT_OK) return rc;
+    if (d_out && (rc = check_device_range(d_out, sizeof(float) * (size_t)L)) != SLIMFIT_OK) return rc;
+    if (live && (rc = check_device_range(live, 3 * sizeof(float))) != SLIMFIT_OK) return rc;
+    if (frozen && (rc = check_device_range(frozen, (size_t)L)) != SLIMFIT_OK) return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const char *ws = static_cast<const char *>(workspace);
+    double *partials = reinterpret_cast<double *>(static_cast<char *>(workspace) + table_bytes(L));
+    const uint32_t t = (uint32_t)step;
+    const Step s = {beta1, beta2, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps, (float)lr,
+                    (float)(lr / (1.0 - power(beta1, t))), (float)(1.0 / __builtin_sqrt(1.0 - power(beta2, t))), grad_factor, floor, seed, t};
+    const Header want = header_of(L, lay, w_dt, grad_dt, bits, block);
+    if (lay.chunks > 0) {
+        const unsigned grid = (unsigned)lay.chunks;
+        if (w_dt == SLIMFIT_F32 && grad_dt == SLIMFIT_F32)
+            launch_adamw<float, float>(bits, d_out != nullptr, grid, st, ws, L, lay.chunks, want.block, s, live, frozen, partials);
+        else if (w_dt == SLIMFIT_F32)
+            launch_adamw<float, uint16_t>(bits, d_out != nullptr, grid, st, ws, L, lay.chunks, want.block, s, live, frozen, partials);
+        else if (grad_dt == SLIMFIT_F32)
+            launch_adamw<uint16_t, float>(bits, d_out != nullptr, grid, st, ws, L, lay.chunks, want.block, s, live, frozen, partials);
+        else
+            launch_adamw<uint16_t, uint16_t>(bits, d_out != nullptr, grid, st, ws, L, lay.chunks, want.block, s, live, frozen, partials);
+    }
+    if (d_out) launch(finish_kernel, (unsigned)L, kWave, 0, st, ws, L, lay.chunks, want, partials, d_out);
+    return launch_status();
+}
+
+extern "C" int32_t slimfit_adamw_states(const uint8_t *m, const float *m_scales, const uint8_t *v, const float *v_scales, int64_t n, int32_t block,
+                                        float *m_out, float *v_out, void *stream)
+{
+    StreamScope capture_aware(stream);
+    if (n < 0) return SLIMFIT_ERR_INVALID_ARG;
+    if (block != 32 && block != 64 && block != 128 && block != 256) return SLIMFIT_ERR_UNSUPPORTED;
+    if (n > ((int64_t)1 << 40)) return SLIMFIT_ERR_UNSUPPORTED;
+    if (n == 0) return SLIMFIT_OK;
+    if (!m || !m_scales || !v || !v_scales || !m_out || !v_out) return SLIMFIT_ERR_INVALID_ARG;
+    if (!aligned_to(m, 16) || !aligned_to(v, 16) || !aligned_to(m_out, 16) || !aligned_to(v_out, 16) || !aligned_to(m_scales, 4) || !aligned_to(v_scales, 4))
+        return SLIMFIT_ERR_ALIGNMENT;
+    const size_t codes = (size_t)n, scales = 4 * (((size_t)n + (size_t)block - 1) / (size_t)block), out = 4 * (size_t)n;
+    if (meet(m_out, out, v_out, out)) return SLIMFIT_ERR_INVALID_ARG;
+    for (float *o : {m_out, v_out})
+        if (meet(o, out, m, codes) || meet(o, out, v, codes) || meet(o, out, m_scales, scales) || meet(o, out, v_scales, scales)) return SLIMFIT_ERR_INVALID_ARG;
+    int32_t rc;
+    if ((rc = check_device_range(m, codes)) != SLIMFIT_OK || (rc = check_device_range(v, codes)) != SLIMFIT_OK) return rc;
+    if ((rc = check_device_range(m_scales, scales)) != SLIMFIT_OK || (rc = check_device_range(v_scales, scales)) != SLIMFIT_OK) return rc;
+    if ((rc = check_device_range(m_out, out)) != SLIMFIT_OK || (rc = check_device_range(v_out, out)) != SLIMFIT_OK) return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    constexpr int64_t kMost = kMaxGridThreads * kPer;
+    for (int64_t first = 0; first < n; first += kMost) {
+        const int64_t left = n - first < kMost ? n - first : kMost;
+        launch(states_kernel, (unsigned)((left + kPass - 1) / kPass), kThreads, 0, st, m, m_scales, v, v_scales, n, __builtin_ctz((unsigned)block), m_out, v_out,
+               first);
+    }
+    return launch_status();
+}
