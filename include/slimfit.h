@@ -687,6 +687,57 @@ int32_t slimfit_heads_norm_rotate_backward(const void *dq, const void *dkt, cons
                                            void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
+ * (c-att) Attention without its probabilities in memory, for rows of any length: the forward pass goes over
+ *     the keys once, the backward pass forms the probabilities again from two numbers a query.  For each
+ *     query i and the keys j that it sees,
+ *         s = scale q_i . k_j + bias,   m = max s,   l = sum e^(s - m),   out_i = sum e^(s - m) v_j / l;
+ *         p = e^(s - m) / l,   dp = dout_i . v_j,   delta = dout_i . out_i,   ds = p (dp - delta),
+ *         dq_i = scale sum ds k_j,   dk_j = scale sum ds q_i,   dv_j = sum p dout_i,
+ *     dk and dv over the query heads that share them.
+ *
+ *  layout : SLIMFIT_HEADS_ROWS: q [batch, q_tokens, q_heads, head_dim], k and v [batch, k_tokens, kv_heads, head_dim],
+ *               q_row, k_row and v_row elements from a token's row to the next (the operands may be columns of
+ *               one projection's rows; a multiple of 16 bytes (ALIGNMENT), at most 2^20);
+ *           SLIMFIT_HEADS_APART: q [batch, q_heads, q_tokens, head_dim], k [batch, kv_heads, head_dim, k_tokens],
+ *               v [batch, kv_heads, k_tokens, head_dim], contiguous, as slimfit_split_heads and
+ *               slimfit_heads_norm_rotate_forward leave them (q_row, k_row, v_row are not looked at).
+ *           dq, dk and dv lie like q, k and v, with row lengths of their own.
+ *  out, dout : DEVICE [batch, q_tokens, q_heads, head_dim], contiguous.  All of type dt and 16-byte aligned.
+ *  stats  : DEVICE float[batch, q_heads, q_tokens, 2], 16-byte aligned: m and l.
+ *  scale  : above 0, finite.        causal : not 0: query i sees keys j <= i + k_tokens - q_tokens.
+ *  lengths: DEVICE int32[batch] or NULL: keys of a sequence (held to 0 .. k_tokens); those past it are not looked at,
+ *           whatever they hold, and get gradients of 0.
+ *  A query that sees no key has out 0, m -infinity, l 0 and gives no gradients.
+ *  table  : DEVICE [buckets, q_heads] of dt, or NULL: the learned bias, table[bucket_of[j - i + q_tokens - 1]][head];
+ *           buckets <= 1024.  bucket_of : DEVICE int32[q_tokens + k_tokens - 1], 4-byte aligned; a bucket outside of
+ *           [0, buckets) adds nothing and gets no gradient.  Entries may be -infinity (keys that are not seen) or the
+ *           type's lowest value (keys that count where there are no others).
+ *  dtable : DEVICE [buckets, q_heads] of dt, or NULL: sum of ds over the batch and the pairs of each bucket.
+ *  head_dim : a multiple of 8 (bf16) or 4 (fp32), at most 128; q_heads a multiple of kv_heads (INVALID_ARG) and at most 2^15;
+ *           tokens up to 2^28; batch * q_heads * ceil(tokens / 128) below 2^22 (ERR_UNSUPPORTED).
+ *  fp32: products, sums and statistics in fp32.  bf16: products of bf16 operands summed in fp32; e^(s - m) (p and ds in the
+ *           backward pass) rounded to bf16 once before their products with v (dout, q and k), results rounded once.
+ *  Deterministic: every sum has one owner and one order.  Outputs share memory with nothing else of the call (INVALID_ARG).
+ *  workspace : DEVICE, 16-byte aligned, of the bytes slimfit_attention_workspace reports (backward 0 or 1; with_dtable:
+ *           whether dtable is asked for); contents overwritten.
+ * ---------------------------------------------------------------------- */
+typedef enum { SLIMFIT_HEADS_ROWS = 0, SLIMFIT_HEADS_APART = 1 } slimfit_heads_layout;
+
+int32_t slimfit_attention_workspace(int32_t dt, int32_t layout, int64_t batch, int32_t q_tokens, int32_t k_tokens, int32_t q_heads, int32_t kv_heads,
+                                    int32_t head_dim, int32_t with_dtable, int32_t backward, size_t *bytes);
+
+int32_t slimfit_attention_forward(const void *q, const void *k, const void *v, int32_t dt, int32_t layout, int64_t q_row, int64_t k_row, int64_t v_row,
+                                  int64_t batch, int32_t q_tokens, int32_t k_tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale,
+                                  int32_t causal, const int32_t *lengths, const void *table, int32_t buckets, const int32_t *bucket_of, void *out,
+                                  float *stats, void *workspace, size_t workspace_bytes, void *stream);
+
+int32_t slimfit_attention_backward(const void *dout, const void *q, const void *k, const void *v, int32_t dt, int32_t layout, int64_t q_row,
+                                   int64_t k_row, int64_t v_row, int64_t batch, int32_t q_tokens, int32_t k_tokens, int32_t q_heads, int32_t kv_heads,
+                                   int32_t head_dim, float scale, int32_t causal, const int32_t *lengths, const void *table, int32_t buckets,
+                                   const int32_t *bucket_of, const void *out, const float *stats, void *dq, void *dk, void *dv, int64_t dq_row,
+                                   int64_t dk_row, int64_t dv_row, void *dtable, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * Product of fp32 matrices (the dense products of the linear layers):
  *        out[i][j] = sum over k of a[i][k] * b[j][k]     (b_deep != 0: b is N x K)
  *        out[i][j] = sum over k of a[i][k] * b[k][j]     (b_deep == 0: b is K x N)

@@ -46,6 +46,7 @@ Q_FIXED, Q_BLOCK = 0, 1
 PRUNE_TOPK, PRUNE_THRESHOLD = 0, 1
 ACT_SILU, ACT_GELU = 0, 1
 ROTARY_HALVES, ROTARY_ADJACENT = 0, 1
+HEADS_ROWS, HEADS_APART = 0, 1
 GLOBAL_TILE = 4096                 # SLIMFIT_GLOBAL_TILE: granularity of prune_global's tile pointers
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_HIP, ERR_POINTER = range(7)
@@ -63,6 +64,7 @@ EXPORTS = (
     "slimfit_gated_quant_pack", "slimfit_gated_backward_dequant",
     "slimfit_heads_norm_rotate_forward", "slimfit_heads_norm_rotate_workspace", "slimfit_heads_norm_rotate_backward",
     "slimfit_weight_grad_dequant_workspace", "slimfit_weight_grad_dequant",
+    "slimfit_attention_workspace", "slimfit_attention_forward", "slimfit_attention_backward",
     "slimfit_split_heads", "slimfit_merge_heads", "slimfit_product_workspace", "slimfit_product",
     "slimfit_freeze_count", "slimfit_ils_select", "slimfit_ils_select_blocks",
     "slimfit_ils_update", "slimfit_schedule_random", "slimfit_schedule_progressive",
@@ -995,6 +997,110 @@ def heads_norm_rotate_backward(dq: torch.Tensor, dkt: torch.Tensor, dv: torch.Te
         C.c_int32(positions), C.c_int32(rotary), C.c_int32(pairing), _dev(position_ids), C.c_float(q_scale), _dev(dqkv), _dev(dgamma_q),
         _dev(dgamma_k), _dev(workspace), C.c_size_t(0 if workspace is None else workspace.numel()), _stream(stream))
     _check(rc, "heads_norm_rotate_backward")
+
+
+# ---------------------------------------------------------------- (c-att) attention in one pass over the keys
+
+def distance_buckets(q_tokens: int, k_tokens: int, buckets: int, reach: int, both_ways: bool = True, device="cuda") -> torch.Tensor:
+    """The bucket of each distance, key minus query, for ``bucket_of`` below (int32, q_tokens + k_tokens - 1).  The nearest half of a
+    side's buckets hold one distance each, the others grow with its logarithm up to ``reach``, past which all share the last.
+    ``both_ways``: keys after the query have half of the buckets; otherwise they share bucket 0 with its own place."""
+    far = torch.arange(1 - q_tokens, k_tokens, dtype=torch.float64)
+    side = max(1, buckets // 2 if both_ways else buckets)
+    one = max(1, side // 2)
+    away = far.abs() if both_ways else torch.clamp(-far, min=0)
+    grown = one + torch.log(torch.clamp(away, min=1) / one) / float(np.log(max(reach, one + 1) / one)) * (side - one)
+    bucket = torch.where(away < one, away, torch.clamp(grown.floor(), min=one)).clamp(max=side - 1)
+    if both_ways and buckets > 1:
+        bucket = bucket + torch.where(far > 0, side, 0)
+    return bucket.to(torch.int32).to(device)
+
+
+def _attention_row(t: torch.Tensor, tokens: int, heads: int, dim: int) -> int:
+    """Elements from a token's row to the next of a (batch, tokens, heads, dim) operand."""
+    row = t.stride(1) if tokens > 1 else t.stride(0) if t.shape[0] > 1 else heads * dim
+    _require(t.stride(3) == 1 or dim == 1)
+    _require((t.stride(2) == dim or heads == 1) and (tokens <= 1 or t.stride(1) == row) and (t.shape[0] <= 1 or t.stride(0) == tokens * row))
+    return row
+
+
+def _attention_sizes(q, k, v, layout: int, lengths, table, bucket_of):
+    """(batch, q_tokens, k_tokens, q_heads, kv_heads, dim), (q_row, k_row, v_row); checked against the other tensors."""
+    _require(q.dim() == 4 and k.dim() == 4 and v.dim() == 4 and q.dtype == k.dtype == v.dtype)
+    if layout == HEADS_ROWS:
+        B, Tq, Hq, D = q.shape
+        Tk, Hk = k.shape[1:3]
+        _require(k.shape == (B, Tk, Hk, D) and v.shape == k.shape)
+        rows = tuple(_attention_row(t, T, H, D) if 0 not in (B, T, H, D) else H * D for t, T, H in ((q, Tq, Hq), (k, Tk, Hk), (v, Tk, Hk)))
+    else:
+        _require(layout == HEADS_APART)
+        B, Hq, Tq, D = q.shape
+        Hk, Tk = v.shape[1:3]
+        _require(v.shape == (B, Hk, Tk, D) and k.shape == (B, Hk, D, Tk) and all(t.is_contiguous() for t in (q, k, v)))
+        rows = (0, 0, 0)
+    _require(lengths is None or (lengths.dtype == torch.int32 and lengths.numel() >= B and lengths.is_contiguous()))
+    if table is not None:
+        _require(table.dim() == 2 and table.shape[1] == Hq and table.dtype == q.dtype and table.is_contiguous())
+        _require(bucket_of is not None and bucket_of.dtype == torch.int32 and bucket_of.numel() >= Tq + Tk - 1 and bucket_of.is_contiguous())
+    return (B, Tq, Tk, Hq, Hk, D), rows
+
+
+def attention_workspace(dtype: torch.dtype, layout: int, batch: int, q_tokens: int, k_tokens: int, q_heads: int, kv_heads: int, head_dim: int,
+                        with_dtable: bool = False, backward: bool = False) -> int:
+    out = C.c_size_t(0)
+    _check(lib().slimfit_attention_workspace(
+        C.c_int32(_dt(torch.empty(0, dtype=dtype))), C.c_int32(layout), C.c_int64(batch), C.c_int32(q_tokens), C.c_int32(k_tokens), C.c_int32(q_heads),
+        C.c_int32(kv_heads), C.c_int32(head_dim), C.c_int32(int(bool(with_dtable))), C.c_int32(int(bool(backward))), C.byref(out)), "attention_workspace")
+    return int(out.value)
+
+
+def _at(t: Optional[torch.Tensor]):
+    """A tensor's address, strided or not."""
+    return C.c_void_p(0 if t is None else t.data_ptr())
+
+
+def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, layout: int, scale: float, causal: bool, lengths: Optional[torch.Tensor],
+                      table: Optional[torch.Tensor], bucket_of: Optional[torch.Tensor], out: torch.Tensor, stats: torch.Tensor,
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """out (batch, q_tokens, q_heads, dim) = softmax(scale q k^T + bias) v and stats (batch, q_heads, q_tokens, 2), each query's maximum
+    and sum.  HEADS_ROWS: q (batch, q_tokens, q_heads, dim), k and v (batch, k_tokens, kv_heads, dim), contiguous or columns of one
+    projection's rows; HEADS_APART: q, the transposed k and v as heads_norm_rotate_forward leaves them.  ``lengths`` (int32): keys of each
+    sequence; ``table`` (buckets, q_heads) and ``bucket_of`` (int32, by key - query + q_tokens - 1): the position bias."""
+    (B, Tq, Tk, Hq, Hk, D), rows = _attention_sizes(q, k, v, layout, lengths, table, bucket_of)
+    _require(out.shape == (B, Tq, Hq, D) and out.dtype == q.dtype and out.is_contiguous())
+    _require(stats.dtype == torch.float32 and stats.shape == (B, Hq, Tq, 2) and stats.is_contiguous())
+    _on_current_device(q, k, v, lengths, table, None if table is None else bucket_of, out, stats, workspace)
+    if Tq and B and layout == HEADS_APART:
+        workspace = _own_workspace(workspace, attention_workspace(q.dtype, layout, B, Tq, Tk, Hq, Hk, D), q.device, stream)
+    rc = lib().slimfit_attention_forward(
+        _at(q), _at(k), _at(v), C.c_int32(_dt(q)), C.c_int32(layout), *(C.c_int64(r) for r in rows), C.c_int64(B), C.c_int32(Tq), C.c_int32(Tk), C.c_int32(Hq),
+        C.c_int32(Hk), C.c_int32(D), C.c_float(scale), C.c_int32(int(bool(causal))), _at(lengths), _at(table),
+        C.c_int32(0 if table is None else table.shape[0]), _at(bucket_of), _at(out), _at(stats), _at(workspace),
+        C.c_size_t(0 if workspace is None else workspace.numel()), _stream(stream))
+    _check(rc, "attention_forward")
+
+
+def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, layout: int, scale: float, causal: bool,
+                       lengths: Optional[torch.Tensor], table: Optional[torch.Tensor], bucket_of: Optional[torch.Tensor], out: torch.Tensor,
+                       stats: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor, dtable: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The gradients of q, k, v (laid out like them) and, where it is given, of the table, from out and stats of attention_forward on
+    the same operands; the probabilities are formed again."""
+    sizes, rows = _attention_sizes(q, k, v, layout, lengths, table, bucket_of)
+    d_sizes, d_rows = _attention_sizes(dq, dk, dv, layout, None, None, None)
+    B, Tq, Tk, Hq, Hk, D = sizes
+    _require(d_sizes == sizes and dq.dtype == q.dtype)
+    _require(all(t.shape == (B, Tq, Hq, D) and t.dtype == q.dtype and t.is_contiguous() for t in (dout, out)))
+    _require(stats.dtype == torch.float32 and stats.shape == (B, Hq, Tq, 2) and stats.is_contiguous())
+    _require(dtable is None or (table is not None and dtable.shape == table.shape and dtable.dtype == table.dtype and dtable.is_contiguous()))
+    _on_current_device(dout, q, k, v, lengths, table, None if table is None else bucket_of, out, stats, dq, dk, dv, dtable, workspace)
+    workspace = _own_workspace(workspace, attention_workspace(q.dtype, layout, B, Tq, Tk, Hq, Hk, D, dtable is not None, True), q.device, stream)
+    rc = lib().slimfit_attention_backward(
+        _at(dout), _at(q), _at(k), _at(v), C.c_int32(_dt(q)), C.c_int32(layout), *(C.c_int64(r) for r in rows), C.c_int64(B), C.c_int32(Tq), C.c_int32(Tk),
+        C.c_int32(Hq), C.c_int32(Hk), C.c_int32(D), C.c_float(scale), C.c_int32(int(bool(causal))), _at(lengths), _at(table),
+        C.c_int32(0 if table is None else table.shape[0]), _at(bucket_of), _at(out), _at(stats), _at(dq), _at(dk), _at(dv),
+        *(C.c_int64(r) for r in d_rows), _at(dtable), _at(workspace), C.c_size_t(workspace.numel()), _stream(stream))
+    _check(rc, "attention_backward")
 
 
 def product_workspace(M: int, N: int, K: int) -> int:

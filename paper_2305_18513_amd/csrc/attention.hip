@@ -1,0 +1,314 @@
+// Attention: the calls' checks and launches, and the small passes around the kernels of attention_forward.hpp and attention_backward.hpp:
+// keys that lie transposed are turned into rows first (2 bytes moved for each; the products read rows of either side), and
+// the sums of ds by distance that the waves left are added up over batch and queries, then over each bucket's distances, in order.
+#include "attention.hpp"
+
+namespace slimfit {
+namespace {
+
+constexpr int kTurn = 64;
+
+// kt (head, dim, tokens) -> k (head, tokens, dim): a workgroup takes 64 tokens of up to 64 elements
+template <typename T>
+__global__ void __launch_bounds__(kAttnThreads) turn_kernel(const T *__restrict__ kt, T *__restrict__ k, int dim, int tokens, int blocks, int columns)
+{
+    __shared__ T tile[kTurn][kTurn + 4 / sizeof(T)];
+    const int unit = (int)(blockIdx.x / (unsigned)(blocks * columns)), rest = (int)(blockIdx.x % (unsigned)(blocks * columns));
+    const int t0 = rest / columns * kTurn, d0 = rest % columns * kTurn, x = threadIdx.x % kTurn, y = threadIdx.x / kTurn;
+    const T *const from = kt + (int64_t)unit * dim * tokens;
+    T *const to = k + (int64_t)unit * dim * tokens;
+#pragma unroll
+    for (int i = 0; i < kTurn; i += kAttnThreads / kTurn)
+        if (d0 + y + i < dim && t0 + x < tokens) tile[y + i][x] = from[(int64_t)(d0 + y + i) * tokens + t0 + x];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTurn; i += kAttnThreads / kTurn)
+        if (t0 + y + i < tokens && d0 + x < dim) to[(int64_t)(t0 + y + i) * dim + d0 + x] = tile[x][y + i];
+}
+
+// sums of ds by distance over batch and queries
+__global__ void __launch_bounds__(kAttnThreads) distances_kernel(Attention a, const float *__restrict__ parts, int64_t part_row, int blocks, float *__restrict__ sums)
+{
+    const int all = a.q_tokens + a.k_tokens - 1, head = blockIdx.y, at = blockIdx.x * kAttnThreads + threadIdx.x;
+    if (at >= all) return;
+    double sum = 0.0;
+    for (int b = 0; b < a.batch; ++b) {
+        const int keys = keys_of(a, b);
+        const float *const of = parts + ((int64_t)b * a.q_heads + head) * blocks * kAttnWaves * part_row;
+        for (int block = 0; block < blocks; ++block) {
+            const int written = (key_tiles(a, block * kBlock, keys) + 1) * kTile;
+#pragma unroll
+            for (int w = 0; w < kAttnWaves; ++w) {
+                const int place = at - (a.q_tokens - 1) + block * kBlock + w * kOwn + kOwn - 1;
+                if (place >= 0 && place < written) sum += (double)of[(int64_t)(block * kAttnWaves + w) * part_row + place];
+            }
+        }
+    }
+    sums[(int64_t)head * all + at] = (float)sum;
+}
+
+// a workgroup for each bucket and head
+template <typename T>
+__global__ void __launch_bounds__(kAttnThreads) buckets_kernel(Attention a, const float *__restrict__ sums, T *__restrict__ dtable)
+{
+    __shared__ double part[kAttnWaves];
+    const int all = a.q_tokens + a.k_tokens - 1, bucket = blockIdx.x, head = blockIdx.y;
+    double sum = 0.0;
+    if (a.batch > 0 && a.q_tokens > 0)                      // (no sums otherwise)
+        for (int at = threadIdx.x; at < all; at += kAttnThreads)
+            if (a.bucket_of[at] == bucket) sum += (double)sums[(int64_t)head * all + at];
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x > 0) return;
+    const float x = (float)(((part[0] + part[1]) + part[2]) + part[3]);
+    if constexpr (sizeof(T) == 4) dtable[(int64_t)bucket * a.q_heads + head] = x;
+    else dtable[(int64_t)bucket * a.q_heads + head] = (T)bf16_narrow(x);
+}
+
+struct Sizes {
+    int32_t dt, layout;
+    int64_t batch;
+    int32_t q_tokens, k_tokens, q_heads, kv_heads, head_dim, buckets;
+    size_t e() const { return dtype_size(dt); }
+    int64_t q_count() const { return batch * q_tokens * q_heads * head_dim; }
+    int64_t k_count() const { return batch * k_tokens * kv_heads * head_dim; }
+};
+
+size_t rounded(size_t n) { return (n + 255) & ~(size_t)255; }
+
+int32_t check_sizes(const Sizes &z)
+{
+    if (!dtype_ok(z.dt) || (z.layout != SLIMFIT_HEADS_ROWS && z.layout != SLIMFIT_HEADS_APART)) return SLIMFIT_ERR_INVALID_ARG;
+    if (z.batch < 0 || z.q_tokens < 0 || z.k_tokens < 0 || z.q_heads < 1 || z.kv_heads < 1 || z.q_heads % z.kv_heads != 0 || z.head_dim < 1 || z.buckets < 0)
+        return SLIMFIT_ERR_INVALID_ARG;
+    if (z.head_dim % (16 / (int)z.e()) != 0 || z.head_dim > kMostHeadDim || z.buckets > kMostBuckets || z.q_heads > (1 << 15)) return SLIMFIT_ERR_UNSUPPORTED;
+    if (z.q_tokens > (1 << 28) || z.k_tokens > (1 << 28) || z.batch > (1 << 24)) return SLIMFIT_ERR_UNSUPPORTED;
+    const int64_t blocks = ((int64_t)(z.q_tokens > z.k_tokens ? z.q_tokens : z.k_tokens) + kBlock - 1) / kBlock;
+    // (the turned keys take up to four workgroups for each of these)
+    if (z.batch * z.q_heads * (blocks > 0 ? blocks : 1) >= ((int64_t)1 << 22)) return SLIMFIT_ERR_UNSUPPORTED;
+    return SLIMFIT_OK;
+}
+
+bool turned(const Sizes &z) { return z.layout == SLIMFIT_HEADS_APART && z.batch > 0 && z.k_tokens > 0 && z.q_tokens > 0; }
+size_t turned_bytes(const Sizes &z) { return turned(z) ? rounded((size_t)z.k_count() * z.e()) : 0; }
+int q_blocks(const Sizes &z) { return (z.q_tokens + kBlock - 1) / kBlock; }
+int64_t part_row(const Sizes &z) { return ((int64_t)z.k_tokens + kTile - 1) / kTile * kTile + kTile; }
+
+struct BackwardPlaces {
+    size_t rows, parts, sums, bytes;
+    BackwardPlaces(const Sizes &z, bool table)
+    {
+        rows = turned_bytes(z);
+        parts = rows + rounded((size_t)(z.batch * z.q_heads) * (size_t)z.q_tokens * 12);
+        sums = parts + (table ? rounded((size_t)(z.batch * z.q_heads) * (size_t)q_blocks(z) * kAttnWaves * (size_t)part_row(z) * 4) : 0);
+        bytes = sums + (table ? rounded((size_t)z.q_heads * ((size_t)z.q_tokens + (size_t)z.k_tokens) * 4) : 0);
+    }
+};
+
+// One operand's memory: `rows` rows of `width` bytes, `apart` bytes from one to the next.
+struct Span {
+    const void *at;
+    size_t rows, width, apart;
+    size_t bytes() const { return rows == 0 ? 0 : (rows - 1) * apart + width; }
+};
+bool share(const Span &a, const Span &b)
+{
+    if (a.bytes() == 0 || b.bytes() == 0 || !meet(a.at, a.bytes(), b.at, b.bytes())) return false;
+    if (a.apart != b.apart) return true;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);     // columns of the same rows
+    const size_t off = y >= x ? (size_t)(y - x) % a.apart : a.apart - 1 - (size_t)(x - y - 1) % a.apart;
+    return off < a.width || a.apart - off < b.width;
+}
+
+// q, k, v or their gradients
+Operand operand_of(const void *at, const Sizes &z, int which, int64_t row)
+{
+    const int64_t heads = which == 0 ? z.q_heads : z.kv_heads, tokens = which == 0 ? z.q_tokens : z.k_tokens, D = z.head_dim;
+    if (z.layout == SLIMFIT_HEADS_ROWS) return {at, tokens * row, D, row};
+    return {at, heads * tokens * D, tokens * D, D};
+}
+Span span_of(const void *at, const Sizes &z, int which, int64_t row)
+{
+    const size_t heads = (size_t)(which == 0 ? z.q_heads : z.kv_heads), tokens = (size_t)(which == 0 ? z.q_tokens : z.k_tokens), D = (size_t)z.head_dim;
+    if (z.layout == SLIMFIT_HEADS_ROWS) return {at, (size_t)z.batch * tokens, heads * D * z.e(), (size_t)row * z.e()};
+    const size_t all = (size_t)z.batch * heads * tokens * D * z.e();
+    return {at, all > 0 ? 1u : 0u, all, all};
+}
+Span flat(const void *at, size_t bytes) { return {at, bytes > 0 ? 1u : 0u, bytes, bytes}; }
+
+int32_t check_rows(const Sizes &z, int64_t q_row, int64_t k_row, int64_t v_row)
+{
+    if (z.layout != SLIMFIT_HEADS_ROWS) return SLIMFIT_OK;
+    const int64_t per = 16 / (int64_t)z.e(), kv = (int64_t)z.kv_heads * z.head_dim;
+    if (q_row < (int64_t)z.q_heads * z.head_dim || k_row < kv || v_row < kv) return SLIMFIT_ERR_INVALID_ARG;
+    if (q_row % per != 0 || k_row % per != 0 || v_row % per != 0) return SLIMFIT_ERR_ALIGNMENT;
+    return q_row > (1 << 20) || k_row > (1 << 20) || v_row > (1 << 20) ? SLIMFIT_ERR_UNSUPPORTED : SLIMFIT_OK;
+}
+
+// the spans' pointers, alignment (NULL where there is nothing is fine) and that no output shares memory with anything
+int32_t check_spans(const Span *in, int n_in, const Span *out, int n_out)
+{
+    for (int i = 0; i < n_in + n_out; ++i) {
+        const Span &s = i < n_in ? in[i] : out[i - n_in];
+        if (s.bytes() > 0 && !s.at) return SLIMFIT_ERR_INVALID_ARG;
+    }
+    for (int i = 0; i < n_in + n_out; ++i)
+        if (!aligned_to(i < n_in ? in[i].at : out[i - n_in].at, 16)) return SLIMFIT_ERR_ALIGNMENT;
+    for (int i = 0; i < n_out; ++i) {
+        for (int j = 0; j < n_in; ++j)
+            if (share(out[i], in[j])) return SLIMFIT_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (share(out[i], out[j])) return SLIMFIT_ERR_INVALID_ARG;
+    }
+    return SLIMFIT_OK;
+}
+int32_t check_ranges(const Span *s, int n)
+{
+    int32_t rc;
+    for (int i = 0; i < n; ++i)
+        if ((rc = check_device_range(s[i].at, s[i].bytes())) != SLIMFIT_OK) return rc;
+    return SLIMFIT_OK;
+}
+
+int32_t check_others(const Sizes &z, float scale, const int32_t *lengths, const void *table, const int32_t *bucket_of)
+{
+    if (!(scale > 0.0f) || __builtin_isinf(scale)) return SLIMFIT_ERR_INVALID_ARG;
+    if (table && (z.buckets < 1 || (!bucket_of && z.q_tokens > 0 && z.k_tokens > 0))) return SLIMFIT_ERR_INVALID_ARG;
+    if (!aligned_to(lengths, 4) || !aligned_to(table, z.e()) || (table && !aligned_to(bucket_of, 4))) return SLIMFIT_ERR_ALIGNMENT;
+    return SLIMFIT_OK;
+}
+int32_t check_other_ranges(const Sizes &z, const int32_t *lengths, const void *table, const int32_t *bucket_of)
+{
+    int32_t rc;
+    if (lengths && (rc = check_device_range(lengths, (size_t)z.batch * 4)) != SLIMFIT_OK) return rc;
+    if (!table) return SLIMFIT_OK;
+    if ((rc = check_device_range(table, (size_t)z.buckets * (size_t)z.q_heads * z.e())) != SLIMFIT_OK) return rc;
+    return z.q_tokens > 0 && z.k_tokens > 0 ? check_device_range(bucket_of, ((size_t)z.q_tokens + (size_t)z.k_tokens - 1) * 4) : SLIMFIT_OK;
+}
+int32_t check_workspace(size_t need, const void *ws, size_t bytes)
+{
+    if (need == 0) return SLIMFIT_OK;
+    if (!ws || bytes < need) return SLIMFIT_ERR_WORKSPACE;
+    if (!aligned_to(ws, 16)) return SLIMFIT_ERR_ALIGNMENT;
+    return check_device_range(ws, need);
+}
+
+void turn_keys(const Sizes &z, const void *kt, void *k, hipStream_t st)
+{
+    const int blocks = (z.k_tokens + kTurn - 1) / kTurn, columns = (z.head_dim + kTurn - 1) / kTurn;
+    const unsigned grid = (unsigned)(z.batch * z.kv_heads * blocks * columns);
+    if (z.dt == SLIMFIT_F32) launch(turn_kernel<float>, grid, kAttnThreads, 0, st, static_cast<const float *>(kt), static_cast<float *>(k), z.head_dim, z.k_tokens, blocks, columns);
+    else launch(turn_kernel<uint16_t>, grid, kAttnThreads, 0, st, static_cast<const uint16_t *>(kt), static_cast<uint16_t *>(k), z.head_dim, z.k_tokens, blocks, columns);
+}
+
+Attention attention_of(const Sizes &z, const void *q, const void *k, const void *v, int64_t q_row, int64_t k_row, int64_t v_row, float scale, int32_t causal,
+                       const int32_t *lengths, const void *table, const int32_t *bucket_of)
+{
+    return {operand_of(q, z, 0, q_row), operand_of(k, z, 1, k_row), operand_of(v, z, 1, v_row), (int32_t)z.batch, z.q_tokens, z.k_tokens, z.q_heads, z.kv_heads,
+            z.head_dim, causal != 0, table ? z.buckets : 0, scale, lengths, table, bucket_of};
+}
+
+}  // namespace
+}  // namespace slimfit
+
+using namespace slimfit;
+
+extern "C" int32_t slimfit_attention_workspace(int32_t dt, int32_t layout, int64_t batch, int32_t q_tokens, int32_t k_tokens, int32_t q_heads, int32_t kv_heads,
+                                               int32_t head_dim, int32_t with_dtable, int32_t backward, size_t *bytes)
+{
+    const Sizes z = {dt, layout, batch, q_tokens, k_tokens, q_heads, kv_heads, head_dim, 0};
+    const int32_t rc = check_sizes(z);
+    if (rc != SLIMFIT_OK) return rc;
+    if (!bytes) return SLIMFIT_ERR_INVALID_ARG;
+    *bytes = backward ? BackwardPlaces(z, with_dtable != 0).bytes : turned_bytes(z);
+    return SLIMFIT_OK;
+}
+
+extern "C" int32_t slimfit_attention_forward(const void *q, const void *k, const void *v, int32_t dt, int32_t layout, int64_t q_row, int64_t k_row, int64_t v_row,
+                                             int64_t batch, int32_t q_tokens, int32_t k_tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale,
+                                             int32_t causal, const int32_t *lengths, const void *table, int32_t buckets, const int32_t *bucket_of, void *out,
+                                             float *stats, void *workspace, size_t workspace_bytes, void *stream)
+{
+    StreamScope capture_aware(stream);
+    const Sizes z = {dt, layout, batch, q_tokens, k_tokens, q_heads, kv_heads, head_dim, table ? buckets : 0};
+    int32_t rc = check_sizes(z);
+    if (rc != SLIMFIT_OK || (rc = check_rows(z, q_row, k_row, v_row)) != SLIMFIT_OK) return rc;
+    if ((rc = check_others(z, scale, lengths, table, bucket_of)) != SLIMFIT_OK) return rc;
+    if (batch == 0 || q_tokens == 0) return SLIMFIT_OK;
+    const Span in[] = {span_of(q, z, 0, q_row), span_of(k, z, 1, k_row), span_of(v, z, 1, v_row)};
+    const Span to[] = {flat(out, (size_t)z.q_count() * z.e()), flat(stats, (size_t)(batch * q_heads) * (size_t)q_tokens * 8)};
+    if ((rc = check_spans(in, 3, to, 2)) != SLIMFIT_OK) return rc;
+    const size_t need = turned_bytes(z);
+    if ((rc = check_workspace(need, workspace, workspace_bytes)) != SLIMFIT_OK) return rc;
+    if ((rc = check_ranges(in, 3)) != SLIMFIT_OK || (rc = check_ranges(to, 2)) != SLIMFIT_OK) return rc;
+    if ((rc = check_other_ranges(z, lengths, table, bucket_of)) != SLIMFIT_OK) return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (turned(z)) {
+        turn_keys(z, k, workspace, st);
+        k = workspace;
+    }
+    const Attention a = attention_of(z, q, k, v, q_row, k_row, v_row, scale, causal, lengths, k_tokens > 0 ? table : nullptr, bucket_of);
+    if (dt == SLIMFIT_BF16) attention_forward_bf16(a, out, stats, st);
+    else attention_forward_f32(a, out, stats, st);
+    return launch_status();
+}
+
+extern "C" int32_t slimfit_attention_backward(const void *dout, const void *q, const void *k, const void *v, int32_t dt, int32_t layout, int64_t q_row,
+                                              int64_t k_row, int64_t v_row, int64_t batch, int32_t q_tokens, int32_t k_tokens, int32_t q_heads, int32_t kv_heads,
+                                              int32_t head_dim, float scale, int32_t causal, const int32_t *lengths, const void *table, int32_t buckets,
+                                              const int32_t *bucket_of, const void *out, const float *stats, void *dq, void *dk, void *dv, int64_t dq_row,
+                                              int64_t dk_row, int64_t dv_row, void *dtable, void *workspace, size_t workspace_bytes, void *stream)
+{
+    StreamScope capture_aware(stream);
+    const Sizes z = {dt, layout, batch, q_tokens, k_tokens, q_heads, kv_heads, head_dim, table ? buckets : 0};
+    int32_t rc = check_sizes(z);
+    if (rc != SLIMFIT_OK || (rc = check_rows(z, q_row, k_row, v_row)) != SLIMFIT_OK || (rc = check_rows(z, dq_row, dk_row, dv_row)) != SLIMFIT_OK) return rc;
+    if ((rc = check_others(z, scale, lengths, table, bucket_of)) != SLIMFIT_OK) return rc;
+    if (dtable && !table) return SLIMFIT_ERR_INVALID_ARG;
+    if (!aligned_to(dtable, z.e())) return SLIMFIT_ERR_ALIGNMENT;
+    const size_t q_bytes = (size_t)z.q_count() * z.e(), table_bytes = dtable ? (size_t)buckets * (size_t)q_heads * z.e() : 0;
+    const Span in[] = {span_of(q, z, 0, q_row), span_of(k, z, 1, k_row), span_of(v, z, 1, v_row), flat(dout, q_bytes), flat(out, q_bytes),
+                       flat(stats, (size_t)(batch * q_heads) * (size_t)q_tokens * 8)};
+    const Span to[] = {span_of(dq, z, 0, dq_row), span_of(dk, z, 1, dk_row), span_of(dv, z, 1, dv_row)};
+    if ((rc = check_spans(in, 6, to, 3)) != SLIMFIT_OK) return rc;
+    if (dtable) {
+        const Span d = flat(dtable, table_bytes);
+        for (const Span &s : in)
+            if (share(d, s)) return SLIMFIT_ERR_INVALID_ARG;
+        for (const Span &s : to)
+            if (share(d, s)) return SLIMFIT_ERR_INVALID_ARG;
+        if (meet(dtable, table_bytes, table, table_bytes)) return SLIMFIT_ERR_INVALID_ARG;
+    }
+    const BackwardPlaces at(z, dtable != nullptr);
+    if ((rc = check_workspace(at.bytes, workspace, workspace_bytes)) != SLIMFIT_OK) return rc;
+    if ((rc = check_ranges(in, 6)) != SLIMFIT_OK || (rc = check_ranges(to, 3)) != SLIMFIT_OK) return rc;
+    if ((rc = check_other_ranges(z, lengths, table, bucket_of)) != SLIMFIT_OK || (rc = check_device_range(dtable, table_bytes)) != SLIMFIT_OK) return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    char *const ws = static_cast<char *>(workspace);
+    if (turned(z)) {
+        turn_keys(z, k, ws, st);
+        k = ws;
+    }
+    const bool pairs = batch > 0 && q_tokens > 0 && k_tokens > 0;
+    const Attention a = attention_of(z, q, k, v, q_row, k_row, v_row, scale, causal, lengths, pairs ? table : nullptr, bucket_of);
+    const Operand oq = operand_of(dq, z, 0, dq_row), ok = operand_of(dk, z, 1, dk_row), ov = operand_of(dv, z, 1, dv_row);
+    const bool across = layout == SLIMFIT_HEADS_APART;      // dk lies transposed too: tokens beside each other
+    float *const parts = dtable && pairs ? reinterpret_cast<float *>(ws + at.parts) : nullptr;
+    const Gradients g = {dout, out, stats, dq, dk, dv, oq.b, oq.h, oq.t, ok.b, ok.h, across ? 1 : ok.t, across ? k_tokens : 1, ov.b, ov.h, ov.t,
+                         reinterpret_cast<float *>(ws + at.rows), parts, part_row(z)};
+    if (dt == SLIMFIT_BF16) attention_backward_bf16(a, g, st);
+    else attention_backward_f32(a, g, st);
+    if (dtable) {
+        float *const sums = reinterpret_cast<float *>(ws + at.sums);
+        const int all = q_tokens + k_tokens - 1;
+        if (parts) launch(distances_kernel, dim3((unsigned)((all + kAttnThreads - 1) / kAttnThreads), (unsigned)q_heads), kAttnThreads, 0, st, a, parts, g.part_row, q_blocks(z), sums);
+        Attention b = a;
+        if (!pairs) b.batch = 0;
+        const dim3 grid((unsigned)buckets, (unsigned)q_heads);
+        if (dt == SLIMFIT_BF16) launch(buckets_kernel<uint16_t>, grid, kAttnThreads, 0, st, b, sums, static_cast<uint16_t *>(dtable));
+        else launch(buckets_kernel<float>, grid, kAttnThreads, 0, st, b, sums, static_cast<float *>(dtable));
+    }
+    return launch_status();
+}

@@ -1,0 +1,321 @@
+// Attention backward from recomputed probabilities:  p = e^(s - m) / l,  dp = dout v^T,  delta = sum over d of dout out,  ds = p (dp - delta),
+//     dq = scale ds k,   dk = scale ds^T q,   dv = p^T dout,   dtable[b] = sum of ds over the pairs of bucket b.
+// Two kernels, so that every sum has one owner and one order: a wave of the first holds 32 queries and goes over keys (dq, and the
+// sums of ds by distance), a wave of the second 32 keys and goes over the queries of all heads that share them (dk, dv).  They form s
+// and dp twice: seven products where five would do with sums that meet in memory.
+#pragma once
+
+#include "attention.hpp"
+
+namespace slimfit {
+namespace {
+
+// p = exp2(fma(q k^T, scale log2 e, -first)), or with a bias exp2((s - first) log2 e - second).  A query that sees no key has first
+// or second infinite, its p are 0.
+template <bool BIAS> __device__ __forceinline__ float probability(float s, float scale, float first, float second)
+{
+    return __builtin_amdgcn_exp2f(BIAS ? __builtin_fmaf(s - first, kLog2e, -second) : __builtin_fmaf(s, scale, -first));
+}
+
+constexpr int kSkew = kTile + 4;             // floats of a query's ds in LDS
+
+template <typename T, int D, bool BIAS, bool PARTS>
+__global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 256) ? 1 : 2) queries_kernel(Attention a, Gradients g, int blocks)
+{
+    __shared__ __align__(16) char tiles[kStages<T, D>][2 * kTileBytes<T, D>];
+    __shared__ float column[BIAS ? kMostBuckets : 1], biases[2][BIAS ? kDistances : 1];
+    __shared__ __align__(16) float skew[PARTS ? kAttnWaves : 1][PARTS ? kOwn * kSkew : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int heads = a.batch * a.q_heads, bh = (int)(blockIdx.x % (unsigned)heads);
+    const int turn = (int)(blockIdx.x / (unsigned)heads), block = a.causal ? blocks - 1 - turn : turn;      // the longest first
+    const int batch = bh / a.q_heads, head = bh % a.q_heads, kv = head / (a.q_heads / a.kv_heads);
+    const int q0 = block * kBlock, mine = q0 + wave * kOwn, i = mine + (lane & 31);
+    const T *const q = static_cast<const T *>(a.q.at) + batch * a.q.b + head * a.q.h;
+    const T *const k = static_cast<const T *>(a.k.at) + batch * a.k.b + kv * a.k.h;
+    const T *const v = static_cast<const T *>(a.v.at) + batch * a.v.b + kv * a.v.h;
+    const int keys = keys_of(a, batch), count = key_tiles(a, q0, keys);
+    const int seen = seen_by(a, i, keys), all_see = seen_by(a, mine, keys), any_sees = seen_by(a, min(mine + kOwn, a.q_tokens) - 1, keys);
+    const float scale = a.scale * kLog2e;
+
+    TileLoad<T, D> kl, vl;
+    BiasLoad bl;
+    auto load = [&](int t) {
+        kl.load(k, a.k.t, t * kTile, keys, a.head_dim);
+        vl.load(v, a.v.t, t * kTile, keys, a.head_dim);
+        if constexpr (BIAS) bl.load(a, t * kTile - q0 - (kBlock - 1) + a.q_tokens - 1);
+    };
+    auto store = [&](int to) {
+        kl.store(tiles[to % kStages<T, D>]);
+        vl.store(tiles[to % kStages<T, D>] + kTileBytes<T, D>);
+        if constexpr (BIAS) bl.store(a, column, biases[to]);
+    };
+
+    Own<T, D> own, grad;
+    own.load(q, a.q.t, mine, a.q_tokens, a.head_dim);
+    const int64_t out_row = (int64_t)a.q_heads * a.head_dim, out_at = (int64_t)batch * a.q_tokens * out_row + (int64_t)head * a.head_dim;
+    grad.load(static_cast<const T *>(g.dout) + out_at, out_row, mine, a.q_tokens, a.head_dim);
+    float first = __builtin_inff(), second = __builtin_inff(), delta = 0.0f;
+    {
+        Own<T, D> o;
+        o.load(static_cast<const T *>(g.out) + out_at, out_row, mine, a.q_tokens, a.head_dim);
+#pragma unroll
+        for (int c = 0; c < Own<T, D>::VECTORS; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t x = o.x[c][e], y = grad.x[c][e];
+                if constexpr (sizeof(T) == 4) {
+                    delta = __builtin_fmaf(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y), delta);
+                } else {
+                    delta = __builtin_fmaf(__builtin_bit_cast(float, x << 16), __builtin_bit_cast(float, y << 16), delta);
+                    delta = __builtin_fmaf(__builtin_bit_cast(float, x & 0xFFFF0000u), __builtin_bit_cast(float, y & 0xFFFF0000u), delta);
+                }
+            }
+        delta = both_sum(delta);
+    }
+    if (i < a.q_tokens) {
+        const int64_t at = (int64_t)bh * a.q_tokens + i, all = (int64_t)heads * a.q_tokens;
+        const float top = g.stats[2 * at], total = g.stats[2 * at + 1];
+        if (total > 0.0f) {
+            const float l = __builtin_amdgcn_logf(total);   // to the base of 2
+            first = BIAS ? top : __builtin_fmaf(top, kLog2e, l);
+            second = l;
+        } else if (BIAS) {
+            first = 0.0f;                                   // (second stays infinite)
+        }
+        if (half == 0) {                                    // for the second kernel
+            g.rows[at] = first;
+            g.rows[all + at] = second;
+            g.rows[2 * all + at] = delta;
+        }
+    }
+    f32x16 dq[D / 32];
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n) dq[n] = zeros16();
+    float carry = 0.0f;
+    float *const part = PARTS ? g.parts + ((int64_t)bh * blocks * kAttnWaves + block * kAttnWaves + wave) * g.part_row : nullptr;
+
+    if constexpr (BIAS) {
+        load_column<T>(a, head, column);
+        __syncthreads();
+    }
+    if (count > 0) {
+        load(0);
+        store(0);
+        load(1);
+        __syncthreads();
+    }
+    for (int t = 0; t < count; ++t) {
+        const char *const tile = tiles[t % kStages<T, D>];
+        const int k0 = t * kTile;
+        float now = 0.0f;
+        if (k0 < any_sees) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                f32x16 s = dots<T, D>(tile, 32 * n, own);
+                const f32x16 dp = dots<T, D>(tile + kTileBytes<T, D>, 32 * n, grad);
+                const float *const b = biases[BIAS ? t & 1 : 0] + kBlock - 1 - (i - q0) + 4 * half + 32 * n;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    if constexpr (BIAS) s[r] = __builtin_fmaf(s[r], a.scale, b[8 * (r / 4) + r % 4]);
+                    s[r] = probability<BIAS>(s[r], scale, first, second) * (dp[r] - delta);
+                }
+                if (k0 + 32 * n + 32 > all_see) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (k0 + 32 * n + row_of(r, half) >= seen) s[r] = 0.0f;
+                }
+                if constexpr (PARTS) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        *reinterpret_cast<f32x4 *>(&skew[wave][(lane & 31) * kSkew + 32 * n + 8 * c + 4 * half]) = f32x4{s[4 * c], s[4 * c + 1], s[4 * c + 2], s[4 * c + 3]};
+                }
+                sums<T, D>(tile, 32 * n, s, dq);
+            }
+            if constexpr (PARTS) {
+                // Sums along the diagonals: lane l has that of key - query = l - 31 (within the tile and the wave's queries), then, for the
+                // next tile, which sees these distances 64 lower, that of l + 33.
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                float high = 0.0f;
+#pragma unroll
+                for (int n = 0; n < kOwn; ++n) {
+                    const int key = lane - 31 + n;
+                    const float x = skew[wave][n * kSkew + max(key, 0)];
+                    now += key >= 0 ? x : 0.0f;
+                    const float y = skew[wave][n * kSkew + min(key + kTile, kTile - 1)];
+                    high += key + kTile < kTile ? y : 0.0f;
+                }
+                now += carry;
+                carry = high;
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+        } else if (PARTS) {
+            now = carry;
+            carry = 0.0f;
+        }
+        if constexpr (PARTS) part[k0 + lane] = now;
+        if (kStages<T, D> == 1) __syncthreads();
+        if (t + 1 < count) {
+            store((t + 1) & 1);
+            load(t + 2);
+        }
+        __syncthreads();
+    }
+    if constexpr (PARTS) part[count * kTile + lane] = carry;
+    if (i < a.q_tokens) store_row<T, D>(dq, a.scale, static_cast<T *>(g.dq) + batch * g.dq_b + head * g.dq_h + i * g.dq_t, a.head_dim);
+}
+
+template <typename T, int D, bool BIAS>
+__global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > 128 ? 1 : 2) keys_kernel(Attention a, Gradients g, int blocks)
+{
+    __shared__ __align__(16) char tiles[kStages<T, D>][2 * kTileBytes<T, D>];
+    __shared__ __align__(16) float rows[2][3][kTile];
+    __shared__ float column[BIAS ? kMostBuckets : 1], biases[2][BIAS ? kDistances : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int heads = a.batch * a.kv_heads, bh = (int)(blockIdx.x % (unsigned)heads), block = (int)(blockIdx.x / (unsigned)heads);
+    const int batch = bh / a.kv_heads, kv = bh % a.kv_heads, group = a.q_heads / a.kv_heads;
+    const int k0 = block * kBlock, mine = k0 + wave * kOwn, j = mine + (lane & 31);
+    const int keys = keys_of(a, batch);
+    const float scale = a.scale * kLog2e;
+    const int64_t out_row = (int64_t)a.q_heads * a.head_dim, all = (int64_t)a.batch * a.q_heads * a.q_tokens;
+
+    // queries that see the first of the workgroup's keys, and all of the wave's
+    const int offset = a.k_tokens - a.q_tokens;
+    const int from = a.causal ? max(0, k0 - offset) / kTile : 0, per_head = k0 < keys ? max(0, (a.q_tokens + kTile - 1) / kTile - from) : 0;
+    const int count = per_head * group;
+
+    Own<T, D> own, val;
+    own.load(static_cast<const T *>(a.k.at) + batch * a.k.b + kv * a.k.h, a.k.t, mine, keys, a.head_dim);
+    val.load(static_cast<const T *>(a.v.at) + batch * a.v.b + kv * a.v.h, a.v.t, mine, keys, a.head_dim);
+    f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n) dk[n] = dv[n] = zeros16();
+
+    TileLoad<T, D> ql, gl;
+    BiasLoad bl;
+    float held[3];
+    auto load = [&](int t) {                                // (past the last tile: rows that are not there)
+        const int head = kv * group + min(t / max(per_head, 1), group - 1), q0 = t < count ? (from + t % max(per_head, 1)) * kTile : a.q_tokens;
+        ql.load(static_cast<const T *>(a.q.at) + batch * a.q.b + head * a.q.h, a.q.t, q0, a.q_tokens, a.head_dim);
+        gl.load(static_cast<const T *>(g.dout) + (int64_t)batch * a.q_tokens * out_row + (int64_t)head * a.head_dim, out_row, q0, a.q_tokens, a.head_dim);
+        const int i = q0 + (int)threadIdx.x;
+        const bool in = threadIdx.x < kTile && i < a.q_tokens;
+        const int64_t at = ((int64_t)batch * a.q_heads + head) * a.q_tokens + i;
+        held[0] = in ? g.rows[at] : BIAS ? 0.0f : __builtin_inff();
+        held[1] = in ? g.rows[all + at] : __builtin_inff();
+        held[2] = in ? g.rows[2 * all + at] : 0.0f;
+        if constexpr (BIAS) bl.load(a, k0 - q0 - (kTile - 1) + a.q_tokens - 1);
+    };
+    auto store = [&](int to) {
+        ql.store(tiles[to % kStages<T, D>]);
+        gl.store(tiles[to % kStages<T, D>] + kTileBytes<T, D>);
+        if (threadIdx.x < kTile) {
+#pragma unroll
+            for (int n = 0; n < 3; ++n) rows[to][n][threadIdx.x] = held[n];
+        }
+        if constexpr (BIAS) bl.store(a, column, biases[to]);
+    };
+    if (count > 0) {
+        if constexpr (BIAS) {
+            load_column<T>(a, kv * group, column);
+            __syncthreads();
+        }
+        load(0);
+        store(0);
+        load(1);
+        __syncthreads();
+    }
+    for (int t = 0; t < count; ++t) {
+        const char *const tile = tiles[t % kStages<T, D>];
+        const int q0 = (from + t % per_head) * kTile;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int first = q0 + 32 * n;                  // of 32 queries
+            if (a.causal && first + 31 + offset < mine) continue;      // none of them sees any of the wave's keys
+            f32x16 s = dots<T, D>(tile, 32 * n, own);
+            f32x16 dp = dots<T, D>(tile + kTileBytes<T, D>, 32 * n, val);
+            const float *const b = biases[BIAS ? t & 1 : 0] + kTile - 1 + (j - k0) - 32 * n - 4 * half;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const f32x4 f = *reinterpret_cast<const f32x4 *>(&rows[t & 1][0][32 * n + 8 * c + 4 * half]);
+                const f32x4 e = BIAS ? *reinterpret_cast<const f32x4 *>(&rows[t & 1][1][32 * n + 8 * c + 4 * half]) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                const f32x4 d = *reinterpret_cast<const f32x4 *>(&rows[t & 1][2][32 * n + 8 * c + 4 * half]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float x = s[4 * c + r];
+                    if constexpr (BIAS) x = __builtin_fmaf(x, a.scale, b[-(8 * c + r)]);
+                    s[4 * c + r] = probability<BIAS>(x, scale, f[r], e[r]);
+                    dp[4 * c + r] -= d[r];
+                }
+            }
+            if (mine + 32 > keys || (a.causal && first + offset < mine + 31)) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (j >= keys || (a.causal && j > first + row_of(r, half) + offset)) s[r] = 0.0f;
+            }
+            sums<T, D>(tile + kTileBytes<T, D>, 32 * n, s, dv);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dp[r] *= s[r];
+            sums<T, D>(tile, 32 * n, dp, dk);
+        }
+        if (kStages<T, D> == 1) __syncthreads();
+        if (t + 1 < count) {
+            if constexpr (BIAS) {
+                if ((t + 1) % per_head == 0) {              // the next head's column
+                    __syncthreads();
+                    load_column<T>(a, kv * group + (t + 1) / per_head, column);
+                    __syncthreads();
+                }
+            }
+            store((t + 1) & 1);
+            load(t + 2);
+        }
+        __syncthreads();
+    }
+    if (j >= a.k_tokens) return;
+    store_row<T, D>(dv, 1.0f, static_cast<T *>(g.dv) + batch * g.dv_b + kv * g.dv_h + j * g.dv_t, a.head_dim);
+    T *const to = static_cast<T *>(g.dk) + batch * g.dk_b + kv * g.dk_h + j * g.dk_t;
+    if (g.dk_d == 1) {
+        store_row<T, D>(dk, a.scale, to, a.head_dim);
+    } else {                                                // a head's elements apart, its keys beside each other: 32 of them a store
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int d = 32 * n + row_of(r, half);
+                if (d >= a.head_dim) continue;
+                const float x = dk[n][r] * a.scale;
+                if constexpr (sizeof(T) == 4) to[d * g.dk_d] = x;
+                else to[d * g.dk_d] = (T)bf16_narrow(x);
+            }
+    }
+}
+
+template <typename T, int D>
+void launch_backward(const Attention &a, const Gradients &g, hipStream_t st)
+{
+    const int q_blocks = (a.q_tokens + kBlock - 1) / kBlock, k_blocks = (a.k_tokens + kBlock - 1) / kBlock;
+    const unsigned q_grid = (unsigned)((int64_t)a.batch * a.q_heads * q_blocks), k_grid = (unsigned)((int64_t)a.batch * a.kv_heads * k_blocks);
+    if (q_grid > 0) {
+        if (g.parts) launch(queries_kernel<T, D, true, true>, q_grid, kAttnThreads, 0, st, a, g, q_blocks);
+        else if (a.table) launch(queries_kernel<T, D, true, false>, q_grid, kAttnThreads, 0, st, a, g, q_blocks);
+        else launch(queries_kernel<T, D, false, false>, q_grid, kAttnThreads, 0, st, a, g, q_blocks);
+    }
+    if (k_grid > 0) {
+        if (a.table) launch(keys_kernel<T, D, true>, k_grid, kAttnThreads, 0, st, a, g, k_blocks);
+        else launch(keys_kernel<T, D, false>, k_grid, kAttnThreads, 0, st, a, g, k_blocks);
+    }
+}
+
+template <typename T>
+void attention_backward_of(const Attention &a, const Gradients &g, hipStream_t st)
+{
+    if (a.head_dim <= 32) launch_backward<T, 32>(a, g, st);
+    else if (a.head_dim <= 64) launch_backward<T, 64>(a, g, st);
+    else if (a.head_dim <= 96) launch_backward<T, 96>(a, g, st);
+    else launch_backward<T, 128>(a, g, st);
+}
+
+}  // namespace
+}  // namespace slimfit

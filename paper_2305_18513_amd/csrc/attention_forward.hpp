@@ -1,0 +1,147 @@
+// Attention forward, one pass over the keys:  s = scale q k^T + bias, m = max s, l = sum e^(s - m), out = sum e^(s - m) v / l.
+// A workgroup holds 128 queries of one head, 32 a wave, and goes over tiles of 64 keys and values; maximum, sum and out are kept as
+// they are so far, and taken down by e^(old - new maximum) where a tile raises the maximum.  (s^T lies with a query in each lane, so
+// that the maximum and sum are a lane's own, but for one exchange of the halves.)
+#pragma once
+
+#include "attention.hpp"
+
+namespace slimfit {
+namespace {
+
+template <typename T, int D, bool BIAS>
+__global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2) forward_kernel(Attention a, T *__restrict__ out, float *__restrict__ stats, int blocks)
+{
+    __shared__ __align__(16) char tiles[kStages<T, D>][2 * kTileBytes<T, D>];
+    __shared__ float column[BIAS ? kMostBuckets : 1], biases[2][BIAS ? kDistances : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int heads = a.batch * a.q_heads, bh = (int)(blockIdx.x % (unsigned)heads);
+    const int turn = (int)(blockIdx.x / (unsigned)heads), block = a.causal ? blocks - 1 - turn : turn;      // the longest first
+    const int batch = bh / a.q_heads, head = bh % a.q_heads, kv = head / (a.q_heads / a.kv_heads);
+    const int q0 = block * kBlock, mine = q0 + wave * kOwn, i = mine + (lane & 31);
+    const T *const q = static_cast<const T *>(a.q.at) + batch * a.q.b + head * a.q.h;
+    const T *const k = static_cast<const T *>(a.k.at) + batch * a.k.b + kv * a.k.h;
+    const T *const v = static_cast<const T *>(a.v.at) + batch * a.v.b + kv * a.v.h;
+    const int keys = keys_of(a, batch), count = key_tiles(a, q0, keys);
+    const int seen = seen_by(a, i, keys), all_see = seen_by(a, mine, keys), any_sees = seen_by(a, min(mine + kOwn, a.q_tokens) - 1, keys);
+    const float scale = a.scale * kLog2e;
+
+    Own<T, D> own;
+    own.load(q, a.q.t, mine, a.q_tokens, a.head_dim);
+    f32x16 o[D / 32];
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n) o[n] = zeros16();
+    float top = -__builtin_inff(), total = 0.0f;            // top: of q k^T, or (BIAS) of s
+
+    TileLoad<T, D> kl, vl;
+    BiasLoad bl;
+    auto load = [&](int t) {
+        kl.load(k, a.k.t, t * kTile, keys, a.head_dim);
+        vl.load(v, a.v.t, t * kTile, keys, a.head_dim);
+        if constexpr (BIAS) bl.load(a, t * kTile - q0 - (kBlock - 1) + a.q_tokens - 1);
+    };
+    auto store = [&](int to) {
+        kl.store(tiles[to % kStages<T, D>]);
+        vl.store(tiles[to % kStages<T, D>] + kTileBytes<T, D>);
+        if constexpr (BIAS) bl.store(a, column, biases[to]);
+    };
+    if constexpr (BIAS) {
+        load_column<T>(a, head, column);
+        __syncthreads();
+    }
+    if (count > 0) {
+        load(0);
+        store(0);
+        load(1);
+        __syncthreads();
+    }
+    for (int t = 0; t < count; ++t) {
+        const char *const tile = tiles[t % kStages<T, D>];
+        const int k0 = t * kTile;
+        if (k0 < any_sees) {
+            f32x16 s[2];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                s[n] = dots<T, D>(tile, 32 * n, own);
+                if constexpr (BIAS) {
+                    const float *const b = biases[t & 1] + kBlock - 1 - (i - q0) + 4 * half + 32 * n;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[n][r] = __builtin_fmaf(s[n][r], a.scale, b[8 * (r / 4) + r % 4]);
+                }
+            }
+            if (k0 + kTile > all_see) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (k0 + 32 * n + row_of(r, half) >= seen) s[n][r] = -__builtin_inff();
+            }
+            float high = s[0][0];
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) high = fmaxf(high, s[n][r]);
+            high = fmaxf(top, both_max(high));
+            const float safe = high == -__builtin_inff() ? 0.0f : high;     // no key so far
+            const float by = BIAS ? kLog2e : scale;
+            if (__builtin_amdgcn_ballot_w64(high != top) != 0u) {
+                const float down = __builtin_amdgcn_exp2f((top - safe) * by);
+                total *= down;
+#pragma unroll
+                for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[n][r] *= down;
+                top = high;
+            }
+            const float less = -safe * scale;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    // (with a bias s may be the type's lowest value, which times log2 e is none: the difference comes first)
+                    s[n][r] = __builtin_amdgcn_exp2f(BIAS ? (s[n][r] - safe) * kLog2e : __builtin_fmaf(s[n][r], scale, less));
+                    total += s[n][r];
+                }
+                sums<T, D>(tile + kTileBytes<T, D>, 32 * n, s[n], o);
+            }
+        }
+        if (kStages<T, D> == 1) __syncthreads();
+        if (t + 1 < count) {
+            store((t + 1) & 1);
+            load(t + 2);
+        }
+        __syncthreads();
+    }
+    total = both_sum(total);
+    if (i < a.q_tokens) {
+        const int64_t row = ((int64_t)batch * a.q_tokens + i) * a.q_heads + head;
+        store_row<T, D>(o, total > 0.0f ? 1.0f / total : 0.0f, out + row * a.head_dim, a.head_dim);
+        if (half == 0) {
+            const int64_t at = (int64_t)bh * a.q_tokens + i;
+            stats[2 * at] = BIAS ? top : top * a.scale;
+            stats[2 * at + 1] = total;
+        }
+    }
+}
+
+template <typename T, int D>
+void launch_forward(const Attention &a, T *out, float *stats, hipStream_t st)
+{
+    const int blocks = (a.q_tokens + kBlock - 1) / kBlock;
+    const unsigned grid = (unsigned)((int64_t)a.batch * a.q_heads * blocks);
+    if (a.table) launch(forward_kernel<T, D, true>, grid, kAttnThreads, 0, st, a, out, stats, blocks);
+    else launch(forward_kernel<T, D, false>, grid, kAttnThreads, 0, st, a, out, stats, blocks);
+}
+
+template <typename T>
+void attention_forward_of(const Attention &a, void *out, float *stats, hipStream_t st)
+{
+    T *o = static_cast<T *>(out);
+    if (a.head_dim <= 32) launch_forward<T, 32>(a, o, stats, st);
+    else if (a.head_dim <= 64) launch_forward<T, 64>(a, o, stats, st);
+    else if (a.head_dim <= 96) launch_forward<T, 96>(a, o, stats, st);
+    else launch_forward<T, 128>(a, o, stats, st);
+}
+
+}  // namespace
+}  // namespace slimfit

@@ -1,0 +1,382 @@
+"""Attention's forward and backward pass and its position bias on the GPU against the formulas in 64 bits, element by element, within
+bounds that follow from the number of roundings on each way."""
+import math
+
+import pytest
+import torch
+
+from paper_2305_18513_amd import binding as sf
+from tests.gpu_util import require_gpu
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24                                             # a rounding to fp32
+UB = 2.0 ** -8                                             # to bf16
+
+
+def inputs(B, Tq, Tk, Hq, Hk, D, dtype, layout, seed=0, columns=False, spread=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rand = lambda *s: (torch.randn(*s, generator=g, device="cuda") * spread).to(dtype)  # noqa: E731
+    if layout == sf.HEADS_APART:
+        return rand(B, Hq, Tq, D), rand(B, Hk, D, Tk), rand(B, Hk, Tk, D), rand(B, Tq, Hq, D)
+    if columns:                                            # columns of rows that hold more
+        rq, rk = rand(B, Tq, Hq + 3, D), rand(B, Tk, 2 * Hk + 1, D)
+        return rq[:, :, 1 : Hq + 1], rk[:, :, :Hk], rk[:, :, Hk + 1 :], rand(B, Tq, Hq, D)
+    return rand(B, Tq, Hq, D), rand(B, Tk, Hk, D), rand(B, Tk, Hk, D), rand(B, Tq, Hq, D)
+
+
+def rows_of(t, layout, keys=False):
+    """(B, heads, tokens, D) in 64 bits."""
+    if layout == sf.HEADS_APART:
+        return t.double().transpose(2, 3) if keys else t.double()
+    return t.double().transpose(1, 2)
+
+
+class Reference:
+    def __init__(self, q, k, v, do, layout, scale, causal, lengths, table, bucket_of):
+        self.low = q.dtype == torch.bfloat16
+        q, k, v = rows_of(q, layout), rows_of(k, layout, True), rows_of(v, layout)
+        B, Hq, Tq, D = q.shape
+        Hk, Tk = k.shape[1:3]
+        self.group, self.sizes = Hq // Hk, (B, Tq, Tk, Hq, Hk, D)
+        if lengths is not None:                            # what is past a sequence's end is not looked at
+            gone = (torch.arange(Tk, device="cuda")[None] >= lengths[:, None])[:, None, :, None]
+            k, v = k.masked_fill(gone, 0.0), v.masked_fill(gone, 0.0)
+        self.q, self.scale = q, scale
+        self.k, self.v = k.repeat_interleave(self.group, 1), v.repeat_interleave(self.group, 1)
+        i, j = torch.arange(Tq, device="cuda")[:, None], torch.arange(Tk, device="cuda")[None]
+        s = q @ self.k.transpose(2, 3) * scale
+        self.size = q.abs() @ self.k.abs().transpose(2, 3) * scale                # of s's terms
+        self.at = None
+        if table is not None:
+            self.buckets = table.shape[0]
+            self.at = bucket_of.long()[j - i + Tq - 1]
+            inside = (self.at >= 0) & (self.at < self.buckets)
+            bias = torch.where(inside[None], table.double().t()[:, self.at.clamp(0, self.buckets - 1)], 0.0)
+            s = s + bias
+            self.size = self.size + torch.where(torch.isinf(bias), 0.0, bias.abs())
+            self.at = torch.where(inside, self.at, -1)
+        seen = torch.ones(B, 1, Tq, Tk, dtype=torch.bool, device="cuda")
+        if causal:
+            seen = seen & (j - i <= Tk - Tq)
+        if lengths is not None:
+            seen = seen & (j < lengths[:, None, None, None])
+        s = s.masked_fill(~seen, -math.inf)
+        self.top = s.amax(-1, keepdim=True) if Tk else s.new_full((B, Hq, Tq, 1), -math.inf)
+        some = self.top > -math.inf
+        e = torch.exp(s - torch.where(some, self.top, 0.0))
+        self.total = e.sum(-1, keepdim=True)
+        self.p = torch.where(some, e / torch.where(some, self.total, 1.0), 0.0)
+        self.out = self.p @ self.v
+        # a p's relative error: s's (D products and sums, scale, bias) in it and in the maximum, the exponent's own roundings (a
+        # difference, a product, the constant's half step), the exponential's 2, the sum over the keys, the division.  l's has all of that too.
+        live = s > -math.inf
+        off = torch.where(live, self.size, 0.0) * (D + 6) * U + torch.where(live, s - self.top, 0.0).abs() * 4 * U
+        off = off + torch.where(some, self.top, 0.0).abs().clamp(max=1e4) * 4 * U + 4 * U
+        worst = off.amax(-1, keepdim=True) if Tk else off.new_zeros(B, Hq, Tq, 1)
+        self.p_off = 2 * (off + worst) + (Tk + 8) * U
+        self.top_off = worst
+        self.total_off = 2 * worst + (Tk + 4) * U
+        if do is not None:
+            self.backward(do.double().transpose(1, 2))
+
+    def rounded(self, off, value):
+        """With the result's own rounding, and what lies below the type's normal numbers."""
+        return off * (1 + UB) + UB * value.abs() + 2.0 ** -120 if self.low else off + U * value.abs() + 2.0 ** -120
+
+    def product_off(self):
+        return UB if self.low else 0.0                     # of an operand that is rounded before a product
+
+    def out_off(self):
+        Tk = self.sizes[2]
+        return ((self.p_off + self.product_off() + (Tk + 4) * U) * self.p) @ self.v.abs()
+
+    def backward(self, do):
+        B, Tq, Tk, Hq, Hk, D = self.sizes
+        part = self.product_off()
+        dp, size = do @ self.v.transpose(2, 3), do.abs() @ self.v.abs().transpose(2, 3)
+        delta = (do * self.out).sum(-1, keepdim=True)
+        o_off = self.rounded(self.out_off(), self.out)
+        delta_off = (do.abs() * (o_off + (D + 2) * U * self.out.abs())).sum(-1, keepdim=True)
+        ds = self.p * (dp - delta)
+        ds_off = self.p_off * ds.abs() + self.p * (1 + self.p_off) * ((D + 2) * U * size + delta_off + 2 * U * (dp.abs() + delta.abs())) + 2 * U * ds.abs()
+        self.ds, used = ds, ds_off + part * (ds.abs() + ds_off)
+        self.dq, dq_off = ds @ self.k * self.scale, (used + (Tk + 4) * U * ds.abs()) @ self.k.abs() * self.scale
+        n = Tq * self.group
+        share = lambda t: t.view(B, Hk, self.group, Tk, D).sum(2)  # noqa: E731
+        self.dk = share(ds.transpose(2, 3) @ self.q) * self.scale
+        dk_off = share((used + (n + 4) * U * ds.abs()).transpose(2, 3) @ self.q.abs()) * self.scale
+        self.dv = share(self.p.transpose(2, 3) @ do)
+        dv_off = share((self.p * (self.p_off + part + (n + 4) * U)).transpose(2, 3) @ do.abs())
+        self.offs = dict(dq=self.rounded(dq_off, self.dq), dk=self.rounded(dk_off, self.dk), dv=self.rounded(dv_off, self.dv))
+        if self.at is not None:
+            add = lambda t: torch.stack([(t * (self.at == b)).sum((0, 2, 3)) for b in range(self.buckets)])  # noqa: E731
+            self.dtable = add(ds)
+            self.offs["dtable"] = self.rounded(add(ds_off + 40 * U * ds.abs()), self.dtable)
+
+
+def within(got, want, off, what):
+    bad = (got - want).abs() > off
+    assert not bool(bad.any()) and not bool(torch.isnan(got).any()), "%s: %d of %d, worst %.3g of its bound" % (
+        what, int(bad.sum()), bad.numel(), float(((got - want).abs() / off).max()))
+
+
+class Call:
+    """One forward and backward pass with outputs between sentinels (77), as columns of wider rows where the operands are."""
+
+    def __init__(self, q, k, v, do, layout, scale, causal=False, lengths=None, table=None, bucket_of=None, columns=False):
+        self.args = (q, k, v, layout, scale, causal, lengths, table, bucket_of)
+        self.do, self.kept = do, []
+        self.out = self.new(do.shape, q.dtype)
+        B, Tq, Hq, D = do.shape
+        self.stats = self.new((B, Hq, Tq, 2), torch.float32)
+        if columns:
+            B, Tk, Hk, D = k.shape
+            self.wide_q, self.wide_k = (torch.full(s, 77.0, dtype=q.dtype, device="cuda") for s in ((B, Tq, Hq + 3, D), (B, Tk, 2 * Hk + 1, D)))
+            self.dq, self.dk, self.dv = self.wide_q[:, :, 1 : Hq + 1], self.wide_k[:, :, :Hk], self.wide_k[:, :, Hk + 1 :]
+        else:
+            self.dq, self.dk, self.dv = (self.new(t.shape, t.dtype) for t in (q, k, v))
+        self.dtable = None if table is None else self.new(table.shape, table.dtype)
+        self.columns = columns
+
+    def new(self, shape, dtype):
+        n = math.prod(shape)
+        raw = torch.full((n + 64,), 77.0, dtype=dtype, device="cuda")
+        self.kept.append((raw, n))
+        return raw[32 : 32 + n].view(shape) if n else torch.empty(shape, dtype=dtype, device="cuda")
+
+    def forward(self, **more):
+        sf.attention_forward(*self.args, self.out, self.stats, **more)
+        return self
+
+    def backward(self, **more):
+        sf.attention_backward(self.do, *self.args, self.out, self.stats, self.dq, self.dk, self.dv, self.dtable, **more)
+        return self
+
+    def outputs(self):
+        return [t for t in (self.out, self.stats, self.dq, self.dk, self.dv, self.dtable) if t is not None]
+
+    def check(self):
+        q, k, v, layout, scale, causal, lengths, table, bucket_of = self.args
+        r = Reference(q, k, v, self.do, layout, scale, causal, lengths, table, bucket_of)
+        out = rows_of(self.out, sf.HEADS_ROWS)
+        within(out, r.out, r.rounded(r.out_off(), r.out), "out")
+        top, total = self.stats[..., :1].double(), self.stats[..., 1:].double()
+        none = r.top == -math.inf
+        assert torch.equal(top == -math.inf, none) and bool((total[none] == 0).all()) and bool((out[none.expand_as(out)] == 0).all())
+        within(torch.where(none, 0.0, top), torch.where(none, 0.0, r.top), r.top_off + U * torch.where(none, 0.0, r.top).abs(), "maximum")
+        within(total, r.total, r.total_off * r.total + 1e-40, "sum")
+        within(rows_of(self.dq, layout), r.dq, r.offs["dq"], "dq")
+        within(rows_of(self.dk, layout, True), r.dk, r.offs["dk"], "dk")
+        within(rows_of(self.dv, layout), r.dv, r.offs["dv"], "dv")
+        if self.dtable is not None:
+            within(self.dtable.double(), r.dtable, r.offs["dtable"], "dtable")
+        for raw, n in self.kept:
+            assert bool((raw[:32] == 77).all()) and bool((raw[32 + n :] == 77).all())
+        if self.columns:
+            Hq, Hk = q.shape[2], k.shape[2]
+            assert bool((self.wide_q[:, :, [0, Hq + 1, Hq + 2]] == 77).all()) and bool((self.wide_k[:, :, Hk] == 77).all())
+        return r
+
+
+SHAPES = [(1, 1, 1, 1, 1, 8), (2, 1, 70, 4, 2, 64), (2, 33, 65, 4, 1, 40), (1, 128, 128, 2, 2, 32), (3, 129, 257, 6, 3, 80), (2, 64, 200, 3, 3, 96),
+          (1, 300, 300, 2, 1, 128), (2, 200, 77, 2, 2, 64), (5, 7, 3, 2, 1, 16), (1, 31, 513, 7, 1, 128), (2, 197, 197, 2, 2, 64)]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("causal", [False, True], ids=["all", "causal"])
+@pytest.mark.parametrize("layout,columns", [(sf.HEADS_ROWS, False), (sf.HEADS_ROWS, True), (sf.HEADS_APART, False)], ids=["rows", "columns", "apart"])
+@pytest.mark.parametrize("bias", [False, True], ids=["plain", "bias"])
+def test_against_64_bits(shape, dtype, causal, layout, columns, bias):
+    require_gpu()
+    B, Tq, Tk, Hq, Hk, D = shape
+    q, k, v, do = inputs(*shape, dtype, layout, seed=Tq + Tk, columns=columns)
+    lengths = torch.tensor([(0, Tk + 9, Tk // 2, 1, -3)[b % 5] for b in range(B)], dtype=torch.int32, device="cuda") if columns or bias else None
+    table = of = None
+    if bias:
+        table = torch.randn(9, Hq, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(dtype)
+        of = sf.distance_buckets(Tq, Tk, 9, 40, both_ways=not causal)
+    Call(q, k, v, do, layout, D ** -0.5, causal, lengths, table, of, columns).forward().backward().check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_odd_head_sizes(dtype):
+    require_gpu()
+    for D in ((4, 12, 36, 68, 100, 124) if dtype == torch.float32 else (8, 24, 56, 72, 104, 120)):
+        q, k, v, do = inputs(2, 70, 90, 2, 1, D, dtype, sf.HEADS_ROWS, seed=D)
+        Call(q, k, v, do, sf.HEADS_ROWS, 0.3, True).forward().backward().check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_large_logits(dtype):
+    require_gpu()
+    q, k, v, do = inputs(2, 100, 130, 2, 2, 64, dtype, sf.HEADS_ROWS, seed=4, spread=3.0)
+    Call(q, k, v, do, sf.HEADS_ROWS, 0.5).forward().backward().check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("layout", [sf.HEADS_ROWS, sf.HEADS_APART])
+def test_what_is_past_the_lengths_is_not_looked_at(dtype, layout):
+    require_gpu()
+    shape = (3, 50, 150, 4, 2, 64)
+    q, k, v, do = inputs(*shape, dtype, layout, seed=2)
+    lengths = torch.tensor([70, 0, 128], dtype=torch.int32, device="cuda")
+    table, of = torch.randn(5, 4, device="cuda").to(dtype), sf.distance_buckets(50, 150, 5, 30)
+    clean = Call(q, k, v, do, layout, 0.2, False, lengths, table, of).forward().backward()
+    clean.check()
+    k, v = k.clone(), v.clone()
+    for b, n in enumerate(lengths.tolist()):
+        for bad, at in ((float("nan"), n), (float("inf"), n + 7), (-float("inf"), n + 1)):
+            if layout == sf.HEADS_ROWS:
+                k[b, at:, :, ::3] = bad
+                v[b, at:] = bad
+            else:
+                k[b, :, ::3, at:] = bad
+                v[b, :, at:] = bad
+    spoilt = Call(q, k, v, do, layout, 0.2, False, lengths, table, of).forward().backward()
+    assert all(torch.equal(a, b) for a, b in zip(clean.outputs(), spoilt.outputs()))
+    past = torch.arange(150, device="cuda")[None] >= lengths[:, None]
+    dk = rows_of(spoilt.dk, layout, True).transpose(1, 2)
+    dv = rows_of(spoilt.dv, layout).transpose(1, 2)
+    assert bool((dk[past] == 0).all()) and bool((dv[past] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["infinite", "lowest", "all infinite", "all lowest", "outside"])
+def test_biases_that_mask(dtype, kind):
+    """-infinity takes pairs out, as a mask does; the type's lowest value counts where a query has nothing else, and the buckets
+    outside of the table add nothing."""
+    require_gpu()
+    Tq, Tk = 100, 140
+    q, k, v, do = inputs(2, Tq, Tk, 2, 2, 32, dtype, sf.HEADS_ROWS, seed=3)
+    table = torch.randn(4, 2, generator=torch.Generator(device="cuda").manual_seed(8), device="cuda").to(dtype)
+    low = -math.inf if "infinite" in kind else torch.finfo(dtype).min
+    of = sf.distance_buckets(Tq, Tk, 4, 20)
+    if kind == "outside":
+        of[::3] = -1
+        of[1::7] = 4
+        of[2::11] = 2 ** 31 - 1
+    elif kind.startswith("all"):
+        table[:, 0] = low                                  # the first head sees nothing, or everything alike
+    else:
+        table[1] = low
+    call = Call(q, k, v, do, sf.HEADS_ROWS, 0.2, True, None, table, of).forward().backward()
+    r = call.check()
+    if kind == "all lowest":                               # a query's keys count alike: logits below half a step of the lowest value vanish
+        assert float((call.stats[:, 0, :, 1].double() - torch.arange(Tk - Tq + 1, Tk + 1, device="cuda")).abs().max()) == 0.0
+    if kind == "all infinite":
+        assert bool((call.out[:, :, 0] == 0).all()) and bool((call.dq[:, :, 0] == 0).all()) and bool((r.total[:, 0] == 0).all())
+
+
+def test_no_keys_no_queries_no_batch():
+    require_gpu()
+    for dtype in (torch.float32, torch.bfloat16):
+        for B, Tq, Tk in ((2, 5, 0), (2, 0, 5), (0, 5, 5)):
+            for layout in (sf.HEADS_ROWS, sf.HEADS_APART):
+                q, k, v, do = inputs(B, Tq, Tk, 4, 2, 16, dtype, layout)
+                table, of = torch.randn(3, 4, device="cuda").to(dtype), torch.zeros(max(0, Tq + Tk - 1), dtype=torch.int32, device="cuda")
+                c = Call(q, k, v, do, layout, 0.5, True, None, table, of).forward().backward()
+                torch.cuda.synchronize()
+                assert all(bool((t == 0).all()) for t in (c.out, c.dq, c.dk, c.dv, c.dtable))
+                assert bool((c.stats[..., 0] == -math.inf).all()) and bool((c.stats[..., 1] == 0).all())
+
+
+def test_the_same_call_gives_the_same_bits_on_any_stream():
+    require_gpu()
+    for dtype in (torch.float32, torch.bfloat16):
+        q, k, v, do = inputs(3, 300, 280, 6, 2, 64, dtype, sf.HEADS_APART, seed=5)
+        table, of = torch.randn(12, 6, device="cuda").to(dtype), sf.distance_buckets(300, 280, 12, 60)
+        lengths = torch.tensor([280, 100, 7], dtype=torch.int32, device="cuda")
+        calls = [Call(q, k, v, do, sf.HEADS_APART, 0.125, False, lengths, table, of) for _ in range(3)]
+        torch.cuda.synchronize()
+        calls[0].forward().backward()
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        need = [sf.attention_workspace(dtype, sf.HEADS_APART, 3, 300, 280, 6, 2, 64, True, back) for back in (False, True)]
+        held = [[torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda") for n in need] for _ in range(2)]      # NaN, wherever it is read
+        torch.cuda.synchronize()
+        for c, s, ws in zip(calls[1:], streams, held):     # side by side
+            c.forward(workspace=ws[0], stream=s.cuda_stream)
+        for c, s, ws in zip(calls[1:], streams, held):
+            c.backward(workspace=ws[1], stream=s.cuda_stream)
+        torch.cuda.synchronize()
+        for c in calls[1:]:
+            assert all(torch.equal(a, b) for a, b in zip(calls[0].outputs(), c.outputs()))
+        with pytest.raises(ValueError):                    # whose workspace would be freed too early
+            calls[0].backward(stream=streams[0].cuda_stream)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_captured_and_replayed(dtype):
+    require_gpu()
+    shape = (2, 150, 170, 4, 2, 64)
+    table, of = torch.randn(12, 4, device="cuda").to(dtype), sf.distance_buckets(150, 170, 12, 60)
+    lengths = torch.tensor([170, 90], dtype=torch.int32, device="cuda")
+    q, k, v, do = inputs(*shape, dtype, sf.HEADS_APART, seed=0)
+    c = Call(q, k, v, do, sf.HEADS_APART, 0.125, True, lengths, table, of)
+    e = Call(q, k, v, do, sf.HEADS_APART, 0.125, True, lengths, table, of)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.forward().backward()
+    for seed in (1, 2, 3):
+        for to, now in zip((q, k, v, do), inputs(*shape, dtype, sf.HEADS_APART, seed=seed)):
+            to.copy_(now)
+        lengths.copy_(torch.tensor([170 - seed, 40 * seed], dtype=torch.int32))
+        table.mul_(0.9)
+        e.forward().backward()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(c.outputs(), e.outputs()))
+    c.check()
+
+
+def test_gradients_against_differences():
+    """Along a random direction the loss <out, dout> of the kernel's own forward pass changes as the gradients say.  A central difference
+    of step h is off by h^2 / 6 of the third derivative (its terms are of the loss's size times the direction's to the third: with
+    h = 1/16 below 2e-3 of them) and by the loss's own rounding over h: 2^-24 times 16 times the square root of its terms."""
+    require_gpu()
+    q, k, v, do = inputs(2, 40, 60, 4, 2, 32, torch.float32, sf.HEADS_ROWS, seed=6)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    table, of = torch.randn(6, 4, generator=g, device="cuda"), sf.distance_buckets(40, 60, 6, 20)
+    base = Call(q, k, v, do, sf.HEADS_ROWS, 32 ** -0.5, False, None, table, of).forward().backward()
+    h = 1.0 / 16
+    for name, at, grad in (("q", q, base.dq), ("k", k, base.dk), ("v", v, base.dv), ("table", table, base.dtable)):
+        way = torch.randn(at.shape, generator=g, device="cuda")
+        way /= way.norm()
+
+        def loss(sign):
+            new = {n: t + sign * h * way if n == name else t for n, t in (("q", q), ("k", k), ("v", v), ("table", table))}
+            c = Call(new["q"], new["k"], new["v"], do, sf.HEADS_ROWS, 32 ** -0.5, False, None, new["table"], of).forward()
+            return (c.out.double() * do.double()).sum()
+
+        got, want = float((loss(1) - loss(-1)) / (2 * h)), float((grad.double() * way.double()).sum())
+        size = float(grad.double().norm())                 # a unit direction's change is at most that
+        assert abs(got - want) <= 2e-3 * size + 16 * U * math.sqrt(do.numel()), name
+
+
+def test_offsets_past_32_bits():
+    """Keys and values as columns of rows so long that the last lie past 2^32 elements."""
+    require_gpu()
+    row, Tk, D = 1 << 20, 4200, 64
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB of GPU memory")
+    wide, dwide = (torch.empty(1, Tk, row // D, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q, k, v, do = inputs(1, 70, Tk, 2, 2, D, torch.bfloat16, sf.HEADS_ROWS, seed=9)
+    wide[:, :, 5:7], wide[:, :, -2:] = k, v
+    a = Call(q, k, v, do, sf.HEADS_ROWS, 0.125).forward().backward()
+    b = Call(q, wide[:, :, 5:7], wide[:, :, -2:], do, sf.HEADS_ROWS, 0.125)
+    b.dk, b.dv = dwide[:, :, 3:5], dwide[:, :, -2:]
+    b.forward().backward()
+    assert all(torch.equal(x, y) for x, y in zip(a.outputs(), b.outputs()))
+    a.check()
+
+
+def test_many_tokens():
+    require_gpu()
+    for dtype, T in ((torch.bfloat16, 4097), (torch.float32, 2500)):
+        q, k, v, do = inputs(1, T, T, 2, 1, 64, dtype, sf.HEADS_APART, seed=T)
+        table, of = torch.randn(32, 2, device="cuda").to(dtype), sf.distance_buckets(T, T, 32, 500, False)
+        Call(q, k, v, do, sf.HEADS_APART, 0.125, True, None, table, of).forward().backward().check()
