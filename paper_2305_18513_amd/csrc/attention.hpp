@@ -76,9 +76,21 @@ __device__ __forceinline__ u32x4 load16(Buffer b, int at)
 constexpr int kNowhere = -16;                // an offset past every descriptor's end
 
 template <typename T> constexpr int kPerVector = 16 / (int)sizeof(T);
-// a row of a tile in LDS: 16 bytes more than it holds, so that rows' vectors begin four banks apart
-template <typename T, int D> constexpr int kPitch = D * (int)sizeof(T) + 16;
+// A tile's rows in LDS.  fp32: 16 bytes more than a row holds, so that rows' vectors begin four banks apart.  bf16: rows of 4, 8 or 16
+// vectors whose places are exchanged by the row (`turn_of`): sixteen rows' vectors of the same number, which `dots` reads at a
+// time, lie in different banks, and so do four rows' of four beside each other, which `across` reads (with the padding instead
+// half of the reads' time went into conflicts, 52 of 104 million cycles of 2048 x 2048 by 128 and 256 heads).
+template <typename T, int D> constexpr int kRowVectors = D / kPerVector<T> == 12 ? 16 : D / kPerVector<T>;
+template <typename T, int D> constexpr int kPitch = sizeof(T) == 4 ? D * 4 + 16 : kRowVectors<T, D> * 16;
 template <typename T, int D> constexpr int kTileBytes = kTile * kPitch<T, D>;
+template <typename T, int D>
+__device__ __forceinline__ int turn_of(int row)
+{
+    if constexpr (sizeof(T) == 4) return 0;
+    else if constexpr (kRowVectors<T, D> == 16) return ((row & 3) << 2) | ((row >> 2) & 3);
+    else if constexpr (kRowVectors<T, D> == 8) return ((row & 2) << 1) | ((row >> 2) & 3);
+    else return (row >> 2) & 3;
+}
 // two stages of LDS where they fit, so that a tile is laid down while the one before it is read
 template <typename T, int D> constexpr int kStages = kTileBytes<T, D> <= 20 * 1024 ? 2 : 1;
 
@@ -111,7 +123,7 @@ struct TileLoad {
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             const int n = (int)threadIdx.x + i * kAttnThreads, r = n / VECTORS, c = n % VECTORS;
-            *reinterpret_cast<u32x4 *>(lds + r * kPitch<T, D> + c * 16) = held[i];
+            *reinterpret_cast<u32x4 *>(lds + r * kPitch<T, D> + (c ^ turn_of<T, D>(r)) * 16) = held[i];
         }
     }
 };
@@ -131,6 +143,12 @@ struct Own {
             const int n = 2 * c + (lane >> 5);
             x[c] = load16(b, n * kPerVector<T> < dim ? r * ((int)row * (int)sizeof(T)) + n * 16 : kNowhere);
         }
+    }
+    // Waits for the rows here.  Left to their first use, inside the loop over tiles, the wait would be for the tiles' loads too.
+    __device__ __forceinline__ void arrive()
+    {
+#pragma unroll
+        for (int c = 0; c < VECTORS; ++c) asm volatile("" : "+v"(x[c]));
     }
 };
 
@@ -162,19 +180,19 @@ template <typename T, int D>
 __device__ __forceinline__ f32x16 dots(const char *tile, int first, const Own<T, D> &own)
 {
     const int lane = threadIdx.x & 63;
-    const char *at = tile + (first + (lane & 31)) * kPitch<T, D> + (lane >> 5) * 16;
+    const char *at = tile + (first + (lane & 31)) * kPitch<T, D>;
+    const int turn = turn_of<T, D>(lane & 31);
     f32x16 s = zeros16();
 #pragma unroll
-    for (int c = 0; c < Own<T, D>::VECTORS; ++c) s = multiply16<T>(*reinterpret_cast<const u32x4 *>(at + c * 32), own.x[c], s);
+    for (int c = 0; c < Own<T, D>::VECTORS; ++c) s = multiply16<T>(*reinterpret_cast<const u32x4 *>(at + ((2 * c + (lane >> 5)) ^ turn) * 16), own.x[c], s);
     return s;
 }
 
 typedef __attribute__((address_space(3))) s16x4 *LdsVector;
-template <int BYTES>
-__device__ __forceinline__ bf16x8 across(const char *at)          // four rows' elements of a column, and those 8 rows (BYTES) on
+__device__ __forceinline__ bf16x8 across(const char *at, const char *and_at)          // four rows' elements of a column, twice
 {
     const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsVector)(at));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsVector)(at + BYTES));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsVector)(and_at));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
@@ -185,14 +203,17 @@ template <typename T, int D> __device__ __forceinline__ void sums(const char *ti
     const int lane = threadIdx.x & 63, half = lane >> 5;
     constexpr int P = kPitch<T, D>;
     if constexpr (sizeof(T) == 2) {
-        const char *at = tile + (first + 4 * half + (lane & 15) / 4) * P + (16 * ((lane >> 4) & 1) + (lane & 3) * 4) * 2;
+        const int row = 4 * half + (lane & 15) / 4, vector = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), turn = turn_of<T, D>(row);
+        const char *at = tile + (first + row) * P + (lane & 1) * 8;      // (8 rows on, the turn is another by 2)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const u32x4 b = {bf16_narrow2(x[8 * c], x[8 * c + 1]), bf16_narrow2(x[8 * c + 2], x[8 * c + 3]), bf16_narrow2(x[8 * c + 4], x[8 * c + 5]),
                              bf16_narrow2(x[8 * c + 6], x[8 * c + 7])};
 #pragma unroll
             for (int i = 0; i < D / 32; ++i)
-                out[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(across<8 * P>(at + 16 * c * P + i * 64), __builtin_bit_cast(bf16x8, b), out[i], 0, 0, 0);
+                out[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    across(at + 16 * c * P + ((4 * i + vector) ^ turn) * 16, at + (16 * c + 8) * P + ((4 * i + vector) ^ turn ^ 2) * 16),
+                    __builtin_bit_cast(bf16x8, b), out[i], 0, 0, 0);
         }
     } else {
         const char *at = tile + (first + 4 * half) * P + (lane & 31) * 4;

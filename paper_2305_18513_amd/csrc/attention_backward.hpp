@@ -101,6 +101,8 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
     if (count > 0) {
         load(0);
         store(0);
+        own.arrive();
+        grad.arrive();
         load(1);
         __syncthreads();
     }
@@ -223,6 +225,8 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > 128 ? 1 : 2) key
         }
         load(0);
         store(0);
+        own.arrive();
+        val.arrive();
         load(1);
         __syncthreads();
     }

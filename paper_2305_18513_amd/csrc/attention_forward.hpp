@@ -31,7 +31,10 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
     f32x16 o[D / 32];
 #pragma unroll
     for (int n = 0; n < D / 32; ++n) o[n] = zeros16();
-    float top = -__builtin_inff(), total = 0.0f;            // top: of q k^T, or (BIAS) of s
+    // Of q k^T, or (BIAS) of s: the maximum so far, and what the exponentials are taken against.  That follows only where the maximum has
+    // risen by 2^8 and more: e^(s - base) and its sums have room for that, and out is rarely taken down.
+    float top = -__builtin_inff(), base = -__builtin_inff(), total = 0.0f;
+    const float by = BIAS ? kLog2e : scale, room = 8.0f / by;
 
     TileLoad<T, D> kl, vl;
     BiasLoad bl;
@@ -52,6 +55,7 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
     if (count > 0) {
         load(0);
         store(0);
+        own.arrive();
         load(1);
         __syncthreads();
     }
@@ -81,19 +85,17 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
             for (int n = 0; n < 2; ++n)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) high = fmaxf(high, s[n][r]);
-            high = fmaxf(top, both_max(high));
-            const float safe = high == -__builtin_inff() ? 0.0f : high;     // no key so far
-            const float by = BIAS ? kLog2e : scale;
-            if (__builtin_amdgcn_ballot_w64(high != top) != 0u) {
-                const float down = __builtin_amdgcn_exp2f((top - safe) * by);
+            top = fmaxf(top, both_max(high));
+            if (__builtin_amdgcn_ballot_w64(top > base + room) != 0u) {
+                const float down = __builtin_amdgcn_exp2f((base - (top == -__builtin_inff() ? 0.0f : top)) * by);     // (no key so far: 0 of 0)
                 total *= down;
 #pragma unroll
                 for (int n = 0; n < D / 32; ++n)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) o[n][r] *= down;
-                top = high;
+                base = top;
             }
-            const float less = -safe * scale;
+            const float safe = base == -__builtin_inff() ? 0.0f : base, less = -safe * scale;
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
 #pragma unroll
@@ -113,9 +115,11 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
         __syncthreads();
     }
     total = both_sum(total);
+    const float inverse = total > 0.0f ? 1.0f / total : 0.0f;
+    if (total > 0.0f) total *= __builtin_amdgcn_exp2f((base - top) * by);       // against the maximum itself, for the backward pass
     if (i < a.q_tokens) {
         const int64_t row = ((int64_t)batch * a.q_tokens + i) * a.q_heads + head;
-        store_row<T, D>(o, total > 0.0f ? 1.0f / total : 0.0f, out + row * a.head_dim, a.head_dim);
+        store_row<T, D>(o, inverse, out + row * a.head_dim, a.head_dim);
         if (half == 0) {
             const int64_t at = (int64_t)bh * a.q_tokens + i;
             stats[2 * at] = BIAS ? top : top * a.scale;

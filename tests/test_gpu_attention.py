@@ -269,6 +269,20 @@ def test_biases_that_mask(dtype, kind):
         assert bool((call.out[:, :, 0] == 0).all()) and bool((call.dq[:, :, 0] == 0).all()) and bool((r.total[:, 0] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_first_keys_that_are_not_seen(dtype):
+    """Some queries of a wave see nothing of the first tiles, and what they see later is 1000 lower than what their neighbours saw."""
+    require_gpu()
+    Tq, Tk = 64, 320
+    q, k, v, do = inputs(1, Tq, Tk, 2, 2, 64, dtype, sf.HEADS_ROWS, seed=12)
+    table = torch.tensor([[0.0, 2.0], [-math.inf, -math.inf], [-1000.0, -900.0]], device="cuda").to(dtype)
+    far = torch.arange(1 - Tq, Tk, device="cuda")
+    of = torch.where(far >= 200, 2, torch.where(far >= -20, 1, 0)).to(torch.int32)
+    call = Call(q, k, v, do, sf.HEADS_ROWS, 0.125, False, None, table, of).forward().backward()
+    r = call.check()
+    assert bool((r.top[0, 0, :20] < -900).all()) and bool((r.top[0, 0, 21:] > -10).all())
+
+
 def test_no_keys_no_queries_no_batch():
     require_gpu()
     for dtype in (torch.float32, torch.bfloat16):
