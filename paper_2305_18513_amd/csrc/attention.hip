@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(kAttnThreads) distances_kernel(Attention a, co
         const int keys = keys_of(a, b);
         const float *const of = parts + ((int64_t)b * a.q_heads + head) * blocks * kAttnWaves * part_row;
         for (int block = 0; block < blocks; ++block) {
-            const int written = (key_tiles(a, block * kBlock, keys) + 1) * kTile;
+            const int written = key_tiles(a, block * kBlock, keys) * kTile + kOwn;
 #pragma unroll
             for (int w = 0; w < kAttnWaves; ++w) {
                 const int place = at - (a.q_tokens - 1) + block * kBlock + w * kOwn + kOwn - 1;

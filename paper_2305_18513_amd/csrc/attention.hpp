@@ -62,6 +62,30 @@ __device__ __forceinline__ int key_tiles(const Attention &a, int q0, int keys)
     return (seen_by(a, min(q0 + kBlock, a.q_tokens) - 1, keys) + kTile - 1) / kTile;
 }
 
+// Workgroups go to the eight XCDs in turn, and each has its own L2: the work of one pair of sequence and key head, whose `each` times
+// `blocks` workgroups read the same keys and values (or queries), stays on one.  There the pairs go one after another or, where blocks
+// differ in length (causal), the first block of all of them, then the second, so that what is left at the end is short.
+struct Place {
+    int unit, block, in;
+    __device__ __forceinline__ Place(int units, int blocks, int each, bool by_block)
+    {
+        const int b = (int)blockIdx.x, whole = units / 8, first = whole * 8 * blocks * each;
+        int n = b / 8, xcd = b % 8, here = whole, step = 8, base = 0;
+        if (b >= first) {                                   // the last few pairs go round all XCDs
+            n = b - first;
+            xcd = 0;
+            here = units % 8;
+            step = 1;
+            base = whole * 8;
+        }
+        in = n % each;
+        n /= each;
+        const int local = by_block ? n % here : n / blocks;
+        block = by_block ? n / here : n % blocks;
+        unit = base + xcd + local * step;
+    }
+};
+
 typedef __amdgpu_buffer_rsrc_t Buffer;
 __device__ __forceinline__ Buffer buffer_at(const void *at, int64_t bytes)        // reads past its end give 0
 {
@@ -91,8 +115,6 @@ __device__ __forceinline__ int turn_of(int row)
     else if constexpr (kRowVectors<T, D> == 8) return ((row & 2) << 1) | ((row >> 2) & 3);
     else return (row >> 2) & 3;
 }
-// two stages of LDS where they fit, so that a tile is laid down while the one before it is read
-template <typename T, int D> constexpr int kStages = kTileBytes<T, D> <= 20 * 1024 ? 2 : 1;
 
 // rows [first, first + count) of a head, `row` elements apart, from its first element on
 template <typename T>
@@ -101,30 +123,59 @@ __device__ __forceinline__ Buffer rows_from(const T *head, int64_t row, int firs
     return buffer_at(head + first * row, count > 0 ? ((count - 1) * row + dim) * (int64_t)sizeof(T) : 0);
 }
 
-// A workgroup's tile on its way from memory to LDS.
+// One side's tiles on their way from memory to LDS: `fetch` asks for a tile, `land` (and, after all of them, `landed`) makes it whole; what
+// lies in its place has to be through before the fetch.  bf16 goes straight to LDS, each lane's 16 bytes to the next place of the wave's
+// kilobyte, asked for from where they belong; fp32, whose rows are padded, through registers.
 template <typename T, int D>
-struct TileLoad {
-    static constexpr int VECTORS = D / kPerVector<T>, EACH = kTile * VECTORS / kAttnThreads;
+struct Tiles {
+    static constexpr bool DIRECT = sizeof(T) == 2;
+    static constexpr int VECTORS = DIRECT ? kRowVectors<T, D> : D / kPerVector<T>, EACH = kTile * VECTORS / kAttnThreads;
     static_assert(kTile * VECTORS % kAttnThreads == 0, "every thread takes as many");
-    u32x4 held[EACH];
+    int from[EACH];
+    u32x4 held[DIRECT ? 1 : EACH];
 
-    __device__ __forceinline__ void load(const T *head, int64_t row, int first, int end, int dim)
+    __device__ __forceinline__ static int vector(int i)     // the thread's i-th of the tile's vectors
     {
-        const Buffer b = rows_from(head, row, first, min(end - first, kTile), dim);
-        const int bytes = (int)row * (int)sizeof(T);
+        return DIRECT ? ((int)(threadIdx.x >> 6) * EACH + i) * kWave + (int)(threadIdx.x & 63) : (int)threadIdx.x + i * kAttnThreads;
+    }
+    __device__ __forceinline__ void start(int64_t row, int dim)
+    {
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            const int n = (int)threadIdx.x + i * kAttnThreads, r = n / VECTORS, c = n % VECTORS;
-            held[i] = load16(b, c * kPerVector<T> < dim ? r * bytes + c * 16 : kNowhere);
+            const int r = vector(i) / VECTORS, c = (vector(i) % VECTORS) ^ turn_of<T, D>(r);
+            from[i] = c * kPerVector<T> < dim ? r * ((int)row * (int)sizeof(T)) + c * 16 : kNowhere;
         }
     }
-    __device__ __forceinline__ void store(char *lds) const
+    __device__ __forceinline__ void fetch(const T *head, int64_t row, int first, int end, int dim, char *lds)
     {
+        const int64_t count = min(end - first, kTile), bytes = count > 0 ? ((count - 1) * row + dim) * (int64_t)sizeof(T) : 0;
+        if constexpr (DIRECT) {
+            const uint64_t at = reinterpret_cast<uint64_t>(head + first * row);
+            u32x4 d = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)) & 0xFFFFu,
+                       (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bytes), 0x00020000u};
+            const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane(
+                (int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + (int)(threadIdx.x >> 6) * EACH * 1024);
+            // (in these terms, and not as the builtin, because the compiler would have the next read of any tile wait for it)
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int n = (int)threadIdx.x + i * kAttnThreads, r = n / VECTORS, c = n % VECTORS;
-            *reinterpret_cast<u32x4 *>(lds + r * kPitch<T, D> + (c ^ turn_of<T, D>(r)) * 16) = held[i];
+            for (int i = 0; i < EACH; ++i)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to + i * 1024), "v"(from[i]), "s"(d) : "memory");
+        } else {
+            const Buffer b = buffer_at(head + first * row, bytes);
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) held[i] = load16(b, from[i]);
         }
+    }
+    __device__ __forceinline__ void land(char *lds) const
+    {
+        if constexpr (!DIRECT) {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) *reinterpret_cast<u32x4 *>(lds + vector(i) / VECTORS * kPitch<T, D> + vector(i) % VECTORS * 16) = held[i];
+        }
+    }
+    __device__ __forceinline__ static void landed()
+    {
+        if constexpr (DIRECT) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        __syncthreads();
     }
 };
 
@@ -186,6 +237,21 @@ __device__ __forceinline__ f32x16 dots(const char *tile, int first, const Own<T,
 #pragma unroll
     for (int c = 0; c < Own<T, D>::VECTORS; ++c) s = multiply16<T>(*reinterpret_cast<const u32x4 *>(at + ((2 * c + (lane >> 5)) ^ turn) * 16), own.x[c], s);
     return s;
+}
+
+// both halves of a tile, whose products do not wait for one another
+template <typename T, int D>
+__device__ __forceinline__ void dots2(const char *tile, const Own<T, D> &own, f32x16 (&s)[2])
+{
+    const int lane = threadIdx.x & 63;
+    const char *at = tile + (lane & 31) * kPitch<T, D>;
+    const int turn = turn_of<T, D>(lane & 31);
+    s[0] = s[1] = zeros16();
+#pragma unroll
+    for (int c = 0; c < Own<T, D>::VECTORS; ++c)
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+            s[n] = multiply16<T>(*reinterpret_cast<const u32x4 *>(at + n * 32 * kPitch<T, D> + ((2 * c + (lane >> 5)) ^ turn) * 16), own.x[c], s[n]);
 }
 
 typedef __attribute__((address_space(3))) s16x4 *LdsVector;

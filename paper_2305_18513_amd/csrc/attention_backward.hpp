@@ -17,18 +17,19 @@ template <bool BIAS> __device__ __forceinline__ float probability(float s, float
     return __builtin_amdgcn_exp2f(BIAS ? __builtin_fmaf(s - first, kLog2e, -second) : __builtin_fmaf(s, scale, -first));
 }
 
-constexpr int kSkew = kTile + 4;             // floats of a query's ds in LDS
+constexpr int kSkew = kOwn + 4;              // floats of a query's ds in LDS
 
 template <typename T, int D, bool BIAS, bool PARTS>
 __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 256) ? 1 : 2) queries_kernel(Attention a, Gradients g, int blocks)
 {
-    __shared__ __align__(16) char tiles[kStages<T, D>][2 * kTileBytes<T, D>];
+    __shared__ __align__(1024) char tiles[2][2 * kTileBytes<T, D>];
     __shared__ float column[BIAS ? kMostBuckets : 1], biases[2][BIAS ? kDistances : 1];
     __shared__ __align__(16) float skew[PARTS ? kAttnWaves : 1][PARTS ? kOwn * kSkew : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int heads = a.batch * a.q_heads, bh = (int)(blockIdx.x % (unsigned)heads);
-    const int turn = (int)(blockIdx.x / (unsigned)heads), block = a.causal ? blocks - 1 - turn : turn;      // the longest first
-    const int batch = bh / a.q_heads, head = bh % a.q_heads, kv = head / (a.q_heads / a.kv_heads);
+    const int group = a.q_heads / a.kv_heads;
+    const Place place(a.batch * a.kv_heads, blocks, group, a.causal != 0);
+    const int block = a.causal ? blocks - 1 - place.block : place.block;       // the longest first
+    const int batch = place.unit / a.kv_heads, kv = place.unit % a.kv_heads, head = kv * group + place.in, bh = batch * a.q_heads + head;
     const int q0 = block * kBlock, mine = q0 + wave * kOwn, i = mine + (lane & 31);
     const T *const q = static_cast<const T *>(a.q.at) + batch * a.q.b + head * a.q.h;
     const T *const k = static_cast<const T *>(a.k.at) + batch * a.k.b + kv * a.k.h;
@@ -37,17 +38,20 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
     const int seen = seen_by(a, i, keys), all_see = seen_by(a, mine, keys), any_sees = seen_by(a, min(mine + kOwn, a.q_tokens) - 1, keys);
     const float scale = a.scale * kLog2e;
 
-    TileLoad<T, D> kl, vl;
+    Tiles<T, D> kl, vl;
     BiasLoad bl;
-    auto load = [&](int t) {
-        kl.load(k, a.k.t, t * kTile, keys, a.head_dim);
-        vl.load(v, a.v.t, t * kTile, keys, a.head_dim);
+    kl.start(a.k.t, a.head_dim);
+    vl.start(a.v.t, a.head_dim);
+    auto fetch = [&](int t) {
+        kl.fetch(k, a.k.t, t * kTile, keys, a.head_dim, tiles[t & 1]);
+        vl.fetch(v, a.v.t, t * kTile, keys, a.head_dim, tiles[t & 1] + kTileBytes<T, D>);
         if constexpr (BIAS) bl.load(a, t * kTile - q0 - (kBlock - 1) + a.q_tokens - 1);
     };
-    auto store = [&](int to) {
-        kl.store(tiles[to % kStages<T, D>]);
-        vl.store(tiles[to % kStages<T, D>] + kTileBytes<T, D>);
-        if constexpr (BIAS) bl.store(a, column, biases[to]);
+    auto land = [&](int t) {
+        kl.land(tiles[t & 1]);
+        vl.land(tiles[t & 1] + kTileBytes<T, D>);
+        if constexpr (BIAS) bl.store(a, column, biases[t & 1]);
+        kl.landed();
     };
 
     Own<T, D> own, grad;
@@ -73,7 +77,7 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
         delta = both_sum(delta);
     }
     if (i < a.q_tokens) {
-        const int64_t at = (int64_t)bh * a.q_tokens + i, all = (int64_t)heads * a.q_tokens;
+        const int64_t at = (int64_t)bh * a.q_tokens + i, all = (int64_t)a.batch * a.q_heads * a.q_tokens;
         const float top = g.stats[2 * at], total = g.stats[2 * at + 1];
         if (total > 0.0f) {
             const float l = __builtin_amdgcn_logf(total);   // to the base of 2
@@ -99,17 +103,15 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
         __syncthreads();
     }
     if (count > 0) {
-        load(0);
-        store(0);
+        fetch(0);
         own.arrive();
         grad.arrive();
-        load(1);
-        __syncthreads();
+        land(0);
     }
     for (int t = 0; t < count; ++t) {
-        const char *const tile = tiles[t % kStages<T, D>];
+        const char *const tile = tiles[t & 1];
         const int k0 = t * kTile;
-        float now = 0.0f;
+        fetch(t + 1);
         if (k0 < any_sees) {
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
@@ -127,56 +129,46 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
                         if (k0 + 32 * n + row_of(r, half) >= seen) s[r] = 0.0f;
                 }
                 if constexpr (PARTS) {
+                    // Sums along the diagonals: lane l has that of key - query = l - 31 (within 32 keys and the wave's queries); what the upper
+                    // lanes have the next 32 keys see 32 lower.
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
-                        *reinterpret_cast<f32x4 *>(&skew[wave][(lane & 31) * kSkew + 32 * n + 8 * c + 4 * half]) = f32x4{s[4 * c], s[4 * c + 1], s[4 * c + 2], s[4 * c + 3]};
+                        *reinterpret_cast<f32x4 *>(&skew[wave][(lane & 31) * kSkew + 8 * c + 4 * half]) = f32x4{s[4 * c], s[4 * c + 1], s[4 * c + 2], s[4 * c + 3]};
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                    float now = 0.0f;
+#pragma unroll
+                    for (int m = 0; m < kOwn; ++m) {
+                        const int key = lane - 31 + m;
+                        const float x = skew[wave][m * kSkew + (key & 31)];
+                        now += key == (key & 31) ? x : 0.0f;
+                    }
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                    if (half == 0) part[k0 + 32 * n + lane] = now + carry;
+                    carry = __shfl_xor(now, 32, kWave);
                 }
                 sums<T, D>(tile, 32 * n, s, dq);
             }
-            if constexpr (PARTS) {
-                // Sums along the diagonals: lane l has that of key - query = l - 31 (within the tile and the wave's queries), then, for the
-                // next tile, which sees these distances 64 lower, that of l + 33.
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                float high = 0.0f;
-#pragma unroll
-                for (int n = 0; n < kOwn; ++n) {
-                    const int key = lane - 31 + n;
-                    const float x = skew[wave][n * kSkew + max(key, 0)];
-                    now += key >= 0 ? x : 0.0f;
-                    const float y = skew[wave][n * kSkew + min(key + kTile, kTile - 1)];
-                    high += key + kTile < kTile ? y : 0.0f;
-                }
-                now += carry;
-                carry = high;
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-            }
         } else if (PARTS) {
-            now = carry;
+            part[k0 + lane] = half == 0 ? carry : 0.0f;
             carry = 0.0f;
         }
-        if constexpr (PARTS) part[k0 + lane] = now;
-        if (kStages<T, D> == 1) __syncthreads();
-        if (t + 1 < count) {
-            store((t + 1) & 1);
-            load(t + 2);
-        }
-        __syncthreads();
+        land(t + 1);
     }
-    if constexpr (PARTS) part[count * kTile + lane] = carry;
+    if (PARTS && half == 0) part[count * kTile + lane] = carry;
     if (i < a.q_tokens) store_row<T, D>(dq, a.scale, static_cast<T *>(g.dq) + batch * g.dq_b + head * g.dq_h + i * g.dq_t, a.head_dim);
 }
 
 template <typename T, int D, bool BIAS>
 __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > 128 ? 1 : 2) keys_kernel(Attention a, Gradients g, int blocks)
 {
-    __shared__ __align__(16) char tiles[kStages<T, D>][2 * kTileBytes<T, D>];
+    __shared__ __align__(1024) char tiles[2][2 * kTileBytes<T, D>];
     __shared__ __align__(16) float rows[2][3][kTile];
     __shared__ float column[BIAS ? kMostBuckets : 1], biases[2][BIAS ? kDistances : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int heads = a.batch * a.kv_heads, bh = (int)(blockIdx.x % (unsigned)heads), block = (int)(blockIdx.x / (unsigned)heads);
-    const int batch = bh / a.kv_heads, kv = bh % a.kv_heads, group = a.q_heads / a.kv_heads;
+    const Place place(a.batch * a.kv_heads, blocks, 1, a.causal != 0);
+    const int batch = place.unit / a.kv_heads, kv = place.unit % a.kv_heads, block = place.block, group = a.q_heads / a.kv_heads;
     const int k0 = block * kBlock, mine = k0 + wave * kOwn, j = mine + (lane & 31);
     const int keys = keys_of(a, batch);
     const float scale = a.scale * kLog2e;
@@ -194,13 +186,20 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > 128 ? 1 : 2) key
 #pragma unroll
     for (int n = 0; n < D / 32; ++n) dk[n] = dv[n] = zeros16();
 
-    TileLoad<T, D> ql, gl;
+    Tiles<T, D> ql, gl;
     BiasLoad bl;
     float held[3];
-    auto load = [&](int t) {                                // (past the last tile: rows that are not there)
-        const int head = kv * group + min(t / max(per_head, 1), group - 1), q0 = t < count ? (from + t % max(per_head, 1)) * kTile : a.q_tokens;
-        ql.load(static_cast<const T *>(a.q.at) + batch * a.q.b + head * a.q.h, a.q.t, q0, a.q_tokens, a.head_dim);
-        gl.load(static_cast<const T *>(g.dout) + (int64_t)batch * a.q_tokens * out_row + (int64_t)head * a.head_dim, out_row, q0, a.q_tokens, a.head_dim);
+    ql.start(a.q.t, a.head_dim);
+    gl.start(out_row, a.head_dim);
+    // Tiles of queries from the last to the first, of each the heads in turn, so that the workgroups of a pair read the same ones at
+    // about the same time, whatever their keys' place.
+    auto head_of = [&](int t) { return kv * group + t % group; };
+    auto first_of = [&](int t) { return t < count ? (from + per_head - 1 - t / group) * kTile : a.q_tokens; };      // (past the last tile: rows that are not there)
+    auto fetch = [&](int t) {
+        const int head = head_of(t), q0 = first_of(t);
+        ql.fetch(static_cast<const T *>(a.q.at) + batch * a.q.b + head * a.q.h, a.q.t, q0, a.q_tokens, a.head_dim, tiles[t & 1]);
+        gl.fetch(static_cast<const T *>(g.dout) + (int64_t)batch * a.q_tokens * out_row + (int64_t)head * a.head_dim, out_row, q0, a.q_tokens, a.head_dim,
+                 tiles[t & 1] + kTileBytes<T, D>);
         const int i = q0 + (int)threadIdx.x;
         const bool in = threadIdx.x < kTile && i < a.q_tokens;
         const int64_t at = ((int64_t)batch * a.q_heads + head) * a.q_tokens + i;
@@ -209,30 +208,30 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > 128 ? 1 : 2) key
         held[2] = in ? g.rows[2 * all + at] : 0.0f;
         if constexpr (BIAS) bl.load(a, k0 - q0 - (kTile - 1) + a.q_tokens - 1);
     };
-    auto store = [&](int to) {
-        ql.store(tiles[to % kStages<T, D>]);
-        gl.store(tiles[to % kStages<T, D>] + kTileBytes<T, D>);
+    auto land = [&](int t) {
+        ql.land(tiles[t & 1]);
+        gl.land(tiles[t & 1] + kTileBytes<T, D>);
         if (threadIdx.x < kTile) {
 #pragma unroll
-            for (int n = 0; n < 3; ++n) rows[to][n][threadIdx.x] = held[n];
+            for (int n = 0; n < 3; ++n) rows[t & 1][n][threadIdx.x] = held[n];
         }
-        if constexpr (BIAS) bl.store(a, column, biases[to]);
+        if constexpr (BIAS) bl.store(a, column, biases[t & 1]);
+        ql.landed();
     };
     if (count > 0) {
         if constexpr (BIAS) {
-            load_column<T>(a, kv * group, column);
+            load_column<T>(a, head_of(0), column);
             __syncthreads();
         }
-        load(0);
-        store(0);
+        fetch(0);
         own.arrive();
         val.arrive();
-        load(1);
-        __syncthreads();
+        land(0);
     }
     for (int t = 0; t < count; ++t) {
-        const char *const tile = tiles[t % kStages<T, D>];
-        const int q0 = (from + t % per_head) * kTile;
+        const char *const tile = tiles[t & 1];
+        const int q0 = first_of(t);
+        fetch(t + 1);
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             const int first = q0 + 32 * n;                  // of 32 queries
@@ -263,19 +262,14 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > 128 ? 1 : 2) key
             for (int r = 0; r < 16; ++r) dp[r] *= s[r];
             sums<T, D>(tile, 32 * n, dp, dk);
         }
-        if (kStages<T, D> == 1) __syncthreads();
-        if (t + 1 < count) {
-            if constexpr (BIAS) {
-                if ((t + 1) % per_head == 0) {              // the next head's column
-                    __syncthreads();
-                    load_column<T>(a, kv * group + (t + 1) / per_head, column);
-                    __syncthreads();
-                }
+        if constexpr (BIAS) {
+            if (group > 1 && t + 1 < count) {               // the next head's column
+                __syncthreads();
+                load_column<T>(a, head_of(t + 1), column);
+                __syncthreads();
             }
-            store((t + 1) & 1);
-            load(t + 2);
         }
-        __syncthreads();
+        land(t + 1);
     }
     if (j >= a.k_tokens) return;
     store_row<T, D>(dv, 1.0f, static_cast<T *>(g.dv) + batch * g.dv_b + kv * g.dv_h + j * g.dv_t, a.head_dim);

@@ -12,12 +12,13 @@ namespace {
 template <typename T, int D, bool BIAS>
 __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2) forward_kernel(Attention a, T *__restrict__ out, float *__restrict__ stats, int blocks)
 {
-    __shared__ __align__(16) char tiles[kStages<T, D>][2 * kTileBytes<T, D>];
+    __shared__ __align__(1024) char key_tiles_[2][kTileBytes<T, D>], value_tiles[2][kTileBytes<T, D>];
     __shared__ float column[BIAS ? kMostBuckets : 1], biases[2][BIAS ? kDistances : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int heads = a.batch * a.q_heads, bh = (int)(blockIdx.x % (unsigned)heads);
-    const int turn = (int)(blockIdx.x / (unsigned)heads), block = a.causal ? blocks - 1 - turn : turn;      // the longest first
-    const int batch = bh / a.q_heads, head = bh % a.q_heads, kv = head / (a.q_heads / a.kv_heads);
+    const int group = a.q_heads / a.kv_heads;
+    const Place place(a.batch * a.kv_heads, blocks, group, a.causal != 0);
+    const int block = a.causal ? blocks - 1 - place.block : place.block;       // the longest first
+    const int batch = place.unit / a.kv_heads, kv = place.unit % a.kv_heads, head = kv * group + place.in, bh = batch * a.q_heads + head;
     const int q0 = block * kBlock, mine = q0 + wave * kOwn, i = mine + (lane & 31);
     const T *const q = static_cast<const T *>(a.q.at) + batch * a.q.b + head * a.q.h;
     const T *const k = static_cast<const T *>(a.k.at) + batch * a.k.b + kv * a.k.h;
@@ -36,38 +37,44 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
     float top = -__builtin_inff(), base = -__builtin_inff(), total = 0.0f;
     const float by = BIAS ? kLog2e : scale, room = 8.0f / by;
 
-    TileLoad<T, D> kl, vl;
+    Tiles<T, D> kl, vl;
     BiasLoad bl;
-    auto load = [&](int t) {
-        kl.load(k, a.k.t, t * kTile, keys, a.head_dim);
-        vl.load(v, a.v.t, t * kTile, keys, a.head_dim);
-        if constexpr (BIAS) bl.load(a, t * kTile - q0 - (kBlock - 1) + a.q_tokens - 1);
-    };
-    auto store = [&](int to) {
-        kl.store(tiles[to % kStages<T, D>]);
-        vl.store(tiles[to % kStages<T, D>] + kTileBytes<T, D>);
-        if constexpr (BIAS) bl.store(a, column, biases[to]);
-    };
-    if constexpr (BIAS) {
-        load_column<T>(a, head, column);
-        __syncthreads();
-    }
+    kl.start(a.k.t, a.head_dim);
+    vl.start(a.v.t, a.head_dim);
+    auto fetch_keys = [&](int t) { kl.fetch(k, a.k.t, t * kTile, keys, a.head_dim, key_tiles_[t & 1]); };
+    auto fetch_values = [&](int t) { vl.fetch(v, a.v.t, t * kTile, keys, a.head_dim, value_tiles[t & 1]); };
+    auto fetch_bias = [&](int t) { if constexpr (BIAS) bl.load(a, t * kTile - q0 - (kBlock - 1) + a.q_tokens - 1); };
+    auto land_bias = [&](int t) { if constexpr (BIAS) bl.store(a, column, biases[t & 1]); };
+
+    // A tile's products with the queries are formed while the exponentials of the one before it are: keys are a tile ahead of values.
+    f32x16 s[2][2];
     if (count > 0) {
-        load(0);
-        store(0);
+        if constexpr (BIAS) load_column<T>(a, head, column);
+        fetch_keys(0);
+        kl.land(key_tiles_[0]);
+        fetch_keys(1);
+        kl.land(key_tiles_[1]);
+        fetch_values(0);
+        vl.land(value_tiles[0]);
+        fetch_bias(0);
         own.arrive();
-        load(1);
+        if constexpr (BIAS) {
+            __syncthreads();
+            land_bias(0);
+        }
+        kl.landed();
+        dots2<T, D>(key_tiles_[0], own, s[0]);
         __syncthreads();
     }
-    for (int t = 0; t < count; ++t) {
-        const char *const tile = tiles[t % kStages<T, D>];
+    auto step = [&](int t, f32x16 (&s)[2], f32x16 (&next)[2]) {
         const int k0 = t * kTile;
+        fetch_keys(t + 2);
+        fetch_values(t + 1);
+        fetch_bias(t + 1);
         if (k0 < any_sees) {
-            f32x16 s[2];
+            if constexpr (BIAS) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                s[n] = dots<T, D>(tile, 32 * n, own);
-                if constexpr (BIAS) {
+                for (int n = 0; n < 2; ++n) {
                     const float *const b = biases[t & 1] + kBlock - 1 - (i - q0) + 4 * half + 32 * n;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[n][r] = __builtin_fmaf(s[n][r], a.scale, b[8 * (r / 4) + r % 4]);
@@ -96,6 +103,7 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
                 base = top;
             }
             const float safe = base == -__builtin_inff() ? 0.0f : base, less = -safe * scale;
+            dots2<T, D>(key_tiles_[(t + 1) & 1], own, next);           // (past the last tile: of keys that are not there, unused)
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
 #pragma unroll
@@ -104,15 +112,39 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
                     s[n][r] = __builtin_amdgcn_exp2f(BIAS ? (s[n][r] - safe) * kLog2e : __builtin_fmaf(s[n][r], scale, less));
                     total += s[n][r];
                 }
-                sums<T, D>(tile + kTileBytes<T, D>, 32 * n, s[n], o);
+                sums<T, D>(value_tiles[t & 1], 32 * n, s[n], o);
             }
+#ifndef SLIMFIT_SCHED
+#define SLIMFIT_SCHED 2
+#endif
+#if SLIMFIT_SCHED
+            if constexpr (sizeof(T) == 2) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+                for (int x = 0; x < D / 8; ++x) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, SLIMFIT_SCHED, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x400, 128 / D, 0);
+                }
+#pragma unroll
+                for (int x = 0; x < D / 8; ++x) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, SLIMFIT_SCHED, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x400, 128 / D, 0);
+                }
+            }
+#endif
         }
-        if (kStages<T, D> == 1) __syncthreads();
-        if (t + 1 < count) {
-            store((t + 1) & 1);
-            load(t + 2);
-        }
-        __syncthreads();
+        kl.land(key_tiles_[t & 1]);
+        vl.land(value_tiles[(t + 1) & 1]);
+        land_bias(t + 1);
+        kl.landed();
+    };
+    for (int t = 0; t < count; t += 2) {
+        step(t, s[0], s[1]);
+        if (t + 1 < count) step(t + 1, s[1], s[0]);
     }
     total = both_sum(total);
     const float inverse = total > 0.0f ? 1.0f / total : 0.0f;
