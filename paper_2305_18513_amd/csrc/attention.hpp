@@ -123,36 +123,43 @@ __device__ __forceinline__ Buffer rows_from(const T *head, int64_t row, int firs
     return buffer_at(head + first * row, count > 0 ? ((count - 1) * row + dim) * (int64_t)sizeof(T) : 0);
 }
 
-// One side's tiles on their way from memory to LDS: `fetch` asks for a tile, `land` (and, after all of them, `landed`) makes it whole; what
-// lies in its place has to be through before the fetch.  bf16 goes straight to LDS, each lane's 16 bytes to the next place of the wave's
-// kilobyte, asked for from where they belong; fp32, whose rows are padded, through registers.
-template <typename T, int D>
+// One side's tiles on their way from memory to LDS: `fetch` asks for the tile where this stands, `land` (and, after all of them, `landed`)
+// makes it whole; what lies in its place has to be through before the fetch.  bf16 goes straight to LDS, each lane's 16 bytes to the
+// next place of the wave's kilobyte, asked for from where they belong; fp32, whose rows are padded, through registers.  A step
+// from tile to tile is two additions (with addresses formed anew for each tile scalar instructions were a fourth of the loops).
+template <typename T, int D, int ROWS = kTile>
 struct Tiles {
     static constexpr bool DIRECT = sizeof(T) == 2;
-    static constexpr int VECTORS = DIRECT ? kRowVectors<T, D> : D / kPerVector<T>, EACH = kTile * VECTORS / kAttnThreads;
-    static_assert(kTile * VECTORS % kAttnThreads == 0, "every thread takes as many");
+    static constexpr int VECTORS = DIRECT ? kRowVectors<T, D> : D / kPerVector<T>, EACH = ROWS * VECTORS / kAttnThreads;
+    static_assert(ROWS * VECTORS % kAttnThreads == 0, "every thread takes as many");
     int from[EACH];
     u32x4 held[DIRECT ? 1 : EACH];
+    uint64_t at;                             // the tile's first element
+    int64_t left, step;                      // bytes from there to the end of what there is; from a tile to the next
 
     __device__ __forceinline__ static int vector(int i)     // the thread's i-th of the tile's vectors
     {
         return DIRECT ? ((int)(threadIdx.x >> 6) * EACH + i) * kWave + (int)(threadIdx.x & 63) : (int)threadIdx.x + i * kAttnThreads;
     }
-    __device__ __forceinline__ void start(int64_t row, int dim)
+    // rows [0, end) of a head, `row` elements apart, from row `first` on
+    __device__ __forceinline__ void start(const T *head, int64_t row, int first, int end, int dim)
     {
+        at = reinterpret_cast<uint64_t>(head + first * row);
+        left = end > 0 ? ((end - 1 - first) * row + dim) * (int64_t)sizeof(T) : 0;
+        step = ROWS * row * (int64_t)sizeof(T);
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             const int r = vector(i) / VECTORS, c = (vector(i) % VECTORS) ^ turn_of<T, D>(r);
             from[i] = c * kPerVector<T> < dim ? r * ((int)row * (int)sizeof(T)) + c * 16 : kNowhere;
         }
     }
-    __device__ __forceinline__ void fetch(const T *head, int64_t row, int first, int end, int dim, char *lds)
+    __device__ __forceinline__ void forward() { at += step; left -= step; }
+    __device__ __forceinline__ void fetch(char *lds)
     {
-        const int64_t count = min(end - first, kTile), bytes = count > 0 ? ((count - 1) * row + dim) * (int64_t)sizeof(T) : 0;
+        const int64_t bytes = left < 0 ? 0 : left < 0xFFFFFFF0LL ? left : 0xFFFFFFF0LL;
         if constexpr (DIRECT) {
-            const uint64_t at = reinterpret_cast<uint64_t>(head + first * row);
-            u32x4 d = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)) & 0xFFFFu,
-                       (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bytes), 0x00020000u};
+            const u32x4 d = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)) & 0xFFFFu,
+                             (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bytes), 0x00020000u};
             const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane(
                 (int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + (int)(threadIdx.x >> 6) * EACH * 1024);
             // (in these terms, and not as the builtin, because the compiler would have the next read of any tile wait for it)
@@ -160,7 +167,7 @@ struct Tiles {
             for (int i = 0; i < EACH; ++i)
                 asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to + i * 1024), "v"(from[i]), "s"(d) : "memory");
         } else {
-            const Buffer b = buffer_at(head + first * row, bytes);
+            const Buffer b = buffer_at(reinterpret_cast<const void *>(at), bytes);
 #pragma unroll
             for (int i = 0; i < EACH; ++i) held[i] = load16(b, from[i]);
         }
@@ -236,6 +243,20 @@ __device__ __forceinline__ f32x16 dots(const char *tile, int first, const Own<T,
     f32x16 s = zeros16();
 #pragma unroll
     for (int c = 0; c < Own<T, D>::VECTORS; ++c) s = multiply16<T>(*reinterpret_cast<const u32x4 *>(at + ((2 * c + (lane >> 5)) ^ turn) * 16), own.x[c], s);
+    return s;
+}
+
+// the same with the wave's own rows in LDS too, from `own` on
+template <typename T, int D>
+__device__ __forceinline__ f32x16 dots_of(const char *tile, int first, const char *own)
+{
+    const int lane = threadIdx.x & 63, at = (lane & 31) * kPitch<T, D>, turn = turn_of<T, D>(lane & 31);
+    f32x16 s = zeros16();
+#pragma unroll
+    for (int c = 0; c < Own<T, D>::VECTORS; ++c) {
+        const int vector = at + ((2 * c + (lane >> 5)) ^ turn) * 16;
+        s = multiply16<T>(*reinterpret_cast<const u32x4 *>(tile + first * kPitch<T, D> + vector), *reinterpret_cast<const u32x4 *>(own + vector), s);
+    }
     return s;
 }
 

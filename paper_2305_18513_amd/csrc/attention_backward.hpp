@@ -7,6 +7,8 @@
 
 #include "attention.hpp"
 
+#include <type_traits>
+
 namespace slimfit {
 namespace {
 
@@ -40,11 +42,13 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
 
     Tiles<T, D> kl, vl;
     BiasLoad bl;
-    kl.start(a.k.t, a.head_dim);
-    vl.start(a.v.t, a.head_dim);
+    kl.start(k, a.k.t, 0, keys, a.head_dim);
+    vl.start(v, a.v.t, 0, keys, a.head_dim);
     auto fetch = [&](int t) {
-        kl.fetch(k, a.k.t, t * kTile, keys, a.head_dim, tiles[t & 1]);
-        vl.fetch(v, a.v.t, t * kTile, keys, a.head_dim, tiles[t & 1] + kTileBytes<T, D>);
+        kl.fetch(tiles[t & 1]);
+        vl.fetch(tiles[t & 1] + kTileBytes<T, D>);
+        kl.forward();
+        vl.forward();
         if constexpr (BIAS) bl.load(a, t * kTile - q0 - (kBlock - 1) + a.q_tokens - 1);
     };
     auto land = [&](int t) {
@@ -124,9 +128,9 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
                     s[r] = probability<BIAS>(s[r], scale, first, second) * (dp[r] - delta);
                 }
                 if (k0 + 32 * n + 32 > all_see) {
+                    const int some = seen - k0 - 32 * n - 4 * half;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (k0 + 32 * n + row_of(r, half) >= seen) s[r] = 0.0f;
+                    for (int r = 0; r < 16; ++r) s[r] = row_of(r, 0) < some ? s[r] : 0.0f;
                 }
                 if constexpr (PARTS) {
                     // Sums along the diagonals: lane l has that of key - query = l - 31 (within 32 keys and the wave's queries); what the upper
@@ -160,11 +164,16 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
     if (i < a.q_tokens) store_row<T, D>(dq, a.scale, static_cast<T *>(g.dq) + batch * g.dq_b + head * g.dq_h + i * g.dq_t, a.head_dim);
 }
 
+// bf16 heads of 96 and 128: two waves a SIMD have no room for all of the wave's own rows, of which the values stay in LDS, with smaller
+// tiles to make up for them.
+template <typename T, int D> constexpr bool kValuesInLds = sizeof(T) == 2 && D > 64;
+
 template <typename T, int D, bool BIAS>
-__global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > 128 ? 1 : 2) keys_kernel(Attention a, Gradients g, int blocks)
+__global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 32 ? 1 : 2) keys_kernel(Attention a, Gradients g, int blocks)
 {
-    __shared__ __align__(1024) char tiles[2][2 * kTileBytes<T, D>];
-    __shared__ __align__(16) float rows[2][3][kTile];
+    constexpr int ROWS = kValuesInLds<T, D> ? 32 : kTile, BYTES = ROWS * kPitch<T, D>;
+    __shared__ __align__(1024) char tiles[2][2 * BYTES], values[kValuesInLds<T, D> ? kBlock * kPitch<T, D> : 16];
+    __shared__ __align__(16) float rows[2][3][ROWS];
     __shared__ float column[BIAS ? kMostBuckets : 1], biases[2][BIAS ? kDistances : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const Place place(a.batch * a.kv_heads, blocks, 1, a.causal != 0);
@@ -176,42 +185,54 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > 128 ? 1 : 2) key
 
     // queries that see the first of the workgroup's keys, and all of the wave's
     const int offset = a.k_tokens - a.q_tokens;
-    const int from = a.causal ? max(0, k0 - offset) / kTile : 0, per_head = k0 < keys ? max(0, (a.q_tokens + kTile - 1) / kTile - from) : 0;
+    const int from = a.causal ? max(0, k0 - offset) / ROWS : 0, per_head = k0 < keys ? max(0, (a.q_tokens + ROWS - 1) / ROWS - from) : 0;
     const int count = per_head * group;
 
-    Own<T, D> own, val;
+    Own<T, D> own;
+    Own<T, kValuesInLds<T, D> ? 32 : D> val;
     own.load(static_cast<const T *>(a.k.at) + batch * a.k.b + kv * a.k.h, a.k.t, mine, keys, a.head_dim);
-    val.load(static_cast<const T *>(a.v.at) + batch * a.v.b + kv * a.v.h, a.v.t, mine, keys, a.head_dim);
+    const T *const v = static_cast<const T *>(a.v.at) + batch * a.v.b + kv * a.v.h;
+    if constexpr (!kValuesInLds<T, D>) val.load(v, a.v.t, mine, keys, a.head_dim);
     f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
     for (int n = 0; n < D / 32; ++n) dk[n] = dv[n] = zeros16();
 
-    Tiles<T, D> ql, gl;
+    Tiles<T, D, ROWS> ql, gl;
     BiasLoad bl;
     float held[3];
-    ql.start(a.q.t, a.head_dim);
-    gl.start(out_row, a.head_dim);
     // Tiles of queries from the last to the first, of each the heads in turn, so that the workgroups of a pair read the same ones at
     // about the same time, whatever their keys' place.
-    auto head_of = [&](int t) { return kv * group + t % group; };
-    auto first_of = [&](int t) { return t < count ? (from + per_head - 1 - t / group) * kTile : a.q_tokens; };      // (past the last tile: rows that are not there)
+    int q0 = (from + per_head - 1) * ROWS, next = 0;        // where `fetch` stands: the tile's first query, the head of the group
+    ql.start(static_cast<const T *>(a.q.at) + batch * a.q.b + kv * group * a.q.h, a.q.t, q0, a.q_tokens, a.head_dim);
+    gl.start(static_cast<const T *>(g.dout) + (int64_t)batch * a.q_tokens * out_row + (int64_t)kv * group * a.head_dim, out_row, q0, a.q_tokens, a.head_dim);
+    const int64_t q_head = a.q.h * (int64_t)sizeof(T), out_head = a.head_dim * (int64_t)sizeof(T);
+    const float *row_at = g.rows + ((int64_t)batch * a.q_heads + kv * group) * a.q_tokens + q0 + (int64_t)threadIdx.x;
     auto fetch = [&](int t) {
-        const int head = head_of(t), q0 = first_of(t);
-        ql.fetch(static_cast<const T *>(a.q.at) + batch * a.q.b + head * a.q.h, a.q.t, q0, a.q_tokens, a.head_dim, tiles[t & 1]);
-        gl.fetch(static_cast<const T *>(g.dout) + (int64_t)batch * a.q_tokens * out_row + (int64_t)head * a.head_dim, out_row, q0, a.q_tokens, a.head_dim,
-                 tiles[t & 1] + kTileBytes<T, D>);
-        const int i = q0 + (int)threadIdx.x;
-        const bool in = threadIdx.x < kTile && i < a.q_tokens;
-        const int64_t at = ((int64_t)batch * a.q_heads + head) * a.q_tokens + i;
-        held[0] = in ? g.rows[at] : BIAS ? 0.0f : __builtin_inff();
-        held[1] = in ? g.rows[all + at] : __builtin_inff();
-        held[2] = in ? g.rows[2 * all + at] : 0.0f;
-        if constexpr (BIAS) bl.load(a, k0 - q0 - (kTile - 1) + a.q_tokens - 1);
+        ql.fetch(tiles[t & 1]);
+        gl.fetch(tiles[t & 1] + BYTES);
+        const bool in = threadIdx.x < ROWS && q0 + (int)threadIdx.x < a.q_tokens && t < count;
+        held[0] = in ? row_at[0] : BIAS ? 0.0f : __builtin_inff();
+        held[1] = BIAS && in ? row_at[all] : __builtin_inff();
+        held[2] = in ? row_at[2 * all] : 0.0f;
+        if constexpr (BIAS) bl.load(a, k0 - q0 - (ROWS - 1) + a.q_tokens - 1);
+        if (++next < group) {
+            ql.at += q_head;
+            gl.at += out_head;
+            row_at += a.q_tokens;
+        } else {
+            next = 0;
+            q0 -= ROWS;
+            ql.at -= (group - 1) * q_head + ql.step;
+            gl.at -= (group - 1) * out_head + gl.step;
+            row_at -= (int64_t)(group - 1) * a.q_tokens + ROWS;
+            ql.left = t + 1 < count ? ql.left + ql.step : 0;
+            gl.left = t + 1 < count ? gl.left + gl.step : 0;
+        }
     };
     auto land = [&](int t) {
         ql.land(tiles[t & 1]);
-        gl.land(tiles[t & 1] + kTileBytes<T, D>);
-        if (threadIdx.x < kTile) {
+        gl.land(tiles[t & 1] + BYTES);
+        if (threadIdx.x < ROWS) {
 #pragma unroll
             for (int n = 0; n < 3; ++n) rows[t & 1][n][threadIdx.x] = held[n];
         }
@@ -220,25 +241,36 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > 128 ? 1 : 2) key
     };
     if (count > 0) {
         if constexpr (BIAS) {
-            load_column<T>(a, head_of(0), column);
+            load_column<T>(a, kv * group, column);
             __syncthreads();
         }
         fetch(0);
+        if constexpr (kValuesInLds<T, D>) {
+            Tiles<T, D, kBlock> vl;
+            vl.start(v, a.v.t, k0, keys, a.head_dim);
+            vl.fetch(values);
+        } else {
+            val.arrive();
+        }
         own.arrive();
-        val.arrive();
         land(0);
     }
+    // the first query that sees the lane's key
+    const int visible = j >= keys ? 0x7FFFFFFF : a.causal ? j - offset : -0x7FFFFFFF;
     for (int t = 0; t < count; ++t) {
         const char *const tile = tiles[t & 1];
-        const int q0 = first_of(t);
+        const int here = (from + per_head - 1 - t / group) * ROWS;
         fetch(t + 1);
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const int first = q0 + 32 * n;                  // of 32 queries
-            if (a.causal && first + 31 + offset < mine) continue;      // none of them sees any of the wave's keys
+        for (int n = 0; n < ROWS / 32; ++n) {
+            const int first = here + 32 * n;                // of 32 queries
+            if (sizeof(T) == 4 && a.causal && first + 31 + offset < mine) continue;      // none of them sees any of the wave's keys
             f32x16 s = dots<T, D>(tile, 32 * n, own);
-            f32x16 dp = dots<T, D>(tile + kTileBytes<T, D>, 32 * n, val);
-            const float *const b = biases[BIAS ? t & 1 : 0] + kTile - 1 + (j - k0) - 32 * n - 4 * half;
+            f32x16 dp;
+            if constexpr (kValuesInLds<T, D>) dp = dots_of<T, D>(tile + BYTES, 32 * n, values + wave * kOwn * kPitch<T, D>);
+            else dp = dots<T, D>(tile + BYTES, 32 * n, val);
+            const float *const b = biases[BIAS ? t & 1 : 0] + ROWS - 1 + (j - k0) - 32 * n - 4 * half;
+            const int none = visible > first + 64 ? 64 : visible < first ? 0 : visible - first;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const f32x4 f = *reinterpret_cast<const f32x4 *>(&rows[t & 1][0][32 * n + 8 * c + 4 * half]);
@@ -248,24 +280,28 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > 128 ? 1 : 2) key
                 for (int r = 0; r < 4; ++r) {
                     float x = s[4 * c + r];
                     if constexpr (BIAS) x = __builtin_fmaf(x, a.scale, b[-(8 * c + r)]);
-                    s[4 * c + r] = probability<BIAS>(x, scale, f[r], e[r]);
-                    dp[4 * c + r] -= d[r];
+                    x = probability<BIAS>(x, scale, f[r], e[r]);
+                    if constexpr (kValuesInLds<T, D>) x = 8 * c + 4 * half + r >= none ? x : 0.0f;
+                    s[4 * c + r] = x;
+                    dp[4 * c + r] = x * (dp[4 * c + r] - d[r]);
                 }
             }
-            if (mine + 32 > keys || (a.causal && first + offset < mine + 31)) {
+            // (a branch around the masks is the quicker one, but not where registers are short: D of 128, 2709 us without, 3744 with)
+            if (!kValuesInLds<T, D> && (mine + 32 > keys || (a.causal && first + offset < mine + 31))) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (j >= keys || (a.causal && j > first + row_of(r, half) + offset)) s[r] = 0.0f;
+                for (int r = 0; r < 16; ++r) {
+                    const bool in = row_of(r, 0) + 4 * half >= none;
+                    s[r] = in ? s[r] : 0.0f;
+                    dp[r] = in ? dp[r] : 0.0f;
+                }
             }
-            sums<T, D>(tile + kTileBytes<T, D>, 32 * n, s, dv);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) dp[r] *= s[r];
+            sums<T, D>(tile + BYTES, 32 * n, s, dv);
             sums<T, D>(tile, 32 * n, dp, dk);
         }
         if constexpr (BIAS) {
             if (group > 1 && t + 1 < count) {               // the next head's column
                 __syncthreads();
-                load_column<T>(a, head_of(t + 1), column);
+                load_column<T>(a, kv * group + (t + 1) % group, column);
                 __syncthreads();
             }
         }
