@@ -1070,8 +1070,9 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, layout:
     _require(out.shape == (B, Tq, Hq, D) and out.dtype == q.dtype and out.is_contiguous())
     _require(stats.dtype == torch.float32 and stats.shape == (B, Hq, Tq, 2) and stats.is_contiguous())
     _on_current_device(q, k, v, lengths, table, None if table is None else bucket_of, out, stats, workspace)
-    if Tq and B and layout == HEADS_APART:
-        workspace = _own_workspace(workspace, attention_workspace(q.dtype, layout, B, Tq, Tk, Hq, Hk, D), q.device, stream)
+    need = attention_workspace(q.dtype, layout, B, Tq, Tk, Hq, Hk, D)
+    if need > 0:
+        workspace = _own_workspace(workspace, need, q.device, stream)
     rc = lib().slimfit_attention_forward(
         _at(q), _at(k), _at(v), C.c_int32(_dt(q)), C.c_int32(layout), *(C.c_int64(r) for r in rows), C.c_int64(B), C.c_int32(Tq), C.c_int32(Tk), C.c_int32(Hq),
         C.c_int32(Hk), C.c_int32(D), C.c_float(scale), C.c_int32(int(bool(causal))), _at(lengths), _at(table),

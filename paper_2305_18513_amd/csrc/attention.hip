@@ -93,8 +93,35 @@ int32_t check_sizes(const Sizes &z)
 
 bool turned(const Sizes &z) { return z.layout == SLIMFIT_HEADS_APART && z.batch > 0 && z.k_tokens > 0 && z.q_tokens > 0; }
 size_t turned_bytes(const Sizes &z) { return turned(z) ? rounded((size_t)z.k_count() * z.e()) : 0; }
-int q_blocks(const Sizes &z) { return (z.q_tokens + kBlock - 1) / kBlock; }
 int64_t part_row(const Sizes &z) { return ((int64_t)z.k_tokens + kTile - 1) / kTile * kTile + kTile; }
+
+int q_blocks(const Sizes &z) { return (z.q_tokens + kBlock - 1) / kBlock; }
+
+// How many workgroups share a sequence's keys out, or 0: 128 queries of a head a workgroup.  (us with those, with few queries)
+//   bf16, up to 16 queries: 16 x 4096 keys, 32 heads on 8 by 128: 1 query 121, 48; 16 132, 63; 32 139, 120; 64 142, 243;
+//         64 x 1024, 8 heads of 64: 1 24.5, 25.4; 16 25.3, 25.7; 64 25.5, 48.5.
+//   fp32, where padded queries cost products, up to 64: the first 1 1146, 137; 64 1153, 926; the second 1 137, 48; 64 142, 105.
+//   Any where there are few workgroups otherwise and keys are many: bf16, 1 x 4096, 32 heads on 8 by 128: 128 queries 95, 46; 8 x 1024,
+//         12 heads of 64: 64 queries 18.6, 13.1; of 128 keys 5.7, 6.8.
+// A workgroup for each compute unit is enough (16 x 4096 and 1 query: 256 workgroups 48, 512 54, 1024 60), but for fp32 heads of up
+// to 64, two of which fit one (8 x 4096, 12 heads: 65, 47, 55).
+int few_splits(const Sizes &z)
+{
+    if (z.batch == 0 || z.q_tokens == 0 || z.k_tokens == 0) return 0;
+    const int64_t others = z.batch * z.q_heads * q_blocks(z);
+    if (z.q_tokens > (z.dt == SLIMFIT_BF16 ? 16 : 64) && (others > 128 || z.k_tokens < 512)) return 0;
+    const int64_t rows = (int64_t)(z.q_heads / z.kv_heads) * z.q_tokens, blocks = z.batch * z.kv_heads * ((rows + kOwn - 1) / kOwn);
+    const int64_t tiles = (z.k_tokens + kFewTile - 1) / kFewTile;
+    int64_t splits = (z.dt == SLIMFIT_F32 && z.head_dim <= 64 ? 512 : 256) / blocks;
+    if (splits > tiles) splits = tiles;
+    if (splits > kMostSplits) splits = kMostSplits;
+    return splits < 1 ? 1 : (int)splits;
+}
+size_t part_bytes(const Sizes &z)
+{
+    const int splits = few_splits(z);
+    return splits > 1 ? rounded((size_t)(z.batch * z.q_heads) * (size_t)z.q_tokens * (size_t)splits * ((size_t)z.head_dim + 2) * 4) : 0;
+}
 
 struct BackwardPlaces {
     size_t rows, parts, sums, bytes;
@@ -222,7 +249,7 @@ extern "C" int32_t slimfit_attention_workspace(int32_t dt, int32_t layout, int64
     const int32_t rc = check_sizes(z);
     if (rc != SLIMFIT_OK) return rc;
     if (!bytes) return SLIMFIT_ERR_INVALID_ARG;
-    *bytes = backward ? BackwardPlaces(z, with_dtable != 0).bytes : turned_bytes(z);
+    *bytes = backward ? BackwardPlaces(z, with_dtable != 0).bytes : turned_bytes(z) + part_bytes(z);
     return SLIMFIT_OK;
 }
 
@@ -240,7 +267,7 @@ extern "C" int32_t slimfit_attention_forward(const void *q, const void *k, const
     const Span in[] = {span_of(q, z, 0, q_row), span_of(k, z, 1, k_row), span_of(v, z, 1, v_row)};
     const Span to[] = {flat(out, (size_t)z.q_count() * z.e()), flat(stats, (size_t)(batch * q_heads) * (size_t)q_tokens * 8)};
     if ((rc = check_spans(in, 3, to, 2)) != SLIMFIT_OK) return rc;
-    const size_t need = turned_bytes(z);
+    const size_t need = turned_bytes(z) + part_bytes(z);
     if ((rc = check_workspace(need, workspace, workspace_bytes)) != SLIMFIT_OK) return rc;
     if ((rc = check_ranges(in, 3)) != SLIMFIT_OK || (rc = check_ranges(to, 2)) != SLIMFIT_OK) return rc;
     if ((rc = check_other_ranges(z, lengths, table, bucket_of)) != SLIMFIT_OK) return rc;
@@ -250,8 +277,9 @@ extern "C" int32_t slimfit_attention_forward(const void *q, const void *k, const
         k = workspace;
     }
     const Attention a = attention_of(z, q, k, v, q_row, k_row, v_row, scale, causal, lengths, k_tokens > 0 ? table : nullptr, bucket_of);
-    if (dt == SLIMFIT_BF16) attention_forward_bf16(a, out, stats, st);
-    else attention_forward_f32(a, out, stats, st);
+    float *const parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + turned_bytes(z));
+    if (dt == SLIMFIT_BF16) attention_forward_bf16(a, out, stats, parts, few_splits(z), st);
+    else attention_forward_f32(a, out, stats, parts, few_splits(z), st);
     return launch_status();
 }
 

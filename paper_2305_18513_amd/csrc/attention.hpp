@@ -25,6 +25,8 @@ constexpr int kAttnWaves = 4;
 constexpr int kOwn = 32;                     // rows of a wave
 constexpr int kBlock = kOwn * kAttnWaves;    // rows of a workgroup
 constexpr int kTile = 64;                    // rows of a tile
+constexpr int kFewTile = 128;                // keys of a tile of the kernel for few queries, 32 a wave
+constexpr int kMostSplits = 64;              // workgroups that share a sequence's keys out there
 constexpr int kDistances = kBlock + kTile;   // distances between a workgroup's rows and a tile's, and one
 constexpr int kMostBuckets = 1024;
 constexpr int kMostHeadDim = 128;
@@ -371,9 +373,9 @@ __device__ __forceinline__ void load_column(const Attention &a, int head, float 
     for (int i = threadIdx.x; i < a.buckets; i += kAttnThreads) column[i] = widened(static_cast<const T *>(a.table)[(int64_t)i * a.q_heads + head]);
 }
 
-// host side (attention.hip)
-void attention_forward_f32(const Attention &a, void *out, float *stats, hipStream_t st);
-void attention_forward_bf16(const Attention &a, void *out, float *stats, hipStream_t st);
+// The launches.  splits 0: 128 queries a workgroup; above: few queries, the keys shared out over so many workgroups, whose sums meet in parts.
+void attention_forward_f32(const Attention &a, void *out, float *stats, float *parts, int splits, hipStream_t st);
+void attention_forward_bf16(const Attention &a, void *out, float *stats, float *parts, int splits, hipStream_t st);
 
 struct Gradients {
     const void *dout, *out;

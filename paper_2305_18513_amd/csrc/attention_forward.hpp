@@ -4,7 +4,7 @@
 // that the maximum and sum are a lane's own, but for one exchange of the halves.)
 #pragma once
 
-#include "attention.hpp"
+#include "attention_few.hpp"
 
 namespace slimfit {
 namespace {
@@ -164,14 +164,21 @@ void launch_forward(const Attention &a, T *out, float *stats, hipStream_t st)
     else launch(forward_kernel<T, D, false>, grid, kAttnThreads, 0, st, a, out, stats, blocks);
 }
 
+template <typename T, int D>
+void launch_either(const Attention &a, T *out, float *stats, float *parts, int splits, hipStream_t st)
+{
+    if (splits > 0) launch_few<T, D>(a, out, stats, parts, splits, st);
+    else launch_forward<T, D>(a, out, stats, st);
+}
+
 template <typename T>
-void attention_forward_of(const Attention &a, void *out, float *stats, hipStream_t st)
+void attention_forward_of(const Attention &a, void *out, float *stats, float *parts, int splits, hipStream_t st)
 {
     T *o = static_cast<T *>(out);
-    if (a.head_dim <= 32) launch_forward<T, 32>(a, o, stats, st);
-    else if (a.head_dim <= 64) launch_forward<T, 64>(a, o, stats, st);
-    else if (a.head_dim <= 96) launch_forward<T, 96>(a, o, stats, st);
-    else launch_forward<T, 128>(a, o, stats, st);
+    if (a.head_dim <= 32) launch_either<T, 32>(a, o, stats, parts, splits, st);
+    else if (a.head_dim <= 64) launch_either<T, 64>(a, o, stats, parts, splits, st);
+    else if (a.head_dim <= 96) launch_either<T, 96>(a, o, stats, parts, splits, st);
+    else launch_either<T, 128>(a, o, stats, parts, splits, st);
 }
 
 }  // namespace

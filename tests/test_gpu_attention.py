@@ -371,6 +371,33 @@ def test_gradients_against_differences():
         assert abs(got - want) <= 2e-3 * size + 16 * U * math.sqrt(do.numel()), name
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(64, 1, 2100, 8, 2, 128), (70, 1, 1500, 8, 8, 64), (3, 5, 1030, 14, 2, 96), (2, 32, 700, 4, 4, 32), (1, 1, 5000, 7, 1, 80), (300, 2, 300, 2, 2, 40),
+                                   (600, 1, 700, 1, 1, 128), (2, 30, 900, 6, 2, 128)], ids=lambda s: "x".join(map(str, s)))
+def test_few_queries(shape, dtype):
+    """Single tokens and a few over long keys, which are shared out over workgroups, some of several tiles, with sequences of any length."""
+    require_gpu()
+    B, Tq, Tk, Hq, Hk, D = shape
+    g = torch.Generator(device="cuda").manual_seed(B)
+    lengths = torch.randint(0, Tk + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    lengths[0] = Tk
+    for causal, bias, layout in ((False, False, sf.HEADS_ROWS), (True, True, sf.HEADS_ROWS), (True, False, sf.HEADS_APART)):
+        q, k, v, do = inputs(*shape, dtype, layout, seed=Tk, columns=layout == sf.HEADS_ROWS)
+        table = torch.randn(9, Hq, generator=g, device="cuda").to(dtype) if bias else None
+        of = sf.distance_buckets(Tq, Tk, 9, 400, False) if bias else None
+        c = Call(q, k, v, do, layout, D ** -0.5, causal, lengths if not causal or bias else None, table, of).forward()
+        r = Reference(q, k, v, None, layout, D ** -0.5, *c.args[5:])
+        out = rows_of(c.out, sf.HEADS_ROWS)
+        within(out, r.out, r.rounded(r.out_off(), r.out), "out")
+        none = r.top == -math.inf
+        top, total = c.stats[..., :1].double(), c.stats[..., 1:].double()
+        assert torch.equal(top == -math.inf, none) and bool((total[none] == 0).all()) and bool((out[none.expand_as(out)] == 0).all())
+        within(torch.where(none, 0.0, top), torch.where(none, 0.0, r.top), r.top_off + U * torch.where(none, 0.0, r.top).abs(), "maximum")
+        within(total, r.total, r.total_off * r.total + 1e-40, "sum")
+        for raw, n in c.kept:
+            assert bool((raw[:32] == 77).all()) and bool((raw[32 + n :] == 77).all())
+
+
 def test_offsets_past_32_bits():
     """Keys and values as columns of rows so long that the last lie past 2^32 elements."""
     require_gpu()
