@@ -354,12 +354,18 @@ def adamw_plan(w: Sequence[torch.Tensor], grad: Sequence[Optional[torch.Tensor]]
     _check(rc, "adamw_plan")
 
 
+_native_adamw_run = _fast("adamw_run")
+
+
 def adamw_run(numel: Sequence[int], w_dt: int, grad_dt: int, bits: int, block: int, lr: float, beta1: float, beta2: float, eps: float, step: int,
               workspace: torch.Tensor, grad_factor: float = 1.0, seed: int = 0, live: Optional[torch.Tensor] = None,
               frozen: Optional[torch.Tensor] = None, floor: float = 0.0, d_out: Optional[torch.Tensor] = None, stream=None) -> None:
     """One step of the planned layers.  ``live`` (float32: lr, step, grad_factor) takes the place of those arguments when the kernel
     runs; ``frozen`` (uint8 or bool) leaves layers out; ``d_out`` receives the layers' distances."""
-    n = numel if isinstance(numel, np.ndarray) and numel.dtype == np.int64 and numel.flags.c_contiguous else _numel_array(numel)
+    rc = _native_adamw_run(numel, w_dt, grad_dt, bits, block, lr, beta1, beta2, eps, step, workspace, grad_factor, seed, live, frozen, floor, d_out, stream)
+    if rc is not NotImplemented:
+        return None if rc is None else _check(rc, "adamw_run")
+    n = _numel_array(numel)
     _require(d_out is None or (d_out.dtype == torch.float32 and d_out.numel() >= n.size))
     _require(live is None or (live.dtype == torch.float32 and live.numel() >= 3))
     _require(frozen is None or (frozen.dtype in (torch.uint8, torch.bool) and frozen.numel() >= n.size))
@@ -1059,6 +1065,9 @@ def _at(t: Optional[torch.Tensor]):
     return C.c_void_p(0 if t is None else t.data_ptr())
 
 
+_native_attention_forward = _fast("attention_forward")
+
+
 def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, layout: int, scale: float, causal: bool, lengths: Optional[torch.Tensor],
                       table: Optional[torch.Tensor], bucket_of: Optional[torch.Tensor], out: torch.Tensor, stats: torch.Tensor,
                       workspace: Optional[torch.Tensor] = None, stream=None) -> None:
@@ -1066,6 +1075,9 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, layout:
     and sum.  HEADS_ROWS: q (batch, q_tokens, q_heads, dim), k and v (batch, k_tokens, kv_heads, dim), contiguous or columns of one
     projection's rows; HEADS_APART: q, the transposed k and v as heads_norm_rotate_forward leaves them.  ``lengths`` (int32): keys of each
     sequence; ``table`` (buckets, q_heads) and ``bucket_of`` (int32, by key - query + q_tokens - 1): the position bias."""
+    rc = _native_attention_forward(q, k, v, layout, scale, causal, lengths, table, bucket_of, out, stats, workspace, stream)
+    if rc is not NotImplemented:
+        return None if rc is None else _check(rc, "attention_forward")
     (B, Tq, Tk, Hq, Hk, D), rows = _attention_sizes(q, k, v, layout, lengths, table, bucket_of)
     _require(out.shape == (B, Tq, Hq, D) and out.dtype == q.dtype and out.is_contiguous())
     _require(stats.dtype == torch.float32 and stats.shape == (B, Hq, Tq, 2) and stats.is_contiguous())
@@ -1081,12 +1093,18 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, layout:
     _check(rc, "attention_forward")
 
 
+_native_attention_backward = _fast("attention_backward")
+
+
 def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, layout: int, scale: float, causal: bool,
                        lengths: Optional[torch.Tensor], table: Optional[torch.Tensor], bucket_of: Optional[torch.Tensor], out: torch.Tensor,
                        stats: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor, dtable: Optional[torch.Tensor] = None,
                        workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """The gradients of q, k, v (laid out like them) and, where it is given, of the table, from out and stats of attention_forward on
     the same operands; the probabilities are formed again."""
+    rc = _native_attention_backward(dout, q, k, v, layout, scale, causal, lengths, table, bucket_of, out, stats, dq, dk, dv, dtable, workspace, stream)
+    if rc is not NotImplemented:
+        return None if rc is None else _check(rc, "attention_backward")
     sizes, rows = _attention_sizes(q, k, v, layout, lengths, table, bucket_of)
     d_sizes, d_rows = _attention_sizes(dq, dk, dv, layout, None, None, None)
     B, Tq, Tk, Hq, Hk, D = sizes

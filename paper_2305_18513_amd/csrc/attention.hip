@@ -8,55 +8,81 @@ namespace {
 
 constexpr int kTurn = 64;
 
-// kt (head, dim, tokens) -> k (head, tokens, dim): a workgroup takes 64 tokens of up to 64 elements
+// kt (head, dim, tokens) -> k (head, tokens, dim): a workgroup takes 64 tokens of up to 64 elements.  Rows of dim begin on 16 bytes,
+// those of tokens where they do (`even`: on 16 bytes too): 16 bytes a thread out, and in where that can be.
 template <typename T>
-__global__ void __launch_bounds__(kAttnThreads) turn_kernel(const T *__restrict__ kt, T *__restrict__ k, int dim, int tokens, int blocks, int columns)
+__global__ void __launch_bounds__(kAttnThreads) turn_kernel(const T *__restrict__ kt, T *__restrict__ k, int dim, int tokens, int blocks, int columns, int even)
 {
-    __shared__ T tile[kTurn][kTurn + 4 / sizeof(T)];
+    constexpr int E = kPerVector<T>, LINE = kTurn / E, LINES = kAttnThreads / LINE;
+    __shared__ T tile[kTurn][kTurn + 4 / sizeof(T)];        // [element][token]: an odd number of banks apart
     const int unit = (int)(blockIdx.x / (unsigned)(blocks * columns)), rest = (int)(blockIdx.x % (unsigned)(blocks * columns));
-    const int t0 = rest / columns * kTurn, d0 = rest % columns * kTurn, x = threadIdx.x % kTurn, y = threadIdx.x / kTurn;
+    const int t0 = rest / columns * kTurn, d0 = rest % columns * kTurn;
     const T *const from = kt + (int64_t)unit * dim * tokens;
     T *const to = k + (int64_t)unit * dim * tokens;
+    if (even) {
+        const int x = threadIdx.x % LINE * E, y = threadIdx.x / LINE;
 #pragma unroll
-    for (int i = 0; i < kTurn; i += kAttnThreads / kTurn)
-        if (d0 + y + i < dim && t0 + x < tokens) tile[y + i][x] = from[(int64_t)(d0 + y + i) * tokens + t0 + x];
+        for (int i = 0; i < kTurn; i += LINES) {
+            if (d0 + y + i >= dim || t0 + x >= tokens) continue;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(from + (int64_t)(d0 + y + i) * tokens + t0 + x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const uint32_t w = v[e * (int)sizeof(T) / 4];
+                if constexpr (sizeof(T) == 4) tile[y + i][x + e] = __builtin_bit_cast(float, w);
+                else tile[y + i][x + e] = (T)(w >> (16 * (e & 1)));
+            }
+        }
+    } else {
+        const int x = threadIdx.x % kTurn, y = threadIdx.x / kTurn;
+#pragma unroll
+        for (int i = 0; i < kTurn; i += kAttnThreads / kTurn)
+            if (d0 + y + i < dim && t0 + x < tokens) tile[y + i][x] = from[(int64_t)(d0 + y + i) * tokens + t0 + x];
+    }
     __syncthreads();
+    const int x = threadIdx.x % LINE * E, y = threadIdx.x / LINE;
 #pragma unroll
-    for (int i = 0; i < kTurn; i += kAttnThreads / kTurn)
-        if (t0 + y + i < tokens && d0 + x < dim) to[(int64_t)(t0 + y + i) * dim + d0 + x] = tile[x][y + i];
+    for (int i = 0; i < kTurn; i += LINES) {
+        if (t0 + y + i >= tokens || d0 + x >= dim) continue;
+        u32x4 v;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if constexpr (sizeof(T) == 4) v[w] = __builtin_bit_cast(uint32_t, tile[x + w][y + i]);
+            else v[w] = (uint32_t)tile[x + 2 * w][y + i] | (uint32_t)tile[x + 2 * w + 1][y + i] << 16;
+        }
+        *reinterpret_cast<u32x4 *>(to + (int64_t)(t0 + y + i) * dim + d0 + x) = v;
+    }
 }
 
-// sums of ds by distance over batch and queries
-__global__ void __launch_bounds__(kAttnThreads) distances_kernel(Attention a, const float *__restrict__ parts, int64_t part_row, int blocks, float *__restrict__ sums)
+// Sums of ds by distance over `each` blocks of 128 queries of all sequences': blockIdx.z has its share, in order.
+__global__ void __launch_bounds__(kAttnThreads) distances_kernel(Attention a, const float *__restrict__ parts, int64_t part_row, int blocks, int each, float *__restrict__ sums)
 {
     const int all = a.q_tokens + a.k_tokens - 1, head = blockIdx.y, at = blockIdx.x * kAttnThreads + threadIdx.x;
     if (at >= all) return;
+    const int end = min(a.batch * blocks, ((int)blockIdx.z + 1) * each);
     double sum = 0.0;
-    for (int b = 0; b < a.batch; ++b) {
-        const int keys = keys_of(a, b);
-        const float *const of = parts + ((int64_t)b * a.q_heads + head) * blocks * kAttnWaves * part_row;
-        for (int block = 0; block < blocks; ++block) {
-            const int written = key_tiles(a, block * kBlock, keys) * kTile + kOwn;
+    for (int n = (int)blockIdx.z * each; n < end; ++n) {
+        const int b = n / blocks, block = n % blocks, written = key_tiles(a, block * kBlock, keys_of(a, b)) * kTile + kOwn;
+        const float *const of = parts + (((int64_t)b * a.q_heads + head) * blocks + block) * kAttnWaves * part_row;
 #pragma unroll
-            for (int w = 0; w < kAttnWaves; ++w) {
-                const int place = at - (a.q_tokens - 1) + block * kBlock + w * kOwn + kOwn - 1;
-                if (place >= 0 && place < written) sum += (double)of[(int64_t)(block * kAttnWaves + w) * part_row + place];
-            }
+        for (int w = 0; w < kAttnWaves; ++w) {
+            const int place = at - (a.q_tokens - 1) + block * kBlock + w * kOwn + kOwn - 1;
+            if (place >= 0 && place < written) sum += (double)of[w * part_row + place];
         }
     }
-    sums[(int64_t)head * all + at] = (float)sum;
+    sums[((int64_t)blockIdx.z * a.q_heads + head) * all + at] = (float)sum;
 }
 
 // a workgroup for each bucket and head
 template <typename T>
-__global__ void __launch_bounds__(kAttnThreads) buckets_kernel(Attention a, const float *__restrict__ sums, T *__restrict__ dtable)
+__global__ void __launch_bounds__(kAttnThreads) buckets_kernel(Attention a, const float *__restrict__ sums, int shares, T *__restrict__ dtable)
 {
     __shared__ double part[kAttnWaves];
     const int all = a.q_tokens + a.k_tokens - 1, bucket = blockIdx.x, head = blockIdx.y;
     double sum = 0.0;
-    if (a.batch > 0 && a.q_tokens > 0)                      // (no sums otherwise)
+    if (shares > 0)                                         // (no sums otherwise)
         for (int at = threadIdx.x; at < all; at += kAttnThreads)
-            if (a.bucket_of[at] == bucket) sum += (double)sums[(int64_t)head * all + at];
+            if (a.bucket_of[at] == bucket)
+                for (int z = 0; z < shares; ++z) sum += (double)sums[((int64_t)z * a.q_heads + head) * all + at];
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, kWave);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
@@ -93,9 +119,15 @@ int32_t check_sizes(const Sizes &z)
 
 bool turned(const Sizes &z) { return z.layout == SLIMFIT_HEADS_APART && z.batch > 0 && z.k_tokens > 0 && z.q_tokens > 0; }
 size_t turned_bytes(const Sizes &z) { return turned(z) ? rounded((size_t)z.k_count() * z.e()) : 0; }
-int64_t part_row(const Sizes &z) { return ((int64_t)z.k_tokens + kTile - 1) / kTile * kTile + kTile; }
-
 int q_blocks(const Sizes &z) { return (z.q_tokens + kBlock - 1) / kBlock; }
+// blocks of queries that one share of the sums by distance adds up (16 x 512, 12 heads: 64 in one share 57 us, 8 each 6.6), and the shares
+int64_t share_of(const Sizes &z)
+{
+    const int64_t all = z.batch * q_blocks(z);
+    return all <= 8 * 32 ? 8 : (all + 31) / 32;
+}
+int64_t shares_of(const Sizes &z) { return (z.batch * q_blocks(z) + share_of(z) - 1) / share_of(z); }
+int64_t part_row(const Sizes &z) { return ((int64_t)z.k_tokens + kTile - 1) / kTile * kTile + kTile; }
 
 // How many workgroups share a sequence's keys out, or 0: 128 queries of a head a workgroup.  (us with those, with few queries)
 //   bf16, up to 16 queries: 16 x 4096 keys, 32 heads on 8 by 128: 1 query 121, 48; 16 132, 63; 32 139, 120; 64 142, 243;
@@ -130,7 +162,7 @@ struct BackwardPlaces {
         rows = turned_bytes(z);
         parts = rows + rounded((size_t)(z.batch * z.q_heads) * (size_t)z.q_tokens * 12);
         sums = parts + (table ? rounded((size_t)(z.batch * z.q_heads) * (size_t)q_blocks(z) * kAttnWaves * (size_t)part_row(z) * 4) : 0);
-        bytes = sums + (table ? rounded((size_t)z.q_heads * ((size_t)z.q_tokens + (size_t)z.k_tokens) * 4) : 0);
+        bytes = sums + (table ? rounded((size_t)shares_of(z) * (size_t)z.q_heads * ((size_t)z.q_tokens + (size_t)z.k_tokens) * 4) : 0);
     }
 };
 
@@ -224,10 +256,10 @@ int32_t check_workspace(size_t need, const void *ws, size_t bytes)
 
 void turn_keys(const Sizes &z, const void *kt, void *k, hipStream_t st)
 {
-    const int blocks = (z.k_tokens + kTurn - 1) / kTurn, columns = (z.head_dim + kTurn - 1) / kTurn;
+    const int blocks = (z.k_tokens + kTurn - 1) / kTurn, columns = (z.head_dim + kTurn - 1) / kTurn, even = z.k_tokens % (16 / (int)z.e()) == 0;
     const unsigned grid = (unsigned)(z.batch * z.kv_heads * blocks * columns);
-    if (z.dt == SLIMFIT_F32) launch(turn_kernel<float>, grid, kAttnThreads, 0, st, static_cast<const float *>(kt), static_cast<float *>(k), z.head_dim, z.k_tokens, blocks, columns);
-    else launch(turn_kernel<uint16_t>, grid, kAttnThreads, 0, st, static_cast<const uint16_t *>(kt), static_cast<uint16_t *>(k), z.head_dim, z.k_tokens, blocks, columns);
+    if (z.dt == SLIMFIT_F32) launch(turn_kernel<float>, grid, kAttnThreads, 0, st, static_cast<const float *>(kt), static_cast<float *>(k), z.head_dim, z.k_tokens, blocks, columns, even);
+    else launch(turn_kernel<uint16_t>, grid, kAttnThreads, 0, st, static_cast<const uint16_t *>(kt), static_cast<uint16_t *>(k), z.head_dim, z.k_tokens, blocks, columns, even);
 }
 
 Attention attention_of(const Sizes &z, const void *q, const void *k, const void *v, int64_t q_row, int64_t k_row, int64_t v_row, float scale, int32_t causal,
@@ -331,12 +363,13 @@ extern "C" int32_t slimfit_attention_backward(const void *dout, const void *q, c
     if (dtable) {
         float *const sums = reinterpret_cast<float *>(ws + at.sums);
         const int all = q_tokens + k_tokens - 1;
-        if (parts) launch(distances_kernel, dim3((unsigned)((all + kAttnThreads - 1) / kAttnThreads), (unsigned)q_heads), kAttnThreads, 0, st, a, parts, g.part_row, q_blocks(z), sums);
-        Attention b = a;
-        if (!pairs) b.batch = 0;
+        const int shares = parts ? (int)shares_of(z) : 0;
+        if (parts)
+            launch(distances_kernel, dim3((unsigned)((all + kAttnThreads - 1) / kAttnThreads), (unsigned)q_heads, (unsigned)shares), kAttnThreads, 0, st, a, parts, g.part_row,
+                   q_blocks(z), (int)share_of(z), sums);
         const dim3 grid((unsigned)buckets, (unsigned)q_heads);
-        if (dt == SLIMFIT_BF16) launch(buckets_kernel<uint16_t>, grid, kAttnThreads, 0, st, b, sums, static_cast<uint16_t *>(dtable));
-        else launch(buckets_kernel<float>, grid, kAttnThreads, 0, st, b, sums, static_cast<float *>(dtable));
+        if (dt == SLIMFIT_BF16) launch(buckets_kernel<uint16_t>, grid, kAttnThreads, 0, st, a, sums, shares, static_cast<uint16_t *>(dtable));
+        else launch(buckets_kernel<float>, grid, kAttnThreads, 0, st, a, sums, shares, static_cast<float *>(dtable));
     }
     return launch_status();
 }

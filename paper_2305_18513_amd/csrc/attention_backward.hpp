@@ -27,6 +27,7 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
     __shared__ __align__(1024) char tiles[2][2 * kTileBytes<T, D>];
     __shared__ float column[BIAS ? kMostBuckets : 1], biases[2][BIAS ? kDistances : 1];
     __shared__ __align__(16) float skew[PARTS ? kAttnWaves : 1][PARTS ? kOwn * kSkew : 1];
+    __shared__ int buckets[2][PARTS ? kDistances : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int group = a.q_heads / a.kv_heads;
     const Place place(a.batch * a.kv_heads, blocks, group, a.causal != 0);
@@ -55,6 +56,8 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
         kl.land(tiles[t & 1]);
         vl.land(tiles[t & 1] + kTileBytes<T, D>);
         if constexpr (BIAS) bl.store(a, column, biases[t & 1]);
+        if constexpr (PARTS)
+            if (threadIdx.x < kDistances) buckets[t & 1][threadIdx.x] = bl.bucket;
         kl.landed();
     };
 
@@ -133,24 +136,41 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
                     for (int r = 0; r < 16; ++r) s[r] = row_of(r, 0) < some ? s[r] : 0.0f;
                 }
                 if constexpr (PARTS) {
-                    // Sums along the diagonals: lane l has that of key - query = l - 31 (within 32 keys and the wave's queries); what the upper
-                    // lanes have the next 32 keys see 32 lower.
+                    // Sums by distance, key - query.  Within 32 keys and the wave's 32 queries lane l has those of l - 31 (lower) and of l + 1
+                    // (upper), which the next 32 keys see 32 lower.  Where all 63 are of one bucket, as far ones are, their sum goes to one of them.
+                    const int *const b = buckets[t & 1] + kBlock - kOwn - wave * kOwn + 32 * n;
+                    const int mine_of = b[min(lane, 62)];
+                    float lower = 0.0f, upper = 0.0f;
+                    if (__builtin_amdgcn_ballot_w64(mine_of != __builtin_amdgcn_readfirstlane(mine_of)) == 0u) {
+                        float x[16];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        *reinterpret_cast<f32x4 *>(&skew[wave][(lane & 31) * kSkew + 8 * c + 4 * half]) = f32x4{s[4 * c], s[4 * c + 1], s[4 * c + 2], s[4 * c + 3]};
-                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                    __builtin_amdgcn_wave_barrier();
-                    float now = 0.0f;
+                        for (int r = 0; r < 16; ++r) x[r] = s[r];
 #pragma unroll
-                    for (int m = 0; m < kOwn; ++m) {
-                        const int key = lane - 31 + m;
-                        const float x = skew[wave][m * kSkew + (key & 31)];
-                        now += key == (key & 31) ? x : 0.0f;
+                        for (int w = 8; w >= 1; w >>= 1)
+#pragma unroll
+                            for (int r = 0; r < w; ++r) x[r] += x[r + w];
+                        const float all_of = group_sum_f32(x[0], kWave);
+                        lower = lane == 0 ? all_of : 0.0f;
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            *reinterpret_cast<f32x4 *>(&skew[wave][(lane & 31) * kSkew + 8 * c + 4 * half]) = f32x4{s[4 * c], s[4 * c + 1], s[4 * c + 2], s[4 * c + 3]};
+                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                        for (int m = 0; m < kOwn / 2; ++m) {                  // half of the queries each half of the wave
+                            const int query = 16 * half + m, key = (lane & 31) + query + 1;
+                            const float x = skew[wave][query * kSkew + (key & 31)];
+                            upper += key < 32 ? x : 0.0f;
+                            lower += key < 32 ? 0.0f : x;
+                        }
+                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                        __builtin_amdgcn_wave_barrier();
+                        lower = both_sum(lower);
+                        upper = both_sum(upper);
                     }
-                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                    __builtin_amdgcn_wave_barrier();
-                    if (half == 0) part[k0 + 32 * n + lane] = now + carry;
-                    carry = __shfl_xor(now, 32, kWave);
+                    if (half == 0) part[k0 + 32 * n + lane] = lower + carry;
+                    carry = upper;
                 }
                 sums<T, D>(tile, 32 * n, s, dq);
             }

@@ -32,7 +32,8 @@ namespace {
     X(layernorm_backward_dequant) X(layernorm_param_grads) X(layernorm_param_grads_workspace) X(layer_delta_run)         \
     X(split_heads) X(merge_heads) X(product) X(gated_quant_pack) X(gated_backward_dequant)                             \
     X(heads_norm_rotate_forward) X(heads_norm_rotate_backward) X(heads_norm_rotate_workspace)                          \
-    X(weight_grad_dequant) X(weight_grad_dequant_workspace)
+    X(weight_grad_dequant) X(weight_grad_dequant_workspace)                                                            \
+    X(attention_forward) X(attention_backward) X(attention_workspace) X(adamw_run)
 #define X(name) decltype(&slimfit_##name) name##_fn = nullptr;
 SLIMFIT_CALLS(X)
 #undef X
@@ -51,7 +52,7 @@ struct Args {
         --left;
         return *at++;
     }
-    const at::Tensor *tensor()
+    const at::Tensor *tensor(bool strided = false)
     {
         PyObject *o = next();
         if (!THPVariable_CheckExact(o)) { ok = false; return nullptr; }
@@ -61,7 +62,7 @@ struct Args {
                                                c10::DispatchKey::Functionalize, c10::DispatchKey::Negative,
                                                c10::DispatchKey::Conjugate, c10::DispatchKey::ZeroTensor});
         if (!t.defined() || !t.is_cuda() || t.layout() != c10::kStrided || t.key_set().has_any(wrapped) || !t.has_storage() ||
-            !t.is_contiguous()) {
+            (!strided && !t.is_contiguous())) {
             ok = false;
             return nullptr;
         }
@@ -87,15 +88,16 @@ struct Args {
         if (v < INT32_MIN || v > INT32_MAX) { ok = false; return 0; }
         return (int32_t)v;
     }
-    float f32()
+    double f64()
     {
         PyObject *o = next();
-        if (PyFloat_CheckExact(o)) return (float)PyFloat_AS_DOUBLE(o);
-        if (!PyLong_Check(o)) { ok = false; return 0.0f; }
+        if (PyFloat_CheckExact(o)) return PyFloat_AS_DOUBLE(o);
+        if (!PyLong_Check(o)) { ok = false; return 0.0; }
         const double v = PyLong_AsDouble(o);
         if (v == -1.0 && PyErr_Occurred()) { PyErr_Clear(); ok = false; }
-        return (float)v;
+        return v;
     }
+    float f32() { return (float)f64(); }
     int32_t truth()                                         // what bool() makes of it
     {
         const int v = PyObject_IsTrue(next());
@@ -748,6 +750,148 @@ PyObject *heads_norm_rotate_backward(PyObject *, PyObject *const *args, Py_ssize
                                               gqp, gkp, tp, h.positions, h.rotary, pairing, ip, q_scale, op, dgqp, dgkp, w.at, w.bytes, st));
 }
 
+// What attention's two calls share: sizes, row lengths, and that tensors agree with them (strided operands are columns of rows).
+struct Attended {
+    int64_t B, Tq, Tk, Hq, Hk, D, row[3] = {0, 0, 0};
+    int32_t buckets = 0;
+    static bool row_of(const at::Tensor *t, int64_t tokens, int64_t heads, int64_t dim, int64_t &row)
+    {
+        row = heads * dim;
+        if (t->numel() == 0) return true;
+        const auto s = t->strides();
+        const int64_t batch = t->size(0);
+        row = tokens > 1 ? s[1] : batch > 1 ? s[0] : heads * dim;
+        return (s[3] == 1 || dim == 1) && (s[2] == dim || heads == 1) && (batch <= 1 || s[0] == tokens * row);
+    }
+    bool read(const at::Tensor *q, const at::Tensor *k, const at::Tensor *v, int32_t layout, const at::Tensor *lengths, const at::Tensor *table, const at::Tensor *of)
+    {
+        if (q->dim() != 4 || k->dim() != 4 || v->dim() != 4 || !activation(q) || !same_type(q, k) || !same_type(q, v)) return false;
+        B = q->size(0), D = q->size(3);
+        if (layout == SLIMFIT_HEADS_ROWS) {
+            Tq = q->size(1), Hq = q->size(2), Tk = k->size(1), Hk = k->size(2);
+            if (k->size(0) != B || k->size(3) != D || v->sizes() != k->sizes()) return false;
+            if (!row_of(q, Tq, Hq, D, row[0]) || !row_of(k, Tk, Hk, D, row[1]) || !row_of(v, Tk, Hk, D, row[2])) return false;
+        } else if (layout == SLIMFIT_HEADS_APART) {
+            Hq = q->size(1), Tq = q->size(2), Hk = v->size(1), Tk = v->size(2);
+            if (v->size(0) != B || v->size(3) != D || k->size(0) != B || k->size(1) != Hk || k->size(2) != D || k->size(3) != Tk) return false;
+            if (!q->is_contiguous() || !k->is_contiguous() || !v->is_contiguous()) return false;
+        } else {
+            return false;
+        }
+        if (Tq > INT32_MAX || Tk > INT32_MAX || Hq > INT32_MAX || Hk > INT32_MAX || D > INT32_MAX) return false;
+        if (lengths && (!is(lengths, at::kInt) || lengths->numel() < B)) return false;
+        if (table) {
+            if (table->dim() != 2 || table->size(1) != Hq || table->size(0) > INT32_MAX || !same_type(table, q)) return false;
+            if (!of || !is(of, at::kInt) || of->numel() < Tq + Tk - 1) return false;
+            buckets = (int32_t)table->size(0);
+        }
+        return true;
+    }
+    bool rows(const at::Tensor *t, const at::Tensor *q) const
+    {
+        return t->dim() == 4 && t->size(0) == B && t->size(1) == Tq && t->size(2) == Hq && t->size(3) == D && same_type(t, q);
+    }
+    bool stats_fit(const at::Tensor *t) const
+    {
+        return f32(t) && t->dim() == 4 && t->size(0) == B && t->size(1) == Hq && t->size(2) == Tq && t->size(3) == 2;
+    }
+    bool need(const at::Tensor *q, int32_t layout, bool dtable, bool backward, size_t &bytes) const
+    {
+        return attention_workspace_fn(dtype_of(q), layout, B, (int32_t)Tq, (int32_t)Tk, (int32_t)Hq, (int32_t)Hk, (int32_t)D, dtable, backward, &bytes) == SLIMFIT_OK;
+    }
+};
+
+PyObject *attention_forward(PyObject *, PyObject *const *args, Py_ssize_t n_args)
+{
+    Args a(args, n_args, 13);
+    const at::Tensor *q = a.tensor(true), *k = a.tensor(true), *v = a.tensor(true);
+    const int32_t layout = a.i32();
+    const float scale = a.f32();
+    const int32_t causal = a.truth();
+    const at::Tensor *lengths = a.tensor_or_none(), *table = a.tensor_or_none(), *of = a.tensor_or_none(), *out = a.tensor(), *stats = a.tensor(),
+                     *workspace = a.tensor_or_none();
+    void *st = a.stream();
+    Attended z;
+    size_t need = 0;
+    if (a.ok)
+        a.need(z.read(q, k, v, layout, lengths, table, of) && z.rows(out, q) && z.stats_fit(stats) &&
+               here(q, k, v, lengths, table, table ? of : nullptr, out, stats, workspace) && z.need(q, layout, false, false, need));
+    Scratch w;
+    if (!a.ok || ((need > 0 || workspace) && !w.take(workspace, a.own_stream, need, q))) return general();
+    const void *qp = ptr(q), *kp = ptr(k), *vp = ptr(v), *tp = ptr(table);
+    const int32_t *lp = ptr<int32_t>(lengths), *bp = table ? ptr<int32_t>(of) : nullptr;
+    void *op = ptr(out);
+    float *sp = ptr<float>(stats);
+    const int32_t dt = dtype_of(q);
+    SLIMFIT_RUN(attention_forward_fn(qp, kp, vp, dt, layout, z.row[0], z.row[1], z.row[2], z.B, (int32_t)z.Tq, (int32_t)z.Tk, (int32_t)z.Hq, (int32_t)z.Hk,
+                                     (int32_t)z.D, scale, causal, lp, tp, z.buckets, bp, op, sp, w.at, w.bytes, st));
+}
+
+PyObject *attention_backward(PyObject *, PyObject *const *args, Py_ssize_t n_args)
+{
+    Args a(args, n_args, 18);
+    const at::Tensor *dout = a.tensor(), *q = a.tensor(true), *k = a.tensor(true), *v = a.tensor(true);
+    const int32_t layout = a.i32();
+    const float scale = a.f32();
+    const int32_t causal = a.truth();
+    const at::Tensor *lengths = a.tensor_or_none(), *table = a.tensor_or_none(), *of = a.tensor_or_none(), *out = a.tensor(), *stats = a.tensor(),
+                     *dq = a.tensor(true), *dk = a.tensor(true), *dv = a.tensor(true), *dtable = a.tensor_or_none(), *workspace = a.tensor_or_none();
+    void *st = a.stream();
+    Attended z, d;
+    size_t need = 0;
+    if (a.ok)
+        a.need(z.read(q, k, v, layout, lengths, table, of) && d.read(dq, dk, dv, layout, nullptr, nullptr, nullptr) && same_type(q, dq) &&
+               dq->sizes() == q->sizes() && dk->sizes() == k->sizes() && dv->sizes() == v->sizes() && z.rows(out, q) && z.rows(dout, q) && z.stats_fit(stats) &&
+               (!dtable || (table && dtable->sizes() == table->sizes() && same_type(dtable, table))) &&
+               here(dout, q, k, v, lengths, table, table ? of : nullptr, out, stats, dq, dk, dv, dtable, workspace) &&
+               z.need(q, layout, dtable != nullptr, true, need));
+    Scratch w;
+    if (!a.ok || !w.take(workspace, a.own_stream, need, q)) return general();
+    const void *gp = ptr(dout), *qp = ptr(q), *kp = ptr(k), *vp = ptr(v), *tp = ptr(table), *op = ptr(out);
+    const int32_t *lp = ptr<int32_t>(lengths), *bp = table ? ptr<int32_t>(of) : nullptr;
+    const float *sp = ptr<float>(stats);
+    void *dqp = ptr(dq), *dkp = ptr(dk), *dvp = ptr(dv), *dtp = ptr(dtable);
+    const int32_t dt = dtype_of(q);
+    SLIMFIT_RUN(attention_backward_fn(gp, qp, kp, vp, dt, layout, z.row[0], z.row[1], z.row[2], z.B, (int32_t)z.Tq, (int32_t)z.Tk, (int32_t)z.Hq, (int32_t)z.Hk,
+                                      (int32_t)z.D, scale, causal, lp, tp, z.buckets, bp, op, sp, dqp, dkp, dvp, d.row[0], d.row[1], d.row[2], dtp, w.at, w.bytes,
+                                      st));
+}
+
+PyObject *adamw_run(PyObject *, PyObject *const *args, Py_ssize_t n_args)
+{
+    Args a(args, n_args, 18);
+    PyObject *numel = a.next();
+    const int32_t w_dt = a.i32(), grad_dt = a.i32(), bits = a.i32(), block = a.i32();
+    const double lr = a.f64(), beta1 = a.f64(), beta2 = a.f64(), eps = a.f64();
+    const int64_t step = a.i64();
+    const at::Tensor *workspace = a.tensor();
+    const float factor = a.f32();
+    const int64_t seed = a.i64();
+    const at::Tensor *live = a.tensor_or_none(), *frozen = a.tensor_or_none();
+    const float floor = a.f32();
+    const at::Tensor *d = a.tensor_or_none();
+    void *st = a.stream();
+    a.need(PyList_CheckExact(numel) || PyTuple_CheckExact(numel));
+    std::vector<int64_t> sizes;
+    if (a.ok) {
+        const Py_ssize_t L = PySequence_Fast_GET_SIZE(numel);
+        a.need(L > 0 && L <= INT32_MAX && is(workspace, at::kByte) && (!d || (f32(d) && d->numel() >= L)) && (!live || (f32(live) && live->numel() >= 3)) &&
+               (!frozen || ((is(frozen, at::kByte) || is(frozen, at::kBool)) && frozen->numel() >= L)) && here(workspace, live, frozen, d));
+        Args each(PySequence_Fast_ITEMS(numel), L, L);
+        sizes.reserve((size_t)L);
+        for (Py_ssize_t i = 0; i < L && a.ok; ++i) sizes.push_back(each.i64());
+        a.need(each.ok);
+    }
+    if (!a.ok) return general();
+    const float *lp = ptr<float>(live);
+    const uint8_t *fp = ptr<uint8_t>(frozen);
+    float *dp = ptr<float>(d);
+    void *wp = ptr(workspace);
+    const size_t bytes = workspace->nbytes();
+    SLIMFIT_RUN(adamw_run_fn(sizes.data(), (int32_t)sizes.size(), w_dt, grad_dt, bits, block, lr, beta1, beta2, eps, step, factor, (uint32_t)seed, lp, fp, floor, dp,
+                             wp, bytes, st));
+}
+
 // a C++ exception must not cross into the interpreter (torch's allocator raises one when memory runs out: the general
 // path, which asks again, raises torch's own)
 template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)>
@@ -763,7 +907,7 @@ PyObject *guarded(PyObject *self, PyObject *const *args, Py_ssize_t n)
 // bind(addresses): the library's functions in the order of CALLS
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
-    void *address[32];
+    void *address[40];
     Py_ssize_t want = 0;
 #define X(name) ++want;
     SLIMFIT_CALLS(X)
@@ -792,7 +936,7 @@ PyMethodDef methods[] = {
     METHOD(layernorm_forward), METHOD(layernorm_backward), METHOD(layernorm_backward_pruned), METHOD(layernorm_forward_quant_pack),
     METHOD(layernorm_backward_dequant), METHOD(layernorm_param_grads), METHOD(layer_delta_run), METHOD(split_heads), METHOD(merge_heads),
     METHOD(product), METHOD(gated_quant_pack), METHOD(gated_backward_dequant), METHOD(heads_norm_rotate_forward),
-    METHOD(heads_norm_rotate_backward), METHOD(weight_grad_dequant),
+    METHOD(heads_norm_rotate_backward), METHOD(weight_grad_dequant), METHOD(attention_forward), METHOD(attention_backward), METHOD(adamw_run),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
