@@ -262,10 +262,15 @@ __device__ __forceinline__ f32x16 dots_of(const char *tile, int first, const cha
     return s;
 }
 
-// both halves of a tile, whose products do not wait for one another
+// both halves of a tile, whose products do not wait for one another; fp32, where products are what takes the time: as many as `halves`
 template <typename T, int D>
-__device__ __forceinline__ void dots2(const char *tile, const Own<T, D> &own, f32x16 (&s)[2])
+__device__ __forceinline__ void dots2(const char *tile, const Own<T, D> &own, f32x16 (&s)[2], int halves)
 {
+    if constexpr (sizeof(T) == 4) {
+        s[0] = halves > 0 ? dots<T, D>(tile, 0, own) : zeros16();
+        s[1] = halves > 1 ? dots<T, D>(tile, 32, own) : zeros16();
+        return;
+    }
     const int lane = threadIdx.x & 63;
     const char *at = tile + (lane & 31) * kPitch<T, D>;
     const int turn = turn_of<T, D>(lane & 31);

@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
     const T *const k = static_cast<const T *>(a.k.at) + batch * a.k.b + kv * a.k.h;
     const T *const v = static_cast<const T *>(a.v.at) + batch * a.v.b + kv * a.v.h;
     const int keys = keys_of(a, batch), count = key_tiles(a, q0, keys);
-    const int seen = seen_by(a, i, keys), all_see = seen_by(a, mine, keys), any_sees = seen_by(a, min(mine + kOwn, a.q_tokens) - 1, keys);
+    const int seen = seen_by(a, i, keys), all_see = seen_by(a, mine, keys), any_sees = mine < a.q_tokens ? seen_by(a, min(mine + kOwn, a.q_tokens) - 1, keys) : 0;
     const float scale = a.scale * kLog2e;
 
     Tiles<T, D> kl, vl;
@@ -122,6 +122,8 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
         if (k0 < any_sees) {
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
+                // (products are what takes fp32's time; with the sums by distance every half is gone through)
+                if (sizeof(T) == 4 && !PARTS && k0 + 32 * n >= any_sees) continue;
                 f32x16 s = dots<T, D>(tile, 32 * n, own);
                 const f32x16 dp = dots<T, D>(tile + kTileBytes<T, D>, 32 * n, grad);
                 const float *const b = biases[BIAS ? t & 1 : 0] + kBlock - 1 - (i - q0) + 4 * half + 32 * n;
@@ -189,7 +191,7 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
 template <typename T, int D> constexpr bool kValuesInLds = sizeof(T) == 2 && D > 64;
 
 template <typename T, int D, bool BIAS>
-__global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 32 ? 1 : 2) keys_kernel(Attention a, Gradients g, int blocks)
+__global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2) keys_kernel(Attention a, Gradients g, int blocks)
 {
     constexpr int ROWS = kValuesInLds<T, D> ? 32 : kTile, BYTES = ROWS * kPitch<T, D>;
     __shared__ __align__(1024) char tiles[2][2 * BYTES], values[kValuesInLds<T, D> ? kBlock * kPitch<T, D> : 16];
@@ -284,7 +286,8 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 32 ? 1 : 2
 #pragma unroll
         for (int n = 0; n < ROWS / 32; ++n) {
             const int first = here + 32 * n;                // of 32 queries
-            if (sizeof(T) == 4 && a.causal && first + 31 + offset < mine) continue;      // none of them sees any of the wave's keys
+            // none of them sees any of the wave's keys, or none is there (products are what takes fp32's time)
+            if (sizeof(T) == 4 && (mine >= keys || first >= a.q_tokens || (a.causal && first + 31 + offset < mine))) continue;
             f32x16 s = dots<T, D>(tile, 32 * n, own);
             f32x16 dp;
             if constexpr (kValuesInLds<T, D>) dp = dots_of<T, D>(tile + BYTES, 32 * n, values + wave * kOwn * kPitch<T, D>);

@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
     const T *const k = static_cast<const T *>(a.k.at) + batch * a.k.b + kv * a.k.h;
     const T *const v = static_cast<const T *>(a.v.at) + batch * a.v.b + kv * a.v.h;
     const int keys = keys_of(a, batch), count = key_tiles(a, q0, keys);
-    const int seen = seen_by(a, i, keys), all_see = seen_by(a, mine, keys), any_sees = seen_by(a, min(mine + kOwn, a.q_tokens) - 1, keys);
+    const int seen = seen_by(a, i, keys), all_see = seen_by(a, mine, keys), any_sees = mine < a.q_tokens ? seen_by(a, min(mine + kOwn, a.q_tokens) - 1, keys) : 0;
     const float scale = a.scale * kLog2e;
 
     Own<T, D> own;
@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
             land_bias(0);
         }
         kl.landed();
-        dots2<T, D>(keys_lds[0], own, s[0]);
+        dots2<T, D>(keys_lds[0], own, s[0], (any_sees + 31) / 32);
         __syncthreads();
     }
     auto step = [&](int t, f32x16 (&s)[2], f32x16 (&next)[2]) {
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
                 base = top;
             }
             const float safe = base == -__builtin_inff() ? 0.0f : base, less = -safe * scale;
-            dots2<T, D>(keys_lds[(t + 1) & 1], own, next);           // (past the last tile: of keys that are not there, unused)
+            dots2<T, D>(keys_lds[(t + 1) & 1], own, next, (any_sees - k0 - kTile + 31) / 32);           // (past the last tile: of keys that are not there, unused)
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
 #pragma unroll
@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
                     s[n][r] = __builtin_amdgcn_exp2f(BIAS ? (s[n][r] - safe) * kLog2e : __builtin_fmaf(s[n][r], scale, less));
                     total += s[n][r];
                 }
-                sums<T, D>(values_lds[t & 1], 32 * n, s[n], o);
+                if (sizeof(T) == 2 || k0 + 32 * n < any_sees) sums<T, D>(values_lds[t & 1], 32 * n, s[n], o);
             }
             if constexpr (sizeof(T) == 2) {                 // products, reads and exponentials in turn: 402 us without, 373 with (2048 x 2048 by 128, 256 heads)
                 __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
