@@ -34,6 +34,11 @@ fp32 operands of sizes at which it is the quicker one, and torch's otherwise.
                      turned by its token's position in the same pass; caches the
                      query and key columns in `bits` bits (0: keeps the rows
                      themselves) and rstd; norms that are frozen get no gradients.
+  AttentionFunction  softmax(scale q k^T + bias) v over rows of any length, the probabilities formed
+                     again in the backward pass: it keeps its operands, its output and
+                     two numbers a query.  The bias is a learned table by buckets of the
+                     distance, or none; a frozen table gets no gradient.
+  SelfAttentionFunction  the same from the rows of a QKV projection, as they lie.
   SplitHeadsFunction (q, k^T, v) of the attention products from the rows of a QKV
                      projection in one pass, their gradients back in another.
   MatmulFunction     out = a @ b with both operands cached in 8 bits (the paper's
@@ -368,6 +373,69 @@ class HeadsNormRotateFunction(torch.autograd.Function):
         return (dqkv, dgamma_q, dgamma_k) + (None,) * 9
 
 
+def _attend(ctx, q, k, v, layout, scale, causal, lengths, table, bucket_of, saved):
+    """One forward pass; keeps what the backward pass reads (``saved``: what q, k and v are parts of) where it is asked for."""
+    apart = layout == sf.HEADS_APART
+    B, Tq, Hq, D = (q.shape[i] for i in ((0, 2, 1, 3) if apart else (0, 1, 2, 3)))
+    out = torch.empty(B, Tq, Hq, D, dtype=q.dtype, device=q.device)
+    stats = torch.empty(B, Hq, Tq, 2, dtype=torch.float32, device=q.device)
+    table = None if table is None else table.contiguous()
+    sf.attention_forward(q, k, v, layout, scale, causal, lengths, table, bucket_of, out, stats)
+    if any(ctx.needs_input_grad) and _recorded(ctx):
+        ctx.save_for_backward(*saved, out, stats, lengths, table, bucket_of)
+    return out
+
+
+class AttentionFunction(torch.autograd.Function):
+    """out (B, q_tokens, heads, D) of q, k, v.  layout binding.HEADS_ROWS: (B, tokens, heads, D) each; HEADS_APART: (q, k^T, v) as
+    SplitHeadsFunction and HeadsNormRotateFunction give them.  causal: query i sees keys j <= i + k_tokens - q_tokens.  lengths
+    (int32, B): keys of each sequence.  table (buckets, heads) and bucket_of: binding.attention_forward, binding.distance_buckets."""
+
+    @staticmethod
+    def forward(ctx, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, causal: bool = False, lengths=None, table=None, bucket_of=None,
+                layout: int = sf.HEADS_ROWS):
+        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+        ctx.meta = (scale, causal, layout)
+        return _attend(ctx, q, k, v, layout, scale, causal, lengths, table, bucket_of, (q, k, v))
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout: torch.Tensor):
+        q, k, v, out, stats, lengths, table, bucket_of = ctx.saved_tensors
+        scale, causal, layout = ctx.meta
+        dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+        dtable = torch.empty_like(table) if table is not None and ctx.needs_input_grad[6] else None
+        sf.attention_backward(dout.contiguous(), q, k, v, layout, scale, causal, lengths, table, bucket_of, out, stats, dq, dk, dv, dtable)
+        return dq, dk, dv, None, None, None, dtable, None, None
+
+
+class SelfAttentionFunction(torch.autograd.Function):
+    """AttentionFunction on the rows (B, T, (heads + 2 * kv_heads) * D) of a QKV projection: queries, keys and values are its columns, the
+    gradients come as rows of the same kind, and out is the rows (B, T, heads * D) that the next projection takes."""
+
+    @staticmethod
+    def forward(ctx, qkv: torch.Tensor, heads: int, kv_heads: int, scale: float, causal: bool = False, lengths=None, table=None, bucket_of=None):
+        B, T, width = qkv.shape
+        qkv = qkv.contiguous()
+        rows = qkv.view(B, T, heads + 2 * kv_heads, width // (heads + 2 * kv_heads))
+        ctx.meta = (heads, kv_heads, scale, causal)
+        out = _attend(ctx, *rows.split((heads, kv_heads, kv_heads), 2), sf.HEADS_ROWS, scale, causal, lengths, table, bucket_of, (qkv,))
+        return out.view(B, T, -1)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout: torch.Tensor):
+        qkv, out, stats, lengths, table, bucket_of = ctx.saved_tensors
+        heads, kv_heads, scale, causal = ctx.meta
+        B, T, width = qkv.shape
+        dqkv = torch.empty_like(qkv)
+        parts = [t.view(B, T, heads + 2 * kv_heads, -1).split((heads, kv_heads, kv_heads), 2) for t in (qkv, dqkv)]
+        dtable = torch.empty_like(table) if table is not None and ctx.needs_input_grad[6] else None
+        sf.attention_backward(dout.contiguous().view(out.shape), *parts[0], sf.HEADS_ROWS, scale, causal, lengths, table, bucket_of, out, stats, *parts[1],
+                              dtable)
+        return dqkv, None, None, None, None, None, dtable, None
+
+
 def _plain(t: torch.Tensor) -> bool:
     """Whether a kernel may be handed the tensor's memory as it is."""
     return (type(t) in (torch.Tensor, torch.nn.Parameter) and torch._C._has_storage(t) and t.is_cuda
@@ -511,10 +579,12 @@ def encoder_block_params(hidden: int, device="cuda", seed: int = 0, dtype=torch.
 
 
 def frozen_encoder_block(x: torch.Tensor, p: dict, heads: int, wrapped: bool, keep_ppm: int = 100000,
-                         gelu_bits: int = 4, block: int = 64) -> torch.Tensor:
+                         gelu_bits: int = 4, block: int = 64, recompute: bool = False, lengths=None, bias_table=None, bucket_of=None) -> torch.Tensor:
     """One pre-LN encoder block whose layers are all frozen: with ``wrapped`` the activations kept
     for the backward pass are the compressed ones (pruned LayerNorm input, pruned attention probabilities shared by
-    Softmax and MatMul, 4-bit GELU input, nothing for the frozen linear layers); without, plain torch ops."""
+    Softmax and MatMul, 4-bit GELU input, nothing for the frozen linear layers); without, plain torch ops.  With ``wrapped``,
+    ``recompute`` keeps no probabilities: attention forms them again, from the projection's rows, and takes the sequences'
+    ``lengths`` and a position bias (SelfAttentionFunction)."""
     B, T, H = x.shape
     D = H // heads
     F = torch.nn.functional
@@ -526,7 +596,9 @@ def frozen_encoder_block(x: torch.Tensor, p: dict, heads: int, wrapped: bool, ke
         w = {name: t.detach() for name, t in p.items()}    # frozen: the scheduler has switched their gradients off
         h = LayerNormFunction.apply(x, p["g1"], p["b1"], 1e-5, True, keep_ppm)
         qkv = LinearFunction.apply(h, w["wqkv"], None, 8, block)
-        if _rows_of_vectors(D, qkv):
+        if recompute:
+            a = SelfAttentionFunction.apply(qkv, heads, heads, 1.0 / D ** 0.5, False, lengths, bias_table, bucket_of)
+        elif _rows_of_vectors(D, qkv):
             # 1 / sqrt(D) goes onto q where it is a power of two: that commutes with every rounding on the way (entries of q
             # or its gradient below 1e-35 apart, which may become subnormal or leave the 8-bit cache's range), so these are
             # the numbers of the divided products.  Any other divides them.  (32 x 128 x 768, fp32, forward and backward: heads
@@ -539,7 +611,8 @@ def frozen_encoder_block(x: torch.Tensor, p: dict, heads: int, wrapped: bool, ke
             q, k_, v = qkv.chunk(3, dim=-1)
             s = MatmulFunction.apply(split(q).contiguous(), split(k_).transpose(-1, -2).contiguous(), 8, block) / D ** 0.5
             v = split(v).contiguous()
-        a = SoftmaxMatmulFunction.apply(s, v, keep_ppm, 8, block).transpose(1, 2).reshape(B, T, H)
+        if not recompute:
+            a = SoftmaxMatmulFunction.apply(s, v, keep_ppm, 8, block).transpose(1, 2).reshape(B, T, H)
         y = x + LinearFunction.apply(a, w["wo"], None, 8, block)
         h = LayerNormFunction.apply(y, p["g2"], p["b2"], 1e-5, True, keep_ppm)
         h = LinearFunction.apply(h, w["w1"], None, 8, block)
@@ -572,11 +645,13 @@ def decoder_block_params(hidden: int, heads: int, kv_heads: int, ffn: int, devic
 
 
 def decoder_block(x: torch.Tensor, p: dict, heads: int, kv_heads: int, table, position_ids=None, keep_ppm: int = 100000, bits: int = 8,
-                  block: int = 64, act: int = sf.ACT_SILU) -> torch.Tensor:
+                  block: int = 64, act: int = sf.ACT_SILU, recompute: bool = False, lengths=None, bias_table=None, bucket_of=None) -> torch.Tensor:
     """One pre-LN decoder block (causal attention, queries and keys normed and turned, gated feed-forward) with the compressed
     caches of this module.  Whether a layer is frozen is read off its weight: a frozen one keeps nothing of its input (a
     LayerNorm the ``keep_ppm`` largest entries), an active one forms its weight gradient from its ``bits``-bit cache.  A place
-    outside of ``table`` leaves a token unturned, not unseen: padding has to come after the tokens that count."""
+    outside of ``table`` leaves a token unturned, not unseen: padding has to come after the tokens that count.  ``recompute`` keeps
+    no probabilities, and is bound to no number of tokens: attention forms them again, and takes the sequences' ``lengths`` and a
+    position bias (AttentionFunction)."""
     B, T, H = x.shape
     D, group = H // heads, heads // kv_heads
 
@@ -588,10 +663,13 @@ def decoder_block(x: torch.Tensor, p: dict, heads: int, kv_heads: int, table, po
     # a cache's blocks lie in one head; heads that have no whole block keep the rows themselves
     q, kt, v = HeadsNormRotateFunction.apply(qkv, p["gq"], p["gk"], heads, kv_heads, table, sf.ROTARY_HALVES, position_ids, 1.0 / D ** 0.5, 1e-6,
                                              bits if D % 32 == 0 else 0, block if D % block == 0 else 32)
-    s = MatmulFunction.apply(q.view(B, kv_heads, group * T, D), kt, bits, block)           # heads that share keys are rows of one product
-    later = torch.ones(T, T, dtype=torch.bool, device=x.device).triu(1)
-    s = s.view(B, kv_heads, group, T, T).masked_fill(later, -1e30).view(B, kv_heads, group * T, T)
-    a = SoftmaxMatmulFunction.apply(s, v, keep_ppm, bits, block).view(B, heads, T, D).transpose(1, 2).reshape(B, T, H)
+    if recompute:
+        a = AttentionFunction.apply(q, kt, v, 1.0, True, lengths, bias_table, bucket_of, sf.HEADS_APART).view(B, T, H)
+    else:
+        s = MatmulFunction.apply(q.view(B, kv_heads, group * T, D), kt, bits, block)       # heads that share keys are rows of one product
+        later = torch.ones(T, T, dtype=torch.bool, device=x.device).triu(1)
+        s = s.view(B, kv_heads, group, T, T).masked_fill(later, -1e30).view(B, kv_heads, group * T, T)
+        a = SoftmaxMatmulFunction.apply(s, v, keep_ppm, bits, block).view(B, heads, T, D).transpose(1, 2).reshape(B, T, H)
     y = x + LinearFunction.apply(a, p["wo"], None, bits, block, True)
     h = LinearFunction.apply(norm(y, p["g2"], p["b2"]), p["w1"], None, bits, block, True)
     return y + LinearFunction.apply(GatedFunction.apply(h, act, bits, block), p["w2"], None, bits, block, True)
