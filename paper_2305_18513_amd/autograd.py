@@ -578,6 +578,12 @@ def encoder_block_params(hidden: int, device="cuda", seed: int = 0, dtype=torch.
             "w2": mat(hidden, 4 * hidden), "g1": vec(1.0), "b1": vec(0.0), "g2": vec(1.0), "b2": vec(0.0)}
 
 
+def _only_recomputed(*given) -> None:
+    """A block that keeps its probabilities has no lengths and no position bias: given ones are refused, not passed over."""
+    if any(x is not None for x in given):
+        raise ValueError("lengths, bias_table and bucket_of go with recompute")
+
+
 def frozen_encoder_block(x: torch.Tensor, p: dict, heads: int, wrapped: bool, keep_ppm: int = 100000,
                          gelu_bits: int = 4, block: int = 64, recompute: bool = False, lengths=None, bias_table=None, bucket_of=None) -> torch.Tensor:
     """One pre-LN encoder block whose layers are all frozen: with ``wrapped`` the activations kept
@@ -585,6 +591,8 @@ def frozen_encoder_block(x: torch.Tensor, p: dict, heads: int, wrapped: bool, ke
     Softmax and MatMul, 4-bit GELU input, nothing for the frozen linear layers); without, plain torch ops.  With ``wrapped``,
     ``recompute`` keeps no probabilities: attention forms them again, from the projection's rows, and takes the sequences'
     ``lengths`` and a position bias (SelfAttentionFunction)."""
+    if not (wrapped and recompute):
+        _only_recomputed(lengths, bias_table, bucket_of)
     B, T, H = x.shape
     D = H // heads
     F = torch.nn.functional
@@ -652,6 +660,8 @@ def decoder_block(x: torch.Tensor, p: dict, heads: int, kv_heads: int, table, po
     outside of ``table`` leaves a token unturned, not unseen: padding has to come after the tokens that count.  ``recompute`` keeps
     no probabilities, and is bound to no number of tokens: attention forms them again, and takes the sequences' ``lengths`` and a
     position bias (AttentionFunction)."""
+    if not recompute:
+        _only_recomputed(lengths, bias_table, bucket_of)
     B, T, H = x.shape
     D, group = H // heads, heads // kv_heads
 

@@ -107,3 +107,19 @@ def test_binding_refuses():
     if not torch.cuda.is_available():
         with pytest.raises(ValueError):                    # tensors of the host
             sf._on_current_device(q)
+
+
+def test_blocks_refuse_what_kept_probabilities_cannot_do():
+    """Lengths or a bias that a block would pass over."""
+    from paper_2305_18513_amd import autograd as ag
+
+    x, lengths = torch.zeros(1, 4, 64), torch.ones(1, dtype=torch.int32)
+    p = ag.encoder_block_params(64, "cpu")
+    for wrapped, recompute in ((True, False), (False, False), (False, True)):
+        with pytest.raises(ValueError, match="go with recompute"):
+            ag.frozen_encoder_block(x, p, 2, wrapped, recompute=recompute, lengths=lengths)
+    p = ag.decoder_block_params(64, 2, 1, 64, "cpu")
+    with pytest.raises(ValueError, match="go with recompute"):
+        ag.decoder_block(x, p, 2, 1, torch.zeros(4, 32), lengths=lengths)
+    with pytest.raises(ValueError, match="go with recompute"):
+        ag.decoder_block(x, p, 2, 1, torch.zeros(4, 32), bias_table=torch.zeros(3, 2), bucket_of=torch.zeros(7, dtype=torch.int32))
