@@ -320,6 +320,28 @@ template <typename T, int D> __device__ __forceinline__ void sums(const char *ti
     }
 }
 
+// The same for two x of one tile, which is read across once for both.
+template <int D> __device__ __forceinline__ void sums_of_two(const char *tile, int first, const f32x16 &x, f32x16 (&out)[D / 32], const f32x16 &y, f32x16 (&more)[D / 32])
+{
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    constexpr int P = kPitch<uint16_t, D>;
+    const int row = 4 * half + (lane & 15) / 4, vector = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), turn = turn_of<uint16_t, D>(row);
+    const char *at = tile + (first + row) * P + (lane & 1) * 8;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const u32x4 a = {bf16_narrow2(x[8 * c], x[8 * c + 1]), bf16_narrow2(x[8 * c + 2], x[8 * c + 3]), bf16_narrow2(x[8 * c + 4], x[8 * c + 5]),
+                         bf16_narrow2(x[8 * c + 6], x[8 * c + 7])};
+        const u32x4 b = {bf16_narrow2(y[8 * c], y[8 * c + 1]), bf16_narrow2(y[8 * c + 2], y[8 * c + 3]), bf16_narrow2(y[8 * c + 4], y[8 * c + 5]),
+                         bf16_narrow2(y[8 * c + 6], y[8 * c + 7])};
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            const bf16x8 k = across(at + 16 * c * P + ((4 * i + vector) ^ turn) * 16, at + (16 * c + 8) * P + ((4 * i + vector) ^ turn ^ 2) * 16);
+            out[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, __builtin_bit_cast(bf16x8, a), out[i], 0, 0, 0);
+            more[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, __builtin_bit_cast(bf16x8, b), more[i], 0, 0, 0);
+        }
+    }
+}
+
 // both halves of a wave hold the same 32 columns
 __device__ __forceinline__ float both_max(float v)
 {

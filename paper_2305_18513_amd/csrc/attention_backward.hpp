@@ -21,6 +21,18 @@ template <bool BIAS> __device__ __forceinline__ float probability(float s, float
 
 constexpr int kSkew = kOwn + 4;              // floats of a query's ds in LDS
 
+// delta from an out that was rounded to bf16 is off by e = sum of dout (out - rounded), and ds by e p: more than ds's own rounding where a
+// query sees few keys, or one key takes most of it.  The sum of a query's ds is -e, as it should be nothing.  Heads of up to 96
+// form sum of p k beside dq and take e of it off at the end (1024 x 1024 by 64 causal, 256 heads: 81 us without, 98 with; dq's error
+// against 64 bits goes from 2.1 times that of one rounding of the result to 1.4, at inputs with a thousandth of outliers).  Heads of 128 have no
+// registers left for that (469 us without, 702 with the rows of dout in LDS): theirs go over the keys twice where these are no
+// more than kTwiceTiles tiles, once for e.  So do those with a bias, at any length: sums of ds over a bucket of many keys are
+// little but e otherwise (two buckets: 5 % off), and whether the table takes a gradient changes no other.  Keys' gradients take
+// the right delta in any case.
+template <typename T, int D, bool BIAS> constexpr bool kRights = sizeof(T) == 2 && D <= 96 && !BIAS;
+template <typename T, int D, bool BIAS> constexpr bool kTwice = sizeof(T) == 2 && !kRights<T, D, BIAS>;
+constexpr int kTwiceTiles = 2;
+
 template <typename T, int D, bool BIAS, bool PARTS>
 __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 256) ? 1 : 2) queries_kernel(Attention a, Gradients g, int blocks)
 {
@@ -96,12 +108,15 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
         if (half == 0) {                                    // for the second kernel
             g.rows[at] = first;
             g.rows[all + at] = second;
-            g.rows[2 * all + at] = delta;
         }
     }
-    f32x16 dq[D / 32];
+    f32x16 dq[D / 32], pk[kRights<T, D, BIAS> ? D / 32 : 1];
 #pragma unroll
-    for (int n = 0; n < D / 32; ++n) dq[n] = zeros16();
+    for (int n = 0; n < D / 32; ++n) {
+        dq[n] = zeros16();
+        if constexpr (kRights<T, D, BIAS>) pk[n] = zeros16();
+    }
+    float off = 0.0f;                                       // -e
     float carry = 0.0f;
     float *const part = PARTS ? g.parts + ((int64_t)bh * blocks * kAttnWaves + block * kAttnWaves + wave) * g.part_row : nullptr;
 
@@ -109,11 +124,64 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
         load_column<T>(a, head, column);
         __syncthreads();
     }
+    // p and ds of 32 keys
+    auto probabilities = [&](int t, int n, f32x16 &p, f32x16 &ds) {
+        const char *const tile = tiles[t & 1];
+        p = dots<T, D>(tile, 32 * n, own);
+        const f32x16 dp = dots<T, D>(tile + kTileBytes<T, D>, 32 * n, grad);
+        const float *const b = biases[BIAS ? t & 1 : 0] + kBlock - 1 - (i - q0) + 4 * half + 32 * n;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            if constexpr (BIAS) p[r] = __builtin_fmaf(p[r], a.scale, b[8 * (r / 4) + r % 4]);
+            p[r] = probability<BIAS>(p[r], scale, first, second);
+            ds[r] = p[r] * (dp[r] - delta);
+        }
+        const int from = t * kTile + 32 * n;
+        if (from + 32 > all_see) {
+            const int some = seen - from - 4 * half;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const bool in = row_of(r, 0) < some;
+                ds[r] = in ? ds[r] : 0.0f;
+                if constexpr (kRights<T, D, BIAS>) p[r] = in ? p[r] : 0.0f;
+            }
+        }
+    };
+    auto add_up = [&](const f32x16 &ds) {
+        float x = ds[0], y = ds[1];
+#pragma unroll
+        for (int r = 2; r < 16; r += 2) {
+            x += ds[r];
+            y += ds[r + 1];
+        }
+        off += x + y;
+    };
     if (count > 0) {
         fetch(0);
         own.arrive();
         grad.arrive();
         land(0);
+    }
+    if (kTwice<T, D, BIAS> && (BIAS || count <= kTwiceTiles)) {
+        for (int t = 0; t < count; ++t) {
+            fetch(t + 1);
+            if (t * kTile < any_sees)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    f32x16 p, ds;
+                    probabilities(t, n, p, ds);
+                    add_up(ds);
+                }
+            land(t + 1);
+        }
+        delta += both_sum(off);
+        off = 0.0f;
+        if (count > 0) {
+            kl.start(k, a.k.t, 0, keys, a.head_dim);
+            vl.start(v, a.v.t, 0, keys, a.head_dim);
+            fetch(0);
+            land(0);
+        }
     }
     for (int t = 0; t < count; ++t) {
         const char *const tile = tiles[t & 1];
@@ -124,19 +192,9 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
             for (int n = 0; n < 2; ++n) {
                 // (products are what takes fp32's time; with the sums by distance every half is gone through)
                 if (sizeof(T) == 4 && !PARTS && k0 + 32 * n >= any_sees) continue;
-                f32x16 s = dots<T, D>(tile, 32 * n, own);
-                const f32x16 dp = dots<T, D>(tile + kTileBytes<T, D>, 32 * n, grad);
-                const float *const b = biases[BIAS ? t & 1 : 0] + kBlock - 1 - (i - q0) + 4 * half + 32 * n;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    if constexpr (BIAS) s[r] = __builtin_fmaf(s[r], a.scale, b[8 * (r / 4) + r % 4]);
-                    s[r] = probability<BIAS>(s[r], scale, first, second) * (dp[r] - delta);
-                }
-                if (k0 + 32 * n + 32 > all_see) {
-                    const int some = seen - k0 - 32 * n - 4 * half;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = row_of(r, 0) < some ? s[r] : 0.0f;
-                }
+                f32x16 p, s;
+                probabilities(t, n, p, s);
+                if constexpr (sizeof(T) == 2) add_up(s);
                 if constexpr (PARTS) {
                     // Sums by distance, key - query.  Within 32 keys and the wave's 32 queries lane l has those of l - 31 (lower) and of l + 1
                     // (upper), which the next 32 keys see 32 lower.  Where all 63 are of one bucket, as far ones are, their sum goes to one of them.
@@ -174,7 +232,8 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
                     if (half == 0) part[k0 + 32 * n + lane] = lower + carry;
                     carry = upper;
                 }
-                sums<T, D>(tile, 32 * n, s, dq);
+                if constexpr (kRights<T, D, BIAS>) sums_of_two<D>(tile, 32 * n, s, dq, p, pk);
+                else sums<T, D>(tile, 32 * n, s, dq);
             }
         } else if (PARTS) {
             part[k0 + lane] = half == 0 ? carry : 0.0f;
@@ -183,6 +242,14 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
         land(t + 1);
     }
     if (PARTS && half == 0) part[count * kTile + lane] = carry;
+    if constexpr (sizeof(T) == 2) off = both_sum(off);
+    if constexpr (kRights<T, D, BIAS>) {
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dq[n][r] = __builtin_fmaf(-off, pk[n][r], dq[n][r]);
+    }
+    if (half == 0 && i < a.q_tokens) g.rows[2 * (int64_t)a.batch * a.q_heads * a.q_tokens + (int64_t)bh * a.q_tokens + i] = delta + off;      // for the second kernel
     if (i < a.q_tokens) store_row<T, D>(dq, a.scale, static_cast<T *>(g.dq) + batch * g.dq_b + head * g.dq_h + i * g.dq_t, a.head_dim);
 }
 

@@ -421,3 +421,50 @@ def test_many_tokens():
         q, k, v, do = inputs(1, T, T, 2, 1, 64, dtype, sf.HEADS_APART, seed=T)
         table, of = torch.randn(32, 2, device="cuda").to(dtype), sf.distance_buckets(T, T, 32, 500, False)
         Call(q, k, v, do, sf.HEADS_APART, 0.125, True, None, table, of).forward().backward().check()
+
+
+class RightDelta(Reference):
+    """Bounds without the rounding of out in them.  With e the most that delta from a rounded out may be off, ds is first formed with it,
+    p (dp - delta) + e p, and rounded so for a product; the sum of a row's ds then gives e back, but for 32 bits' roundings, and e times
+    sum of p k, of which p is rounded to bf16, is taken off.  Where the right delta is there from the start it is less than that."""
+
+    def backward(self, do):
+        super().backward(do)
+        B, Tq, Tk, Hq, Hk, D = self.sizes
+        dp, size = do @ self.v.transpose(2, 3), do.abs() @ self.v.abs().transpose(2, 3)
+        delta = (do * self.out).sum(-1, keepdim=True)
+        e = (do.abs() * (self.rounded(self.out_off(), self.out) + (D + 2) * U * self.out.abs())).sum(-1, keepdim=True)
+        first = self.ds.abs() + e * self.p
+        # a ds's 32 bits: p's own, dp's D products and sums, the difference; delta's: all of its row's, their sum, and delta' times what the p are off from 1
+        one = self.p_off * first + self.p * (1 + self.p_off) * ((D + 2) * U * size + 2 * U * (dp.abs() + delta.abs() + e)) + 2 * U * first
+        delta_off = (one + (Tk + 8) * U * first + self.p * self.p_off * (delta.abs() + e)).sum(-1, keepdim=True)
+        ds_off = one + self.p * delta_off
+        n, group = Tq * self.group, self.group
+        share = lambda t: t.view(B, Hk, group, Tk, D).sum(2)  # noqa: E731
+        dq_off = (ds_off + UB * (first + e * self.p) * (1 + UB) + (Tk + 4) * U * (first + e * self.p)) @ self.k.abs() * self.scale
+        dk_off = share((ds_off + UB * (self.ds.abs() + ds_off) + (n + 4) * U * self.ds.abs()).transpose(2, 3) @ self.q.abs()) * self.scale
+        self.offs["dq"], self.offs["dk"] = self.rounded(dq_off, self.dq), self.rounded(dk_off, self.dk)
+        if self.at is not None:
+            add = lambda t: torch.stack([(t * (self.at == b)).sum((0, 2, 3)) for b in range(self.buckets)])  # noqa: E731
+            self.offs["dtable"] = self.rounded(add(ds_off + 40 * U * self.ds.abs()), self.dtable)
+
+
+@pytest.mark.parametrize("T,D,buckets", [(7, 128, 0), (128, 128, 0), (128, 104, 0), (100, 128, 2), (300, 64, 0), (300, 96, 0), (300, 40, 0), (300, 64, 2), (260, 96, 2),
+                                         (1, 128, 0), (1, 64, 2)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_gradients_where_few_keys_take_all(T, D, buckets, causal):
+    """A rounded out's part in delta stays out of dq and dk (heads past 96: up to 128 keys), and out of a bucket that all keys share, whose sum is 0."""
+    require_gpu()
+    q, k, v, do = inputs(2, T, T, 4, 2, D, torch.bfloat16, sf.HEADS_ROWS, seed=T + D, spread=1.5)
+    table, of = None, None
+    if buckets:
+        table = torch.randn(buckets, 4, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+        of = torch.zeros(2 * T - 1, dtype=torch.int32, device="cuda")
+    call = Call(q, k, v, do, sf.HEADS_ROWS, D ** -0.5, causal, None, table, of)
+    call.forward()
+    call.backward()
+    ref = RightDelta(q, k, v, do, sf.HEADS_ROWS, D ** -0.5, causal, None, table, of)
+    within(rows_of(call.dq, sf.HEADS_ROWS), ref.dq, ref.offs["dq"], "dq")
+    within(rows_of(call.dk, sf.HEADS_ROWS, True), ref.dk, ref.offs["dk"], "dk")
+    if buckets:
+        within(call.dtable.double(), ref.dtable, ref.offs["dtable"], "dtable")
