@@ -26,7 +26,7 @@ constexpr int kSkew = kOwn + 4;              // floats of a query's ds in LDS
 // form sum of p k beside dq and take e of it off at the end (1024 x 1024 by 64 causal, 256 heads: 81 us without, 98 with; dq's error
 // against 64 bits goes from 2.1 times that of one rounding of the result to 1.4, at inputs with a thousandth of outliers).  Heads of 128 have no
 // registers left for that (469 us without, 702 with the rows of dout in LDS): theirs go over the keys twice where these are no
-// more than kTwiceTiles tiles, once for e.  So do those with a bias, at any length: sums of ds over a bucket of many keys are
+// more than kTwiceTiles tiles, once for delta = sum of p dp.  So do those with a bias, at any length: sums of ds over a bucket of many keys are
 // little but e otherwise (two buckets: 5 % off), and whether the table takes a gradient changes no other.  Keys' gradients take
 // the right delta in any case.
 template <typename T, int D, bool BIAS> constexpr bool kRights = sizeof(T) == 2 && D <= 96 && !BIAS;
@@ -124,37 +124,23 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
         load_column<T>(a, head, column);
         __syncthreads();
     }
-    // p and ds of 32 keys
-    auto probabilities = [&](int t, int n, f32x16 &p, f32x16 &ds) {
+    // p and dp of 32 keys, p of those that a query does not see left as it is; and whether there are any
+    auto pairs = [&](int t, int n, f32x16 &p, f32x16 &dp) {
         const char *const tile = tiles[t & 1];
         p = dots<T, D>(tile, 32 * n, own);
-        const f32x16 dp = dots<T, D>(tile + kTileBytes<T, D>, 32 * n, grad);
+        dp = dots<T, D>(tile + kTileBytes<T, D>, 32 * n, grad);
         const float *const b = biases[BIAS ? t & 1 : 0] + kBlock - 1 - (i - q0) + 4 * half + 32 * n;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             if constexpr (BIAS) p[r] = __builtin_fmaf(p[r], a.scale, b[8 * (r / 4) + r % 4]);
             p[r] = probability<BIAS>(p[r], scale, first, second);
-            ds[r] = p[r] * (dp[r] - delta);
         }
-        const int from = t * kTile + 32 * n;
-        if (from + 32 > all_see) {
-            const int some = seen - from - 4 * half;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const bool in = row_of(r, 0) < some;
-                ds[r] = in ? ds[r] : 0.0f;
-                if constexpr (kRights<T, D, BIAS>) p[r] = in ? p[r] : 0.0f;
-            }
-        }
+        return t * kTile + 32 * n + 32 > all_see;
     };
-    auto add_up = [&](const f32x16 &ds) {
-        float x = ds[0], y = ds[1];
+    auto leave_out = [&](int t, int n, f32x16 &x) {
+        const int some = seen - t * kTile - 32 * n - 4 * half;
 #pragma unroll
-        for (int r = 2; r < 16; r += 2) {
-            x += ds[r];
-            y += ds[r + 1];
-        }
-        off += x + y;
+        for (int r = 0; r < 16; ++r) x[r] = row_of(r, 0) < some ? x[r] : 0.0f;
     };
     if (count > 0) {
         fetch(0);
@@ -163,19 +149,26 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
         land(0);
     }
     if (kTwice<T, D, BIAS> && (BIAS || count <= kTwiceTiles)) {
+        float x = 0.0f, y = 0.0f;
         for (int t = 0; t < count; ++t) {
             fetch(t + 1);
             if (t * kTile < any_sees)
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
-                    f32x16 p, ds;
-                    probabilities(t, n, p, ds);
-                    add_up(ds);
+                    f32x16 p, dp;
+                    if (pairs(t, n, p, dp)) {
+                        leave_out(t, n, p);
+                        leave_out(t, n, dp);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 16; r += 2) {
+                        x = __builtin_fmaf(p[r], dp[r], x);
+                        y = __builtin_fmaf(p[r + 1], dp[r + 1], y);
+                    }
                 }
             land(t + 1);
         }
-        delta += both_sum(off);
-        off = 0.0f;
+        delta = both_sum(x + y);
         if (count > 0) {
             kl.start(k, a.k.t, 0, keys, a.head_dim);
             vl.start(v, a.v.t, 0, keys, a.head_dim);
@@ -193,8 +186,22 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
                 // (products are what takes fp32's time; with the sums by distance every half is gone through)
                 if (sizeof(T) == 4 && !PARTS && k0 + 32 * n >= any_sees) continue;
                 f32x16 p, s;
-                probabilities(t, n, p, s);
-                if constexpr (sizeof(T) == 2) add_up(s);
+                const bool some = pairs(t, n, p, s);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = p[r] * (s[r] - delta);
+                if (some) {
+                    leave_out(t, n, s);
+                    if constexpr (kRights<T, D, BIAS>) leave_out(t, n, p);
+                }
+                if constexpr (sizeof(T) == 2 && !BIAS) {
+                    float x = s[0], y = s[1];
+#pragma unroll
+                    for (int r = 2; r < 16; r += 2) {
+                        x += s[r];
+                        y += s[r + 1];
+                    }
+                    off += x + y;
+                }
                 if constexpr (PARTS) {
                     // Sums by distance, key - query.  Within 32 keys and the wave's 32 queries lane l has those of l - 31 (lower) and of l + 1
                     // (upper), which the next 32 keys see 32 lower.  Where all 63 are of one bucket, as far ones are, their sum goes to one of them.
@@ -242,7 +249,7 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
         land(t + 1);
     }
     if (PARTS && half == 0) part[count * kTile + lane] = carry;
-    if constexpr (sizeof(T) == 2) off = both_sum(off);
+    if constexpr (sizeof(T) == 2 && !BIAS) off = both_sum(off);
     if constexpr (kRights<T, D, BIAS>) {
 #pragma unroll
         for (int n = 0; n < D / 32; ++n)
