@@ -145,14 +145,15 @@ int64_t part_row(const Sizes &z) { return ((int64_t)z.k_tokens + kTile - 1) / kT
 //         64 x 1024, 8 heads of 64: 1 24.5, 25.4; 16 25.3, 25.7; 64 25.5, 48.5.
 //   fp32, where padded queries cost products, up to 64: the first 1 1146, 137; 64 1153, 926; the second 1 137, 48; 64 142, 105.
 //   Any where there are few workgroups otherwise and keys are many: bf16, 1 x 4096, 32 heads on 8 by 128: 128 queries 95, 46; 8 x 1024,
-//         12 heads of 64: 64 queries 18.6, 13.1; of 128 keys 5.7, 6.8.
+//         12 heads of 64: 64 queries 18.6, 13.1; of 128 keys 5.7, 6.8.  fp32, whose products are a wave's time, from 128 keys on: 40 heads of
+//         64, 128 x 128 13.8, 9.6; 300 x 300 27.9, 23.2; 16 heads of 128, 300 x 300 51.4, 27.6; but 64 heads, 192 workgroups otherwise, 54.7, 79.0.
 // A workgroup for each compute unit is enough (16 x 4096 and 1 query: 256 workgroups 48, 512 54, 1024 60), but for fp32 heads of up
 // to 64, two of which fit one (8 x 4096, 12 heads: 65, 47, 55).
 int few_splits(const Sizes &z)
 {
     if (z.batch == 0 || z.q_tokens == 0 || z.k_tokens == 0) return 0;
     const int64_t others = z.batch * z.q_heads * q_blocks(z);
-    if (z.q_tokens > (z.dt == SLIMFIT_BF16 ? 16 : 64) && (others > 128 || z.k_tokens < 512)) return 0;
+    if (z.q_tokens > (z.dt == SLIMFIT_BF16 ? 16 : 64) && (others > 128 || z.k_tokens < (z.dt == SLIMFIT_BF16 ? 512 : 128))) return 0;
     const int64_t rows = (int64_t)(z.q_heads / z.kv_heads) * z.q_tokens, blocks = z.batch * z.kv_heads * ((rows + kOwn - 1) / kOwn);
     const int64_t tiles = (z.k_tokens + kFewTile - 1) / kFewTile;
     int64_t splits = (z.dt == SLIMFIT_F32 && z.head_dim <= 64 ? 512 : 256) / blocks;

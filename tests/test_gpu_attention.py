@@ -468,3 +468,20 @@ def test_gradients_where_few_keys_take_all(T, D, buckets, causal):
     within(rows_of(call.dk, sf.HEADS_ROWS, True), ref.dk, ref.offs["dk"], "dk")
     if buckets:
         within(call.dtable.double(), ref.dtable, ref.offs["dtable"], "dtable")
+
+
+@pytest.mark.parametrize("shape", [(35, 129, 140, 2, 1, 32), (11, 150, 300, 6, 3, 64), (17, 197, 197, 4, 4, 84), (34, 130, 200, 2, 2, 128)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("causal", [False, True], ids=["all", "causal"])
+@pytest.mark.parametrize("bias", [False, True], ids=["plain", "bias"])
+def test_fp32_of_many_workgroups(shape, causal, bias):
+    """Where keys are not shared out: more workgroups of 128 queries than half of the card's units."""
+    require_gpu()
+    B, Tq, Tk, Hq, Hk, D = shape
+    assert B * Hq * ((Tq + 127) // 128) > 128
+    q, k, v, do = inputs(*shape, torch.float32, sf.HEADS_ROWS, seed=Tk)
+    lengths = torch.tensor([(Tk, 0, Tk // 2, 1, Tk + 9)[b % 5] for b in range(B)], dtype=torch.int32, device="cuda") if bias else None
+    table = of = None
+    if bias:
+        table = torch.randn(9, Hq, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+        of = sf.distance_buckets(Tq, Tk, 9, 40, both_ways=not causal)
+    Call(q, k, v, do, sf.HEADS_ROWS, D ** -0.5, causal, lengths, table, of).forward().backward().check()
