@@ -19,9 +19,11 @@ namespace slimfit {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPer = 8;                      // elements of a thread's vectors
-constexpr int kPass = kThreads * kPer;
-constexpr int kChunk = 4 * kPass;            // a multiple of every block
+constexpr int kChunk = 32 * kThreads;        // a multiple of every block
+// Elements of a thread at a time: with states in 32 bits 16 bytes of each, so that what a wave asks for at once is whole lines (85 million weights,
+// a third frozen, in fp32: 287 us, 328 with eight elements in two vectors); with states in 8 bits 8 bytes of codes, for the work on a run's scale is
+// a thread's (6 % more with four).
+template <int BITS> constexpr int kPer = BITS == 8 ? 8 : 4;
 constexpr uint32_t kMagic = 0x534C4157u;     // "SLAW"
 constexpr int kPlanBatch = 32;
 
@@ -83,130 +85,156 @@ __host__ __device__ inline double power(double b, uint32_t n)
     return p;
 }
 
-template <typename T> __device__ __forceinline__ void load8(const T *p, float (&f)[kPer]);
-template <> __device__ __forceinline__ void load8<float>(const float *p, float (&f)[kPer])
+template <int N> __device__ __forceinline__ void load_all(const float *p, float (&f)[N])
 {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < N / 4; ++i) {
         const f32x4 r = load_global<true>(reinterpret_cast<const f32x4 *>(p) + i);
 #pragma unroll
         for (int j = 0; j < 4; ++j) f[4 * i + j] = r[j];
     }
 }
-template <> __device__ __forceinline__ void load8<uint16_t>(const uint16_t *p, float (&f)[kPer])
+template <int N> __device__ __forceinline__ void load_all(const uint16_t *p, float (&f)[N])
 {
-    const u32x4 r = load_global<true>(reinterpret_cast<const u32x4 *>(p));
+    typedef uint32_t V __attribute__((ext_vector_type(N / 2)));
+    const V r = load_global<true>(reinterpret_cast<const V *>(p));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N / 2; ++i) {
         const uint32_t u = r[i];
         f[2 * i] = __builtin_bit_cast(float, u << 16);
         f[2 * i + 1] = __builtin_bit_cast(float, u & 0xFFFF0000u);
     }
 }
-template <typename T> __device__ __forceinline__ void store8(T *p, const float (&f)[kPer]);
-template <> __device__ __forceinline__ void store8<float>(float *p, const float (&f)[kPer])
+template <int N> __device__ __forceinline__ void store_all(float *p, const float (&f)[N])
 {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) store_global<true>(reinterpret_cast<f32x4 *>(p) + i, f32x4{f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]});
+    for (int i = 0; i < N / 4; ++i) store_global<true>(reinterpret_cast<f32x4 *>(p) + i, f32x4{f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]});
 }
-template <> __device__ __forceinline__ void store8<uint16_t>(uint16_t *p, const float (&f)[kPer])
+template <int N> __device__ __forceinline__ void store_all(uint16_t *p, const float (&f)[N])
 {
-    store_global<true>(reinterpret_cast<u32x4 *>(p), u32x4{bf16_narrow2(f[0], f[1]), bf16_narrow2(f[2], f[3]), bf16_narrow2(f[4], f[5]), bf16_narrow2(f[6], f[7])});
+    typedef uint32_t V __attribute__((ext_vector_type(N / 2)));
+    V r;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) r[i] = bf16_narrow2(f[2 * i], f[2 * i + 1]);
+    store_global<true>(reinterpret_cast<V *>(p), r);
 }
 __device__ __forceinline__ float load1(const float *p) { return *p; }
 __device__ __forceinline__ float load1(const uint16_t *p) { return bf16_widen(*p); }
 __device__ __forceinline__ void store1(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store1(uint16_t *p, float v) { *p = (uint16_t)bf16_narrow(v); }
-
-// n of the eight elements (the last vector of a tensor may have fewer), 0 in place of the others
-template <typename T> __device__ __forceinline__ void load_some(const T *p, int n, float (&f)[kPer])
+// n of the elements (the last vector of a tensor may have fewer), 0 in place of the others
+template <typename T, int N> __device__ __forceinline__ void load_some(const T *p, int n, float (&f)[N])
 {
-    if (n >= kPer) return load8<T>(p, f);
+    if (n >= N) return load_all<N>(p, f);
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) f[j] = j < n ? load1(p + j) : 0.0f;
+    for (int j = 0; j < N; ++j) f[j] = j < n ? load1(p + j) : 0.0f;
 }
-template <typename T> __device__ __forceinline__ void store_some(T *p, int n, const float (&f)[kPer])
+template <typename T, int N> __device__ __forceinline__ void store_some(T *p, int n, const float (&f)[N])
 {
-    if (n >= kPer) return store8<T>(p, f);
+    if (n >= N) return store_all<N>(p, f);
 #pragma unroll
-    for (int j = 0; j < kPer; ++j)
+    for (int j = 0; j < N; ++j)
         if (j < n) store1(p + j, f[j]);
 }
-__device__ __forceinline__ u32x2 load_codes(const uint8_t *p, int n)
+template <int N> struct Codes {                             // of N elements, a byte each
+    uint32_t w[N / 4];
+};
+template <int N> __device__ __forceinline__ Codes<N> load_codes(const uint8_t *p, int n)
 {
-    if (n >= kPer) return load_global<true>(reinterpret_cast<const u32x2 *>(p));
-    u32x2 c = {0u, 0u};
+    typedef uint32_t V __attribute__((ext_vector_type(N / 4)));
+    Codes<N> c = {};
+    if (n >= N) {
+        if constexpr (N == 4) {
+            c.w[0] = load_global<true>(reinterpret_cast<const uint32_t *>(p));
+        } else {
+            const V r = load_global<true>(reinterpret_cast<const V *>(p));
 #pragma unroll
-    for (int j = 0; j < kPer; ++j)
-        if (j < n) c[j / 4] |= (uint32_t)p[j] << (8 * (j % 4));
+            for (int i = 0; i < N / 4; ++i) c.w[i] = r[i];
+        }
+        return c;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (j < n) c.w[j / 4] |= (uint32_t)p[j] << (8 * (j % 4));
     return c;
 }
-__device__ __forceinline__ void store_codes(uint8_t *p, int n, u32x2 c)
+template <int N> __device__ __forceinline__ void store_codes(uint8_t *p, int n, const Codes<N> &c)
 {
-    if (n >= kPer) return store_global<true>(reinterpret_cast<u32x2 *>(p), c);
+    typedef uint32_t V __attribute__((ext_vector_type(N / 4)));
+    if (n >= N) {
+        if constexpr (N == 4) {
+            store_global<true>(reinterpret_cast<uint32_t *>(p), c.w[0]);
+        } else {
+            V r;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j)
-        if (j < n) p[j] = (uint8_t)(c[j / 4] >> (8 * (j % 4)));
+            for (int i = 0; i < N / 4; ++i) r[i] = c.w[i];
+            store_global<true>(reinterpret_cast<V *>(p), r);
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (j < n) p[j] = (uint8_t)(c.w[j / 4] >> (8 * (j % 4)));
 }
 
-__device__ __forceinline__ void decode_m(u32x2 c, float scale, float (&f)[kPer])
+template <int N> __device__ __forceinline__ void decode_m(const Codes<N> &c, float scale, float (&f)[N])
 {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[i], true);
+    for (int i = 0; i < N / 4; ++i) {
+        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.w[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.w[i], true);
         f[4 * i] = a[0] * scale;
         f[4 * i + 1] = a[1] * scale;
         f[4 * i + 2] = b[0] * scale;
         f[4 * i + 3] = b[1] * scale;
     }
 }
-__device__ __forceinline__ void decode_v(u32x2 c, float scale, float (&f)[kPer])
+template <int N> __device__ __forceinline__ void decode_v(const Codes<N> &c, float scale, float (&f)[N])
 {
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        const uint32_t code = (c[j / 4] >> (8 * (j % 4))) & 255u;
+    for (int j = 0; j < N; ++j) {
+        const uint32_t code = (c.w[j / 4] >> (8 * (j % 4))) & 255u;
         f[j] = code ? __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, scale) + (code << 20)) : 0.0f;
     }
 }
 // m' of a run's lanes: codes, and the scale in every lane
-__device__ __forceinline__ u32x2 encode_m(const float (&m)[kPer], int lanes, float &scale)
+template <int N> __device__ __forceinline__ Codes<N> encode_m(const float (&m)[N], int lanes, float &scale)
 {
     uint32_t top = 0u;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) top = max(top, __builtin_bit_cast(uint32_t, m[j]) & 0x7FFFFFFFu);
+    for (int j = 0; j < N; ++j) top = max(top, __builtin_bit_cast(uint32_t, m[j]) & 0x7FFFFFFFu);
     const float a = __builtin_bit_cast(float, group_max_u32(top, lanes));
     const float up = 448.0f / a;
     const bool fine = !__builtin_isinf(up);                 // not a run of zeros, nor one whose factor overflows
     const float by = fine ? up : 0.0f;
     scale = fine ? a / 448.0f : 0.0f;
-    u32x2 c;
+    Codes<N> c;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < N / 4; ++i) {
         int w = __builtin_amdgcn_cvt_pk_fp8_f32(m[4 * i] * by, m[4 * i + 1] * by, 0, false);
         w = __builtin_amdgcn_cvt_pk_fp8_f32(m[4 * i + 2] * by, m[4 * i + 3] * by, w, true);
-        c[i] = (uint32_t)w;
+        c.w[i] = (uint32_t)w;
     }
     return c;
 }
 // v' likewise; `first`: the key of the tensor's dither plus the number of the fours before these elements
-__device__ __forceinline__ u32x2 encode_v(const float (&v)[kPer], int lanes, uint32_t first, float &scale)
+template <int N> __device__ __forceinline__ Codes<N> encode_v(const float (&v)[N], int lanes, uint32_t first, float &scale)
 {
     uint32_t top = 0u;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) top = max(top, __builtin_bit_cast(uint32_t, v[j]));
+    for (int j = 0; j < N; ++j) top = max(top, __builtin_bit_cast(uint32_t, v[j]));
     top = group_max_u32(top, lanes) >> 23;
     top = top > 31u ? top - 30u : 1u;
     scale = __builtin_bit_cast(float, top << 23);
-    u32x2 c = {0u, 0u};
+    Codes<N> c = {};
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < N / 4; ++i) {
         const uint32_t word = mix(first + (uint32_t)i);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint32_t bits = __builtin_bit_cast(uint32_t, v[4 * i + j]);
             const uint32_t dither = (j == 0 ? word : __builtin_rotateleft32(word, 8 * j)) >> 12;
             const int code = (int)((bits + dither) >> 20) - (int)(8u * top);
-            c[i] |= (bits ? (uint32_t)min(max(code, 1), 255) : 0u) << (8 * j);
+            c.w[i] |= (uint32_t)(bits ? min(max(code, 1), 255) : 0) << (8 * j);
         }
     }
     return c;
@@ -216,6 +244,7 @@ template <typename TW, typename TG, int BITS, bool SCORE>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const char *__restrict__ ws, int32_t L, int64_t total_chunks, int32_t block, Step s,
                                                          const float *__restrict__ live, const uint8_t *__restrict__ frozen, double *__restrict__ partials)
 {
+    constexpr int N = kPer<BITS>, kPass = kThreads * N;
     __shared__ double lds[kThreads / kWave];
     const Header *h = reinterpret_cast<const Header *>(ws);
     if (h->magic != kMagic || h->n_layers != L || h->total_chunks != total_chunks || h->bits != BITS || h->block != block ||
@@ -242,17 +271,17 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const char *__restrict_
     }
     const int64_t off = (chunk - e.first_chunk) * kChunk;
     const int len = (int)min((int64_t)kChunk, e.numel - off);
-    const int lanes = block / kPer;
+    const int lanes = block / N;
     const float decay = s.lr * e.decay;
     const uint32_t key = BITS == 8 ? mix(s.seed ^ mix(s.step ^ mix((uint32_t)lo + 1u))) + (uint32_t)(off >> 2) : 0u;
     double acc = 0.0;
-#pragma unroll
+#pragma unroll 2
     for (int p = 0; p < kChunk / kPass; ++p) {
         if (p * kPass >= len) break;                        // (all threads together: lanes of a run stay together)
-        const int at = p * kPass + threadIdx.x * kPer;
-        const int n = min(len - at, kPer);
+        const int at = p * kPass + threadIdx.x * N;
+        const int n = min(len - at, N);
         TW *const wp = static_cast<TW *>(e.w) + off + at;
-        float w[kPer], g[kPer], m[kPer], v[kPer];
+        float w[N], g[N], m[N], v[N];
         load_some(wp, n, w);
         load_some(static_cast<const TG *>(e.grad) + off + at, n, g);
         const int64_t run = (off + at) / (BITS == 8 ? block : 1);
@@ -260,22 +289,51 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const char *__restrict_
             load_some(static_cast<float *>(e.m) + off + at, n, m);
             load_some(static_cast<float *>(e.v) + off + at, n, v);
         } else {
-            const u32x2 cm = load_codes(static_cast<uint8_t *>(e.m) + off + at, n), cv = load_codes(static_cast<uint8_t *>(e.v) + off + at, n);
+            const Codes<N> cm = load_codes<N>(static_cast<uint8_t *>(e.m) + off + at, n), cv = load_codes<N>(static_cast<uint8_t *>(e.v) + off + at, n);
             decode_m(cm, n > 0 ? e.m_scales[run] : 0.0f, m);
             decode_v(cv, n > 0 ? e.v_scales[run] : 0.0f, v);
         }
-        float to[kPer];
+        float to[N], d[N];
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
+        for (int j = 0; j < N; ++j) {
             const float gj = g[j] * s.factor;
             m[j] = m[j] * s.b1 + gj * s.one_b1;
             v[j] = v[j] * s.b2 + (gj * s.one_b2) * gj;
-            const float d = -(w[j] * decay + m[j] / (__builtin_sqrtf(v[j]) * s.root + s.eps) * s.rate);
-            to[j] = w[j] + d;
-            if constexpr (SCORE) {
-                const float q = __builtin_fabsf(d) / fmaxf(__builtin_fabsf(w[j]), s.floor);
-                acc += j < n && d != 0.0f ? (double)q : 0.0;
+        }
+        // The instructions for roots and reciprocals are within a step of the last place, and take numbers below the normal ones as 0:
+        // from an eps of 2^-40 on, a v of those is none of its root's sum.  (Divided and rooted by the correctly rounded sequences,
+        // distances too and added up in fp64 one by one: 97 vector instructions an element with 8 bits instead of 59, 361 us instead of 285 for 151 million bf16 weights.)
+        if (s.eps >= 0x1p-40f) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) d[j] = m[j] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[j]) * s.root + s.eps);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) d[j] = m[j] / (__builtin_sqrtf(v[j]) * s.root + s.eps);
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            d[j] = -(w[j] * decay + d[j] * s.rate);
+            to[j] = w[j] + d[j];
+        }
+        if constexpr (SCORE) {                              // (past the end d is 0)
+            float q[N], least = __builtin_inff();
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                q[j] = fmaxf(__builtin_fabsf(w[j]), s.floor);
+                least = fminf(least, q[j]);
             }
+            if (least >= 0x1p-126f) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) q[j] = __builtin_fabsf(d[j]) * __builtin_amdgcn_rcpf(q[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) q[j] = d[j] != 0.0f ? __builtin_fabsf(d[j]) / q[j] : 0.0f;
+            }
+#pragma unroll
+            for (int j = 1; j < N; j *= 2)
+#pragma unroll
+                for (int i = 0; i + j < N; i += 2 * j) q[i] += q[i + j];
+            acc += (double)q[0];
         }
         store_some(wp, n, to);
         if (sizeof(TW) == 4 && e.copy) store_some(e.copy + off + at, n, to);
@@ -283,13 +341,13 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const char *__restrict_
             store_some(static_cast<float *>(e.m) + off + at, n, m);
             store_some(static_cast<float *>(e.v) + off + at, n, v);
         } else {
-            if (n < kPer) {                                 // past the end: nothing that a run's largest could be
+            if (n < N) {                                 // past the end: nothing that a run's largest could be
 #pragma unroll
-                for (int j = 0; j < kPer; ++j)
+                for (int j = 0; j < N; ++j)
                     if (j >= n) m[j] = v[j] = 0.0f;
             }
             float ms, vs;
-            const u32x2 cm = encode_m(m, lanes, ms), cv = encode_v(v, lanes, key + (uint32_t)(at >> 2), vs);
+            const Codes<N> cm = encode_m(m, lanes, ms), cv = encode_v(v, lanes, key + (uint32_t)(at >> 2), vs);
             store_codes(static_cast<uint8_t *>(e.m) + off + at, n, cm);
             store_codes(static_cast<uint8_t *>(e.v) + off + at, n, cv);
             if (n > 0 && (threadIdx.x & (lanes - 1)) == 0) {
@@ -326,16 +384,18 @@ __global__ __launch_bounds__(kWave) void finish_kernel(const char *__restrict__ 
     if (threadIdx.x == 0) d_out[layer] = e.numel > 0 ? (float)(acc / (double)e.numel) : 0.0f;
 }
 
+constexpr int kStates = 4;                   // elements of a thread that reads states back (151 million: 237 us, with eight, whose fp32 numbers are two vectors, 445)
+
 __global__ __launch_bounds__(kThreads) void states_kernel(const uint8_t *__restrict__ m, const float *__restrict__ m_scales, const uint8_t *__restrict__ v,
                                                           const float *__restrict__ v_scales, int64_t n, int shift, float *__restrict__ m_out,
                                                           float *__restrict__ v_out, int64_t first)
 {
-    const int64_t at = first + ((int64_t)blockIdx.x * kThreads + threadIdx.x) * kPer;
+    const int64_t at = first + ((int64_t)blockIdx.x * kThreads + threadIdx.x) * kStates;
     if (at >= n) return;
-    const int some = (int)min((int64_t)kPer, n - at);
-    float a[kPer], b[kPer];
-    decode_m(load_codes(m + at, some), m_scales[at >> shift], a);
-    decode_v(load_codes(v + at, some), v_scales[at >> shift], b);
+    const int some = (int)min((int64_t)kStates, n - at);
+    float a[kStates], b[kStates];
+    decode_m(load_codes<kStates>(m + at, some), m_scales[at >> shift], a);
+    decode_v(load_codes<kStates>(v + at, some), v_scales[at >> shift], b);
     store_some(m_out + at, some, a);
     store_some(v_out + at, some, b);
 }
@@ -530,7 +590,7 @@ extern "C" int32_t slimfit_adamw_states(const uint8_t *m, const float *m_scales,
     if ((rc = check_device_range(m_scales, scales)) != SLIMFIT_OK || (rc = check_device_range(v_scales, scales)) != SLIMFIT_OK) return rc;
     if ((rc = check_device_range(m_out, out)) != SLIMFIT_OK || (rc = check_device_range(v_out, out)) != SLIMFIT_OK) return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    constexpr int64_t kMost = kMaxGridThreads * kPer;
+    constexpr int64_t kMost = kMaxGridThreads * kStates, kPass = kThreads * kStates;
     for (int64_t first = 0; first < n; first += kMost) {
         const int64_t left = n - first < kMost ? n - first : kMost;
         launch(states_kernel, (unsigned)((left + kPass - 1) / kPass), kThreads, 0, st, m, m_scales, v, v_scales, n, __builtin_ctz((unsigned)block), m_out, v_out,
