@@ -2,7 +2,7 @@
 //     g' = factor g,   m' = b1 m + (1 - b1) g',   v' = b2 v + ((1 - b2) g') g',
 //     d = -(lr decay w + lr / (1 - b1^t) * m' / (sqrt(v') / sqrt(1 - b2^t) + eps)),   w' = w + d,   distance = mean |d| / max(|w|, floor).
 //
-// As for the distances alone (layer_delta.hip) the tensors are cut into chunks of kChunk elements, a workgroup each, the table of
+// As for the distances alone (layer_delta.hip) the tensors are cut into chunks of kChunk elements (kShort where there are few), a workgroup each, the table of
 // the tensors lies in the workspace, and each workgroup's sum of terms goes out in fp64 for a second launch that adds them in order.
 //
 // States in 8 bits, a scale for each run of `block` elements:
@@ -19,7 +19,9 @@ namespace slimfit {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 32 * kThreads;        // a multiple of every block
+// Both multiples of every block and of a workgroup's pass.  kShort where there are up to kFew chunks otherwise, two for each compute
+// unit (us with kChunk, kShort: 30 tensors of 16 384 elements 12.2, 7.7; 16 of 262 144 31.2, 22.6; 32 of those 43.8, 44.8).
+constexpr int kChunk = 32 * kThreads, kShort = 8 * kThreads, kFew = 512;
 // Elements of a thread at a time: with states in 32 bits 16 bytes of each, so that what a wave asks for at once is whole lines (85 million weights,
 // a third frozen, in fp32: 287 us, 328 with eight elements in two vectors); with states in 8 bits 8 bytes of codes, for the work on a run's scale is
 // a thread's (6 % more with four).
@@ -31,8 +33,7 @@ struct Header {                              // 64 bytes at the start of the wor
     uint32_t magic;
     int32_t n_layers;
     int64_t total_chunks;
-    int32_t w_dt, grad_dt, bits, block;
-    int64_t pad[4];
+    int32_t w_dt, grad_dt, bits, block, of, pad[7];         // of: elements of a chunk
 };
 static_assert(sizeof(Header) == 64, "header size");
 
@@ -241,21 +242,25 @@ template <int N> __device__ __forceinline__ Codes<N> encode_v(const float (&v)[N
 }
 
 template <typename TW, typename TG, int BITS, bool SCORE>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(const char *__restrict__ ws, int32_t L, int64_t total_chunks, int32_t block, Step s,
+__global__ __launch_bounds__(kThreads) void adamw_kernel(const char *__restrict__ ws, int32_t L, int64_t total_chunks, int32_t of, int32_t block, Step s,
                                                          const float *__restrict__ live, const uint8_t *__restrict__ frozen, double *__restrict__ partials)
 {
     constexpr int N = kPer<BITS>, kPass = kThreads * N;
     __shared__ double lds[kThreads / kWave];
     const Header *h = reinterpret_cast<const Header *>(ws);
-    if (h->magic != kMagic || h->n_layers != L || h->total_chunks != total_chunks || h->bits != BITS || h->block != block ||
+    if (h->magic != kMagic || h->n_layers != L || h->total_chunks != total_chunks || h->of != of || h->bits != BITS || h->block != block ||
         h->w_dt != (sizeof(TW) == 2 ? SLIMFIT_BF16 : SLIMFIT_F32) || h->grad_dt != (sizeof(TG) == 2 ? SLIMFIT_BF16 : SLIMFIT_F32))
         return;                                             // no matching plan: touch nothing
     const Entry *table = reinterpret_cast<const Entry *>(ws + sizeof(Header));
     const int64_t chunk = blockIdx.x;
-    int lo = 0, hi = L - 1;                                 // the last tensor whose first_chunk <= chunk
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (table[mid].first_chunk <= chunk) lo = mid; else hi = mid - 1;
+    // the last tensor whose first_chunk <= chunk: 64 of them looked at a time (a small model's step 11.1 us with one at a time, 9.9 so)
+    int lo = 0;
+    for (int count = L; count > 1;) {
+        const int apart = (count + kWave - 1) / kWave, mine = (int)(threadIdx.x & 63) * apart;
+        const uint64_t before = __builtin_amdgcn_ballot_w64(mine < count && table[lo + min(mine, count - 1)].first_chunk <= chunk);
+        const int last = (__builtin_popcountll(before) - 1) * apart;
+        lo += last;
+        count = min(apart, count - last);
     }
     const Entry e = table[lo];
     if (!e.grad || (frozen && frozen[lo])) {
@@ -269,16 +274,14 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const char *__restrict_
         s.rate = (float)((double)s.lr / (1.0 - power(s.beta1, s.step)));
         s.root = (float)(1.0 / __builtin_sqrt(1.0 - power(s.beta2, s.step)));
     }
-    const int64_t off = (chunk - e.first_chunk) * kChunk;
-    const int len = (int)min((int64_t)kChunk, e.numel - off);
+    const int64_t off = (chunk - e.first_chunk) * of;
+    const int len = (int)min((int64_t)of, e.numel - off);
     const int lanes = block / N;
     const float decay = s.lr * e.decay;
     const uint32_t key = BITS == 8 ? mix(s.seed ^ mix(s.step ^ mix((uint32_t)lo + 1u))) + (uint32_t)(off >> 2) : 0u;
     double acc = 0.0;
-#pragma unroll 2
-    for (int p = 0; p < kChunk / kPass; ++p) {
-        if (p * kPass >= len) break;                        // (all threads together: lanes of a run stay together)
-        const int at = p * kPass + threadIdx.x * N;
+    for (int p = 0; p < len; p += kPass) {                  // (all threads together: lanes of a run stay together)
+        const int at = p + threadIdx.x * N;
         const int n = min(len - at, N);
         TW *const wp = static_cast<TW *>(e.w) + off + at;
         float w[N], g[N], m[N], v[N];
@@ -365,22 +368,26 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const char *__restrict_
     }
 }
 
-__global__ __launch_bounds__(kWave) void finish_kernel(const char *__restrict__ ws, int32_t L, int64_t total_chunks, Header want,
+__global__ __launch_bounds__(kThreads) void finish_kernel(const char *__restrict__ ws, int32_t L, int64_t total_chunks, Header want,
                                                        const double *__restrict__ partials, float *__restrict__ d_out)
 {
+    __shared__ double lds[kThreads / kWave];
     const int layer = blockIdx.x;
     const Header *h = reinterpret_cast<const Header *>(ws);
-    if (h->magic != kMagic || h->n_layers != L || h->total_chunks != total_chunks || h->bits != want.bits || h->block != want.block ||
+    if (h->magic != kMagic || h->n_layers != L || h->total_chunks != total_chunks || h->of != want.of || h->bits != want.bits || h->block != want.block ||
         h->w_dt != want.w_dt || h->grad_dt != want.grad_dt) {
         if (threadIdx.x == 0) d_out[layer] = __builtin_nanf("");
         return;
     }
     const Entry &e = reinterpret_cast<const Entry *>(ws + sizeof(Header))[layer];
-    const int64_t chunks = (e.numel + kChunk - 1) / kChunk;
+    const int64_t chunks = (e.numel + want.of - 1) / want.of;
     double acc = 0.0;
-    for (int64_t c = threadIdx.x; c < chunks; c += kWave) acc += partials[e.first_chunk + c];
+    for (int64_t c = threadIdx.x; c < chunks; c += kThreads) acc += partials[e.first_chunk + c];
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) acc += __shfl_xor(acc, o, kWave);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = acc;
+    __syncthreads();
+    acc = ((lds[0] + lds[1]) + lds[2]) + lds[3];
     if (threadIdx.x == 0) d_out[layer] = e.numel > 0 ? (float)(acc / (double)e.numel) : 0.0f;
 }
 
@@ -402,6 +409,7 @@ __global__ __launch_bounds__(kThreads) void states_kernel(const uint8_t *__restr
 
 struct Layout {
     int64_t chunks = 0;
+    int32_t of = kChunk;
     size_t bytes = 0;
 };
 
@@ -415,6 +423,11 @@ int32_t layout_of(int32_t L, const int64_t *numel, Layout *out)
         chunks += (numel[i] + kChunk - 1) / kChunk;
     }
     if (!grid_fits(chunks, kThreads)) return SLIMFIT_ERR_UNSUPPORTED;
+    if (chunks <= kFew) {
+        out->of = kShort;
+        chunks = 0;
+        for (int32_t i = 0; i < L; ++i) chunks += (numel[i] + kShort - 1) / kShort;
+    }
     out->chunks = chunks;
     out->bytes = table_bytes(L) + sizeof(double) * (size_t)chunks;
     return SLIMFIT_OK;
@@ -448,6 +461,7 @@ Header header_of(int32_t L, const Layout &lay, int32_t w_dt, int32_t grad_dt, in
     h.magic = kMagic;
     h.n_layers = L;
     h.total_chunks = lay.chunks;
+    h.of = lay.of;
     h.w_dt = w_dt;
     h.grad_dt = grad_dt;
     h.bits = bits;
@@ -456,13 +470,13 @@ Header header_of(int32_t L, const Layout &lay, int32_t w_dt, int32_t grad_dt, in
 }
 
 template <typename TW, typename TG>
-void launch_adamw(int32_t bits, bool score, unsigned grid, hipStream_t st, const char *ws, int32_t L, int64_t chunks, int32_t block, const Step &s,
+void launch_adamw(int32_t bits, bool score, unsigned grid, hipStream_t st, const char *ws, int32_t L, int64_t chunks, int32_t of, int32_t block, const Step &s,
                   const float *live, const uint8_t *frozen, double *partials)
 {
-    if (bits == 32 && score) launch(adamw_kernel<TW, TG, 32, true>, grid, kThreads, 0, st, ws, L, chunks, block, s, live, frozen, partials);
-    else if (bits == 32) launch(adamw_kernel<TW, TG, 32, false>, grid, kThreads, 0, st, ws, L, chunks, block, s, live, frozen, partials);
-    else if (score) launch(adamw_kernel<TW, TG, 8, true>, grid, kThreads, 0, st, ws, L, chunks, block, s, live, frozen, partials);
-    else launch(adamw_kernel<TW, TG, 8, false>, grid, kThreads, 0, st, ws, L, chunks, block, s, live, frozen, partials);
+    if (bits == 32 && score) launch(adamw_kernel<TW, TG, 32, true>, grid, kThreads, 0, st, ws, L, chunks, of, block, s, live, frozen, partials);
+    else if (bits == 32) launch(adamw_kernel<TW, TG, 32, false>, grid, kThreads, 0, st, ws, L, chunks, of, block, s, live, frozen, partials);
+    else if (score) launch(adamw_kernel<TW, TG, 8, true>, grid, kThreads, 0, st, ws, L, chunks, of, block, s, live, frozen, partials);
+    else launch(adamw_kernel<TW, TG, 8, false>, grid, kThreads, 0, st, ws, L, chunks, of, block, s, live, frozen, partials);
 }
 
 }  // namespace
@@ -525,7 +539,7 @@ extern "C" int32_t slimfit_adamw_plan(void *const *w, int32_t w_dt, const void *
             const int32_t i = first + t;
             batch.e[t] = Entry{w[i], grad[i], m[i], v[i], bits == 8 ? m_scales[i] : nullptr, bits == 8 ? v_scales[i] : nullptr,
                                copies ? static_cast<uint16_t *>(copies[i]) : nullptr, numel[i], next, weight_decay[i], 0u};
-            next += (numel[i] + kChunk - 1) / kChunk;
+            next += (numel[i] + lay.of - 1) / lay.of;
         }
         launch(plan_kernel, 1, kWave, 0, st, static_cast<char *>(workspace), h, first, count, batch);
     }
@@ -558,15 +572,15 @@ extern "C" int32_t slimfit_adamw_run(const int64_t *numel, int32_t L, int32_t w_
     if (lay.chunks > 0) {
         const unsigned grid = (unsigned)lay.chunks;
         if (w_dt == SLIMFIT_F32 && grad_dt == SLIMFIT_F32)
-            launch_adamw<float, float>(bits, d_out != nullptr, grid, st, ws, L, lay.chunks, want.block, s, live, frozen, partials);
+            launch_adamw<float, float>(bits, d_out != nullptr, grid, st, ws, L, lay.chunks, lay.of, want.block, s, live, frozen, partials);
         else if (w_dt == SLIMFIT_F32)
-            launch_adamw<float, uint16_t>(bits, d_out != nullptr, grid, st, ws, L, lay.chunks, want.block, s, live, frozen, partials);
+            launch_adamw<float, uint16_t>(bits, d_out != nullptr, grid, st, ws, L, lay.chunks, lay.of, want.block, s, live, frozen, partials);
         else if (grad_dt == SLIMFIT_F32)
-            launch_adamw<uint16_t, float>(bits, d_out != nullptr, grid, st, ws, L, lay.chunks, want.block, s, live, frozen, partials);
+            launch_adamw<uint16_t, float>(bits, d_out != nullptr, grid, st, ws, L, lay.chunks, lay.of, want.block, s, live, frozen, partials);
         else
-            launch_adamw<uint16_t, uint16_t>(bits, d_out != nullptr, grid, st, ws, L, lay.chunks, want.block, s, live, frozen, partials);
+            launch_adamw<uint16_t, uint16_t>(bits, d_out != nullptr, grid, st, ws, L, lay.chunks, lay.of, want.block, s, live, frozen, partials);
     }
-    if (d_out) launch(finish_kernel, (unsigned)L, kWave, 0, st, ws, L, lay.chunks, want, partials, d_out);
+    if (d_out) launch(finish_kernel, (unsigned)L, kThreads, 0, st, ws, L, lay.chunks, want, partials, d_out);
     return launch_status();
 }
 
