@@ -210,7 +210,8 @@ int32_t slimfit_apply_update_layer_delta(void *const *w, int32_t w_dt,
  *         g' = grad_factor g,   m' = beta1 m + (1 - beta1) g',   v' = beta2 v + ((1 - beta2) g') g',
  *         d = -(lr weight_decay w + lr / (1 - beta1^t) m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)),
  *         w' = w + d;      d_out = mean over the layer of |d| / max(|w|, floor)  (0 where d is 0).
- *     fp32, each operation rounded; bf16 weights are rounded to nearest even once more.
+ *     fp32, each operation rounded, m' and v' without a fused one; roots and reciprocals of d and the distance to
+ *     within the last place.  bf16 weights are rounded to nearest even once more.
  *
  *  w, grad, m, v : HOST arrays of L DEVICE pointers, 16-byte aligned; numel[i] elements each, of w_dt,
  *                  grad_dt and the states' type.  w, m and v are read and written.  grad[i] NULL: the

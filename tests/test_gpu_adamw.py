@@ -343,3 +343,52 @@ def test_offsets_past_32_bits():
     code, _ = encode_v(np.concatenate((v1[:lead], v1)), 256, np.concatenate((noise[:lead] * 0, noise)))
     assert np.array_equal(v[-4097:].cpu().numpy(), code[lead:])
     assert math.isfinite(float(ms[-1]))
+
+
+@pytest.mark.parametrize("bits,block", [(32, 0), (8, 256)])
+def test_many_tensors_of_many_chunks(bits, block):
+    """More tensors than are looked at together, empty ones among them, and chunks of the long kind (over 512 of 8192 elements)."""
+    require_gpu()
+    sizes = [3, 0, 0, 700, 8192, 1] * 24 + [4_400_003] + [0, 513, 0, 16385, 0] * 15
+    model = Model(sizes, torch.float32, torch.bfloat16, bits, block)
+    model.plan()
+    looked_at = (0, 3, 4, 5, 60, 66, 143, 144, 146, 148, len(sizes) - 4, len(sizes) - 2)
+    before = {i: model.expect(i, 2) for i in looked_at}
+    kept = [t.clone() for t in model.w]
+    model.run(2)
+    torch.cuda.synchronize()
+    for i, b in before.items():
+        check(model, b, i, torch.float32)
+    for i, n in enumerate(sizes):
+        assert (n == 0 and float(model.d[i]) == 0.0) or (float(model.d[i]) > 0.0 and not torch.equal(kept[i], model.w[i]))
+    assert model.untouched_around()
+
+
+@pytest.mark.parametrize("eps", [1e-8, 1e-20, 1e-30])
+def test_numbers_below_the_normal_ones(eps):
+    """A v, an eps and weights at and below the type's least normal number, and a floor of 0: the distance's terms are those of the formula, a weight
+    of 0 that moves makes it infinite, one that does not adds nothing."""
+    require_gpu()
+    tiny = np.float32(2.0 ** -126)
+    w = [np.array([0.0, 1.0], np.float32), np.array([tiny / 4, 2.0, -tiny], np.float32), np.full(9, 0.25, np.float32), np.array([0.0, 0.5], np.float32)]
+    g = [np.zeros(2, np.float32), np.array([2.0 ** -100, 1.0, -1.0], np.float32), np.linspace(1, 9, 9, dtype=np.float32) * np.float32(2.0 ** -66),
+         np.array([1.0, 1.0], np.float32)]
+    put = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+    tw, tg = [put(x) for x in w], [put(x) for x in g]
+    m, v = ([torch.zeros_like(t) for t in tw] for _ in range(2))
+    numel = np.array([x.size for x in w], dtype=np.int64)
+    ws, d = torch.zeros(sf.adamw_workspace(numel), dtype=torch.uint8, device="cuda"), torch.empty(4, device="cuda")
+    sf.adamw_plan(tw, tg, m, v, None, None, [0.0] * 4, 32, 0, ws)
+    sf.adamw_run(numel, sf.F32, sf.F32, 32, 0, 1e-2, 0.9, 0.999, eps, 1, ws, d_out=d)
+    for i in range(4):
+        m64 = m[i].double().cpu().numpy()                  # as they were stored: held products may be below the normal numbers
+        v64 = v[i].double().cpu().numpy()
+        assert np.array_equal(m[i].cpu().numpy(), g[i] * np.float32(1 - 0.9)) and np.array_equal(v[i].cpu().numpy(), (g[i] * np.float32(1 - 0.999)) * g[i])
+        move = 1e-2 / 0.1 * m64 / (np.sqrt(v64 / (1 - 0.999)) + float(np.float32(eps)))
+        want = w[i].astype(np.float64) - move
+        # fifteen roundings of the move; a v below the normal numbers counts as 0 from an eps of 2^-40 on, a root of 2^-63 and so 2^-23 of the sum
+        off = np.abs(move) * 17 * 2.0 ** -24 + np.abs(want) * 2.0 ** -24 + 2.0 ** -149
+        assert np.all(np.abs(tw[i].double().cpu().numpy() - want) <= off)
+    assert float(d[0]) == 0.0 and math.isinf(float(d[3]))
+    terms = np.abs(1e-2 / 0.1 * m[2].double().cpu().numpy() / (np.sqrt(v[2].double().cpu().numpy() / (1 - 0.999)) + float(np.float32(eps)))) / 0.25
+    assert abs(float(d[2]) - terms.mean()) <= 20 * 2.0 ** -24 * terms.mean() + 2.0 ** -149
