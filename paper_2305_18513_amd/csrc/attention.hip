@@ -58,22 +58,24 @@ __global__ void __launch_bounds__(kAttnThreads) turn_kernel(const T *__restrict_
     }
 }
 
-// Sums of ds by distance over `each` blocks of 128 queries of all sequences': blockIdx.z has its share, in order.  What a wave did not
+// Sums of ds by distance over `each` blocks of 128 queries (and shares of their keys) of all sequences': blockIdx.z has its share, in order.  What a wave did not
 // write is past its descriptor's end: 0, with no branch that a load would wait at (512 tokens: 11.6 us with branches, 5.0 without).
-__global__ void __launch_bounds__(kWave) distances_kernel(Attention a, const float *__restrict__ parts, int64_t part_row, int blocks, int each, float *__restrict__ sums)
+__global__ void __launch_bounds__(kWave) distances_kernel(Attention a, const float *__restrict__ parts, int64_t part_row, int blocks, int splits, int each, float *__restrict__ sums)
 {
     const int all = a.q_tokens + a.k_tokens - 1, head = blockIdx.y, at = (int)(blockIdx.x * kWave + threadIdx.x);
-    const int end = min(a.batch * blocks, ((int)blockIdx.z + 1) * each);
+    const int end = min(a.batch * blocks * splits, ((int)blockIdx.z + 1) * each);
     double sum = 0.0;
     for (int n0 = (int)blockIdx.z * each; n0 < end; n0 += kAtOnce) {
         float x[kAtOnce][kAttnWaves];
 #pragma unroll
         for (int m = 0; m < kAtOnce; ++m) {
-            const int n = min(n0 + m, end - 1), b = n / blocks, block = n % blocks, written = key_tiles(a, block * kBlock, keys_of(a, b)) * kTile + kOwn;
-            const float *const of = parts + (((int64_t)b * a.q_heads + head) * blocks + block) * kAttnWaves * part_row;
+            const int n = min(n0 + m, end - 1), split = n % splits, b = n / splits / blocks, block = n / splits % blocks;
+            const int tiles = key_tiles(a, block * kBlock, keys_of(a, b)), t0 = first_of(tiles, split, splits);
+            const int written = (first_of(tiles, split + 1, splits) - t0) * kTile + kOwn;
+            const float *const of = parts + ((((int64_t)b * a.q_heads + head) * blocks + block) * splits + split) * kAttnWaves * part_row;
 #pragma unroll
             for (int w = 0; w < kAttnWaves; ++w) {
-                const int place = at - (a.q_tokens - 1) + block * kBlock + w * kOwn + kOwn - 1;
+                const int place = at - (a.q_tokens - 1) + block * kBlock + w * kOwn + kOwn - 1 - t0 * kTile;
                 const Buffer row = buffer_at(of + w * part_row, n0 + m < end ? (int64_t)written * 4 : 0);
                 // (a sum of an offset below 0 and a constant would be past the end even where it is not)
                 x[m][w] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(row, place < 0 ? kNowhere : place * 4, 0, 0));
@@ -108,6 +110,53 @@ __global__ void __launch_bounds__(kAttnThreads) buckets_kernel(Attention a, cons
     else dtable[(int64_t)bucket * a.q_heads + head] = (T)bf16_narrow(x);
 }
 
+// Where tiles of a block were shared out: dq, dk and dv from the shares' sums, in order, four elements of a row a thread.  (Transposed keys'
+// gradients by element, tokens beside each other.)
+template <typename T> __device__ __forceinline__ void store4(T *to, f32x4 x)
+{
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4 *>(to) = x;
+    else *reinterpret_cast<u32x2 *>(to) = u32x2{bf16_narrow2(x[0], x[1]), bf16_narrow2(x[2], x[3])};
+}
+template <typename T>
+__global__ void __launch_bounds__(kAttnThreads) shares_kernel(Attention a, Gradients g)
+{
+    const int vectors = a.head_dim / 4;
+    const int64_t q_rows = (int64_t)a.batch * a.q_heads * a.q_tokens, k_rows = (int64_t)a.batch * a.kv_heads * a.k_tokens;
+    int64_t n = (int64_t)blockIdx.x * kAttnThreads + threadIdx.x;
+    const bool query = n < q_rows * vectors;
+    if (!query && (n -= q_rows * vectors) >= 2 * k_rows * vectors) return;
+    const int tokens = query ? a.q_tokens : a.k_tokens, heads = query ? a.q_heads : a.kv_heads, width = query ? vectors : 2 * vectors;
+    int64_t row;
+    int v;
+    if (!query && g.dk_d != 1) {
+        const int64_t line = n / tokens;                    // of a pair's vectors
+        row = line / width * tokens + n % tokens;
+        v = (int)(line % width);
+    } else {
+        row = n / width;
+        v = (int)(n % width);
+    }
+    const float *from = (query ? g.dq_parts : g.dk_parts) + (row * width + v) * 4;
+    const int64_t step = (query ? q_rows : k_rows) * width * 4;
+    f32x4 sum = *reinterpret_cast<const f32x4 *>(from);
+    for (int s = 1; s < (query ? g.q_splits : g.k_splits); ++s) sum += *reinterpret_cast<const f32x4 *>(from + s * step);
+    const int64_t pair = row / tokens, token = row % tokens, batch = pair / heads, head = pair % heads;
+    if (query) {
+        store4(static_cast<T *>(g.dq) + batch * g.dq_b + head * g.dq_h + token * g.dq_t + v * 4, sum);
+    } else if (v >= vectors) {
+        store4(static_cast<T *>(g.dv) + batch * g.dv_b + head * g.dv_h + token * g.dv_t + (v - vectors) * 4, sum);
+    } else if (g.dk_d == 1) {
+        store4(static_cast<T *>(g.dk) + batch * g.dk_b + head * g.dk_h + token * g.dk_t + v * 4, sum);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            T *const to = static_cast<T *>(g.dk) + batch * g.dk_b + head * g.dk_h + token * g.dk_t + (v * 4 + e) * g.dk_d;
+            if constexpr (sizeof(T) == 4) *to = sum[e];
+            else *to = (T)bf16_narrow(sum[e]);
+        }
+    }
+}
+
 struct Sizes {
     int32_t dt, layout;
     int64_t batch;
@@ -135,13 +184,36 @@ int32_t check_sizes(const Sizes &z)
 bool turned(const Sizes &z) { return z.layout == SLIMFIT_HEADS_APART && z.batch > 0 && z.k_tokens > 0 && z.q_tokens > 0; }
 size_t turned_bytes(const Sizes &z) { return turned(z) ? rounded((size_t)z.k_count() * z.e()) : 0; }
 int q_blocks(const Sizes &z) { return (z.q_tokens + kBlock - 1) / kBlock; }
+// Backward: how many workgroups share the tiles of a block's other side out where blocks do not fill the card; their sums meet in memory,
+// added up in order by one more launch.  (us of the backward pass in one share, so; T tokens, a head each T / 128 blocks)
+//   fp32, whose tiles take longest, from two tiles on: heads of 128: 1 x 200 120, 53; 6 x 512 249, 69; 1 x 1400 638, 91; 6 x 1400 655, 270; heads
+//   of 32: 1 x 200 37, 21; 40 x 200 38, 32; 6 x 1400 187, 80.  Heads of up to 64, two workgroups of which fit a compute unit, with up to 256
+//   blocks of 8 tiles and more: 16 x 1400 of 64, causal 409, 267, all 342, 334; of 4 tiles not: 96 x 200 71, 89.
+//   bf16, where the queries' shares each go over all keys for delta: as many blocks as four for a tile: heads of 128: 1 x 512 56, 39; 6 x 512 57, 48;
+//   6 x 1400 139, 102; of 32: 1 x 512 22, 20; 1 x 1400 53, 33; 6 x 1400 56, 49; but 16 x 512 24, 28; 40 x 300 20, 26.
+int splits_of(const Sizes &z, int64_t workgroups, int64_t tiles)
+{
+    if (workgroups == 0) return 1;
+    const bool low = z.dt == SLIMFIT_BF16;
+    if (low && (tiles < 8 || workgroups > 4 * tiles)) return 1;
+    int64_t splits = 256 / workgroups, most = low || tiles > 16 ? tiles / 2 : tiles < 8 ? tiles : 8;
+    if (!low && z.head_dim <= 64 && splits == 1 && tiles >= 8) splits = 512 / workgroups;
+    if (splits > most) splits = most;
+    return splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : (int)splits;
+}
+int query_splits(const Sizes &z) { return splits_of(z, z.batch * z.q_heads * q_blocks(z), ((int64_t)z.k_tokens + kTile - 1) / kTile); }
+int key_splits(const Sizes &z)
+{
+    return splits_of(z, z.batch * z.kv_heads * ((z.k_tokens + kBlock - 1) / kBlock), (int64_t)(z.q_heads / z.kv_heads) * ((z.q_tokens + kTile - 1) / kTile));
+}
+bool split(const Sizes &z) { return query_splits(z) > 1 || key_splits(z) > 1; }
 // blocks of queries that one share of the sums by distance adds up (16 x 512, 12 heads: 64 in one share 57 us, 8 each 6.6), and the shares
 int64_t share_of(const Sizes &z)
 {
-    const int64_t all = z.batch * q_blocks(z);
+    const int64_t all = z.batch * q_blocks(z) * query_splits(z);
     return all <= 8 * 32 ? 8 : (all + 31) / 32;
 }
-int64_t shares_of(const Sizes &z) { return (z.batch * q_blocks(z) + share_of(z) - 1) / share_of(z); }
+int64_t shares_of(const Sizes &z) { return (z.batch * q_blocks(z) * query_splits(z) + share_of(z) - 1) / share_of(z); }
 int64_t part_row(const Sizes &z) { return ((int64_t)z.k_tokens + kTile - 1) / kTile * kTile + kTile; }
 
 // How many workgroups share a sequence's keys out, or 0: 128 queries of a head a workgroup.  (us with those, with few queries)
@@ -172,13 +244,15 @@ size_t part_bytes(const Sizes &z)
 }
 
 struct BackwardPlaces {
-    size_t rows, parts, sums, bytes;
+    size_t rows, parts, sums, dq, dk, bytes;
     BackwardPlaces(const Sizes &z, bool table)
     {
         rows = turned_bytes(z);
         parts = rows + rounded((size_t)(z.batch * z.q_heads) * (size_t)z.q_tokens * 12);
-        sums = parts + (table ? rounded((size_t)(z.batch * z.q_heads) * (size_t)q_blocks(z) * kAttnWaves * (size_t)part_row(z) * 4) : 0);
-        bytes = sums + (table ? rounded((size_t)shares_of(z) * (size_t)z.q_heads * ((size_t)z.q_tokens + (size_t)z.k_tokens) * 4) : 0);
+        sums = parts + (table ? rounded((size_t)(z.batch * z.q_heads) * (size_t)(q_blocks(z) * query_splits(z)) * kAttnWaves * (size_t)part_row(z) * 4) : 0);
+        dq = sums + (table ? rounded((size_t)shares_of(z) * (size_t)z.q_heads * ((size_t)z.q_tokens + (size_t)z.k_tokens) * 4) : 0);
+        dk = dq + (split(z) ? rounded((size_t)query_splits(z) * (size_t)z.q_count() * 4) : 0);
+        bytes = dk + (split(z) ? rounded((size_t)key_splits(z) * (size_t)z.k_count() * 8) : 0);
     }
 };
 
@@ -373,16 +447,23 @@ extern "C" int32_t slimfit_attention_backward(const void *dout, const void *q, c
     const bool across = layout == SLIMFIT_HEADS_APART;      // dk lies transposed too: tokens beside each other
     float *const parts = dtable && pairs ? reinterpret_cast<float *>(ws + at.parts) : nullptr;
     const Gradients g = {dout, out, stats, dq, dk, dv, oq.b, oq.h, oq.t, ok.b, ok.h, across ? 1 : ok.t, across ? k_tokens : 1, ov.b, ov.h, ov.t,
-                         reinterpret_cast<float *>(ws + at.rows), parts, part_row(z)};
+                         reinterpret_cast<float *>(ws + at.rows), parts, part_row(z), query_splits(z), key_splits(z), reinterpret_cast<float *>(ws + at.dq),
+                         reinterpret_cast<float *>(ws + at.dk)};
     if (dt == SLIMFIT_BF16) attention_backward_bf16(a, g, st);
     else attention_backward_f32(a, g, st);
+    if (split(z)) {
+        const int64_t vectors = (z.q_count() + 2 * z.k_count()) / 4;
+        const unsigned grid = (unsigned)((vectors + kAttnThreads - 1) / kAttnThreads);
+        if (dt == SLIMFIT_BF16) launch(shares_kernel<uint16_t>, grid, kAttnThreads, 0, st, a, g);
+        else launch(shares_kernel<float>, grid, kAttnThreads, 0, st, a, g);
+    }
     if (dtable) {
         float *const sums = reinterpret_cast<float *>(ws + at.sums);
         const int all = q_tokens + k_tokens - 1;
         const int shares = parts ? (int)shares_of(z) : 0;
         if (parts)
             launch(distances_kernel, dim3((unsigned)((all + kWave - 1) / kWave), (unsigned)q_heads, (unsigned)shares), kWave, 0, st, a, parts, g.part_row,
-                   q_blocks(z), (int)share_of(z), sums);
+                   q_blocks(z), g.q_splits, (int)share_of(z), sums);
         const dim3 grid((unsigned)buckets, (unsigned)q_heads);
         if (dt == SLIMFIT_BF16) launch(buckets_kernel<uint16_t>, grid, kAttnThreads, 0, st, a, sums, shares, static_cast<uint16_t *>(dtable));
         else launch(buckets_kernel<float>, grid, kAttnThreads, 0, st, a, sums, shares, static_cast<float *>(dtable));

@@ -58,6 +58,8 @@ __device__ __forceinline__ int seen_by(const Attention &a, int i, int keys)
 {
     return a.causal ? min(keys, max(0, i + 1 + a.k_tokens - a.q_tokens)) : keys;
 }
+// the first of `all` tiles that the `split`-th of `splits` goes over; the next one's is its end
+__host__ __device__ __forceinline__ int first_of(int all, int split, int splits) { return (int)((int64_t)all * split / splits); }
 // tiles of keys that the 128 queries from q0 on see
 __device__ __forceinline__ int key_tiles(const Attention &a, int q0, int keys)
 {
@@ -412,6 +414,10 @@ struct Gradients {
     float *rows;                             // [3][batch * q_heads * q_tokens]: what p is taken by (two numbers), delta
     float *parts;                            // sums of ds by distance, or NULL
     int64_t part_row;                        // floats of a wave's
+    // workgroups that share the tiles of one block out, and, where that is more than one, their sums: dq [q_splits][batch][q_heads]
+    // [q_tokens][head_dim], dk and dv [k_splits][batch][kv_heads][k_tokens][2][head_dim]
+    int32_t q_splits, k_splits;
+    float *dq_parts, *dk_parts;
 };
 void attention_backward_f32(const Attention &a, const Gradients &g, hipStream_t st);
 void attention_backward_bf16(const Attention &a, const Gradients &g, hipStream_t st);

@@ -29,11 +29,11 @@ constexpr int kSkew = kOwn + 4;              // floats of a query's ds in LDS
 // more than kTwiceTiles tiles, once for delta = sum of p dp.  So do those with a bias, at any length: sums of ds over a bucket of many keys are
 // little but e otherwise (two buckets: 5 % off), and whether the table takes a gradient changes no other.  Keys' gradients take
 // the right delta in any case.
-template <typename T, int D, bool BIAS> constexpr bool kRights = sizeof(T) == 2 && D <= 96 && !BIAS;
-template <typename T, int D, bool BIAS> constexpr bool kTwice = sizeof(T) == 2 && !kRights<T, D, BIAS>;
+template <typename T, int D, bool ALWAYS> constexpr bool kRights = sizeof(T) == 2 && D <= 96 && !ALWAYS;
+template <typename T, int D, bool ALWAYS> constexpr bool kTwice = sizeof(T) == 2 && !kRights<T, D, ALWAYS>;
 constexpr int kTwiceTiles = 2;
 
-template <typename T, int D, bool BIAS, bool PARTS>
+template <typename T, int D, bool BIAS, bool PARTS, bool SPLIT>
 __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 256) ? 1 : 2) queries_kernel(Attention a, Gradients g, int blocks)
 {
     __shared__ __align__(1024) char tiles[2][2 * kTileBytes<T, D>];
@@ -42,21 +42,27 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
     __shared__ int buckets[2][PARTS ? kDistances : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int group = a.q_heads / a.kv_heads;
-    const Place place(a.batch * a.kv_heads, blocks, group, a.causal != 0);
-    const int block = a.causal ? blocks - 1 - place.block : place.block;       // the longest first
+    const int splits = SPLIT ? g.q_splits : 1;
+    const Place place(a.batch * a.kv_heads, blocks * splits, group, a.causal != 0);
+    const int block = a.causal ? blocks - 1 - place.block / splits : place.block / splits, split = place.block % splits;     // the longest first
     const int batch = place.unit / a.kv_heads, kv = place.unit % a.kv_heads, head = kv * group + place.in, bh = batch * a.q_heads + head;
     const int q0 = block * kBlock, mine = q0 + wave * kOwn, i = mine + (lane & 31);
     const T *const q = static_cast<const T *>(a.q.at) + batch * a.q.b + head * a.q.h;
     const T *const k = static_cast<const T *>(a.k.at) + batch * a.k.b + kv * a.k.h;
     const T *const v = static_cast<const T *>(a.v.at) + batch * a.v.b + kv * a.v.h;
-    const int keys = keys_of(a, batch), count = key_tiles(a, q0, keys);
+    const int keys = keys_of(a, batch), all_tiles = key_tiles(a, q0, keys);
+    const int t0 = SPLIT ? first_of(all_tiles, split, splits) : 0, count = SPLIT ? first_of(all_tiles, split + 1, splits) : all_tiles;
     const int seen = seen_by(a, i, keys), all_see = seen_by(a, mine, keys), any_sees = mine < a.q_tokens ? seen_by(a, min(mine + kOwn, a.q_tokens) - 1, keys) : 0;
     const float scale = a.scale * kLog2e;
+    constexpr bool ALWAYS = BIAS || SPLIT;                  // goes over the keys twice at any length
+    // (where tiles are shared out each goes over all of them for delta: from tile `start` to `end` first)
+    const bool twice = kTwice<T, D, ALWAYS> && (ALWAYS ? !SPLIT || split == 0 || count > t0 : all_tiles <= kTwiceTiles);
+    const int start = twice ? 0 : t0, end = twice ? all_tiles : count;
 
     Tiles<T, D> kl, vl;
     BiasLoad bl;
-    kl.start(k, a.k.t, 0, keys, a.head_dim);
-    vl.start(v, a.v.t, 0, keys, a.head_dim);
+    kl.start(k, a.k.t, start * kTile, keys, a.head_dim);
+    vl.start(v, a.v.t, start * kTile, keys, a.head_dim);
     auto fetch = [&](int t) {
         kl.fetch(tiles[t & 1]);
         vl.fetch(tiles[t & 1] + kTileBytes<T, D>);
@@ -105,20 +111,20 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
         } else if (BIAS) {
             first = 0.0f;                                   // (second stays infinite)
         }
-        if (half == 0) {                                    // for the second kernel
+        if (half == 0 && split == 0) {                      // for the second kernel
             g.rows[at] = first;
             g.rows[all + at] = second;
         }
     }
-    f32x16 dq[D / 32], pk[kRights<T, D, BIAS> ? D / 32 : 1];
+    f32x16 dq[D / 32], pk[kRights<T, D, ALWAYS> ? D / 32 : 1];
 #pragma unroll
     for (int n = 0; n < D / 32; ++n) {
         dq[n] = zeros16();
-        if constexpr (kRights<T, D, BIAS>) pk[n] = zeros16();
+        if constexpr (kRights<T, D, ALWAYS>) pk[n] = zeros16();
     }
     float off = 0.0f;                                       // -e
     float carry = 0.0f;
-    float *const part = PARTS ? g.parts + ((int64_t)bh * blocks * kAttnWaves + block * kAttnWaves + wave) * g.part_row : nullptr;
+    float *const part = PARTS ? g.parts + (((int64_t)bh * blocks + block) * splits + split) * kAttnWaves * g.part_row + wave * g.part_row : nullptr;
 
     if constexpr (BIAS) {
         load_column<T>(a, head, column);
@@ -142,15 +148,15 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
 #pragma unroll
         for (int r = 0; r < 16; ++r) x[r] = row_of(r, 0) < some ? x[r] : 0.0f;
     };
-    if (count > 0) {
-        fetch(0);
+    if (end > start) {
+        fetch(start);
         own.arrive();
         grad.arrive();
-        land(0);
+        land(start);
     }
-    if (kTwice<T, D, BIAS> && (BIAS || count <= kTwiceTiles)) {
+    if (twice) {
         float x = 0.0f, y = 0.0f;
-        for (int t = 0; t < count; ++t) {
+        for (int t = start; t < end; ++t) {
             fetch(t + 1);
             if (t * kTile < any_sees)
 #pragma unroll
@@ -169,14 +175,14 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
             land(t + 1);
         }
         delta = both_sum(x + y);
-        if (count > 0) {
-            kl.start(k, a.k.t, 0, keys, a.head_dim);
-            vl.start(v, a.v.t, 0, keys, a.head_dim);
-            fetch(0);
-            land(0);
+        if (count > t0) {
+            kl.start(k, a.k.t, t0 * kTile, keys, a.head_dim);
+            vl.start(v, a.v.t, t0 * kTile, keys, a.head_dim);
+            fetch(t0);
+            land(t0);
         }
     }
-    for (int t = 0; t < count; ++t) {
+    for (int t = t0; t < count; ++t) {
         const char *const tile = tiles[t & 1];
         const int k0 = t * kTile;
         fetch(t + 1);
@@ -191,9 +197,9 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
                 for (int r = 0; r < 16; ++r) s[r] = p[r] * (s[r] - delta);
                 if (some) {
                     leave_out(t, n, s);
-                    if constexpr (kRights<T, D, BIAS>) leave_out(t, n, p);
+                    if constexpr (kRights<T, D, ALWAYS>) leave_out(t, n, p);
                 }
-                if constexpr (sizeof(T) == 2 && !BIAS) {
+                if constexpr (sizeof(T) == 2 && !ALWAYS) {
                     float x = s[0], y = s[1];
 #pragma unroll
                     for (int r = 2; r < 16; r += 2) {
@@ -236,27 +242,32 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
                         lower = both_sum(lower);
                         upper = both_sum(upper);
                     }
-                    if (half == 0) part[k0 + 32 * n + lane] = lower + carry;
+                    if (half == 0) part[k0 - t0 * kTile + 32 * n + lane] = lower + carry;
                     carry = upper;
                 }
-                if constexpr (kRights<T, D, BIAS>) sums_of_two<D>(tile, 32 * n, s, dq, p, pk);
+                if constexpr (kRights<T, D, ALWAYS>) sums_of_two<D>(tile, 32 * n, s, dq, p, pk);
                 else sums<T, D>(tile, 32 * n, s, dq);
             }
         } else if (PARTS) {
-            part[k0 + lane] = half == 0 ? carry : 0.0f;
+            part[k0 - t0 * kTile + lane] = half == 0 ? carry : 0.0f;
             carry = 0.0f;
         }
         land(t + 1);
     }
-    if (PARTS && half == 0) part[count * kTile + lane] = carry;
-    if constexpr (sizeof(T) == 2 && !BIAS) off = both_sum(off);
-    if constexpr (kRights<T, D, BIAS>) {
+    if (PARTS && half == 0) part[(count - t0) * kTile + lane] = carry;
+    if constexpr (sizeof(T) == 2 && !ALWAYS) off = both_sum(off);
+    if constexpr (kRights<T, D, ALWAYS>) {
 #pragma unroll
         for (int n = 0; n < D / 32; ++n)
 #pragma unroll
             for (int r = 0; r < 16; ++r) dq[n][r] = __builtin_fmaf(-off, pk[n][r], dq[n][r]);
     }
-    if (half == 0 && i < a.q_tokens) g.rows[2 * (int64_t)a.batch * a.q_heads * a.q_tokens + (int64_t)bh * a.q_tokens + i] = delta + off;      // for the second kernel
+    if (half == 0 && split == 0 && i < a.q_tokens) g.rows[2 * (int64_t)a.batch * a.q_heads * a.q_tokens + (int64_t)bh * a.q_tokens + i] = delta + off;      // for the second kernel
+    if (SPLIT) {
+        if (i < a.q_tokens)
+            store_row<float, D>(dq, a.scale, g.dq_parts + (((int64_t)split * a.batch * a.q_heads + bh) * a.q_tokens + i) * a.head_dim, a.head_dim);
+        return;
+    }
     if (i < a.q_tokens) store_row<T, D>(dq, a.scale, static_cast<T *>(g.dq) + batch * g.dq_b + head * g.dq_h + i * g.dq_t, a.head_dim);
 }
 
@@ -264,7 +275,7 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
 // tiles to make up for them.
 template <typename T, int D> constexpr bool kValuesInLds = sizeof(T) == 2 && D > 64;
 
-template <typename T, int D, bool BIAS>
+template <typename T, int D, bool BIAS, bool SPLIT>
 __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2) keys_kernel(Attention a, Gradients g, int blocks)
 {
     constexpr int ROWS = kValuesInLds<T, D> ? 32 : kTile, BYTES = ROWS * kPitch<T, D>;
@@ -272,8 +283,9 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
     __shared__ __align__(16) float rows[2][3][ROWS];
     __shared__ float column[BIAS ? kMostBuckets : 1], biases[2][BIAS ? kDistances : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const Place place(a.batch * a.kv_heads, blocks, 1, a.causal != 0);
-    const int batch = place.unit / a.kv_heads, kv = place.unit % a.kv_heads, block = place.block, group = a.q_heads / a.kv_heads;
+    const int splits = SPLIT ? g.k_splits : 1;
+    const Place place(a.batch * a.kv_heads, blocks * splits, 1, a.causal != 0);
+    const int batch = place.unit / a.kv_heads, kv = place.unit % a.kv_heads, block = place.block / splits, split = place.block % splits, group = a.q_heads / a.kv_heads;
     const int k0 = block * kBlock, mine = k0 + wave * kOwn, j = mine + (lane & 31);
     const int keys = keys_of(a, batch);
     const float scale = a.scale * kLog2e;
@@ -282,7 +294,7 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
     // queries that see the first of the workgroup's keys, and all of the wave's
     const int offset = a.k_tokens - a.q_tokens;
     const int from = a.causal ? max(0, k0 - offset) / ROWS : 0, per_head = k0 < keys ? max(0, (a.q_tokens + ROWS - 1) / ROWS - from) : 0;
-    const int count = per_head * group;
+    const int all_tiles = per_head * group, t0 = SPLIT ? first_of(all_tiles, split, splits) : 0, count = SPLIT ? first_of(all_tiles, split + 1, splits) : all_tiles;
 
     Own<T, D> own;
     Own<T, kValuesInLds<T, D> ? 32 : D> val;
@@ -298,11 +310,11 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
     float held[3];
     // Tiles of queries from the last to the first, of each the heads in turn, so that the workgroups of a pair read the same ones at
     // about the same time, whatever their keys' place.
-    int q0 = (from + per_head - 1) * ROWS, next = 0;        // where `fetch` stands: the tile's first query, the head of the group
-    ql.start(static_cast<const T *>(a.q.at) + batch * a.q.b + kv * group * a.q.h, a.q.t, q0, a.q_tokens, a.head_dim);
-    gl.start(static_cast<const T *>(g.dout) + (int64_t)batch * a.q_tokens * out_row + (int64_t)kv * group * a.head_dim, out_row, q0, a.q_tokens, a.head_dim);
+    int q0 = (from + per_head - 1 - t0 / group) * ROWS, next = t0 % group;     // where `fetch` stands: the tile's first query, the head of the group
+    ql.start(static_cast<const T *>(a.q.at) + batch * a.q.b + (kv * group + next) * a.q.h, a.q.t, q0, a.q_tokens, a.head_dim);
+    gl.start(static_cast<const T *>(g.dout) + (int64_t)batch * a.q_tokens * out_row + (int64_t)(kv * group + next) * a.head_dim, out_row, q0, a.q_tokens, a.head_dim);
     const int64_t q_head = a.q.h * (int64_t)sizeof(T), out_head = a.head_dim * (int64_t)sizeof(T);
-    const float *row_at = g.rows + ((int64_t)batch * a.q_heads + kv * group) * a.q_tokens + q0 + (int64_t)threadIdx.x;
+    const float *row_at = g.rows + ((int64_t)batch * a.q_heads + kv * group + next) * a.q_tokens + q0 + (int64_t)threadIdx.x;
     auto fetch = [&](int t) {
         ql.fetch(tiles[t & 1]);
         gl.fetch(tiles[t & 1] + BYTES);
@@ -335,12 +347,12 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
         if constexpr (BIAS) bl.store(a, column, biases[t & 1]);
         ql.landed();
     };
-    if (count > 0) {
+    if (count > t0) {
         if constexpr (BIAS) {
-            load_column<T>(a, kv * group, column);
+            load_column<T>(a, kv * group + t0 % group, column);
             __syncthreads();
         }
-        fetch(0);
+        fetch(t0);
         if constexpr (kValuesInLds<T, D>) {
             Tiles<T, D, kBlock> vl;
             vl.start(v, a.v.t, k0, keys, a.head_dim);
@@ -349,11 +361,11 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
             val.arrive();
         }
         own.arrive();
-        land(0);
+        land(t0);
     }
     // the first query that sees the lane's key
     const int visible = j >= keys ? 0x7FFFFFFF : a.causal ? j - offset : -0x7FFFFFFF;
-    for (int t = 0; t < count; ++t) {
+    for (int t = t0; t < count; ++t) {
         const char *const tile = tiles[t & 1];
         const int here = (from + per_head - 1 - t / group) * ROWS;
         fetch(t + 1);
@@ -405,6 +417,12 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
         land(t + 1);
     }
     if (j >= a.k_tokens) return;
+    if (SPLIT) {
+        float *const to = g.dk_parts + (((int64_t)split * a.batch * a.kv_heads + place.unit) * a.k_tokens + j) * 2 * a.head_dim;
+        store_row<float, D>(dk, a.scale, to, a.head_dim);
+        store_row<float, D>(dv, 1.0f, to + a.head_dim, a.head_dim);
+        return;
+    }
     store_row<T, D>(dv, 1.0f, static_cast<T *>(g.dv) + batch * g.dv_b + kv * g.dv_h + j * g.dv_t, a.head_dim);
     T *const to = static_cast<T *>(g.dk) + batch * g.dk_b + kv * g.dk_h + j * g.dk_t;
     if (g.dk_d == 1) {
@@ -423,20 +441,27 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
     }
 }
 
+template <typename T, int D, bool SPLIT>
+void launch_backward_of(const Attention &a, const Gradients &g, hipStream_t st)
+{
+    const int q_blocks = (a.q_tokens + kBlock - 1) / kBlock, k_blocks = (a.k_tokens + kBlock - 1) / kBlock;
+    const unsigned q_grid = (unsigned)((int64_t)a.batch * a.q_heads * q_blocks * g.q_splits), k_grid = (unsigned)((int64_t)a.batch * a.kv_heads * k_blocks * g.k_splits);
+    if (q_grid > 0) {
+        if (g.parts) launch(queries_kernel<T, D, true, true, SPLIT>, q_grid, kAttnThreads, 0, st, a, g, q_blocks);
+        else if (a.table) launch(queries_kernel<T, D, true, false, SPLIT>, q_grid, kAttnThreads, 0, st, a, g, q_blocks);
+        else launch(queries_kernel<T, D, false, false, SPLIT>, q_grid, kAttnThreads, 0, st, a, g, q_blocks);
+    }
+    if (k_grid > 0) {
+        if (a.table) launch(keys_kernel<T, D, true, SPLIT>, k_grid, kAttnThreads, 0, st, a, g, k_blocks);
+        else launch(keys_kernel<T, D, false, SPLIT>, k_grid, kAttnThreads, 0, st, a, g, k_blocks);
+    }
+}
+
 template <typename T, int D>
 void launch_backward(const Attention &a, const Gradients &g, hipStream_t st)
 {
-    const int q_blocks = (a.q_tokens + kBlock - 1) / kBlock, k_blocks = (a.k_tokens + kBlock - 1) / kBlock;
-    const unsigned q_grid = (unsigned)((int64_t)a.batch * a.q_heads * q_blocks), k_grid = (unsigned)((int64_t)a.batch * a.kv_heads * k_blocks);
-    if (q_grid > 0) {
-        if (g.parts) launch(queries_kernel<T, D, true, true>, q_grid, kAttnThreads, 0, st, a, g, q_blocks);
-        else if (a.table) launch(queries_kernel<T, D, true, false>, q_grid, kAttnThreads, 0, st, a, g, q_blocks);
-        else launch(queries_kernel<T, D, false, false>, q_grid, kAttnThreads, 0, st, a, g, q_blocks);
-    }
-    if (k_grid > 0) {
-        if (a.table) launch(keys_kernel<T, D, true>, k_grid, kAttnThreads, 0, st, a, g, k_blocks);
-        else launch(keys_kernel<T, D, false>, k_grid, kAttnThreads, 0, st, a, g, k_blocks);
-    }
+    if (g.q_splits > 1 || g.k_splits > 1) launch_backward_of<T, D, true>(a, g, st);
+    else launch_backward_of<T, D, false>(a, g, st);
 }
 
 template <typename T>

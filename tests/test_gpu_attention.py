@@ -485,3 +485,21 @@ def test_fp32_of_many_workgroups(shape, causal, bias):
         table = torch.randn(9, Hq, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
         of = sf.distance_buckets(Tq, Tk, 9, 40, both_ways=not causal)
     Call(q, k, v, do, sf.HEADS_ROWS, D ** -0.5, causal, lengths, table, of).forward().backward().check()
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 700, 2, 1, 32), (1, 700, 700, 1, 1, 64), (2, 513, 1100, 3, 1, 96), (1, 1031, 530, 2, 2, 128), (3, 640, 64, 1, 1, 40), (1, 1500, 1500, 1, 1, 128),
+                                   (1, 40, 2100, 4, 4, 64)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["all", "causal_lengths", "bias", "causal_bias_lengths", "apart"])
+def test_blocks_whose_tiles_are_shared_out(shape, dtype, kind):
+    """So few blocks that workgroups share their tiles out, also more workgroups than a block has tiles (early queries, short sequences)."""
+    require_gpu()
+    B, Tq, Tk, Hq, Hk, D = shape
+    layout, causal = sf.HEADS_APART if kind == "apart" else sf.HEADS_ROWS, "causal" in kind
+    q, k, v, do = inputs(*shape, dtype, layout, seed=Tq, columns=kind == "bias")
+    lengths = torch.tensor([(Tk - 5, 0, 70)[b % 3] for b in range(B)], dtype=torch.int32, device="cuda") if "lengths" in kind else None
+    table = of = None
+    if "bias" in kind:
+        table = torch.randn(9, Hq, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(dtype)
+        of = sf.distance_buckets(Tq, Tk, 9, 400, both_ways=not causal)
+    Call(q, k, v, do, layout, D ** -0.5, causal, lengths, table, of, kind == "bias").forward().backward().check()
