@@ -186,20 +186,30 @@ size_t turned_bytes(const Sizes &z) { return turned(z) ? rounded((size_t)z.k_cou
 int q_blocks(const Sizes &z) { return (z.q_tokens + kBlock - 1) / kBlock; }
 // Backward: how many workgroups share the tiles of a block's other side out where blocks do not fill the card; their sums meet in memory,
 // added up in order by one more launch.  (us of the backward pass in one share, so; T tokens, a head each T / 128 blocks)
-//   fp32, whose tiles take longest, from two tiles on: heads of 128: 1 x 200 120, 53; 6 x 512 249, 69; 1 x 1400 638, 91; 6 x 1400 655, 270; heads
-//   of 32: 1 x 200 37, 21; 40 x 200 38, 32; 6 x 1400 187, 80.  Heads of up to 64, two workgroups of which fit a compute unit, with up to 256
-//   blocks of 8 tiles and more: 16 x 1400 of 64, causal 409, 267, all 342, 334; of 4 tiles not: 96 x 200 71, 89.
-//   bf16, where the queries' shares each go over all keys for delta: as many blocks as four for a tile: heads of 128: 1 x 512 56, 39; 6 x 512 57, 48;
-//   6 x 1400 139, 102; of 32: 1 x 512 22, 20; 1 x 1400 53, 33; 6 x 1400 56, 49; but 16 x 512 24, 28; 40 x 300 20, 26.
+//   fp32, whose tiles take longest: as many as make the rounds of 256 workgroups times the tiles of one, and one more for its start, the least, up
+//   to 320 blocks.  Heads of 128: 1 x 200 120, 53; 6 x 512 249, 69; 1 x 1400 638, 91; 6 x 1400 655, 270; 16 x 1400 causal 695, 428; 24 x 1400 1310,
+//   1010; 4 x 4097 2450, 1210.  Of 32: 1 x 200 37, 21; 40 x 200 38, 32; 6 x 1400 187, 85.  (With 384 blocks of 128, 96 x 512, all 508, 475, but causal
+//   312, 384; with 792, 24 x 4097, all 7540, 6490, but causal 3525, 3924.)
+//   bf16, where the queries' shares each go over all keys for delta: up to as many blocks as four for a tile: heads of 128: 1 x 512 56, 39; 6 x 512 57,
+//   48; 6 x 1400 139, 102; of 32: 1 x 512 22, 20; 1 x 1400 53, 33; 6 x 1400 56, 49; but 16 x 512 24, 28; 40 x 300 20, 26.
 int splits_of(const Sizes &z, int64_t workgroups, int64_t tiles)
 {
     if (workgroups == 0) return 1;
-    const bool low = z.dt == SLIMFIT_BF16;
-    if (low && (tiles < 8 || workgroups > 4 * tiles)) return 1;
-    int64_t splits = 256 / workgroups, most = low || tiles > 16 ? tiles / 2 : tiles < 8 ? tiles : 8;
-    if (!low && z.head_dim <= 64 && splits == 1 && tiles >= 8) splits = 512 / workgroups;
-    if (splits > most) splits = most;
-    return splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : (int)splits;
+    if (z.dt == SLIMFIT_BF16) {
+        if (tiles < 8 || workgroups > 4 * tiles) return 1;
+        const int64_t splits = 256 / workgroups < tiles / 2 ? 256 / workgroups : tiles / 2;
+        return splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : (int)splits;
+    }
+    int best = 1;
+    int64_t least = 0;
+    for (int s = 1; s <= kMostSplits && s <= tiles && (s == 1 || workgroups <= 320); ++s) {
+        const int64_t cost = 8 * ((workgroups * s + 255) / 256) * ((tiles + s - 1) / s + 1) + s;
+        if (s == 1 || cost < least) {
+            best = s;
+            least = cost;
+        }
+    }
+    return best;
 }
 int query_splits(const Sizes &z) { return splits_of(z, z.batch * z.q_heads * q_blocks(z), ((int64_t)z.k_tokens + kTile - 1) / kTile); }
 int key_splits(const Sizes &z)
