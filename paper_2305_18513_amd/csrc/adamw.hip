@@ -13,6 +13,9 @@
 //       rounded up with the probability of what is cut off: 20 bits of dither are added to the fp32 bits before the cut.  The
 //       dither is a function of seed, step, tensor and place alone.  A v' that is not 0 never becomes 0 (m' / eps would explode).
 // m' and v' are rounded products and their rounded sum, without a fused multiply-add, so that the codes are defined.
+//
+// What bounds it: memory with states in 32 bits (56 million fp32 weights, 1.57 GB: 290 us, 5.0 TB/s), vector instructions and memory about alike with
+// 8 (151 million bf16 weights, 1.5 GB: 285 to 310 us, 93 % of them issuing); a small model, the launches.
 #include "common.hpp"
 
 namespace slimfit {

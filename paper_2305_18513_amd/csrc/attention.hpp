@@ -68,7 +68,8 @@ __device__ __forceinline__ int key_tiles(const Attention &a, int q0, int keys)
 
 // Workgroups go to the eight XCDs in turn, and each has its own L2: the work of one pair of sequence and key head, whose `each` times
 // `blocks` workgroups read the same keys and values (or queries), stays on one.  There the pairs go one after another or, where blocks
-// differ in length (causal), the first block of all of them, then the second, so that what is left at the end is short.
+// differ in length (causal), the first block of all of them, then the second, so that what is left at the end is short.  (2048 x 2048 by
+// 128 causal, 32 heads on 8, 8 sequences: 370 us in the grid's order, 317 to 335 so; 1024 x 1024 by 64 causal 61, 60.)
 struct Place {
     int unit, block, in;
     __device__ __forceinline__ Place(int units, int blocks, int each, bool by_block)
