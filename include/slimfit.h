@@ -239,7 +239,8 @@ int32_t slimfit_apply_update_layer_delta(void *const *w, int32_t w_dt,
  *  frozen        : DEVICE uint8[L] or NULL: layers of 1 are frozen (the mask of slimfit_ils_select).
  *  d_out         : DEVICE float[L] or NULL (no distances).
  *  A gradient that is not finite makes its weight, and with 8 bits its block's states, NaN.
- *  Nothing of a layer may share memory with another part of it (INVALID_ARG).  numel <= 2^33 (ERR_UNSUPPORTED).
+ *  What is written may share memory with nothing else of the plan, in no layer (INVALID_ARG); gradients may with each
+ *  other.  numel <= 2^33 (ERR_UNSUPPORTED).
  *
  *  slimfit_adamw_plan writes the table into the workspace (256-byte aligned, of the bytes that
  *  slimfit_adamw_workspace reports), slimfit_adamw_run steps the planned layers; numel, L, types, bits and block

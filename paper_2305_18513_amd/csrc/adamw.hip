@@ -18,6 +18,10 @@
 // 8 (151 million bf16 weights, 1.5 GB: 285 to 310 us, 93 % of them issuing); a small model, the launches.
 #include "common.hpp"
 
+#include <algorithm>
+#include <memory>
+#include <new>
+
 namespace slimfit {
 namespace {
 
@@ -509,7 +513,28 @@ extern "C" int32_t slimfit_adamw_plan(void *const *w, int32_t w_dt, const void *
     if (L == 0) return SLIMFIT_OK;
     if (!w || !grad || !m || !v || !weight_decay || (bits == 8 && (!m_scales || !v_scales))) return SLIMFIT_ERR_INVALID_ARG;
     if (copies && w_dt != SLIMFIT_F32) return SLIMFIT_ERR_INVALID_ARG;
+    // memory of all layers: what is written may be named once only (a tensor of two layers would be stepped by both at once)
+    struct Range { uintptr_t at, end; bool written; };
+    const std::unique_ptr<Range[]> ranges(new (std::nothrow) Range[(size_t)L * 7 + 1]);
+    if (!ranges) return SLIMFIT_ERR_WORKSPACE;
+    size_t n_ranges = 0;
+    auto apart = [&] {
+        std::sort(ranges.get(), ranges.get() + n_ranges, [](const Range &a, const Range &b) { return a.at < b.at; });
+        uintptr_t written = 0, any = 0;                     // ends so far
+        for (size_t i = 0; i < n_ranges; ++i) {
+            const Range &x = ranges[i];
+            if (x.at < (x.written ? any : written)) return false;
+            any = std::max(any, x.end);
+            if (x.written) written = std::max(written, x.end);
+        }
+        return true;
+    };
     for (int pass = 0; pass < 2; ++pass) {                  // what can be told without the runtime comes first
+        if (pass == 1 && workspace) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(workspace);
+            ranges[n_ranges++] = {at, at + lay.bytes, true};
+        }
+        if (pass == 1 && !apart()) return SLIMFIT_ERR_INVALID_ARG;
         if (pass == 1 && (rc = check_workspace(lay, workspace, workspace_bytes)) != SLIMFIT_OK) return rc;
         for (int32_t i = 0; i < L; ++i) {
             if (!(weight_decay[i] >= 0.0f) || __builtin_isinf(weight_decay[i])) return SLIMFIT_ERR_INVALID_ARG;
@@ -525,9 +550,10 @@ extern "C" int32_t slimfit_adamw_plan(void *const *w, int32_t w_dt, const void *
                     continue;
                 }
                 if (pass == 0 && !aligned_to(a.p, a.align)) return SLIMFIT_ERR_ALIGNMENT;
-                if (pass == 0)
-                    for (const auto &b : part)
-                        if (&a != &b && b.p && meet(a.p, a.bytes, b.p, b.bytes)) return SLIMFIT_ERR_INVALID_ARG;
+                if (pass == 0) {
+                    const uintptr_t at = reinterpret_cast<uintptr_t>(a.p);
+                    ranges[n_ranges++] = {at, at + a.bytes, &a != &part[6]};     // (the gradient is read)
+                }
                 if (pass == 1 && (rc = check_device_range(a.p, a.bytes)) != SLIMFIT_OK) return rc;
             }
         }

@@ -121,7 +121,7 @@ template <typename T>
 __global__ void __launch_bounds__(kAttnThreads) shares_kernel(Attention a, Gradients g)
 {
     const int vectors = a.head_dim / 4;
-    const int64_t q_rows = (int64_t)a.batch * a.q_heads * a.q_tokens, k_rows = (int64_t)a.batch * a.kv_heads * a.k_tokens;
+    const int64_t q_rows = g.q_splits > 1 ? (int64_t)a.batch * a.q_heads * a.q_tokens : 0, k_rows = g.k_splits > 1 ? (int64_t)a.batch * a.kv_heads * a.k_tokens : 0;
     int64_t n = (int64_t)blockIdx.x * kAttnThreads + threadIdx.x;
     const bool query = n < q_rows * vectors;
     if (!query && (n -= q_rows * vectors) >= 2 * k_rows * vectors) return;
@@ -216,7 +216,6 @@ int key_splits(const Sizes &z)
 {
     return splits_of(z, z.batch * z.kv_heads * ((z.k_tokens + kBlock - 1) / kBlock), (int64_t)(z.q_heads / z.kv_heads) * ((z.q_tokens + kTile - 1) / kTile));
 }
-bool split(const Sizes &z) { return query_splits(z) > 1 || key_splits(z) > 1; }
 // blocks of queries that one share of the sums by distance adds up (16 x 512, 12 heads: 64 in one share 57 us, 8 each 6.6), and the shares
 int64_t share_of(const Sizes &z)
 {
@@ -261,8 +260,8 @@ struct BackwardPlaces {
         parts = rows + rounded((size_t)(z.batch * z.q_heads) * (size_t)z.q_tokens * 12);
         sums = parts + (table ? rounded((size_t)(z.batch * z.q_heads) * (size_t)(q_blocks(z) * query_splits(z)) * kAttnWaves * (size_t)part_row(z) * 4) : 0);
         dq = sums + (table ? rounded((size_t)shares_of(z) * (size_t)z.q_heads * ((size_t)z.q_tokens + (size_t)z.k_tokens) * 4) : 0);
-        dk = dq + (split(z) ? rounded((size_t)query_splits(z) * (size_t)z.q_count() * 4) : 0);
-        bytes = dk + (split(z) ? rounded((size_t)key_splits(z) * (size_t)z.k_count() * 8) : 0);
+        dk = dq + (query_splits(z) > 1 ? rounded((size_t)query_splits(z) * (size_t)z.q_count() * 4) : 0);
+        bytes = dk + (key_splits(z) > 1 ? rounded((size_t)key_splits(z) * (size_t)z.k_count() * 8) : 0);
     }
 };
 
@@ -461,8 +460,7 @@ extern "C" int32_t slimfit_attention_backward(const void *dout, const void *q, c
                          reinterpret_cast<float *>(ws + at.dk)};
     if (dt == SLIMFIT_BF16) attention_backward_bf16(a, g, st);
     else attention_backward_f32(a, g, st);
-    if (split(z)) {
-        const int64_t vectors = (z.q_count() + 2 * z.k_count()) / 4;
+    if (const int64_t vectors = ((g.q_splits > 1 ? z.q_count() : 0) + (g.k_splits > 1 ? 2 * z.k_count() : 0)) / 4; vectors > 0) {
         const unsigned grid = (unsigned)((vectors + kAttnThreads - 1) / kAttnThreads);
         if (dt == SLIMFIT_BF16) launch(shares_kernel<uint16_t>, grid, kAttnThreads, 0, st, a, g);
         else launch(shares_kernel<float>, grid, kAttnThreads, 0, st, a, g);

@@ -448,26 +448,33 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
 }
 
 template <typename T, int D, bool SPLIT>
-void launch_backward_of(const Attention &a, const Gradients &g, hipStream_t st)
+void launch_queries(const Attention &a, const Gradients &g, int blocks, hipStream_t st)
 {
-    const int q_blocks = (a.q_tokens + kBlock - 1) / kBlock, k_blocks = (a.k_tokens + kBlock - 1) / kBlock;
-    const unsigned q_grid = (unsigned)((int64_t)a.batch * a.q_heads * q_blocks * g.q_splits), k_grid = (unsigned)((int64_t)a.batch * a.kv_heads * k_blocks * g.k_splits);
-    if (q_grid > 0) {
-        if (g.parts) launch(queries_kernel<T, D, true, true, SPLIT>, q_grid, kAttnThreads, 0, st, a, g, q_blocks);
-        else if (a.table) launch(queries_kernel<T, D, true, false, SPLIT>, q_grid, kAttnThreads, 0, st, a, g, q_blocks);
-        else launch(queries_kernel<T, D, false, false, SPLIT>, q_grid, kAttnThreads, 0, st, a, g, q_blocks);
-    }
-    if (k_grid > 0) {
-        if (a.table) launch(keys_kernel<T, D, true, SPLIT>, k_grid, kAttnThreads, 0, st, a, g, k_blocks);
-        else launch(keys_kernel<T, D, false, SPLIT>, k_grid, kAttnThreads, 0, st, a, g, k_blocks);
-    }
+    const unsigned grid = (unsigned)((int64_t)a.batch * a.q_heads * blocks * g.q_splits);
+    if (g.parts) launch(queries_kernel<T, D, true, true, SPLIT>, grid, kAttnThreads, 0, st, a, g, blocks);
+    else if (a.table) launch(queries_kernel<T, D, true, false, SPLIT>, grid, kAttnThreads, 0, st, a, g, blocks);
+    else launch(queries_kernel<T, D, false, false, SPLIT>, grid, kAttnThreads, 0, st, a, g, blocks);
+}
+template <typename T, int D, bool SPLIT>
+void launch_keys(const Attention &a, const Gradients &g, int blocks, hipStream_t st)
+{
+    const unsigned grid = (unsigned)((int64_t)a.batch * a.kv_heads * blocks * g.k_splits);
+    if (a.table) launch(keys_kernel<T, D, true, SPLIT>, grid, kAttnThreads, 0, st, a, g, blocks);
+    else launch(keys_kernel<T, D, false, SPLIT>, grid, kAttnThreads, 0, st, a, g, blocks);
 }
 
 template <typename T, int D>
 void launch_backward(const Attention &a, const Gradients &g, hipStream_t st)
 {
-    if (g.q_splits > 1 || g.k_splits > 1) launch_backward_of<T, D, true>(a, g, st);
-    else launch_backward_of<T, D, false>(a, g, st);
+    const int q_blocks = (a.q_tokens + kBlock - 1) / kBlock, k_blocks = (a.k_tokens + kBlock - 1) / kBlock;
+    if (a.batch > 0 && q_blocks > 0) {
+        if (g.q_splits > 1) launch_queries<T, D, true>(a, g, q_blocks, st);
+        else launch_queries<T, D, false>(a, g, q_blocks, st);
+    }
+    if (a.batch > 0 && k_blocks > 0) {
+        if (g.k_splits > 1) launch_keys<T, D, true>(a, g, k_blocks, st);
+        else launch_keys<T, D, false>(a, g, k_blocks, st);
+    }
 }
 
 template <typename T>

@@ -98,3 +98,22 @@ def test_binding_refuses():
         sf.adamw_run(np.array([8]), 0, 0, 32, 0, 1e-3, 0.9, 0.999, 1e-8, 1, ws, live=t(2))
     with pytest.raises(ValueError):
         sf.adamw_states(codes[0], t(1), codes[0], t(2), 64, t(100), t(100))
+
+
+def test_plan_refuses_what_two_layers_share(lib):
+    """A tensor, a state or the table's memory that two layers would write at once; gradients may be one tensor's."""
+    base = dict(w=1 << 20, g=1 << 21, m=1 << 22, v=1 << 23, ms=1 << 24, vs=1 << 25)
+
+    def call(second, bits=8, ws=1 << 26):
+        first, n = dict(base), (L * 2)(4096, 4096)
+        other = {k: x + (1 << 30) for k, x in first.items()}
+        other.update(second)
+        pair = lambda k: (P * 2)(first[k], other[k])  # noqa: E731
+        return lib.slimfit_adamw_plan(pair("w"), I(0), pair("g"), I(0), pair("m"), pair("v"), pair("ms"), pair("vs"), P(0), (F * 2)(0.0, 0.0), I(bits), I(64), n,
+                                      I(2), P(ws), C.c_size_t(64), P(0))
+
+    assert call({}) == call(dict(g=base["g"])) == call(dict(w=(1 << 20) + 4 * 4096)) == sf.ERR_WORKSPACE          # (64 bytes are too few: the last check here)
+    for bad in (dict(w=base["w"]), dict(w=(1 << 20) + 4 * 4096 - 16), dict(m=base["m"]), dict(v=base["m"] + 4080), dict(ms=base["vs"] + 252), dict(g=base["w"]),
+                dict(vs=base["g"])):
+        assert call(bad) == sf.ERR_INVALID_ARG, bad
+    assert call({}, ws=base["m"]) == call({}, ws=(1 << 30) + base["g"]) == sf.ERR_INVALID_ARG

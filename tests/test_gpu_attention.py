@@ -503,3 +503,12 @@ def test_blocks_whose_tiles_are_shared_out(shape, dtype, kind):
         table = torch.randn(9, Hq, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(dtype)
         of = sf.distance_buckets(Tq, Tk, 9, 400, both_ways=not causal)
     Call(q, k, v, do, layout, D ** -0.5, causal, lengths, table, of, kind == "bias").forward().backward().check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 4500, 140, 5, 1, 32), (1, 140, 9000, 2, 2, 64), (40, 700, 600, 4, 1, 64), (30, 130, 1100, 6, 1, 128)], ids=lambda s: "x".join(map(str, s)))
+def test_blocks_of_one_side_are_shared_out(shape, dtype):
+    """Tiles shared out for the queries' sums alone, or for the keys'."""
+    require_gpu()
+    q, k, v, do = inputs(*shape, dtype, sf.HEADS_ROWS, seed=shape[1])
+    Call(q, k, v, do, sf.HEADS_ROWS, shape[5] ** -0.5, True).forward().backward().check()
