@@ -14,13 +14,14 @@
 //       dither is a function of seed, step, tensor and place alone.  A v' that is not 0 never becomes 0 (m' / eps would explode).
 // m' and v' are rounded products and their rounded sum, without a fused multiply-add, so that the codes are defined.
 //
-// What bounds it: memory with states in 32 bits (56 million fp32 weights, 1.57 GB: 290 us, 5.0 TB/s), vector instructions and memory about alike with
-// 8 (151 million bf16 weights, 1.5 GB: 285 to 310 us, 93 % of them issuing); a small model, the launches.
+// What bounds it: memory (fp32 weights and states, 16.8 million, 470 MB: 86 us, 5.5 TB/s; 151 million bf16 weights with states in 8 bits, 1.46 GB: 260 to
+// 275 us, 5.5 TB/s, where vector instructions are as much); a small model, the launches.
 #include "common.hpp"
 
 #include <algorithm>
 #include <memory>
 #include <new>
+#include <type_traits>
 
 namespace slimfit {
 namespace {
@@ -287,9 +288,9 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const char *__restrict_
     const float decay = s.lr * e.decay;
     const uint32_t key = BITS == 8 ? mix(s.seed ^ mix(s.step ^ mix((uint32_t)lo + 1u))) + (uint32_t)(off >> 2) : 0u;
     double acc = 0.0;
-    for (int p = 0; p < len; p += kPass) {                  // (all threads together: lanes of a run stay together)
+    auto pass = [&](auto whole, int p) {                    // (all threads together: lanes of a run stay together)
         const int at = p + threadIdx.x * N;
-        const int n = min(len - at, N);
+        const int n = decltype(whole)::value ? N : min(len - at, N);
         TW *const wp = static_cast<TW *>(e.w) + off + at;
         float w[N], g[N], m[N], v[N];
         load_some(wp, n, w);
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const char *__restrict_
         }
         // The instructions for roots and reciprocals are within a step of the last place, and take numbers below the normal ones as 0:
         // from an eps of 2^-40 on, a v of those is none of its root's sum.  (Divided and rooted by the correctly rounded sequences,
-        // distances too and added up in fp64 one by one: 97 vector instructions an element with 8 bits instead of 59, 361 us instead of 285 for 151 million bf16 weights.)
+        // distances too and added up in fp64 one by one: 97 vector instructions an element with 8 bits instead of 59, 361 us instead of 290 for 151 million bf16 weights.)
         if (s.eps >= 0x1p-40f) {
 #pragma unroll
             for (int j = 0; j < N; ++j) d[j] = m[j] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[j]) * s.root + s.eps);
@@ -365,6 +366,12 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const char *__restrict_
                 e.v_scales[run] = vs;
             }
         }
+    };
+    // A pass that is whole asks for everything before it waits for anything (151 million bf16 weights, 8 bits: 290 us with a branch and a wait
+    // at each load, as in a tensor's last pass, 260 so).
+    for (int p = 0; p < len; p += kPass) {
+        if (p + kPass <= len) pass(std::true_type(), p);
+        else pass(std::false_type(), p);
     }
     if constexpr (SCORE) {
 #pragma unroll
