@@ -225,7 +225,7 @@ int64_t share_of(const Sizes &z)
 int64_t shares_of(const Sizes &z) { return (z.batch * q_blocks(z) * query_splits(z) + share_of(z) - 1) / share_of(z); }
 int64_t part_row(const Sizes &z) { return ((int64_t)z.k_tokens + kTile - 1) / kTile * kTile + kTile; }
 
-// How many workgroups share a sequence's keys out, or 0: 128 queries of a head a workgroup.  (us with those, with few queries)
+// How many workgroups share a sequence's keys out, or 0: 128 queries of a head a workgroup.  (us with those, with few queries, on the same operands again and again)
 //   bf16, up to 16 queries: 16 x 4096 keys, 32 heads on 8 by 128: 1 query 121, 48; 16 132, 63; 32 139, 120; 64 142, 243;
 //         64 x 1024, 8 heads of 64: 1 24.5, 25.4; 16 25.3, 25.7; 64 25.5, 48.5.
 //   fp32, where padded queries cost products, up to 64: the first 1 1146, 137; 64 1153, 926; the second 1 137, 48; 64 142, 105.

@@ -2,8 +2,8 @@
 // of heads reads its keys once), each of the four waves a quarter of a tile of 128 keys, and the keys of a sequence shared out over
 // `splits` workgroups where there are few rows in all.  The waves' sums meet in LDS, the workgroups' in memory, in order.
 //
-// What bounds it is the reading of keys and values: one query each of 16 sequences of up to 4096 tokens, 32 heads on 8 by 128, 134 MB, in 32 to
-// 43 us by where they lie, 3.1 to 4.2 TB/s.
+// What bounds it is the reading of keys and values: one query each of 16 sequences of 4096 tokens, 32 heads on 8 by 128, 268 MB, with the joining launch
+// in 56 us, 4.8 TB/s; 64 sequences 5.8.
 #pragma once
 
 #include "attention.hpp"
@@ -55,10 +55,14 @@ __global__ void __launch_bounds__(kAttnThreads, 1) few_kernel(Attention a, T *__
     Tiles<T, D, kFewTile> kl, vl;
     kl.start(static_cast<const T *>(a.k.at) + batch * a.k.b + kv * a.k.h, a.k.t, from * kFewTile, keys, a.head_dim);
     vl.start(static_cast<const T *>(a.v.at) + batch * a.v.b + kv * a.v.h, a.v.t, from * kFewTile, keys, a.head_dim);
-    auto fetch = [&](int t) {
+    auto fetch_keys = [&](int t) {
+        if (t >= to) kl.left = 0;
         kl.fetch(tiles[t % STAGES]);
-        vl.fetch(tiles[t % STAGES] + BYTES);
         kl.forward();
+    };
+    auto fetch_values = [&](int t) {
+        if (t >= to) vl.left = 0;
+        vl.fetch(tiles[t % STAGES] + BYTES);
         vl.forward();
     };
     auto land = [&](int t) {
@@ -66,16 +70,38 @@ __global__ void __launch_bounds__(kAttnThreads, 1) few_kernel(Attention a, T *__
         vl.land(tiles[t % STAGES] + BYTES);
         kl.landed();
     };
+    // bf16: a wave's quarter of a tile is what it has fetched itself, so that it waits for that alone, and asks for what comes two tiles on as
+    // soon as the place is free.  Keys and values in turn: three more are under way behind the one it waits for.  (With a barrier for all
+    // of a tile 61 us for those 56; 16 x 2048, 12 heads of 64: 26.9, 21.5.)
+    constexpr bool ALONE = Tiles<T, D, kFewTile>::DIRECT;
+    auto arrived = [] { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * Tiles<T, D, kFewTile>::EACH) : "memory"); };
+    auto read = [] { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); };
     if (from < to) {
-        fetch(from);
-        own.arrive();
-        land(from);
+        fetch_keys(from);
+        fetch_values(from);
+        if constexpr (ALONE) {
+            fetch_keys(from + 1);
+            fetch_values(from + 1);
+            own.arrive();
+        } else {
+            own.arrive();
+            land(from);
+        }
     }
     for (int t = from; t < to; ++t) {
         const char *const tile = tiles[t % STAGES];
         const int k0 = t * kFewTile + wave * kOwn;
-        fetch(t + 1);
+        if constexpr (ALONE) {
+            arrived();
+        } else {
+            fetch_keys(t + 1);
+            fetch_values(t + 1);
+        }
         f32x16 s = dots<T, D>(tile, wave * kOwn, own);
+        if constexpr (ALONE) {
+            read();
+            fetch_keys(t + 2);
+        }
         if constexpr (BIAS) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -106,10 +132,18 @@ __global__ void __launch_bounds__(kAttnThreads, 1) few_kernel(Attention a, T *__
             s[r] = __builtin_amdgcn_exp2f(BIAS ? (s[r] - safe) * kLog2e : __builtin_fmaf(s[r], scale, less));
             total += s[r];
         }
-        sums<T, D>(tile + BYTES, wave * kOwn, s, o);
-        if (STAGES == 1) __syncthreads();
-        land(t + 1);
+        if constexpr (ALONE) {
+            arrived();
+            sums<T, D>(tile + BYTES, wave * kOwn, s, o);
+            read();
+            fetch_values(t + 2);
+        } else {
+            sums<T, D>(tile + BYTES, wave * kOwn, s, o);
+            if (STAGES == 1) __syncthreads();
+            land(t + 1);
+        }
     }
+    if constexpr (ALONE) kl.landed();
     // the four waves' sums
     total = both_sum(total);
     if (half == 0) {
