@@ -67,10 +67,11 @@ __global__ void __launch_bounds__(kWave) distances_kernel(Attention a, const flo
     double sum = 0.0;
     for (int n0 = (int)blockIdx.z * each; n0 < end; n0 += kAtOnce) {
         float x[kAtOnce][kAttnWaves];
+        const int keys = keys_of(a, min(n0 + (int)(threadIdx.x % kAtOnce), end - 1) / splits / blocks);                 // a block's a lane
 #pragma unroll
         for (int m = 0; m < kAtOnce; ++m) {
             const int n = min(n0 + m, end - 1), split = n % splits, b = n / splits / blocks, block = n / splits % blocks;
-            const int tiles = key_tiles(a, block * kBlock, keys_of(a, b)), t0 = first_of(tiles, split, splits);
+            const int tiles = key_tiles(a, block * kBlock, __builtin_amdgcn_readlane(keys, m)), t0 = first_of(tiles, split, splits);
             const int written = (first_of(tiles, split + 1, splits) - t0) * kTile + kOwn;
             const float *const of = parts + ((((int64_t)b * a.q_heads + head) * blocks + block) * splits + split) * kAttnWaves * part_row;
 #pragma unroll
@@ -96,10 +97,21 @@ __global__ void __launch_bounds__(kAttnThreads) buckets_kernel(Attention a, cons
     __shared__ double part[kAttnWaves];
     const int all = a.q_tokens + a.k_tokens - 1, bucket = blockIdx.x, head = blockIdx.y;
     double sum = 0.0;
-    if (shares > 0)                                         // (no sums otherwise)
-        for (int at = threadIdx.x; at < all; at += kAttnThreads)
-            if (a.bucket_of[at] == bucket)
-                for (int z = 0; z < shares; ++z) sum += (double)sums[((int64_t)z * a.q_heads + head) * all + at];
+    const int64_t apart = (int64_t)a.q_heads * all;
+    const float *const from = sums + (int64_t)head * all;
+    for (int at0 = 0; at0 < (shares > 0 ? all : 0); at0 += kAttnThreads) {      // (no sums otherwise)
+        const int at = at0 + (int)threadIdx.x;
+        const bool in = at < all && a.bucket_of[min(at, all - 1)] == bucket;
+        if (__builtin_amdgcn_ballot_w64(in) == 0u) continue;
+        for (int z0 = 0; z0 < shares; z0 += kAtOnce) {      // (as above: what is not the bucket's is past the end)
+            float x[kAtOnce];
+#pragma unroll
+            for (int z = 0; z < kAtOnce; ++z)
+                x[z] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(buffer_at(from + (z0 + z) * apart, z0 + z < shares ? (int64_t)all * 4 : 0), in ? at * 4 : kNowhere, 0, 0));
+#pragma unroll
+            for (int z = 0; z < kAtOnce; ++z) sum += (double)x[z];
+        }
+    }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, kWave);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
