@@ -32,7 +32,8 @@ constexpr int kSkew = kOwn + 4;              // floats of a query's ds in LDS
 // form sum of p k beside dq and take e of it off at the end (1024 x 1024 by 64 causal, 256 heads: 81 us without, 98 with; dq's error
 // against 64 bits goes from 2.1 times that of one rounding of the result to 1.4, at inputs with a thousandth of outliers).  Heads of 128 have no
 // registers left for that (469 us without, 702 with the rows of dout in LDS): theirs go over the keys twice where these are no
-// more than kTwiceTiles tiles, once for delta = sum of p dp.  So do those with a bias, at any length: sums of ds over a bucket of many keys are
+// more than kTwiceTiles tiles, or one takes more than half of some query's p (a sum of exponentials below 2: in a seventh to a fourth of the
+// blocks at such inputs, and dq's error 1.4 roundings again), once for delta = sum of p dp.  So do those with a bias, at any length: sums of ds over a bucket of many keys are
 // little but e otherwise (two buckets: 5 % off), and whether the table takes a gradient changes no other.  Keys' gradients take
 // the right delta in any case.
 template <typename T, int D, bool ALWAYS> constexpr bool kRights = sizeof(T) == 2 && D <= 96 && !ALWAYS;
@@ -62,7 +63,15 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
     const float scale = a.scale * kLog2e;
     constexpr bool ALWAYS = BIAS || SPLIT;                  // goes over the keys twice at any length
     // (where tiles are shared out each goes over all of them for delta: from tile `start` to `end` first)
-    const bool twice = kTwice<T, D, ALWAYS> && (ALWAYS ? !SPLIT || split == 0 || count > t0 : all_tiles <= kTwiceTiles);
+    bool twice = kTwice<T, D, ALWAYS> && (ALWAYS ? !SPLIT || split == 0 || count > t0 : all_tiles <= kTwiceTiles), wave_twice = true;
+    if constexpr (kTwice<T, D, ALWAYS> && !ALWAYS) {
+        __shared__ int one_takes_most[kAttnWaves];
+        const float total = i < a.q_tokens ? g.stats[2 * ((int64_t)bh * a.q_tokens + i) + 1] : 0.0f;
+        wave_twice = twice || __builtin_amdgcn_ballot_w64(total > 0.0f && total < 2.0f) != 0u;      // (the largest of e^(s - m) is 1)
+        if (lane == 0) one_takes_most[wave] = wave_twice;
+        __syncthreads();
+        twice = (one_takes_most[0] | one_takes_most[1] | one_takes_most[2] | one_takes_most[3]) != 0;
+    }
     const int start = twice ? 0 : t0, end = twice ? all_tiles : count;
 
     Tiles<T, D> kl, vl;
@@ -164,7 +173,7 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
         float x = 0.0f, y = 0.0f;
         for (int t = start; t < end; ++t) {
             fetch(t + 1);
-            if (t * kTile < any_sees)
+            if (wave_twice && t * kTile < any_sees)
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
                     f32x16 p, dp;
@@ -180,7 +189,7 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
                 }
             land(t + 1);
         }
-        delta = both_sum(x + y);
+        if (wave_twice) delta = both_sum(x + y);
         if (count > t0) {
             kl.start(k, a.k.t, t0 * kTile, keys, a.head_dim);
             vl.start(v, a.v.t, t0 * kTile, keys, a.head_dim);

@@ -512,3 +512,20 @@ def test_blocks_of_one_side_are_shared_out(shape, dtype):
     require_gpu()
     q, k, v, do = inputs(*shape, dtype, sf.HEADS_ROWS, seed=shape[1])
     Call(q, k, v, do, sf.HEADS_ROWS, shape[5] ** -0.5, True).forward().backward().check()
+
+
+@pytest.mark.parametrize("T,D", [(300, 128), (601, 104), (1100, 128)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_wide_heads_where_one_key_takes_most(T, D, causal):
+    """Logits far apart: delta is formed anew for 32 queries where one key takes more than half of some query; the others' dq is looked at elsewhere."""
+    require_gpu()
+    q, k, v, do = inputs(2, T, T, 4 if T < 1000 else 16, 2, D, torch.bfloat16, sf.HEADS_ROWS, seed=T + D, spread=1.7)
+    call = Call(q, k, v, do, sf.HEADS_ROWS, D ** -0.5, causal).forward().backward()
+    ref = RightDelta(q, k, v, do, sf.HEADS_ROWS, D ** -0.5, causal, None, None, None)
+    whole = T // 32 * 32
+    most = call.stats[:, :, :whole, 1].reshape(*call.stats.shape[:2], -1, 32)
+    anew = (most < 2).any(-1).repeat_interleave(32, -1)[..., None]
+    assert float(anew.float().mean()) > 0.25
+    off = torch.where(anew, ref.offs["dq"][:, :, :whole], math.inf)
+    within(rows_of(call.dq, sf.HEADS_ROWS)[:, :, :whole], ref.dq[:, :, :whole], off, "dq")
+    within(rows_of(call.dk, sf.HEADS_ROWS, True), ref.dk, ref.offs["dk"], "dk")
