@@ -290,8 +290,10 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
 // tiles to make up for them.
 template <typename T, int D> constexpr bool kValuesInLds = sizeof(T) == 2 && D > 64;
 
+// (fp32 heads of 64 with a bias: two waves a SIMD keep some registers in memory, 165 us for one wave's 178, 8 x 512, 12 heads; where blocks are
+// shared out there is one workgroup a compute unit anyway, 36 and 31, 2 x 300.)
 template <typename T, int D, bool BIAS, bool SPLIT>
-__global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2) keys_kernel(Attention a, Gradients g, int blocks)
+__global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > (BIAS && SPLIT ? 32 : 64) ? 1 : 2) keys_kernel(Attention a, Gradients g, int blocks)
 {
     constexpr int ROWS = kValuesInLds<T, D> ? 32 : kTile, BYTES = ROWS * kPitch<T, D>;
     __shared__ __align__(1024) char tiles[2][2 * BYTES], values[kValuesInLds<T, D> ? kBlock * kPitch<T, D> : 16];
