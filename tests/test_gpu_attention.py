@@ -529,3 +529,43 @@ def test_wide_heads_where_one_key_takes_most(T, D, causal):
     off = torch.where(anew, ref.offs["dq"][:, :, :whole], math.inf)
     within(rows_of(call.dq, sf.HEADS_ROWS)[:, :, :whole], ref.dq[:, :, :whole], off, "dq")
     within(rows_of(call.dk, sf.HEADS_ROWS, True), ref.dk, ref.offs["dk"], "dk")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_the_most_buckets(dtype):
+    """1024 of them, each with a distance or two of its own, over tiles that are shared out."""
+    require_gpu()
+    q, k, v, do = inputs(1, 700, 650, 2, 1, 32, dtype, sf.HEADS_ROWS, seed=11)
+    table = torch.randn(1024, 2, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").to(dtype)
+    of = (torch.arange(700 + 650 - 1, dtype=torch.int32, device="cuda") * 7) % 1100          # some outside of the table
+    Call(q, k, v, do, sf.HEADS_ROWS, 0.2, False, None, table, of).forward().backward().check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("bias", [False, True], ids=["plain", "bias"])
+def test_shared_out_tiles_captured_and_replayed(dtype, bias):
+    """The shares' sums meet in one order: eager, captured and replayed calls give the same bits, also after other operands went through the graph."""
+    require_gpu()
+    q, k, v, do = inputs(1, 900, 1100, 2, 1, 128, dtype, sf.HEADS_ROWS, seed=2)
+    table = torch.randn(9, 2, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(dtype) if bias else None
+    of = sf.distance_buckets(900, 1100, 9, 400, both_ways=False) if bias else None
+    c = Call(q, k, v, do, sf.HEADS_ROWS, 0.1, True, None, table, of).forward().backward()
+    want = [t.clone() for t in c.outputs()]
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        c.forward().backward()
+        with torch.cuda.graph(graph, stream=stream):
+            c.forward().backward()
+    torch.cuda.current_stream().wait_stream(stream)
+    kept = q.clone()
+    for turn in range(3):
+        for t in c.outputs():
+            t.fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(c.outputs(), want)), turn
+        q.copy_(q.flip(0).roll(1, 1))
+        graph.replay()
+        assert not torch.equal(c.out, want[0])
+        q.copy_(kept)
