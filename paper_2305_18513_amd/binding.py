@@ -88,10 +88,15 @@ def _require(ok: bool) -> None:
 
 def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
     """The library launches on the current device's stream: a tensor of another device (or of the host) is refused."""
+    current = None
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
+        if t is None:
+            continue
+        if current is None and t.is_cuda:
+            current = torch.cuda.current_device()
+        if not t.is_cuda or t.get_device() != current:
             raise ValueError("every tensor has to be on the current GPU, this one is on %s" % t.device)
-        if t is not None and (t.is_neg() or t._is_zerotensor()):
+        if t.is_neg() or t._is_zerotensor():
             raise ValueError("a tensor's values have to be what its memory holds")
 
 
@@ -319,7 +324,9 @@ def adamw_workspace(numel: Sequence[int]) -> int:
 
 
 def _maybe_ptr_array(tensors: Sequence[Optional[torch.Tensor]]):
-    return (C.c_void_p * max(1, len(tensors)))(*[None if t is None else _dev(t).value for t in tensors])
+    if any(t is not None and not t.is_contiguous() for t in tensors):
+        raise ValueError("tensor must be contiguous")
+    return (C.c_void_p * max(1, len(tensors)))(*[None if t is None else t.data_ptr() for t in tensors])
 
 
 def adamw_plan(w: Sequence[torch.Tensor], grad: Sequence[Optional[torch.Tensor]], m: Sequence[torch.Tensor], v: Sequence[torch.Tensor],
@@ -332,19 +339,18 @@ def adamw_plan(w: Sequence[torch.Tensor], grad: Sequence[Optional[torch.Tensor]]
     present = [g for g in grad if g is not None]
     _require(not L or (_same_dtype(w) and (not present or _same_dtype(present))))
     held = torch.uint8 if bits == 8 else torch.float32
-    for i in range(L):
-        n = w[i].numel()
-        _require(grad[i] is None or grad[i].numel() == n)
-        _require(m[i].dtype == v[i].dtype == held and m[i].numel() == v[i].numel() == n)
-        if copies is not None and copies[i] is not None:
-            _require(w[i].dtype == torch.float32 and copies[i].dtype == torch.bfloat16 and copies[i].numel() == n)
+    sizes = [t.numel() for t in w]
+    _require(all(g is None or g.numel() == n for g, n in zip(grad, sizes)))
+    _require(all(t.dtype == held and t.numel() == n for each in (m, v) for t, n in zip(each, sizes)))
+    if copies is not None:
+        _require(all(t is None or (x.dtype == torch.float32 and t.dtype == torch.bfloat16 and t.numel() == n) for t, x, n in zip(copies, w, sizes)))
     if bits == 8:
         _require(m_scales is not None and v_scales is not None and len(m_scales) == L and len(v_scales) == L)
-        _require(all(s.dtype == torch.float32 and s.numel() >= -(-w[i].numel() // max(block, 1)) for each in (m_scales, v_scales) for i, s in enumerate(each)))
+        _require(all(s.dtype == torch.float32 and s.numel() >= -(-n // max(block, 1)) for each in (m_scales, v_scales) for s, n in zip(each, sizes)))
     _require(workspace.dtype == torch.uint8)
     for each in (w, grad, m, v, copies or (), (m_scales if bits == 8 else None) or (), (v_scales if bits == 8 else None) or (), (workspace,)):
         _on_current_device(*each)
-    numel = _numel_array([t.numel() for t in w])
+    numel = _numel_array(sizes)
     decay = np.ascontiguousarray(weight_decay, dtype=np.float32)
     rc = lib().slimfit_adamw_plan(
         _ptr_array(w), C.c_int32(_dt(w[0]) if L else F32), _maybe_ptr_array(grad), C.c_int32(_dt(present[0]) if present else F32), _ptr_array(m),
