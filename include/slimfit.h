@@ -708,10 +708,11 @@ int32_t slimfit_heads_norm_rotate_backward(const void *dq, const void *dkt, cons
  *  stats  : DEVICE float[batch, q_heads, q_tokens, 2], 16-byte aligned: m and l.
  *  scale  : above 0, finite.        causal : not 0: query i sees keys j <= i + k_tokens - q_tokens.
  *  lengths: DEVICE int32[batch] or NULL: keys of a sequence (held to 0 .. k_tokens); those past it are not looked at,
- *           whatever they hold, and get gradients of 0.
+ *           whatever they hold, and get gradients of 0.  They move neither the causal order nor the bias: both are counted from k_tokens.
  *  A query that sees no key has out 0, m -infinity, l 0 and gives no gradients.
  *  table  : DEVICE [buckets, q_heads] of dt, or NULL: the learned bias, table[bucket_of[j - i + q_tokens - 1]][head];
- *           buckets <= 1024.  bucket_of : DEVICE int32[q_tokens + k_tokens - 1], 4-byte aligned; a bucket outside of
+ *           buckets <= 1024.  bucket_of : DEVICE int32[q_tokens + k_tokens - 1], 4-byte aligned.  (Where query i stands at key
+ *           i + k_tokens - q_tokens, as in the causal order, entry n is the distance n + 1 - k_tokens.)  A bucket outside of
  *           [0, buckets) adds nothing and gets no gradient.  Entries may be -infinity (keys that are not seen) or the
  *           type's lowest value (keys that count where there are no others).
  *  dtable : DEVICE [buckets, q_heads] of dt, or NULL: sum of ds over the batch and the pairs of each bucket.

@@ -389,7 +389,8 @@ def _attend(ctx, q, k, v, layout, scale, causal, lengths, table, bucket_of, save
 class AttentionFunction(torch.autograd.Function):
     """out (B, q_tokens, heads, D) of q, k, v.  layout binding.HEADS_ROWS: (B, tokens, heads, D) each; HEADS_APART: (q, k^T, v) as
     SplitHeadsFunction and HeadsNormRotateFunction give them.  causal: query i sees keys j <= i + k_tokens - q_tokens.  lengths
-    (int32, B): keys of each sequence.  table (buckets, heads) and bucket_of: binding.attention_forward, binding.distance_buckets."""
+    (int32, B): keys of each sequence; they move neither the causal order nor the distances of the bias, which are counted from k_tokens.
+    table (buckets, heads) and bucket_of: binding.attention_forward, binding.distance_buckets."""
 
     @staticmethod
     def forward(ctx, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, causal: bool = False, lengths=None, table=None, bucket_of=None,

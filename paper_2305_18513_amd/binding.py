@@ -1013,11 +1013,15 @@ def heads_norm_rotate_backward(dq: torch.Tensor, dkt: torch.Tensor, dv: torch.Te
 
 # ---------------------------------------------------------------- (c-att) attention in one pass over the keys
 
-def distance_buckets(q_tokens: int, k_tokens: int, buckets: int, reach: int, both_ways: bool = True, device="cuda") -> torch.Tensor:
+def distance_buckets(q_tokens: int, k_tokens: int, buckets: int, reach: int, both_ways: bool = True, device="cuda", first_query: Optional[int] = None) -> torch.Tensor:
     """The bucket of each distance, key minus query, for ``bucket_of`` below (int32, q_tokens + k_tokens - 1).  The nearest half of a
     side's buckets hold one distance each, the others grow with its logarithm up to ``reach``, past which all share the last.
-    ``both_ways``: keys after the query have half of the buckets; otherwise they share bucket 0 with its own place."""
-    far = torch.arange(1 - q_tokens, k_tokens, dtype=torch.float64)
+    ``both_ways``: keys after the query have half of the buckets; otherwise they share bucket 0 with its own place.  ``first_query``: the
+    key that query 0 stands at.  None: k_tokens - q_tokens without ``both_ways``, where the causal order has it (tokens over a cache of
+    earlier keys get the buckets of a whole pass's last rows), and 0 with it."""
+    if first_query is None:
+        first_query = 0 if both_ways else k_tokens - q_tokens
+    far = torch.arange(1 - q_tokens, k_tokens, dtype=torch.float64) - first_query
     side = max(1, buckets // 2 if both_ways else buckets)
     one = max(1, side // 2)
     away = far.abs() if both_ways else torch.clamp(-far, min=0)

@@ -88,6 +88,28 @@ def test_distance_buckets():
             assert bool((past[1:] >= past[:-1]).all())
 
 
+@pytest.mark.parametrize("buckets", [1, 2, 7, 32])
+def test_distances_stand_where_the_causal_order_does(buckets):
+    """The last tokens over all keys, and keys over which some queries come too early, have the buckets of the same rows and columns of a whole pass."""
+    T = 300
+    whole = sf.distance_buckets(T, T, buckets, 128, both_ways=False, device="cpu")
+    row = lambda of, i, Tq, Tk: of[torch.arange(Tk) - i + Tq - 1]  # noqa: E731
+    for n in (1, 3, 16, 299):
+        few = sf.distance_buckets(n, T, buckets, 128, both_ways=False, device="cpu")
+        assert few.numel() == n + T - 1
+        for i in range(n):
+            assert torch.equal(row(few, i, n, T), row(whole, T - n + i, T, T))
+        late = sf.distance_buckets(T, n, buckets, 128, both_ways=False, device="cpu")     # the last n keys
+        for i in range(0, T, 7):
+            assert torch.equal(row(late, i, T, n), row(whole, i, T, T)[T - n :])
+    assert sf.distance_buckets(1, 4096, 32, 128, both_ways=False, device="cpu").unique().numel() == 32
+    both = sf.distance_buckets(T, T, buckets, 128, device="cpu")                          # both ways: on request
+    few = sf.distance_buckets(4, T, buckets, 128, device="cpu", first_query=T - 4)
+    assert all(torch.equal(row(few, i, 4, T), row(both, T - 4 + i, T, T)) for i in range(4))
+    few = sf.distance_buckets(4, T, buckets, 128, device="cpu")
+    assert all(torch.equal(row(few, i, 4, T), row(both, i, T, T)) for i in range(4))
+
+
 def test_binding_refuses():
     z = lambda *s, dtype=torch.float32: torch.zeros(*s, dtype=dtype)  # noqa: E731
     q, k, v, out, stats = z(2, 5, 4, 8), z(2, 7, 2, 8), z(2, 7, 2, 8), z(2, 5, 4, 8), z(2, 4, 5, 2)

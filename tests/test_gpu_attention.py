@@ -569,3 +569,19 @@ def test_shared_out_tiles_captured_and_replayed(dtype, bias):
         graph.replay()
         assert not torch.equal(c.out, want[0])
         q.copy_(kept)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 3, 16, 40, 200])
+def test_the_last_tokens_over_all_keys_are_the_whole_passes_last_rows(dtype, n):
+    """A decoder with a position bias that varies, trained over whole rows and asked for a few tokens over the keys before them."""
+    require_gpu()
+    T, Hq, Hk, D = 700, 4, 2, 64
+    q, k, v, do = inputs(2, T, T, Hq, Hk, D, dtype, sf.HEADS_ROWS, seed=T + n)
+    table = (2.0 * torch.randn(32, Hq, generator=torch.Generator(device="cuda").manual_seed(4), device="cuda")).to(dtype)
+    whole = Reference(q, k, v, do, sf.HEADS_ROWS, D ** -0.5, True, None, table, sf.distance_buckets(T, T, 32, 128, both_ways=False))
+    few = Call(q[:, -n:].contiguous(), k, v, do[:, -n:].contiguous(), sf.HEADS_ROWS, D ** -0.5, True, None, table, sf.distance_buckets(n, T, 32, 128, both_ways=False))
+    few.forward().backward()
+    within(rows_of(few.out, sf.HEADS_ROWS), whole.out[:, :, -n:], whole.rounded(whole.out_off(), whole.out)[:, :, -n:], "out")
+    within(rows_of(few.dq, sf.HEADS_ROWS), whole.dq[:, :, -n:], whole.offs["dq"][:, :, -n:], "dq")
+    few.check()
