@@ -722,7 +722,7 @@ int32_t slimfit_heads_norm_rotate_backward(const void *dq, const void *dkt, cons
  *           backward pass) rounded to bf16 once before their products with v (dout, q and k), results rounded once.
  *           The rounding of out, which delta would carry into every ds of a query, is taken off (head_dim over 96 without a
  *           bias: where a query sees up to 128 keys or one key has more than half of its p, of 128 queries any).
- *  Deterministic: every sum has one owner and one order.  Outputs share memory with nothing else of the call (INVALID_ARG).
+ *  Deterministic: every sum has one owner and one order.  Outputs and the workspace share memory with nothing else of the call (INVALID_ARG).
  *  workspace : DEVICE, 16-byte aligned, of the bytes slimfit_attention_workspace reports (backward 0 or 1; with_dtable:
  *           whether dtable is asked for); contents overwritten.
  * ---------------------------------------------------------------------- */

@@ -357,11 +357,30 @@ int32_t check_other_ranges(const Sizes &z, const int32_t *lengths, const void *t
     if ((rc = check_device_range(table, (size_t)z.buckets * (size_t)z.q_heads * z.e())) != SLIMFIT_OK) return rc;
     return z.q_tokens > 0 && z.k_tokens > 0 ? check_device_range(bucket_of, ((size_t)z.q_tokens + (size_t)z.k_tokens - 1) * 4) : SLIMFIT_OK;
 }
-int32_t check_workspace(size_t need, const void *ws, size_t bytes)
+// what a call reads beside its operands
+struct Others {
+    Span s[3];
+    Others(const Sizes &z, const int32_t *lengths, const void *table, const int32_t *bucket_of)
+        : s{flat(lengths, lengths ? (size_t)z.batch * 4 : 0), flat(table, table ? (size_t)z.buckets * (size_t)z.q_heads * z.e() : 0),
+            flat(bucket_of, table && z.q_tokens > 0 && z.k_tokens > 0 ? ((size_t)z.q_tokens + (size_t)z.k_tokens - 1) * 4 : 0)}
+    {
+    }
+};
+bool any_share(const Span *a, int n_a, const Span *b, int n_b)
+{
+    for (int i = 0; i < n_a; ++i)
+        for (int j = 0; j < n_b; ++j)
+            if (share(a[i], b[j])) return true;
+    return false;
+}
+// the workspace, which shares memory with nothing else of the call
+int32_t check_workspace(size_t need, const void *ws, size_t bytes, const Span *in, int n_in, const Span *out, int n_out, const Others &others)
 {
     if (need == 0) return SLIMFIT_OK;
     if (!ws || bytes < need) return SLIMFIT_ERR_WORKSPACE;
     if (!aligned_to(ws, 16)) return SLIMFIT_ERR_ALIGNMENT;
+    const Span w = flat(ws, need);
+    if (any_share(&w, 1, in, n_in) || any_share(&w, 1, out, n_out) || any_share(&w, 1, others.s, 3)) return SLIMFIT_ERR_INVALID_ARG;
     return check_device_range(ws, need);
 }
 
@@ -409,9 +428,11 @@ extern "C" int32_t slimfit_attention_forward(const void *q, const void *k, const
     if (batch == 0 || q_tokens == 0) return SLIMFIT_OK;
     const Span in[] = {span_of(q, z, 0, q_row), span_of(k, z, 1, k_row), span_of(v, z, 1, v_row)};
     const Span to[] = {flat(out, (size_t)z.q_count() * z.e()), flat(stats, (size_t)(batch * q_heads) * (size_t)q_tokens * 8)};
+    const Others others(z, lengths, table, bucket_of);
     if ((rc = check_spans(in, 3, to, 2)) != SLIMFIT_OK) return rc;
+    if (any_share(to, 2, others.s, 3)) return SLIMFIT_ERR_INVALID_ARG;
     const size_t need = turned_bytes(z) + part_bytes(z);
-    if ((rc = check_workspace(need, workspace, workspace_bytes)) != SLIMFIT_OK) return rc;
+    if ((rc = check_workspace(need, workspace, workspace_bytes, in, 3, to, 2, others)) != SLIMFIT_OK) return rc;
     if ((rc = check_ranges(in, 3)) != SLIMFIT_OK || (rc = check_ranges(to, 2)) != SLIMFIT_OK) return rc;
     if ((rc = check_other_ranges(z, lengths, table, bucket_of)) != SLIMFIT_OK) return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -442,18 +463,12 @@ extern "C" int32_t slimfit_attention_backward(const void *dout, const void *q, c
     const size_t q_bytes = (size_t)z.q_count() * z.e(), table_bytes = dtable ? (size_t)buckets * (size_t)q_heads * z.e() : 0;
     const Span in[] = {span_of(q, z, 0, q_row), span_of(k, z, 1, k_row), span_of(v, z, 1, v_row), flat(dout, q_bytes), flat(out, q_bytes),
                        flat(stats, (size_t)(batch * q_heads) * (size_t)q_tokens * 8)};
-    const Span to[] = {span_of(dq, z, 0, dq_row), span_of(dk, z, 1, dk_row), span_of(dv, z, 1, dv_row)};
+    const Span to[] = {span_of(dq, z, 0, dq_row), span_of(dk, z, 1, dk_row), span_of(dv, z, 1, dv_row), flat(dtable, table_bytes)};
+    const Others others(z, lengths, table, bucket_of);
     if ((rc = check_spans(in, 6, to, 3)) != SLIMFIT_OK) return rc;
-    if (dtable) {
-        const Span d = flat(dtable, table_bytes);
-        for (const Span &s : in)
-            if (share(d, s)) return SLIMFIT_ERR_INVALID_ARG;
-        for (const Span &s : to)
-            if (share(d, s)) return SLIMFIT_ERR_INVALID_ARG;
-        if (meet(dtable, table_bytes, table, table_bytes)) return SLIMFIT_ERR_INVALID_ARG;
-    }
+    if (any_share(to + 3, 1, in, 6) || any_share(to + 3, 1, to, 3) || any_share(to, 4, others.s, 3)) return SLIMFIT_ERR_INVALID_ARG;
     const BackwardPlaces at(z, dtable != nullptr);
-    if ((rc = check_workspace(at.bytes, workspace, workspace_bytes)) != SLIMFIT_OK) return rc;
+    if ((rc = check_workspace(at.bytes, workspace, workspace_bytes, in, 6, to, 4, others)) != SLIMFIT_OK) return rc;
     if ((rc = check_ranges(in, 6)) != SLIMFIT_OK || (rc = check_ranges(to, 3)) != SLIMFIT_OK) return rc;
     if ((rc = check_other_ranges(z, lengths, table, bucket_of)) != SLIMFIT_OK || (rc = check_device_range(dtable, table_bytes)) != SLIMFIT_OK) return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);

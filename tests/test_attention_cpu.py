@@ -64,6 +64,30 @@ def test_calls(lib, back):
         assert call(out=1 << 30) == call(stats=(1 << 31) + 16) == call(stats=1 << 33) == sf.ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("back", [False, True])
+def test_calls_refuse_what_shares_memory(lib, back):
+    """Outputs over the lengths, the table or the distances, and a workspace over anything: part of either is enough."""
+    call = _call(lib, back)
+    few = dict(lengths=1 << 20, table=1 << 21, buckets=4, of=1 << 22, layout=1)           # 8 bytes, 64, 116
+    small = dict(few, ws_bytes=64)
+    assert call(**small) == sf.ERR_WORKSPACE                # all but the workspace is fine
+    outs = ("dq", "dk", "dv", "dtable") if back else ("out", "stats")
+    for name in outs:
+        for at in (1 << 20, 1 << 21, (1 << 21) + 48, 1 << 22, (1 << 22) + 112):
+            assert call(**dict(small, **{name: at})) == sf.ERR_INVALID_ARG, (name, at)
+        assert call(**dict(small, **{name: (1 << 22) + 128})) == sf.ERR_WORKSPACE, name
+        # (what is not read may be anywhere)
+        assert call(**dict(small, table=0, **{name: 1 << 22})) == (sf.ERR_INVALID_ARG if name == "dtable" else sf.ERR_WORKSPACE)
+    need = sf.attention_workspace(torch.float32, sf.HEADS_APART, 2, 10, 20, 4, 2, 64, back, back)
+    full = dict(few, ws=1 << 35, ws_bytes=need, **(dict(dtable=1 << 23) if back else {}))
+    for name in outs + ("q", "k", "v", "lengths", "table", "of") + (("dout", "out", "stats") if back else ()):
+        for at in (1 << 35, (1 << 35) + need - 16):
+            assert call(**dict(full, **{name: at})) == sf.ERR_INVALID_ARG, name
+    if not torch.cuda.is_available():                       # elsewhere the look-up of pointers says so
+        assert call(**full) not in (sf.ERR_INVALID_ARG, sf.ERR_WORKSPACE, sf.ERR_ALIGNMENT, sf.OK)
+        assert call(**dict(full, q=(1 << 35) + need)) not in (sf.ERR_INVALID_ARG, sf.OK)
+
+
 def test_workspace(lib):
     size = lambda **kw: sf.attention_workspace(**dict(dict(dtype=torch.bfloat16, layout=sf.HEADS_ROWS, batch=2, q_tokens=100, k_tokens=50, q_heads=4,  # noqa: E731
                                                            kv_heads=2, head_dim=64), **kw))
