@@ -240,7 +240,8 @@ int32_t slimfit_apply_update_layer_delta(void *const *w, int32_t w_dt,
  *  d_out         : DEVICE float[L] or NULL (no distances).
  *  A gradient that is not finite makes its weight, and with 8 bits its block's states, NaN.
  *  What is written may share memory with nothing else of the plan, in no layer (INVALID_ARG); gradients may with each
- *  other.  numel <= 2^33 (ERR_UNSUPPORTED).
+ *  other.  A run's d_out and workspace share memory with nothing else of its arguments (INVALID_ARG), nor may d_out, live
+ *  and frozen with what the plan writes (which a run cannot see).  numel <= 2^33 (ERR_UNSUPPORTED).
  *
  *  slimfit_adamw_plan writes the table into the workspace (256-byte aligned, of the bytes that
  *  slimfit_adamw_workspace reports), slimfit_adamw_run steps the planned layers; numel, L, types, bits and block

@@ -594,6 +594,13 @@ extern "C" int32_t slimfit_adamw_run(const int64_t *numel, int32_t L, int32_t w_
     if ((rc = layout_of(L, numel, &lay)) != SLIMFIT_OK) return rc;
     if (L == 0) return SLIMFIT_OK;
     if (!aligned_to(d_out, 4) || !aligned_to(live, 4)) return SLIMFIT_ERR_ALIGNMENT;
+    if (workspace) {
+        const size_t d_bytes = d_out ? sizeof(float) * (size_t)L : 0, live_bytes = live ? 3 * sizeof(float) : 0, frozen_bytes = frozen ? (size_t)L : 0;
+        auto shares = [](const void *a, size_t a_bytes, const void *b, size_t b_bytes) { return a_bytes > 0 && b_bytes > 0 && meet(a, a_bytes, b, b_bytes); };
+        if (shares(workspace, lay.bytes, d_out, d_bytes) || shares(workspace, lay.bytes, live, live_bytes) || shares(workspace, lay.bytes, frozen, frozen_bytes) ||
+            shares(d_out, d_bytes, live, live_bytes) || shares(d_out, d_bytes, frozen, frozen_bytes))
+            return SLIMFIT_ERR_INVALID_ARG;
+    }
     if ((rc = check_workspace(lay, workspace, workspace_bytes)) != SLIMFIT_OK) return rc;
     if (d_out && (rc = check_device_range(d_out, sizeof(float) * (size_t)L)) != SLIMFIT_OK) return rc;
     if (live && (rc = check_device_range(live, 3 * sizeof(float))) != SLIMFIT_OK) return rc;

@@ -67,6 +67,23 @@ def test_run(lib):
     assert call(ws=0) == call(ws_bytes=8) == sf.ERR_WORKSPACE
 
 
+def test_run_refuses_what_shares_memory(lib):
+    """Distances over what the step reads, and a workspace over anything."""
+    need = sf.adamw_workspace([1000] * 5)
+
+    def call(ws=1 << 26, d=1 << 27, live=1 << 28, frozen=1 << 29):
+        return lib.slimfit_adamw_run(_numel(*[1000] * 5), I(5), I(0), I(0), I(32), I(0), D(1e-3), D(0.9), D(0.999), D(1e-8), L(1), F(1.0), C.c_uint32(0), P(live),
+                                     P(frozen), F(0.0), P(d), P(ws), C.c_size_t(need), P(0))
+
+    for name in ("d", "live", "frozen"):
+        for at in (1 << 26, (1 << 26) + need - 4):
+            assert call(**{name: at}) == sf.ERR_INVALID_ARG, name
+    assert call(d=(1 << 28) + 8) == call(live=(1 << 27) + 16) == call(d=(1 << 29) + 4) == call(frozen=(1 << 27) + 19) == sf.ERR_INVALID_ARG
+    if not torch.cuda.is_available():                      # elsewhere the look-up of pointers says so
+        for fine in (dict(), dict(d=(1 << 28) + 12), dict(frozen=(1 << 27) + 20), dict(live=1 << 29), dict(d=0, live=0, frozen=0)):
+            assert call(**fine) not in (sf.ERR_INVALID_ARG, sf.OK), fine
+
+
 def test_states(lib):
     def call(m=1 << 20, ms=1 << 21, v=1 << 22, vs=1 << 23, n=1000, block=64, mo=1 << 24, vo=1 << 25):
         return lib.slimfit_adamw_states(P(m), P(ms), P(v), P(vs), L(n), I(block), P(mo), P(vo), P(0))
