@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
     if (i < a.q_tokens) {
         const int64_t at = (int64_t)bh * a.q_tokens + i, all = (int64_t)a.batch * a.q_heads * a.q_tokens;
         const float top = g.stats[2 * at], total = g.stats[2 * at + 1];
-        if (total > 0.0f) {
+        if (!(total <= 0.0f)) {                             // (a sum of NaN too: its p are NaN)
             const float l = __builtin_amdgcn_logf(total);   // to the base of 2
             first = BIAS ? top : __builtin_fmaf(top, kLog2e, l);
             second = l;

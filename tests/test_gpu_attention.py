@@ -585,3 +585,34 @@ def test_the_last_tokens_over_all_keys_are_the_whole_passes_last_rows(dtype, n):
     within(rows_of(few.out, sf.HEADS_ROWS), whole.out[:, :, -n:], whole.rounded(whole.out_off(), whole.out)[:, :, -n:], "out")
     within(rows_of(few.dq, sf.HEADS_ROWS), whole.dq[:, :, -n:], whole.offs["dq"][:, :, -n:], "dq")
     few.check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 70, 150, 4, 2, 64), (40, 150, 150, 4, 2, 64), (40, 130, 260, 4, 2, 128), (1, 1, 700, 4, 2, 96)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("bias", [False, True], ids=["plain", "bias"])
+@pytest.mark.parametrize("what", ["q", "k", "v"])
+def test_a_nan_that_is_seen_is_in_all_that_it_is_in_by_the_formulas(shape, dtype, bias, what):
+    """In a query, a key or a value of one head: NaN in each result that it enters and in no other, and other sequences' results are those without it."""
+    require_gpu()
+    B, Tq, Tk, Hq, Hk, D = shape
+    group = Hq // Hk
+    q, k, v, do = inputs(*shape, dtype, sf.HEADS_ROWS, seed=Tk)
+    table = torch.randn(9, Hq, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(dtype) if bias else None
+    of = sf.distance_buckets(Tq, Tk, 9, 40) if bias else None
+    clean = Call(q, k, v, do, sf.HEADS_ROWS, D ** -0.5, False, None, table, of).forward().backward()
+    at = dict(q=q.clone(), k=k.clone(), v=v.clone())
+    at[what][B - 1, (Tq if what == "q" else Tk) // 2, (Hq if what == "q" else Hk) - 1, 3] = math.nan      # of the last sequence, in the last head
+    got = Call(at["q"], at["k"], at["v"], do, sf.HEADS_ROWS, D ** -0.5, False, None, table, of).forward().backward()
+    q, k, v, do = (t[-1].double().transpose(0, 1) for t in (at["q"], at["k"].repeat_interleave(group, 2), at["v"].repeat_interleave(group, 2), do))
+    p = torch.softmax(q @ k.mT, -1)                        # (NaN wherever the scaled and biased ones are)
+    out = p @ v
+    ds = p * (do @ v.mT - (do * out).sum(-1, keepdim=True))
+    shared = lambda t: t.view(Hk, group, Tk, D).sum(1)  # noqa: E731
+    for name, t in dict(out=out, dq=ds @ k, dk=shared(ds.mT @ q), dv=shared(p.mT @ do)).items():
+        nan, new, old = torch.isnan(t).transpose(0, 1), getattr(got, name), getattr(clean, name)
+        assert bool(nan.any()) == (what != "v" or name != "dv"), name
+        assert torch.equal(torch.isnan(new[-1]), nan) and torch.equal(new[:-1], old[:-1]), name
+    if bias:
+        i, j = torch.arange(Tq, device="cuda")[:, None], torch.arange(Tk, device="cuda")[None]
+        bucket = of.long()[j - i + Tq - 1]
+        assert torch.equal(torch.isnan(got.dtable), torch.stack([(torch.isnan(ds) & (bucket == b)).any(2).any(1) for b in range(9)]))
