@@ -707,7 +707,7 @@ int32_t slimfit_heads_norm_rotate_backward(const void *dq, const void *dkt, cons
  *           dq, dk and dv lie like q, k and v, with row lengths of their own.
  *  out, dout : DEVICE [batch, q_tokens, q_heads, head_dim], contiguous.  All of type dt and 16-byte aligned.
  *  stats  : DEVICE float[batch, q_heads, q_tokens, 2], 16-byte aligned: m and l.
- *  scale  : above 0, finite.        causal : not 0: query i sees keys j <= i + k_tokens - q_tokens.
+ *  scale  : above 0, below 2^127.   causal : not 0: query i sees keys j <= i + k_tokens - q_tokens.
  *  lengths: DEVICE int32[batch] or NULL: keys of a sequence (held to 0 .. k_tokens); those past it are not looked at,
  *           whatever they hold, and get gradients of 0.  They move neither the causal order nor the bias: both are counted from k_tokens.
  *  A query that sees no key has out 0, m -infinity, l 0 and gives no gradients.

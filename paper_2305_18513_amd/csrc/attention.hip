@@ -344,7 +344,7 @@ int32_t check_ranges(const Span *s, int n)
 
 int32_t check_others(const Sizes &z, float scale, const int32_t *lengths, const void *table, const int32_t *bucket_of)
 {
-    if (!(scale > 0.0f) || __builtin_isinf(scale)) return SLIMFIT_ERR_INVALID_ARG;
+    if (!(scale > 0.0f) || scale >= 0x1p127f) return SLIMFIT_ERR_INVALID_ARG;     // (scale log2 e has to be a number)
     if (table && (z.buckets < 1 || (!bucket_of && z.q_tokens > 0 && z.k_tokens > 0))) return SLIMFIT_ERR_INVALID_ARG;
     if (!aligned_to(lengths, 4) || !aligned_to(table, z.e()) || (table && !aligned_to(bucket_of, 4))) return SLIMFIT_ERR_ALIGNMENT;
     return SLIMFIT_OK;

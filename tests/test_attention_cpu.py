@@ -88,6 +88,16 @@ def test_calls_refuse_what_shares_memory(lib, back):
         assert call(**dict(full, q=(1 << 35) + need)) not in (sf.ERR_INVALID_ARG, sf.OK)
 
 
+@pytest.mark.parametrize("back", [False, True])
+def test_calls_refuse_scales_without_a_logarithm_of_base_2(lib, back):
+    call = _call(lib, back)
+    for scale in (2.0 ** 127, 3e38):
+        assert call(scale=scale) == sf.ERR_INVALID_ARG
+    if not torch.cuda.is_available():
+        for scale in (1.7e38, 1e-38, 2.0 ** -149):
+            assert call(scale=scale) not in (sf.ERR_INVALID_ARG, sf.OK)
+
+
 def test_workspace(lib):
     size = lambda **kw: sf.attention_workspace(**dict(dict(dtype=torch.bfloat16, layout=sf.HEADS_ROWS, batch=2, q_tokens=100, k_tokens=50, q_heads=4,  # noqa: E731
                                                            kv_heads=2, head_dim=64), **kw))

@@ -616,3 +616,35 @@ def test_a_nan_that_is_seen_is_in_all_that_it_is_in_by_the_formulas(shape, dtype
         i, j = torch.arange(Tq, device="cuda")[:, None], torch.arange(Tk, device="cuda")[None]
         bucket = of.long()[j - i + Tq - 1]
         assert torch.equal(torch.isnan(got.dtable), torch.stack([(torch.isnan(ds) & (bucket == b)).any(2).any(1) for b in range(9)]))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1e-37, 1.7e38, 3e38], ids=str)
+@pytest.mark.parametrize("shape", [(36, 200, 200, 4, 2, 64), (36, 130, 150, 4, 2, 128), (1, 3, 700, 4, 2, 32)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("bias", [False, True], ids=["plain", "bias"])
+def test_the_least_and_the_largest_scales(dtype, scale, shape, bias):
+    """Logits of all but 0, whose keys count alike (or by their bias); from 2^127 on, where scale log2 e has no number, the call is refused."""
+    require_gpu()
+    B, Tq, Tk, Hq, Hk, D = shape
+    q, k, v, do = inputs(*shape, dtype, sf.HEADS_ROWS, seed=Tk)
+    if scale > 1:
+        q.zero_()
+    table = torch.randn(9, Hq, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(dtype) if bias else None
+    of = sf.distance_buckets(Tq, Tk, 9, 40, both_ways=False) if bias else None
+    call = Call(q, k, v, do, sf.HEADS_ROWS, scale, True, None, table, of)
+    if scale >= 2.0 ** 127:
+        for one in (call.forward, call.backward):
+            with pytest.raises(sf.SlimfitError):
+                one()
+        return
+    call.forward().backward()
+    r = Reference(q, k, v, do, sf.HEADS_ROWS, float(torch.tensor(scale, dtype=torch.float32)), True, None, table, of)
+    assert torch.equal(call.stats[..., 1] > 0, r.total[..., 0] > 0)
+    within(rows_of(call.out, sf.HEADS_ROWS), r.out, r.rounded(r.out_off(), r.out), "out")
+    within(call.stats[..., 1:].double(), r.total, r.total_off * r.total + 1e-40, "sum")
+    within(rows_of(call.dv, sf.HEADS_ROWS), r.dv, r.offs["dv"], "dv")
+    if bias:
+        within(call.dtable.double(), r.dtable, r.offs["dtable"], "dtable")
+    if scale < 1:
+        within(rows_of(call.dq, sf.HEADS_ROWS), r.dq, r.offs["dq"], "dq")
+        within(rows_of(call.dk, sf.HEADS_ROWS, True), r.dk, r.offs["dk"], "dk")
