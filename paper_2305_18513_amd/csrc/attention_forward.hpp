@@ -39,7 +39,8 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 64 ? 1 : 2
     // Of q k^T, or (BIAS) of s: the maximum so far, and what the exponentials are taken against.  That follows only where the maximum has
     // risen by 2^8 and more: e^(s - base) and its sums have room for that, and out is rarely taken down.
     float top = -__builtin_inff(), base = -__builtin_inff(), total = 0.0f;
-    const float by = BIAS ? kLog2e : scale, room = 8.0f / by;
+    // (A finite room, also for the least scales: -infinity and an infinite one would be none.)
+    const float by = BIAS ? kLog2e : scale, room = fminf(8.0f / by, 0x1.fffffep127f);
 
     Tiles<T, D> kl, vl;
     BiasLoad bl;

@@ -619,7 +619,7 @@ def test_a_nan_that_is_seen_is_in_all_that_it_is_in_by_the_formulas(shape, dtype
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
-@pytest.mark.parametrize("scale", [1e-37, 1.7e38, 3e38], ids=str)
+@pytest.mark.parametrize("scale", [1e-37, 1e-38, 2.0 ** -126, 2.0 ** -149, 1.7e38, 3e38], ids=str)
 @pytest.mark.parametrize("shape", [(36, 200, 200, 4, 2, 64), (36, 130, 150, 4, 2, 128), (1, 3, 700, 4, 2, 32)], ids=lambda s: "x".join(map(str, s)))
 @pytest.mark.parametrize("bias", [False, True], ids=["plain", "bias"])
 def test_the_least_and_the_largest_scales(dtype, scale, shape, bias):
