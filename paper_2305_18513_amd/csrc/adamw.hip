@@ -311,10 +311,11 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const char *__restrict_
             m[j] = m[j] * s.b1 + gj * s.one_b1;
             v[j] = v[j] * s.b2 + (gj * s.one_b2) * gj;
         }
-        // The instructions for roots and reciprocals are within a step of the last place, and take numbers below the normal ones as 0:
-        // from an eps of 2^-40 on, a v of those is none of its root's sum.  (Divided and rooted by the correctly rounded sequences,
-        // distances too and added up in fp64 one by one: 97 vector instructions an element with 8 bits instead of 59, 361 us instead of 290 for 151 million bf16 weights.)
-        if (s.eps >= 0x1p-40f) {
+        // The instructions for roots and reciprocals are within a step of the last place, and take numbers below the normal ones as 0: a root
+        // of those, up to 2^-63, counts `root` times, so from an eps of 2^-40 of these on it is none of their sum.  (Divided and rooted by the
+        // correctly rounded sequences, distances too and added up in fp64 one by one: 97 vector instructions an element with 8 bits instead of 59,
+        // 361 us instead of 290 for 151 million bf16 weights.)
+        if (s.eps >= 0x1p-40f * s.root) {
 #pragma unroll
             for (int j = 0; j < N; ++j) d[j] = m[j] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[j]) * s.root + s.eps);
         } else {

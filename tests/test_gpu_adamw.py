@@ -392,3 +392,25 @@ def test_numbers_below_the_normal_ones(eps):
     assert float(d[0]) == 0.0 and math.isinf(float(d[3]))
     terms = np.abs(1e-2 / 0.1 * m[2].double().cpu().numpy() / (np.sqrt(v[2].double().cpu().numpy() / (1 - 0.999)) + float(np.float32(eps)))) / 0.25
     assert abs(float(d[2]) - terms.mean()) <= 20 * 2.0 ** -24 * terms.mean() + 2.0 ** -149
+
+
+@pytest.mark.parametrize("eps", [1e-10, 1e-11, 1e-12, 9.2e-13, 9e-13])
+@pytest.mark.parametrize("beta2", [0.999, 1.0 - 1e-6, 0.5])
+@pytest.mark.parametrize("live", [False, True])
+def test_an_eps_near_what_a_root_below_the_normal_numbers_adds(eps, beta2, live):
+    """At the first step a root of v counts 1 / sqrt(1 - beta2) times, up to a thousand here, beside eps.  Weights of 0, so that the move itself is
+    seen: fifteen roundings, and one of the weight."""
+    require_gpu()
+    tiny = 2.0 ** -126
+    g = np.sqrt(np.array([0.9, 0.99, 0.5, 0.1, 0.01, 1.01, 4.0, 1e6]) * tiny / (1 - beta2)).astype(np.float32)
+    w, grad = torch.zeros(g.size, device="cuda"), torch.from_numpy(g).cuda()
+    m, v = torch.zeros_like(w), torch.zeros_like(w)
+    ws, d = torch.zeros(sf.adamw_workspace([g.size]), dtype=torch.uint8, device="cuda"), torch.empty(1, device="cuda")
+    sf.adamw_plan([w], [grad], [m], [v], None, None, [0.0], 32, 0, ws)
+    now = torch.tensor([0.25, 1.0, 1.0], device="cuda") if live else None
+    sf.adamw_run([g.size], sf.F32, sf.F32, 32, 0, 0.25, 0.9, beta2, eps, 1, ws, live=now, floor=1.0, d_out=d)
+    m64, v64 = m.double().cpu().numpy(), v.double().cpu().numpy()
+    assert np.array_equal(v.cpu().numpy(), (g * np.float32(1 - beta2)) * g) and int((v64 < tiny).sum()) >= 4
+    move = 0.25 / 0.1 * m64 / (np.sqrt(v64 / (1 - beta2)) + float(np.float32(eps)))
+    assert np.all(np.abs(w.double().cpu().numpy() + move) <= np.abs(move) * 16 * 2.0 ** -24 + 2.0 ** -149)
+    assert abs(float(d) - move.mean()) <= 18 * 2.0 ** -24 * move.mean() + 2.0 ** -149
