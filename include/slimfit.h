@@ -238,7 +238,8 @@ int32_t slimfit_apply_update_layer_delta(void *const *w, int32_t w_dt,
  *                  of the arguments (a captured graph is replayed with other values; step up to 2^24).
  *  frozen        : DEVICE uint8[L] or NULL: layers of 1 are frozen (the mask of slimfit_ils_select).
  *  d_out         : DEVICE float[L] or NULL (no distances).
- *  A gradient that is not finite makes its weight, and with 8 bits its block's states, NaN.
+ *  A gradient that is not finite makes its weight, and with 8 bits its block's states, NaN; with 8 bits a v' that overflows makes
+ *  its block's v NaN (scale 2^98, codes 244).
  *  What is written may share memory with nothing else of the plan, in no layer (INVALID_ARG); gradients may with each
  *  other.  A run's d_out and workspace share memory with nothing else of its arguments (INVALID_ARG), nor may d_out, live
  *  and frozen with what the plan writes (which a run cannot see).  numel <= 2^33 (ERR_UNSUPPORTED).

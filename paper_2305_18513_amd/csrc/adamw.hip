@@ -12,6 +12,7 @@
 //       Rounding to the nearest would never let a v decay (a step takes 0.001 of it, half a step of the code is 0.06), so v' is
 //       rounded up with the probability of what is cut off: 20 bits of dither are added to the fp32 bits before the cut.  The
 //       dither is a function of seed, step, tensor and place alone.  A v' that is not 0 never becomes 0 (m' / eps would explode).
+//       A run with a v' that is not finite is NaN as a whole, as its m is: no scale has codes for that one and for the others.
 // m' and v' are rounded products and their rounded sum, without a fused multiply-add, so that the codes are defined.
 //
 // What bounds it: memory (fp32 weights and states, 16.8 million, 470 MB: 86 us, 5.5 TB/s; 151 million bf16 weights with states in 8 bits, 1.46 GB: 260 to
@@ -34,6 +35,7 @@ constexpr int kChunk = 32 * kThreads, kShort = 8 * kThreads, kFew = 512;
 // a third frozen, in fp32: 287 us, 328 with eight elements in two vectors); with states in 8 bits 8 bytes of codes, for the work on a run's scale is
 // a thread's (6 % more with four).
 template <int BITS> constexpr int kPer = BITS == 8 ? 8 : 4;
+constexpr int kNoNumber = 244;               // of a v over a scale of 2^98: 0x70800000 + (244 << 20) is 0x7FC00000
 constexpr uint32_t kMagic = 0x534C4157u;     // "SLAW"
 constexpr int kPlanBatch = 32;
 
@@ -232,7 +234,9 @@ template <int N> __device__ __forceinline__ Codes<N> encode_v(const float (&v)[N
 #pragma unroll
     for (int j = 0; j < N; ++j) top = max(top, __builtin_bit_cast(uint32_t, v[j]));
     top = group_max_u32(top, lanes) >> 23;
-    top = top > 31u ? top - 30u : 1u;
+    const bool none = top >= 255u;                          // one is not finite: NaN, by a code that is one over this scale
+    const int zero = none ? kNoNumber : 0, least = none ? kNoNumber : 1, most = none ? kNoNumber : 255;
+    top = none ? 225u : top > 31u ? top - 30u : 1u;
     scale = __builtin_bit_cast(float, top << 23);
     Codes<N> c = {};
 #pragma unroll
@@ -243,7 +247,7 @@ template <int N> __device__ __forceinline__ Codes<N> encode_v(const float (&v)[N
             const uint32_t bits = __builtin_bit_cast(uint32_t, v[4 * i + j]);
             const uint32_t dither = (j == 0 ? word : __builtin_rotateleft32(word, 8 * j)) >> 12;
             const int code = (int)((bits + dither) >> 20) - (int)(8u * top);
-            c.w[i] |= (uint32_t)(bits ? min(max(code, 1), 255) : 0) << (8 * j);
+            c.w[i] |= (uint32_t)(bits ? min(max(code, least), most) : zero) << (8 * j);
         }
     }
     return c;

@@ -414,3 +414,30 @@ def test_an_eps_near_what_a_root_below_the_normal_numbers_adds(eps, beta2, live)
     move = 0.25 / 0.1 * m64 / (np.sqrt(v64 / (1 - beta2)) + float(np.float32(eps)))
     assert np.all(np.abs(w.double().cpu().numpy() + move) <= np.abs(move) * 16 * 2.0 ** -24 + 2.0 ** -149)
     assert abs(float(d) - move.mean()) <= 18 * 2.0 ** -24 * move.mean() + 2.0 ** -149
+
+
+@pytest.mark.parametrize("block", [32, 64, 256])
+@pytest.mark.parametrize("bad", [math.nan, -math.nan, math.inf, -math.inf, 3e21])
+def test_a_v_that_is_not_finite_is_its_whole_blocks(bad, block):
+    """In 8 bits a block's v are all NaN then (a scale for so large a number has no codes for the others), those without a gradient too, and the
+    next step's weights with them; the blocks beside it go on.  A gradient of 3e21 is finite, its v' (9e39) is not."""
+    require_gpu()
+    n = 5 * block + 3
+    model, other = (Model([n], torch.float32, torch.float32, 8, block, seed=5) for _ in range(2))
+    here = torch.arange(n, device="cuda") // block == 2
+    for m in (model, other):
+        m.g[0][2 * block + 1 :: 7] = 0.0
+    model.g[0][2 * block + 5] = bad
+    outs = [torch.empty(n, device="cuda") for _ in range(4)]
+    for step in (1, 2):
+        for m in (model, other):
+            m.plan()
+            m.run(step, grad_factor=1.0)
+        for m, (m_out, v_out) in ((model, outs[:2]), (other, outs[2:])):
+            sf.adamw_states(m.m[0], m.ms[0], m.v[0], m.vs[0], block, m_out, v_out)
+        assert bool(torch.isnan(outs[1][here]).all())
+        assert bool(torch.isnan(outs[0][here]).all()) or bad == 3e21
+        assert torch.equal(outs[0][~here], outs[2][~here]) and torch.equal(outs[1][~here], outs[3][~here])
+        assert torch.equal(model.w[0][~here], other.w[0][~here])
+    assert bool(torch.isnan(model.w[0][here]).all())
+    assert model.untouched_around()
