@@ -421,7 +421,7 @@ class SelfAttentionFunction(torch.autograd.Function):
         rows = qkv.view(B, T, heads + 2 * kv_heads, width // (heads + 2 * kv_heads))
         ctx.meta = (heads, kv_heads, scale, causal)
         out = _attend(ctx, *rows.split((heads, kv_heads, kv_heads), 2), sf.HEADS_ROWS, scale, causal, lengths, table, bucket_of, (qkv,))
-        return out.view(B, T, -1)
+        return out.view(B, T, out.shape[2] * out.shape[3])
 
     @staticmethod
     @once_differentiable
@@ -430,7 +430,7 @@ class SelfAttentionFunction(torch.autograd.Function):
         heads, kv_heads, scale, causal = ctx.meta
         B, T, width = qkv.shape
         dqkv = torch.empty_like(qkv)
-        parts = [t.view(B, T, heads + 2 * kv_heads, -1).split((heads, kv_heads, kv_heads), 2) for t in (qkv, dqkv)]
+        parts = [t.view(B, T, heads + 2 * kv_heads, out.shape[3]).split((heads, kv_heads, kv_heads), 2) for t in (qkv, dqkv)]
         dtable = torch.empty_like(table) if table is not None and ctx.needs_input_grad[6] else None
         sf.attention_backward(dout.contiguous().view(out.shape), *parts[0], sf.HEADS_ROWS, scale, causal, lengths, table, bucket_of, out, stats, *parts[1],
                               dtable)

@@ -207,3 +207,22 @@ def test_a_captured_step_replays_to_the_eager_gradients():
         torch.cuda.synchronize()
         for a, b in zip(captured, [t.detach().clone() for t in step()]):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("B,T", [(0, 5), (2, 0), (0, 0)])
+def test_no_sequences_and_no_tokens(B, T):
+    """A batch that is empty, or whose sequences are: empty results and gradients, and a table's that is 0."""
+    require_gpu()
+    Hq, Hk, D = 4, 2, 16
+    table = torch.randn(3, Hq, device="cuda", requires_grad=True)
+    of = torch.zeros(max(0, 2 * T - 1), dtype=torch.int32, device="cuda")
+    rows = torch.randn(B, T, (Hq + 2 * Hk) * D, device="cuda", requires_grad=True)
+    y = ag.SelfAttentionFunction.apply(rows, Hq, Hk, 0.25, True, None, table, of)
+    assert y.shape == (B, T, Hq * D)
+    drows, dtable = torch.autograd.grad(y.sum(), (rows, table))
+    assert drows.shape == rows.shape and bool((dtable == 0).all())
+    q, k, v = (torch.randn(B, T, h, D, device="cuda", requires_grad=True) for h in (Hq, Hk, Hk))
+    y = ag.AttentionFunction.apply(q, k, v, 0.25, True, None, table, of)
+    assert y.shape == (B, T, Hq, D)
+    *grads, dtable = torch.autograd.grad(y.sum(), (q, k, v, table))
+    assert all(g.shape == t.shape for g, t in zip(grads, (q, k, v))) and bool((dtable == 0).all())
