@@ -235,7 +235,12 @@ int64_t share_of(const Sizes &z)
     return all <= 8 * 32 ? 8 : (all + 31) / 32;
 }
 int64_t shares_of(const Sizes &z) { return (z.batch * q_blocks(z) * query_splits(z) + share_of(z) - 1) / share_of(z); }
-int64_t part_row(const Sizes &z) { return ((int64_t)z.k_tokens + kTile - 1) / kTile * kTile + kTile; }
+// floats that a wave has for its sums by distance: those of the largest share of a block's tiles, and 32 more
+int64_t part_row(const Sizes &z)
+{
+    const int64_t tiles = ((int64_t)z.k_tokens + kTile - 1) / kTile, splits = query_splits(z);
+    return ((tiles + splits - 1) / splits + 1) * kTile;
+}
 
 // How many workgroups share a sequence's keys out, or 0: 128 queries of a head a workgroup.  (us with those, with few queries, on the same operands again and again)
 //   bf16, up to 16 queries: 16 x 4096 keys, 32 heads on 8 by 128: 1 query 121, 48; 16 132, 63; 32 139, 120; 64 142, 243;

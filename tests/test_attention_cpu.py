@@ -109,6 +109,13 @@ def test_workspace(lib):
     assert lib.slimfit_attention_workspace(I(0), I(0), L(1), I(1), I(1), I(1), I(1), I(130), I(0), I(0), C.byref(out)) == sf.ERR_UNSUPPORTED
 
 
+def test_the_workspace_of_shared_out_tiles():
+    """The sums by distance of shares: what they write, not a whole row of keys for each of up to 64."""
+    size = lambda table: sf.attention_workspace(torch.bfloat16, sf.HEADS_ROWS, 1, 128, 1 << 20, 1, 1, 128, table, True)  # noqa: E731
+    # 64 shares of 256 tiles, 4 waves' rows of 257 * 64 floats each; 8 shares of the sums over 128 + 2^20 distances
+    assert 0 < size(True) - size(False) <= 64 * 4 * 257 * 64 * 4 + 8 * (128 + (1 << 20)) * 4 + 512
+
+
 def test_distance_buckets():
     one = sf.distance_buckets(5, 5, 8, 16, both_ways=False, device="cpu")
     assert one.dtype == torch.int32 and one.tolist() == [4, 3, 2, 1, 0, 0, 0, 0, 0]
