@@ -726,7 +726,10 @@ int32_t slimfit_heads_norm_rotate_backward(const void *dq, const void *dkt, cons
  *           bias: where a query sees up to 128 keys or one key has more than half of its p, of 128 queries any).
  *  Deterministic: every sum has one owner and one order.  Outputs and the workspace share memory with nothing else of the call (INVALID_ARG).
  *  workspace : DEVICE, 16-byte aligned, of the bytes slimfit_attention_workspace reports (backward 0 or 1; with_dtable:
- *           whether dtable is asked for); contents overwritten.
+ *           whether dtable is asked for); contents overwritten.  It grows by tokens, not by pairs: keys that lie transposed once more; where few
+ *           queries share keys out, up to 64 partial results a query; backward 12 bytes a query and head, up to 64 partial gradients a row where
+ *           there are few blocks of 128; and for dtable up to 256 MB, or the larger of 32 KB and 16 batch q_heads bytes a key where that is more, and
+ *           up to 32 sums a head and distance.
  * ---------------------------------------------------------------------- */
 typedef enum { SLIMFIT_HEADS_ROWS = 0, SLIMFIT_HEADS_APART = 1 } slimfit_heads_layout;
 

@@ -7,6 +7,7 @@ namespace slimfit {
 namespace {
 
 constexpr int kTurn = 64;
+constexpr int64_t kTurnBytes = (int64_t)256 << 20, kTurnWorkgroups = 2048;      // (`turn_blocks`)
 constexpr int kAtOnce = 8;                   // blocks of queries whose sums by distance are under way at a time
 
 // kt (head, dim, tokens) -> k (head, tokens, dim): a workgroup takes 64 tokens of up to 64 elements, 16 bytes a thread in and out.  Rows of dim
@@ -58,25 +59,27 @@ __global__ void __launch_bounds__(kAttnThreads) turn_kernel(const T *__restrict_
     }
 }
 
-// Sums of ds by distance over `each` blocks of 128 queries (and shares of their keys) of all sequences': blockIdx.z has its share, in order.  What a wave did not
+// Sums of ds by distance over `each` of `blocks` blocks of 128 queries from the first_block-th on (and shares of their keys) of all sequences: blockIdx.z has its
+// share, in order, added to that of the blocks before.  What a wave did not
 // write is past its descriptor's end: 0, with no branch that a load would wait at (512 tokens: 11.6 us with branches, 5.0 without).
-__global__ void __launch_bounds__(kWave) distances_kernel(Attention a, const float *__restrict__ parts, int64_t part_row, int blocks, int splits, int each, float *__restrict__ sums)
+__global__ void __launch_bounds__(kWave) distances_kernel(Attention a, const float *__restrict__ parts, int64_t part_row, int first_block, int blocks, int splits, int each, float *__restrict__ sums)
 {
     const int all = a.q_tokens + a.k_tokens - 1, head = blockIdx.y, at = (int)(blockIdx.x * kWave + threadIdx.x);
     const int end = min(a.batch * blocks * splits, ((int)blockIdx.z + 1) * each);
-    double sum = 0.0;
+    float *const to = sums + ((int64_t)blockIdx.z * a.q_heads + head) * all + at;
+    double sum = first_block > 0 && at < all ? (double)*to : 0.0;
     for (int n0 = (int)blockIdx.z * each; n0 < end; n0 += kAtOnce) {
         float x[kAtOnce][kAttnWaves];
         const int keys = keys_of(a, min(n0 + (int)(threadIdx.x % kAtOnce), end - 1) / splits / blocks);                 // a block's a lane
 #pragma unroll
         for (int m = 0; m < kAtOnce; ++m) {
             const int n = min(n0 + m, end - 1), split = n % splits, b = n / splits / blocks, block = n / splits % blocks;
-            const int tiles = key_tiles(a, block * kBlock, __builtin_amdgcn_readlane(keys, m)), t0 = first_of(tiles, split, splits);
+            const int q0 = (first_block + block) * kBlock, tiles = key_tiles(a, q0, __builtin_amdgcn_readlane(keys, m)), t0 = first_of(tiles, split, splits);
             const int written = (first_of(tiles, split + 1, splits) - t0) * kTile + kOwn;
             const float *const of = parts + ((((int64_t)b * a.q_heads + head) * blocks + block) * splits + split) * kAttnWaves * part_row;
 #pragma unroll
             for (int w = 0; w < kAttnWaves; ++w) {
-                const int place = at - (a.q_tokens - 1) + block * kBlock + w * kOwn + kOwn - 1 - t0 * kTile;
+                const int place = at - (a.q_tokens - 1) + q0 + w * kOwn + kOwn - 1 - t0 * kTile;
                 const Buffer row = buffer_at(of + w * part_row, n0 + m < end ? (int64_t)written * 4 : 0);
                 // (a sum of an offset below 0 and a constant would be past the end even where it is not)
                 x[m][w] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(row, place < 0 ? kNowhere : place * 4, 0, 0));
@@ -87,7 +90,7 @@ __global__ void __launch_bounds__(kWave) distances_kernel(Attention a, const flo
 #pragma unroll
             for (int w = 0; w < kAttnWaves; ++w) sum += (double)x[m][w];
     }
-    if (at < all) sums[((int64_t)blockIdx.z * a.q_heads + head) * all + at] = (float)sum;
+    if (at < all) *to = (float)sum;
 }
 
 // a workgroup for each bucket and head
@@ -228,19 +231,29 @@ int key_splits(const Sizes &z)
 {
     return splits_of(z, z.batch * z.kv_heads * ((z.k_tokens + kBlock - 1) / kBlock), (int64_t)(z.q_heads / z.kv_heads) * ((z.q_tokens + kTile - 1) / kTile));
 }
-// blocks of queries that one share of the sums by distance adds up (16 x 512, 12 heads: 64 in one share 57 us, 8 each 6.6), and the shares
-int64_t share_of(const Sizes &z)
-{
-    const int64_t all = z.batch * q_blocks(z) * query_splits(z);
-    return all <= 8 * 32 ? 8 : (all + 31) / 32;
-}
-int64_t shares_of(const Sizes &z) { return (z.batch * q_blocks(z) * query_splits(z) + share_of(z) - 1) / share_of(z); }
 // floats that a wave has for its sums by distance: those of the largest share of a block's tiles, and 32 more
 int64_t part_row(const Sizes &z)
 {
     const int64_t tiles = ((int64_t)z.k_tokens + kTile - 1) / kTile, splits = query_splits(z);
     return ((tiles + splits - 1) / splits + 1) * kTile;
 }
+// Blocks of queries whose sums by distance are held at a time, a launch each: kTurnBytes of these or, at long rows, as many as make kTurnWorkgroups,
+// so that they take memory by the keys and not by the pairs.  (Blocks whose tiles are shared out are fewer.)  16 x 4096 x 4096, 16 heads of 64: three
+// launches 7080 us, one 7085; with no kTurnBytes 300 x 512 x 512, 12 heads, is in four, 2221 us for 1944.
+int turn_blocks(const Sizes &z)
+{
+    if (z.batch == 0 || q_blocks(z) == 0) return q_blocks(z);
+    const int64_t units = z.batch * z.q_heads, by_bytes = kTurnBytes / (units * kAttnWaves * part_row(z) * 4), by_workgroups = kTurnWorkgroups / units;
+    const int64_t most = by_bytes > by_workgroups ? by_bytes : by_workgroups;
+    return most < 1 ? 1 : most < q_blocks(z) ? (int)most : q_blocks(z);
+}
+// blocks of queries that one share of the sums by distance adds up (16 x 512, 12 heads: 64 in one share 57 us, 8 each 6.6), and the shares
+int64_t share_of(const Sizes &z)
+{
+    const int64_t all = z.batch * turn_blocks(z) * query_splits(z);
+    return all <= 8 * 32 ? 8 : (all + 31) / 32;
+}
+int64_t shares_of(const Sizes &z) { return (z.batch * turn_blocks(z) * query_splits(z) + share_of(z) - 1) / share_of(z); }
 
 // How many workgroups share a sequence's keys out, or 0: 128 queries of a head a workgroup.  (us with those, with few queries, on the same operands again and again)
 //   bf16, up to 16 queries: 16 x 4096 keys, 32 heads on 8 by 128: 1 query 121, 48; 16 132, 63; 32 139, 120; 64 142, 243;
@@ -275,7 +288,7 @@ struct BackwardPlaces {
     {
         rows = turned_bytes(z);
         parts = rows + rounded((size_t)(z.batch * z.q_heads) * (size_t)z.q_tokens * 12);
-        sums = parts + (table ? rounded((size_t)(z.batch * z.q_heads) * (size_t)(q_blocks(z) * query_splits(z)) * kAttnWaves * (size_t)part_row(z) * 4) : 0);
+        sums = parts + (table ? rounded((size_t)(z.batch * z.q_heads) * (size_t)(turn_blocks(z) * query_splits(z)) * kAttnWaves * (size_t)part_row(z) * 4) : 0);
         dq = sums + (table ? rounded((size_t)shares_of(z) * (size_t)z.q_heads * ((size_t)z.q_tokens + (size_t)z.k_tokens) * 4) : 0);
         dk = dq + (query_splits(z) > 1 ? rounded((size_t)query_splits(z) * (size_t)z.q_count() * 4) : 0);
         bytes = dk + (key_splits(z) > 1 ? rounded((size_t)key_splits(z) * (size_t)z.k_count() * 8) : 0);
@@ -487,23 +500,27 @@ extern "C" int32_t slimfit_attention_backward(const void *dout, const void *q, c
     const Operand oq = operand_of(dq, z, 0, dq_row), ok = operand_of(dk, z, 1, dk_row), ov = operand_of(dv, z, 1, dv_row);
     const bool across = layout == SLIMFIT_HEADS_APART;      // dk lies transposed too: tokens beside each other
     float *const parts = dtable && pairs ? reinterpret_cast<float *>(ws + at.parts) : nullptr;
-    const Gradients g = {dout, out, stats, dq, dk, dv, oq.b, oq.h, oq.t, ok.b, ok.h, across ? 1 : ok.t, across ? k_tokens : 1, ov.b, ov.h, ov.t,
-                         reinterpret_cast<float *>(ws + at.rows), parts, part_row(z), query_splits(z), key_splits(z), reinterpret_cast<float *>(ws + at.dq),
-                         reinterpret_cast<float *>(ws + at.dk)};
-    if (dt == SLIMFIT_BF16) attention_backward_bf16(a, g, st);
-    else attention_backward_f32(a, g, st);
+    Gradients g = {dout, out, stats, dq, dk, dv, oq.b, oq.h, oq.t, ok.b, ok.h, across ? 1 : ok.t, across ? k_tokens : 1, ov.b, ov.h, ov.t,
+                   reinterpret_cast<float *>(ws + at.rows), parts, part_row(z), 0, 0, false, query_splits(z), key_splits(z), reinterpret_cast<float *>(ws + at.dq),
+                   reinterpret_cast<float *>(ws + at.dk)};
+    float *const sums = reinterpret_cast<float *>(ws + at.sums);
+    const int all = q_tokens + k_tokens - 1, shares = parts ? (int)shares_of(z) : 0, turn = parts ? turn_blocks(z) : q_blocks(z);
+    do {
+        g.blocks = q_blocks(z) - g.first_block < turn ? q_blocks(z) - g.first_block : turn;
+        g.all_rows = g.first_block + g.blocks == q_blocks(z);
+        if (dt == SLIMFIT_BF16) attention_backward_bf16(a, g, st);
+        else attention_backward_f32(a, g, st);
+        if (parts)
+            launch(distances_kernel, dim3((unsigned)((all + kWave - 1) / kWave), (unsigned)q_heads, (unsigned)shares), kWave, 0, st, a, parts, g.part_row,
+                   g.first_block, g.blocks, g.q_splits, (int)share_of(z), sums);
+        g.first_block += g.blocks;
+    } while (!g.all_rows);
     if (const int64_t vectors = ((g.q_splits > 1 ? z.q_count() : 0) + (g.k_splits > 1 ? 2 * z.k_count() : 0)) / 4; vectors > 0) {
         const unsigned grid = (unsigned)((vectors + kAttnThreads - 1) / kAttnThreads);
         if (dt == SLIMFIT_BF16) launch(shares_kernel<uint16_t>, grid, kAttnThreads, 0, st, a, g);
         else launch(shares_kernel<float>, grid, kAttnThreads, 0, st, a, g);
     }
     if (dtable) {
-        float *const sums = reinterpret_cast<float *>(ws + at.sums);
-        const int all = q_tokens + k_tokens - 1;
-        const int shares = parts ? (int)shares_of(z) : 0;
-        if (parts)
-            launch(distances_kernel, dim3((unsigned)((all + kWave - 1) / kWave), (unsigned)q_heads, (unsigned)shares), kWave, 0, st, a, parts, g.part_row,
-                   q_blocks(z), g.q_splits, (int)share_of(z), sums);
         const dim3 grid((unsigned)buckets, (unsigned)q_heads);
         if (dt == SLIMFIT_BF16) launch(buckets_kernel<uint16_t>, grid, kAttnThreads, 0, st, a, sums, shares, static_cast<uint16_t *>(dtable));
         else launch(buckets_kernel<float>, grid, kAttnThreads, 0, st, a, sums, shares, static_cast<float *>(dtable));

@@ -415,6 +415,8 @@ struct Gradients {
     float *rows;                             // [3][batch * q_heads * q_tokens]: what p is taken by (two numbers), delta
     float *parts;                            // sums of ds by distance, or NULL
     int64_t part_row;                        // floats of a wave's
+    int32_t first_block, blocks;             // of queries: those of one launch, whose sums by distance parts holds
+    bool all_rows;                           // the last of these launches, after which the keys' gradients follow
     // workgroups that share the tiles of one block out, and, where that is more than one, their sums: dq [q_splits][batch][q_heads]
     // [q_tokens][head_dim], dk and dv [k_splits][batch][kv_heads][k_tokens][2][head_dim]
     int32_t q_splits, k_splits;

@@ -51,7 +51,8 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
     const int group = a.q_heads / a.kv_heads;
     const int splits = SPLIT ? g.q_splits : 1;
     const Place place(a.batch * a.kv_heads, blocks * splits, group, a.causal != 0);
-    const int block = a.causal ? blocks - 1 - place.block / splits : place.block / splits, split = place.block % splits;     // the longest first
+    const int at_block = a.causal ? blocks - 1 - place.block / splits : place.block / splits, split = place.block % splits;     // the longest first
+    const int block = PARTS ? g.first_block + at_block : at_block;
     const int batch = place.unit / a.kv_heads, kv = place.unit % a.kv_heads, head = kv * group + place.in, bh = batch * a.q_heads + head;
     const int q0 = block * kBlock, mine = q0 + wave * kOwn, i = mine + (lane & 31);
     const T *const q = static_cast<const T *>(a.q.at) + batch * a.q.b + head * a.q.h;
@@ -139,7 +140,7 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
     }
     float off = 0.0f;                                       // -e
     float carry = 0.0f;
-    float *const part = PARTS ? g.parts + (((int64_t)bh * blocks + block) * splits + split) * kAttnWaves * g.part_row + wave * g.part_row : nullptr;
+    float *const part = PARTS ? g.parts + (((int64_t)bh * blocks + at_block) * splits + split) * kAttnWaves * g.part_row + wave * g.part_row : nullptr;
 
     if constexpr (BIAS) {
         load_column<T>(a, head, column);
@@ -477,12 +478,12 @@ void launch_keys(const Attention &a, const Gradients &g, int blocks, hipStream_t
 template <typename T, int D>
 void launch_backward(const Attention &a, const Gradients &g, hipStream_t st)
 {
-    const int q_blocks = (a.q_tokens + kBlock - 1) / kBlock, k_blocks = (a.k_tokens + kBlock - 1) / kBlock;
-    if (a.batch > 0 && q_blocks > 0) {
-        if (g.q_splits > 1) launch_queries<T, D, true>(a, g, q_blocks, st);
-        else launch_queries<T, D, false>(a, g, q_blocks, st);
+    const int k_blocks = (a.k_tokens + kBlock - 1) / kBlock;
+    if (a.batch > 0 && g.blocks > 0) {
+        if (g.q_splits > 1) launch_queries<T, D, true>(a, g, g.blocks, st);
+        else launch_queries<T, D, false>(a, g, g.blocks, st);
     }
-    if (a.batch > 0 && k_blocks > 0) {
+    if (a.batch > 0 && k_blocks > 0 && g.all_rows) {
         if (g.k_splits > 1) launch_keys<T, D, true>(a, g, k_blocks, st);
         else launch_keys<T, D, false>(a, g, k_blocks, st);
     }

@@ -116,6 +116,14 @@ def test_the_workspace_of_shared_out_tiles():
     assert 0 < size(True) - size(False) <= 64 * 4 * 257 * 64 * 4 + 8 * (128 + (1 << 20)) * 4 + 512
 
 
+def test_the_tables_gradient_takes_memory_by_the_length():
+    """Not by the pairs: 256 MB, or 32 KB a key, or 16 bytes a key, sequence and head, and up to 33 sums for each head and distance."""
+    for B, T, H in ((1, 65536, 16), (16, 4096, 16), (16, 16384, 16), (300, 1024, 12), (1, 1 << 20, 1), (4000, 500, 16)):
+        for dtype in (torch.float32, torch.bfloat16):
+            size = lambda table: sf.attention_workspace(dtype, sf.HEADS_ROWS, B, T, T, H, H, 64, table, True)  # noqa: E731, B023
+            assert size(True) - size(False) <= max(256 << 20, (T + 127) * max(32768, 16 * B * H)) + 33 * H * 2 * T * 4 + 512, (B, T, H)
+
+
 def test_distance_buckets():
     one = sf.distance_buckets(5, 5, 8, 16, both_ways=False, device="cpu")
     assert one.dtype == torch.int32 and one.tolist() == [4, 3, 2, 1, 0, 0, 0, 0, 0]

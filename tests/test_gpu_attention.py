@@ -648,3 +648,44 @@ def test_the_least_and_the_largest_scales(dtype, scale, shape, bias):
     if scale < 1:
         within(rows_of(call.dq, sf.HEADS_ROWS), r.dq, r.offs["dq"], "dq")
         within(rows_of(call.dk, sf.HEADS_ROWS, True), r.dk, r.offs["dk"], "dk")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(41, 1500, 1400, 50, 25, 32), (1, 9000, 9100, 32, 32, 32), (700, 130, 1100, 12, 12, 32)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("causal", [False, True], ids=["all", "causal"])
+def test_sums_by_distance_in_turns(shape, dtype, causal):
+    """More sums than are held: blocks of queries in turns (five, five and two of twelve; 64 and seven; one and one), each added to the sums of those
+    before, also where a replayed graph finds another call's sums there."""
+    require_gpu()
+    B, Tq, Tk, Hq, Hk, D = shape
+    q, k, v, do = inputs(*shape, dtype, sf.HEADS_ROWS, seed=Tk)
+    lengths = torch.tensor([(Tk, 0, Tk // 2, 1, Tk + 9)[b % 5] for b in range(B)], dtype=torch.int32, device="cuda")
+    table = torch.randn(9, Hq, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(dtype)
+    of = sf.distance_buckets(Tq, Tk, 9, 200, both_ways=not causal)
+    call = Call(q, k, v, do, sf.HEADS_ROWS, D ** -0.5, causal, lengths, table, of).forward().backward()
+    want = [t.clone() for t in call.outputs()]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call.backward()
+    for _ in range(2):
+        for t in (call.dq, call.dk, call.dv, call.dtable):
+            t.fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(call.outputs(), want))
+    del graph, want
+    per, heads = max(1, 20_000_000 // (Hq * Tq * Tk)), 2 if B == 1 else Hq                # what is looked at in 64 bits at a time
+    dtable, off = torch.zeros(2, 9, Hq, dtype=torch.float64, device="cuda")
+    for b in range(0, B, per):
+        for h in range(0, Hq, heads):
+            few, q_heads, k_heads = slice(b, b + per), slice(h, h + heads), slice(h, h + heads) if B == 1 else slice(0, Hk)
+            r = Reference(q[few, :, q_heads], k[few, :, k_heads], v[few, :, k_heads], do[few, :, q_heads], sf.HEADS_ROWS, D ** -0.5, causal, lengths[few],
+                          table[:, q_heads], of)
+            for name, keys in (("dq", False), ("dk", True), ("dv", False)):
+                within(rows_of(getattr(call, name)[few, :, q_heads if name == "dq" else k_heads], sf.HEADS_ROWS, keys), getattr(r, name), r.offs[name], name)
+            one = r.offs["dtable"] - (UB if r.low else U) * r.dtable.abs() - 2.0 ** -120
+            dtable[:, q_heads] += r.dtable
+            off[:, q_heads] += one / (1 + UB) if r.low else one
+            del r
+    # (each turn's sums are rounded to fp32 once more, three times at most, of the 40 that `off` has for what is 20 otherwise)
+    within(call.dtable.double(), dtable, off * (1 + UB) + UB * dtable.abs() + 2.0 ** -120 if dtype == torch.bfloat16 else off + U * dtable.abs() + 2.0 ** -120, "dtable")
