@@ -689,3 +689,36 @@ def test_sums_by_distance_in_turns(shape, dtype, causal):
             del r
     # (each turn's sums are rounded to fp32 once more, three times at most, of the 40 that `off` has for what is 20 otherwise)
     within(call.dtable.double(), dtable, off * (1 + UB) + UB * dtable.abs() + 2.0 ** -120 if dtype == torch.bfloat16 else off + U * dtable.abs() + 2.0 ** -120, "dtable")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(64, 1, 2100, 8, 2, 128), (3, 5, 1030, 14, 2, 96), (2, 16, 700, 4, 4, 32), (1, 1, 5000, 7, 1, 80), (300, 2, 300, 2, 2, 40), (2, 15, 900, 6, 2, 64),
+                                   (1, 70, 1500, 4, 2, 64)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("causal", [False, True], ids=["all", "causal"])
+def test_few_queries_whose_keys_biases_differ(shape, dtype, causal):
+    """A bucket drawn for each distance, some outside of the table: each key of a query has a bias of its own, each head another."""
+    require_gpu()
+    B, Tq, Tk, Hq, Hk, D = shape
+    g = torch.Generator(device="cuda").manual_seed(Tk)
+    lengths = torch.randint(0, Tk + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    lengths[0] = Tk
+    q, k, v, do = inputs(*shape, dtype, sf.HEADS_ROWS, seed=Tk, columns=True)
+    table = (2.0 * torch.randn(50, Hq, generator=g, device="cuda")).to(dtype)
+    of = torch.randint(-3, 53, (Tq + Tk - 1,), generator=g, device="cuda", dtype=torch.int32)
+    call = Call(q, k, v, do, sf.HEADS_ROWS, D ** -0.5, causal, lengths, table, of).forward().backward()
+    call.check()
+
+
+@pytest.mark.parametrize("T,D", [(300, 128), (601, 104), (1100, 128)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_wide_heads_whether_or_not_one_key_takes_most(T, D, causal):
+    """All queries at once: dq within the bounds without the rounding of out where delta is formed anew, within those with it elsewhere."""
+    require_gpu()
+    q, k, v, do = inputs(2, T, T, 4 if T < 1000 else 16, 2, D, torch.bfloat16, sf.HEADS_ROWS, seed=T + D, spread=1.7)
+    call = Call(q, k, v, do, sf.HEADS_ROWS, D ** -0.5, causal).forward().backward()
+    tight = RightDelta(q, k, v, do, sf.HEADS_ROWS, D ** -0.5, causal, None, None, None)
+    wide = Reference(q, k, v, do, sf.HEADS_ROWS, D ** -0.5, causal, None, None, None)
+    groups = torch.nn.functional.pad(call.stats[..., 1], (0, -T % 32), value=9.0).unflatten(2, (-1, 32))
+    anew = ((groups > 0) & (groups < 2)).any(-1).repeat_interleave(32, -1)[:, :, :T, None]
+    assert float(anew.float().mean()) > 0.25
+    within(rows_of(call.dq, sf.HEADS_ROWS), wide.dq, torch.where(anew, tight.offs["dq"], wide.offs["dq"]), "dq")
