@@ -238,6 +238,8 @@ int32_t slimfit_apply_update_layer_delta(void *const *w, int32_t w_dt,
  *                  of the arguments (a captured graph is replayed with other values; step up to 2^24).
  *  frozen        : DEVICE uint8[L] or NULL: layers of 1 are frozen (the mask of slimfit_ils_select).
  *  d_out         : DEVICE float[L] or NULL (no distances).
+ *  The plan holds addresses: what it names stays where it is as long as the plan is run, gradients too (a loop that drops its gradients
+ *  and has them allocated anew, as torch's zero_grad does by default, keeps them instead or plans again).
  *  A gradient that is not finite makes its weight, and with 8 bits its block's states, NaN; with 8 bits a v' that overflows makes
  *  its block's v NaN (scale 2^98, codes 244).
  *  What is written may share memory with nothing else of the plan, in no layer (INVALID_ARG); gradients may with each
@@ -723,7 +725,8 @@ int32_t slimfit_heads_norm_rotate_backward(const void *dq, const void *dkt, cons
  *  fp32: products, sums and statistics in fp32.  bf16: products of bf16 operands summed in fp32; e^(s - m) (p and ds in the
  *           backward pass) rounded to bf16 once before their products with v (dout, q and k), results rounded once.
  *           The rounding of out, which delta would carry into every ds of a query, is taken off (head_dim over 96 without a
- *           bias: where a query sees up to 128 keys or one key has more than half of its p, of 128 queries any).
+ *           bias: where 128 queries see up to 128 keys, or one key has more than half of the p of any of 32; so that dq of a query there may
+ *           differ in its last places with the queries beside it).
  *  Deterministic: every sum has one owner and one order.  Outputs and the workspace share memory with nothing else of the call (INVALID_ARG).
  *  workspace : DEVICE, 16-byte aligned, of the bytes slimfit_attention_workspace reports (backward 0 or 1; with_dtable:
  *           whether dtable is asked for); contents overwritten.  It grows by tokens, not by pairs: keys that lie transposed once more; where few

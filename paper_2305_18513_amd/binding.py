@@ -333,7 +333,8 @@ def adamw_plan(w: Sequence[torch.Tensor], grad: Sequence[Optional[torch.Tensor]]
                m_scales: Optional[Sequence[torch.Tensor]], v_scales: Optional[Sequence[torch.Tensor]], weight_decay: Sequence[float], bits: int,
                block: int, workspace: torch.Tensor, copies: Optional[Sequence[Optional[torch.Tensor]]] = None, stream=None) -> None:
     """Lays down where the weights, gradients (None: frozen) and states of all layers are.  ``bits`` 32: m and v are float32, scales
-    None; 8: uint8 codes and float32 scales of runs of ``block``.  ``copies``: bfloat16 tensors that follow float32 weights."""
+    None; 8: uint8 codes and float32 scales of runs of ``block``.  ``copies``: bfloat16 tensors that follow float32 weights.  The plan holds
+    addresses and keeps no tensor alive: clear gradients in place (``zero_grad(set_to_none=False)``), or plan again once they have moved."""
     L = len(w)
     _require(all(len(s) == L for s in (grad, m, v, weight_decay)) and (copies is None or len(copies) == L))
     present = [g for g in grad if g is not None]

@@ -291,8 +291,9 @@ __global__ void __launch_bounds__(kAttnThreads, D * sizeof(T) > (PARTS ? 128 : 2
 // tiles to make up for them.
 template <typename T, int D> constexpr bool kValuesInLds = sizeof(T) == 2 && D > 64;
 
-// (fp32 heads of 64 with a bias: two waves a SIMD keep some registers in memory, 165 us for one wave's 178, 8 x 512, 12 heads; where blocks are
-// shared out there is one workgroup a compute unit anyway, 36 and 31, 2 x 300.)
+// (fp32 heads of 64 with a bias: two waves a SIMD keep 68 registers in memory, 165 us for one wave's 178, 8 x 512, 12 heads; where blocks are
+// shared out there is one workgroup a compute unit anyway, 36 and 31, 2 x 300.  Of the other kernels for two waves bf16 heads of 128 with a bias keep 20 to 23
+// there; those of 64 with a bias, of 96, and of 128 without, up to 5, fp32 ones of 64 one.)
 template <typename T, int D, bool BIAS, bool SPLIT>
 __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > (BIAS && SPLIT ? 32 : 64) ? 1 : 2) keys_kernel(Attention a, Gradients g, int blocks)
 {
